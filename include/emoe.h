@@ -759,6 +759,101 @@ emoe_status_t emoe_ipc_export(const void *device_ptr, void *handle_out, uint64_t
 emoe_status_t emoe_ipc_open(const void *handle, void **base_out);
 emoe_status_t emoe_ipc_close(void *base);
 
+/* ---- serving from the arenas -------------------------------------------------
+ *
+ * Between two scale steps a rank serves from the arenas that the steps lay out.  These
+ * entry points are the operators that read and write them: new tokens' keys and values go
+ * into the paged cache and come back out of it, decode attention reads it, and a
+ * mixture-of-experts layer runs on an expert arena.  They work on ONE rank's arenas (its
+ * KV heads, its expert slots); what the ranks contribute is summed or gathered by the
+ * caller.
+ *
+ * Common rules.  Every call only enqueues on cuda_stream (a cudaStream_t, NULL = legacy
+ * default stream): no synchronisation, no allocation, capturable into a CUDA graph.
+ * Pointers are DEVICE pointers unless marked host; structs are read before the call
+ * returns.  The arena must be memory of the current device (EMOE_ERR_CUDA otherwise).
+ * Workspaces belong to the caller, hold nothing between calls, need no initial value, are
+ * 256-byte aligned and must not be shared by calls (or replays of captured calls) whose
+ * GPU work can overlap.  What lies in device memory cannot be checked before the launch:
+ * an id outside its range is skipped as each entry point says, and reported through the
+ * optional status word (see emoe_kv_cache_t).  Input and output buffers of one call must
+ * not overlap. */
+
+/* element types */
+#define EMOE_TYPE_BF16 0
+#define EMOE_TYPE_F16 1
+#define EMOE_TYPE_F32 2
+#define EMOE_TYPE_E4M3 3 /* 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities */
+
+/* One rank's paged KV cache, laid out as emoe_reshard_kv moves it:
+ *     [n_layers][2 (K, V)][num_blocks][block_tokens][n_heads][head_dim]
+ * (with EMOE_LAYOUT_KV_HEAD_MAJOR [n_heads][block_tokens] inside a block).  A token SLOT is
+ * block * block_tokens + offset in the block.
+ *
+ * type EMOE_TYPE_E4M3 holds every head vector as codes of 8 bits and ONE scale, a power of two
+ * kept as a byte: value = code * 2^(byte - 127), byte 255 = a vector that is not a number.
+ * The bytes live in a second arena [n_layers][2][num_blocks][block_tokens][n_heads] (same
+ * order inside a block) - itself a KV arena of head_dim 1 and elem_bytes 1, so that a
+ * plan of that shape moves the scales under the same block tables as a plan with elem_bytes 1
+ * moves the codes. */
+typedef struct {
+  void *arena;          /* 16-byte aligned                                              */
+  void *scales;         /* EMOE_TYPE_E4M3: the scale bytes; otherwise NULL                */
+  int32_t *status;      /* optional int32: set to EMOE_ERR_BLOCK_TABLE by a call that met   */
+                        /* a slot or block id outside the pool (never cleared)            */
+  int32_t n_layers;
+  int32_t num_blocks;   /* num_blocks * block_tokens < 2^31                              */
+  int32_t block_tokens;
+  int32_t n_heads;      /* KV heads of this rank                                        */
+  int32_t head_dim;
+  int32_t type;         /* EMOE_TYPE_BF16, _F16 or _E4M3                                 */
+  uint32_t layout;      /* 0 or EMOE_LAYOUT_KV_HEAD_MAJOR                                */
+  uint32_t reserved;    /* zero                                                         */
+} emoe_kv_cache_t;
+
+/* Bytes of the two arenas of a cache (pointers are not looked at; NULL outputs are skipped).
+ * Host only. */
+emoe_status_t emoe_kv_cache_bytes(const emoe_kv_cache_t *cache, uint64_t *arena_bytes,
+                                  uint64_t *scale_bytes);
+
+/* Index of the head vector of (layer, K = 0 | V = 1, slot, head): its bytes start at
+ * index * head_dim * element size in the arena, its scale at byte `index` of the scales.
+ * -1 for anything out of range.  Host only; the kernels use the same arithmetic. */
+int64_t emoe_kv_vector_index(const emoe_kv_cache_t *cache, int32_t layer, int32_t kv, int64_t slot,
+                             int32_t head);
+
+/*
+ * emoe_kv_append - writes n_tokens tokens' keys and values into their slots of one layer,
+ * rounding (nearest even) or quantising them on the way.
+ *
+ * k, v: [n_tokens][n_heads][head_dim] of in_type, k_stride / v_stride elements from one
+ *   token to the next (so a fused projection's output can be passed as it is); 16-byte
+ *   aligned, strides a multiple of 16 bytes (EMOE_ERR_ALIGNMENT).  in_type: the cache's own
+ *   16-bit type or EMOE_TYPE_F32; for an e4m3 cache BF16, F16 or F32 (EMOE_ERR_UNSUPPORTED).
+ * slots: int64 [n_tokens].  A negative slot skips its token; one beyond the pool is skipped
+ *   and reported in the status word.  A slot may be listed once; listed twice, its vectors
+ *   (and nothing else) are undefined.
+ * head_dim: a multiple of 8, at most 256 (EMOE_ERR_UNSUPPORTED).
+ *
+ * Quantisation of a vector x with a = max |x_i|: 2^k is the smallest power of two with
+ * a <= 448 * 2^k, k >= -126 (k = 0 for a zero vector); the codes are x_i * 2^-k rounded to
+ * nearest even.  A vector with a NaN or an infinity gets scale byte 255 and codes 0.
+ */
+emoe_status_t emoe_kv_append(const emoe_kv_cache_t *cache, int32_t layer, const void *k,
+                             const void *v, int64_t k_stride, int64_t v_stride, int32_t in_type,
+                             const int64_t *slots, int32_t n_tokens, void *cuda_stream);
+
+/*
+ * emoe_kv_gather - reads slots of one layer back: k, v [n_tokens][n_heads][head_dim] of
+ * out_type (types, strides and alignment as for emoe_kv_append).  The row of a negative slot
+ * is left as it was, so is one beyond the pool, which is reported.  Slots may repeat.
+ * e4m3 values are exact in BF16 and F32 (as far as those types reach); in F16 they are
+ * rounded and beyond its range infinite.
+ */
+emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const int64_t *slots,
+                             int32_t n_tokens, void *k, void *v, int64_t k_stride,
+                             int64_t v_stride, int32_t out_type, void *cuda_stream);
+
 /* Static string for a status code. */
 const char *emoe_strerror(emoe_status_t status);
 

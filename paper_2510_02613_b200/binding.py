@@ -71,6 +71,12 @@ class _VmmStats(ctypes.Structure):
                                                "total_ms")]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [("arena", _vp), ("scales", _vp), ("status", _vp)] + \
+               [(n, _i32) for n in ("n_layers", "num_blocks", "block_tokens", "n_heads", "head_dim", "type")] + \
+               [("layout", _u32), ("reserved", _u32)]
+
+
 SEGMENT_DTYPE = np.dtype([("src_off", "<u8"), ("dst_off", "<u8"), ("run_bytes", "<u8"),
                           ("src_pitch", "<u8"), ("dst_pitch", "<u8"), ("n_runs", "<u4"),
                           ("src_rank", "<u4"), ("dst_rank", "<u4"), ("group", "<u4")])
@@ -90,7 +96,8 @@ EXPORTS = ("emoe_plan_create", "emoe_plan_create_ex", "emoe_reshard_experts", "e
            "emoe_vmm_create", "emoe_vmm_reshard", "emoe_vmm_dry_run", "emoe_vmm_num_ranks", "emoe_vmm_arena",
            "emoe_vmm_write", "emoe_vmm_read", "emoe_vmm_destroy",
            "emoe_vmm_slots_create", "emoe_vmm_slots_reshard", "emoe_vmm_slots_info", "emoe_vmm_slots_write",
-           "emoe_vmm_slots_read", "emoe_vmm_slots_destroy")
+           "emoe_vmm_slots_read", "emoe_vmm_slots_destroy",
+           "emoe_kv_cache_bytes", "emoe_kv_vector_index", "emoe_kv_append", "emoe_kv_gather")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -217,6 +224,15 @@ def lib() -> ctypes.CDLL:
         f.argtypes = [_vp, _i32, _i32, _vp, _vp]
     L.emoe_vmm_slots_destroy.restype = None
     L.emoe_vmm_slots_destroy.argtypes = [_vp]
+    cache, i64 = ctypes.POINTER(_KvCache), ctypes.c_int64
+    for name, args in (("emoe_kv_cache_bytes", [cache, ctypes.POINTER(_u64), ctypes.POINTER(_u64)]),
+                       ("emoe_kv_append", [cache, _i32, _vp, _vp, i64, i64, _i32, _vp, _i32, _vp]),
+                       ("emoe_kv_gather", [cache, _i32, _vp, _i32, _vp, _vp, i64, i64, _i32, _vp])):
+        f = getattr(L, name)
+        f.restype = _i32
+        f.argtypes = args
+    L.emoe_kv_vector_index.restype = i64
+    L.emoe_kv_vector_index.argtypes = [cache, _i32, _i32, i64, _i32]
     L.emoe_strerror.restype = ctypes.c_char_p
     L.emoe_strerror.argtypes = [_i32]
     _lib = L

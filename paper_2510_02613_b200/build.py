@@ -7,8 +7,8 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "kernels.cu"]
-HEADERS = ["planner.h", "kernels.h", "internal.h", os.path.join("..", "..", "include", "emoe.h")]
+SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "serve.cpp", "kernels.cu", "kv_cache.cu"]
+HEADERS = ["planner.h", "kernels.h", "internal.h", "serve.h", os.path.join("..", "..", "include", "emoe.h")]
 OUT = os.path.join(HERE, "libemoe.so")
 
 
@@ -40,7 +40,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return OUT
     tmp = OUT + ".%d.tmp" % os.getpid()
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-shared", "-Xcompiler", "-fPIC,-Wall", "-x", "cu",
+           "-shared", "-Xcompiler", "-fPIC,-Wall", "-x", "cu", "-t", "0",
            "-o", tmp] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")

@@ -1,0 +1,135 @@
+"""Operators that serve from one rank's arenas between two scale steps: the handles below describe
+an arena as the library lays it out and marshal torch tensors to the C entry points, which only
+enqueue on the stream they are given (None: the legacy default stream, as for the reshard calls).
+
+Tensors are checked for type, shape and device here; ids and lengths that lie in device memory are
+bounds-checked by the kernels (see emoe_kv_cache_t.status)."""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+from . import binding as _b
+from .binding import _check, _stream_handle
+
+BF16, F16, F32, E4M3 = range(4)
+_TYPE_NAMES = {"bf16": BF16, "f16": F16, "e4m3": E4M3}
+_TORCH_TYPES = {"torch.bfloat16": BF16, "torch.float16": F16, "torch.float32": F32}
+_TYPE_BYTES = {BF16: 2, F16: 2, F32: 4, E4M3: 1}
+
+
+def _type_of(name: str) -> int:
+    try:
+        return _TYPE_NAMES[name]
+    except KeyError:
+        raise ValueError("element type %r: one of %s" % (name, ", ".join(_TYPE_NAMES))) from None
+
+
+def _value_type(t, what: str) -> int:
+    try:
+        return _TORCH_TYPES[str(t.dtype)]
+    except KeyError:
+        raise ValueError("%s: bfloat16, float16 or float32, not %s" % (what, t.dtype)) from None
+
+
+def _shaped(t, what: str, shape, dtype: Optional[str] = None, device=None):
+    """t itself; ValueError unless it has this shape (None: any size), type and device."""
+    if len(t.shape) != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
+        raise ValueError("%s: shape %s, wanted %s" % (what, tuple(t.shape), tuple("any" if w is None else w for w in shape)))
+    if dtype is not None and str(t.dtype) != "torch." + dtype:
+        raise ValueError("%s: %s, wanted %s" % (what, t.dtype, dtype))
+    if device is not None and t.device != device:
+        raise ValueError("%s is on %s, the arena on %s" % (what, t.device, device))
+    return t
+
+
+def _dense(t, what: str, inner: int):
+    """t itself; ValueError unless its last `inner` dimensions are densely packed."""
+    step = 1
+    for n, s in list(zip(t.shape, t.stride()))[:-inner - 1:-1]:
+        if n != 1 and s != step:
+            raise ValueError("%s: its last %d dimensions have to be contiguous" % (what, inner))
+        step *= n
+    return t
+
+
+def _arena_pointer(arena, need: int, what: str):
+    """(address, device or None): a tensor has to be large enough and contiguous; an address is taken as it is."""
+    if isinstance(arena, int):
+        return arena, None
+    if not arena.is_contiguous():
+        raise ValueError("%s: not contiguous" % what)
+    if arena.numel() * arena.element_size() < need:
+        raise ValueError("%s: %d bytes, at least %d are needed" % (what, arena.numel() * arena.element_size(), need))
+    return arena.data_ptr(), arena.device
+
+
+class KvCache:
+    """One rank's paged KV cache: emoe_kv_append, emoe_kv_gather, emoe_kv_attend.
+
+    arena: tensor or device address, [n_layers][2][num_blocks][block_tokens][n_heads][head_dim] as
+    emoe_reshard_kv lays it out (head_major: [n_heads][block_tokens] inside a block).  kv_type: "bf16",
+    "f16" or "e4m3"; the last has scale bytes [n_layers][2][num_blocks][block_tokens][n_heads] in
+    `scales`, a KV arena of head_dim 1 and elem_bytes 1.  status: optional int32 tensor of one element,
+    set to 4 (EMOE_ERR_BLOCK_TABLE) by calls that meet an id outside the pool."""
+
+    def __init__(self, arena, *, n_layers: int, num_blocks: int, block_tokens: int, n_heads: int, head_dim: int,
+                 kv_type: str = "bf16", scales=None, head_major: bool = False, status=None):
+        self._c = _b._KvCache(None, None, None, n_layers, num_blocks, block_tokens, n_heads, head_dim, _type_of(kv_type),
+                              _b.LAYOUT_KV_HEAD_MAJOR if head_major else 0, 0)
+        self.kv_type, self.n_heads, self.head_dim, self.block_tokens = self._c.type, n_heads, head_dim, block_tokens
+        sizes = self.bytes()
+        self._c.arena, self.device = _arena_pointer(arena, sizes[0], "arena")
+        if (scales is None) == (self.kv_type == E4M3):
+            raise ValueError("an e4m3 cache has scales, another has none")
+        if scales is not None:
+            self._c.scales, device = _arena_pointer(scales, sizes[1], "scales")
+            if None not in (device, self.device) and device != self.device:
+                raise ValueError("scales are on %s, the arena on %s" % (device, self.device))
+        if status is not None:
+            _shaped(status, "status", (1,), "int32", self.device)
+            self._c.status = status.data_ptr()
+        self._keep = (arena, scales, status)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def for_rank(cls, shape, tp: int, num_blocks: int, arena, kv_type: str = "bf16", **kw) -> "KvCache":
+        """The cache of one of `tp` ranks of a model `shape`, as a plan with that shape lays it out."""
+        if _TYPE_BYTES[_type_of(kv_type)] != shape.elem_bytes:
+            raise ValueError("%s elements have %d bytes, the shape's %d" % (kv_type, _TYPE_BYTES[_type_of(kv_type)], shape.elem_bytes))
+        return cls(arena, n_layers=shape.n_layers, num_blocks=num_blocks, block_tokens=shape.kv_block_tokens,
+                   n_heads=max(1, shape.n_kv_heads // tp), head_dim=shape.head_dim, kv_type=kv_type, **kw)
+
+    def bytes(self):
+        """(bytes of the arena, bytes of the scales)"""
+        a, s = ctypes.c_uint64(), ctypes.c_uint64()
+        _check(_b.lib().emoe_kv_cache_bytes(ctypes.byref(self._c), ctypes.byref(a), ctypes.byref(s)))
+        return a.value, s.value
+
+    def vector_index(self, layer: int, kv: int, slot: int, head: int) -> int:
+        """Index of a head vector in the arena (kv: 0 keys, 1 values), -1 if out of range."""
+        return _b.lib().emoe_kv_vector_index(self._ref, layer, kv, slot, head)
+
+    def _rows(self, x, what, n):
+        _dense(_shaped(x, what, (n, self.n_heads, self.head_dim), None, self.device), what, 2)
+        return x.data_ptr(), (x.stride(0) if n > 1 else self.n_heads * self.head_dim)
+
+    def _copy_args(self, k, v, slots):
+        n = slots.shape[0]
+        _dense(_shaped(slots, "slots", (None,), "int64", self.device), "slots", 1)
+        (kp, ks), (vp, vs) = self._rows(k, "k", n), self._rows(v, "v", n)
+        if k.dtype != v.dtype:
+            raise ValueError("k is %s, v %s" % (k.dtype, v.dtype))
+        return n, kp, ks, vp, vs, _value_type(k, "k")
+
+    def append(self, layer: int, k, v, slots, stream=None) -> None:
+        """Writes tokens' keys and values, [n, n_heads, head_dim] with any stride between tokens, into
+        their slots (int64: block * block_tokens + offset; negative: skipped), quantising where the
+        cache is e4m3."""
+        n, kp, ks, vp, vs, t = self._copy_args(k, v, slots)
+        _check(_b.lib().emoe_kv_append(self._ref, layer, kp, vp, ks, vs, t, slots.data_ptr(), n, _stream_handle(stream)))
+
+    def gather(self, layer: int, slots, k, v, stream=None) -> None:
+        """Reads slots back into k and v; rows of negative slots stay as they were."""
+        n, kp, ks, vp, vs, t = self._copy_args(k, v, slots)
+        _check(_b.lib().emoe_kv_gather(self._ref, layer, slots.data_ptr(), n, kp, vp, ks, vs, t, _stream_handle(stream)))

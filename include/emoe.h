@@ -854,6 +854,51 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
                              int32_t n_tokens, void *k, void *v, int64_t k_stride,
                              int64_t v_stride, int32_t out_type, void *cuda_stream);
 
+/*
+ * emoe_kv_attend - decode attention over the paged cache for a batch whose sequences share a
+ * prefix.  Query head h reads KV head h / (n_q_heads / n_heads).  Query token t of sequence s
+ * (q_len of them, the sequence's last ones) sees the prefix - prefix_len tokens on the blocks
+ * prefix_table lists - and then the sequence's own tokens 0 .. own_lens[s] - q_len + t, which lie
+ * on blocks of their own (row s of block_table, from the start of its first block):
+ *     out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log(sum_j exp(scale * q.k_j)).
+ * The prefix is read once for the whole batch.  A row that sees no token gives 0 and
+ * -infinity.  Sums, maxima and statistics are 32-bit; the softmax weights are rounded to io_type
+ * before they meet v.  The keys and values of the query tokens themselves have to be in the
+ * cache already (emoe_kv_append earlier on the stream).
+ *
+ * Calls over different prefixes, or over parts of one long context, are joined with lse:
+ * out = (out1 e^(lse1-m) + out2 e^(lse2-m)) / (e^(lse1-m) + e^(lse2-m)).
+ *
+ * head_dim: 32, 64, 128 or 256 (EMOE_ERR_UNSUPPORTED).  io_type: the cache's type, or either 16-bit
+ * type for an e4m3 cache.  own_lens beyond max_blocks * block_tokens count as that, negative ones
+ * as 0.  Tokens on a block id outside the pool are left out and reported in the status word.
+ * What lies behind a sequence's length - in its last block, in its row of the table, in the pool -
+ * has no influence, whatever it holds.  prefix_len, and max_blocks as the bound of own_lens, are
+ * host values; a captured call follows own_lens and the tables from replay to replay.
+ * Sizes beyond 2^24 query tokens, 2^28 rows or 2^30 tokens a sequence: EMOE_ERR_TOO_LARGE.
+ */
+typedef struct {
+  const void *q;               /* [n_seqs][q_len][n_q_heads][head_dim], 16-byte aligned          */
+  void *out;                   /* as q                                                         */
+  float *lse;                  /* optional [n_seqs][q_len][n_q_heads], natural logarithm         */
+  int64_t q_stride;            /* elements from one query token to the next, a multiple of 8     */
+  int64_t out_stride;
+  const int32_t *block_table;  /* [n_seqs][max_blocks]; NULL with max_blocks = 0                 */
+  const int32_t *own_lens;     /* [n_seqs]: own tokens, the query tokens included                */
+  const int32_t *prefix_table; /* [ceil(prefix_len / block_tokens)]; NULL with prefix_len = 0    */
+  void *workspace;             /* emoe_kv_attend_workspace bytes                                */
+  uint64_t workspace_bytes;    /* (too few: EMOE_ERR_INVALID_ARG)                               */
+  int32_t n_seqs, q_len, n_q_heads, max_blocks, prefix_len;
+  int32_t io_type;             /* EMOE_TYPE_BF16 or _F16                                        */
+  float scale;                 /* usually 1 / sqrt(head_dim)                                   */
+  uint32_t reserved;           /* zero                                                         */
+} emoe_attend_t;
+emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *cache, int32_t n_seqs, int32_t q_len,
+                                       int32_t n_q_heads, int32_t max_blocks, int32_t prefix_len,
+                                       uint64_t *bytes);
+emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const emoe_attend_t *args,
+                             void *cuda_stream);
+
 /* Static string for a status code. */
 const char *emoe_strerror(emoe_status_t status);
 

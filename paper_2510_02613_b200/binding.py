@@ -77,6 +77,13 @@ class _KvCache(ctypes.Structure):
                [("layout", _u32), ("reserved", _u32)]
 
 
+class _Attend(ctypes.Structure):
+    _fields_ = [("q", _vp), ("out", _vp), ("lse", _vp), ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("block_table", _vp), ("own_lens", _vp), ("prefix_table", _vp), ("workspace", _vp), ("workspace_bytes", _u64)] + \
+               [(n, _i32) for n in ("n_seqs", "q_len", "n_q_heads", "max_blocks", "prefix_len", "io_type")] + \
+               [("scale", ctypes.c_float), ("reserved", _u32)]
+
+
 SEGMENT_DTYPE = np.dtype([("src_off", "<u8"), ("dst_off", "<u8"), ("run_bytes", "<u8"),
                           ("src_pitch", "<u8"), ("dst_pitch", "<u8"), ("n_runs", "<u4"),
                           ("src_rank", "<u4"), ("dst_rank", "<u4"), ("group", "<u4")])
@@ -97,7 +104,8 @@ EXPORTS = ("emoe_plan_create", "emoe_plan_create_ex", "emoe_reshard_experts", "e
            "emoe_vmm_write", "emoe_vmm_read", "emoe_vmm_destroy",
            "emoe_vmm_slots_create", "emoe_vmm_slots_reshard", "emoe_vmm_slots_info", "emoe_vmm_slots_write",
            "emoe_vmm_slots_read", "emoe_vmm_slots_destroy",
-           "emoe_kv_cache_bytes", "emoe_kv_vector_index", "emoe_kv_append", "emoe_kv_gather")
+           "emoe_kv_cache_bytes", "emoe_kv_vector_index", "emoe_kv_append", "emoe_kv_gather",
+           "emoe_kv_attend_workspace", "emoe_kv_attend")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -227,6 +235,8 @@ def lib() -> ctypes.CDLL:
     cache, i64 = ctypes.POINTER(_KvCache), ctypes.c_int64
     for name, args in (("emoe_kv_cache_bytes", [cache, ctypes.POINTER(_u64), ctypes.POINTER(_u64)]),
                        ("emoe_kv_append", [cache, _i32, _vp, _vp, i64, i64, _i32, _vp, _i32, _vp]),
+                       ("emoe_kv_attend_workspace", [cache, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
+                       ("emoe_kv_attend", [cache, _i32, ctypes.POINTER(_Attend), _vp]),
                        ("emoe_kv_gather", [cache, _i32, _vp, _i32, _vp, _vp, i64, i64, _i32, _vp])):
         f = getattr(L, name)
         f.restype = _i32

@@ -1,0 +1,490 @@
+// attend.cu - decode attention over a paged KV cache, a shared prefix computed once for the batch.
+//
+// o = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = scale * log2(e) * q.k_j and m the
+// largest s_j, in one pass over the tokens: each part of the work keeps its own m, sum and
+// unnormalised o in 32 bits, and parts are joined by o = sum 2^(m_i - m) o_i.
+//
+// Work is cut into items (row tile, KV head, token range).  The rows of a KV head are its query
+// heads times the query tokens - of the whole batch for the prefix, which is thereby read once, and
+// of one sequence for that sequence's own tokens.  When there are few rows the token axis is split
+// until the machine is full; a second kernel joins the splits.
+#include <math_constants.h>
+
+#include "convert.cuh"
+#include "serve.h"
+
+namespace emoe {
+namespace {
+
+constexpr int kWarps = 4, kStages = 3, kGroup = 16;  // tokens of one warp's step
+
+struct Item {
+  bool prefix;
+  int seq, head, row0, rows, slot;  // rows of this tile, first row inside the sequence or batch
+  int t0, t1;                       // tokens
+};
+
+__device__ __forceinline__ int own_length(const AttendArgs &a, int seq) {
+  return a.max_blocks ? max(0, min(a.own_lens[seq], a.max_blocks * a.c.block_tokens)) : 0;
+}
+
+__device__ __forceinline__ Item item_of(const AttendArgs &a, uint32_t i) {
+  Item it;
+  const uint32_t heads = a.c.n_heads;
+  if (i < a.prefix_items) {
+    it.prefix = true;
+    it.seq = 0;
+    const uint32_t split = i % a.prefix_splits, j = i / a.prefix_splits;
+    it.head = j % heads;
+    it.row0 = (j / heads) * 16;
+    it.rows = min(16, a.n_seqs * a.seq_rows - it.row0);
+    it.slot = split;
+    it.t0 = split * a.prefix_chunk;
+    it.t1 = min(a.prefix_len, it.t0 + a.prefix_chunk);
+  } else {
+    i -= a.prefix_items;
+    it.prefix = false;
+    const uint32_t split = i % a.own_splits;
+    uint32_t j = i / a.own_splits;
+    it.head = j % heads;
+    j /= heads;
+    const uint32_t tiles = (a.seq_rows + 15) / 16;
+    it.row0 = (j % tiles) * 16;
+    it.seq = j / tiles;
+    it.rows = min(16, a.seq_rows - it.row0);
+    it.slot = a.prefix_splits + split;
+    it.t0 = split * a.own_chunk;
+    it.t1 = min(own_length(a, it.seq), it.t0 + a.own_chunk);
+  }
+  return it;
+}
+
+// Output row (sequence, query token, query head) of a tile row.
+__device__ __forceinline__ int64_t output_row(const AttendArgs &a, int seq, int head, int row) {
+  const int token = row / a.group;   // over the batch for the prefix: seq * q_len + t
+  return ((int64_t)seq * a.q_len + token) * a.n_q_heads + head * a.group + row - token * a.group;
+}
+
+// 16-byte piece c of row r of a tile with CH pieces a row: rotated so that eight rows' equal pieces
+// lie in different banks.
+template <int CH> __device__ __forceinline__ int swizzled(int r, int c) {
+  if constexpr (CH >= 8) return r * CH + (c ^ (r & 7));
+  else if constexpr (CH == 4) return r * CH + (c ^ ((r >> 1) & 3));
+  else return r * CH + (c ^ ((r >> 2) & 1));
+}
+
+__device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int hd, float m, float l) {
+  if (a.lse) a.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * CUDART_LN2_F : -CUDART_INF_F;
+}
+
+// One warp's step covers 16 tokens: K and V rows come through a ring of its own in shared memory
+// (no block barrier in the loop), scores and products on the tensor cores with the 16 rows of the
+// item as the m side (rows that do not exist are zero), running maximum and sum in registers.  The
+// four warps take every fourth group of tokens and are joined at the end.  Bound by the reads of K
+// and V: 3 stages x 4 warps x 8 KB and two blocks an SM keep 128 KB in flight.
+template <typename T, int HD, bool FP8>
+__global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int ES = FP8 ? 1 : 2, CH = HD * ES / 16, kTile = kGroup * HD * ES, kStage = 2 * kTile;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint16_t s_scale[kWarps][kStages][kGroup];
+  __shared__ uint32_t s_valid[kWarps][kStages];
+  __shared__ float s_m[kWarps][16], s_l[kWarps][16];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const Item it = item_of(a, blockIdx.x);
+  const int slots = a.prefix_splits + a.own_splits;
+
+  let_next_start();
+  if (it.t0 >= it.t1 && slots > 1) {   // nothing here: say so to the joining kernel
+    if (threadIdx.x < it.rows)
+      a.part_ml[output_row(a, it.seq, it.head, it.row0 + threadIdx.x) * slots + it.slot] = make_float2(-CUDART_INF_F, 0.f);
+    return;
+  }
+
+  // query rows g and g + 8 of the tile as matrix operands, from global memory
+  uint32_t q[HD / 16][4];
+  int limit[2];   // tokens that the row sees
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int row = g + 8 * half;
+    const bool real = row < it.rows;
+    const int r = real ? it.row0 + row : 0;
+    const int token = r / a.group;
+    const T *src = (const T *)a.q + ((int64_t)it.seq * a.q_len + token) * a.q_stride + (it.head * a.group + r - token * a.group) * HD;
+    limit[half] = !real ? 0 : it.prefix ? it.t1 : own_length(a, it.seq) - a.q_len + token + 1;
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) {
+      if constexpr (!FP8) {
+        const uint32_t *p = (const uint32_t *)(src + ks * 16 + 2 * c);
+        q[ks][half] = real ? p[0] : 0;
+        q[ks][2 + half] = real ? p[4] : 0;
+      } else {   // the order in which codes come out of a word: (0, 2), (1, 3)
+        const uint2 w = real ? *(const uint2 *)(src + (ks >> 1) * 32 + c * 8 + (ks & 1) * 4) : make_uint2(0, 0);
+        q[ks][half] = __byte_perm(w.x, w.y, 0x5410);
+        q[ks][2 + half] = __byte_perm(w.x, w.y, 0x7632);
+      }
+    }
+  }
+
+  const int groups = it.t1 > it.t0 ? (it.t1 - it.t0 + kGroup - 1) / kGroup : 0;
+  const int steps = groups > warp ? (groups - warp + kWarps - 1) / kWarps : 0;
+  const int32_t *table = it.prefix ? a.prefix_table : a.block_table + (int64_t)it.seq * a.max_blocks;
+  uint8_t *const ring = smem + warp * (kStages * kStage);
+  const uint32_t ring_at = shared_address(ring);
+
+  // vector index of this lane's token (lanes 16.. repeat 0..15) of step i, -1 if there is none
+  auto locate = [&](int i) -> int64_t {
+    const int t = it.t0 + (warp + kWarps * i) * kGroup + (lane & 15);
+    if (i >= steps || t >= it.t1) return -1;
+    const uint32_t b = (uint32_t)t / (uint32_t)a.c.block_tokens, off = (uint32_t)t - b * a.c.block_tokens;
+    const int block = table[b];
+    if (block < 0 || block >= a.num_blocks) {
+      if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
+      return -1;
+    }
+    return a.c.head_major ? ((int64_t)block * a.c.n_heads + it.head) * a.c.block_tokens + off
+                          : ((int64_t)block * a.c.block_tokens + off) * a.c.n_heads + it.head;
+  };
+  uint32_t held_scale = 0, held_valid = 0;
+  auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
+    const uint32_t at = ring_at + (i % kStages) * kStage;
+    held_valid = __ballot_sync(0xffffffffu, vec >= 0) & 0xffff;
+    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x7f7f;
+#pragma unroll
+    for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
+      const int id = j * 32 + lane, row = id / CH, ch = id % CH;
+      const int64_t v = __shfl_sync(0xffffffffu, vec, row & 15);
+      if (kGroup * CH % 32 == 0 || id < kGroup * CH) {
+        const int64_t src = v < 0 ? 0 : v * (HD * ES) + ch * 16;
+        const uint32_t dst = at + swizzled<CH>(row, ch) * 16;
+        copy_async_16(dst, a.c.k + src, v < 0 ? 0 : 16);
+        copy_async_16(dst + kTile, a.c.v + src, v < 0 ? 0 : 16);
+      }
+    }
+  };
+  auto keep = [&](int i) {   // what the issue of step i found, for its use
+    if (FP8 && lane < 16) s_scale[warp][i % kStages][lane] = (uint16_t)held_scale;
+    if (lane == 0) s_valid[warp][i % kStages] = held_valid;
+  };
+
+  float o[HD / 8][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (i < steps) {
+      issue(i, locate(i));
+      keep(i);
+    }
+    copy_async_commit();
+  }
+  int64_t next = locate(kStages - 1);
+  for (int i = 0; i < steps; ++i) {
+    const int ahead = i + kStages - 1;
+    if (ahead < steps) issue(ahead, next);
+    copy_async_commit();
+    next = locate(ahead + 1);
+    copy_async_wait<kStages - 1>();
+    __syncwarp();
+
+    const uint32_t k_at = ring_at + (i % kStages) * kStage, v_at = k_at + kTile;
+    const uint32_t valid = s_valid[warp][i % kStages];
+    float s[2][4] = {};
+    if constexpr (!FP8) {
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks) {
+        uint32_t b[4];
+        ldmatrix_x4(b, k_at + swizzled<CH>((lane >> 4) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)) * 16);
+        mma_16816<T>(s[0], q[ks], b[0], b[1]);
+        mma_16816<T>(s[1], q[ks], b[2], b[3]);
+      }
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < HD / 32; ++kb)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint2 w = *(const uint2 *)(ring + (i % kStages) * kStage + swizzled<CH>(j * 8 + g, kb * 2 + (c >> 1)) * 16 + (c & 1) * 8);
+          mma_16816<T>(s[j], q[2 * kb], even_codes<T>(w.x), odd_codes<T>(w.x));
+          mma_16816<T>(s[j], q[2 * kb + 1], even_codes<T>(w.y), odd_codes<T>(w.y));
+        }
+    }
+
+    const int base = it.t0 + (warp + kWarps * i) * kGroup;
+    float v_by[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+    float top[2] = {m[0], m[1]};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int t = j * 8 + 2 * c + e;
+        float by = a.scale_log2;
+        if constexpr (FP8) {   // both scales are powers of two; 255 is not a number
+          const uint32_t b = s_scale[warp][i % kStages][t];
+          const uint32_t kb = b & 255, vb = b >> 8;
+          by *= kb == 255 ? CUDART_NAN_F : __uint_as_float(kb ? kb << 23 : 0x400000u);
+          v_by[j][e] = vb == 255 ? CUDART_NAN_F : __uint_as_float(vb ? vb << 23 : 0x400000u);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float &x = s[j][2 * half + e];
+          x = ((valid >> t) & 1) && base + t < limit[half] ? x * by : -CUDART_INF_F;
+          top[half] = fmaxf(top[half], x);
+        }
+      }
+    float alpha[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
+      top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
+      const float safe = top[half] == -CUDART_INF_F ? 0.f : top[half];
+      alpha[half] = exp2_fast(m[half] - safe);
+      m[half] = top[half];
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float &x = s[j][2 * half + e];
+          x = exp2_fast(x - safe);
+          sum += x;
+          // a masked token's v may be anything (its scale too): its weight is exactly zero
+          if constexpr (FP8) x = x == 0.f ? 0.f : x * v_by[j][e];
+        }
+      l[half] = l[half] * alpha[half] + sum;
+    }
+    if (!__all_sync(0xffffffffu, alpha[0] == 1.f && alpha[1] == 1.f)) {
+#pragma unroll
+      for (int n = 0; n < HD / 8; ++n) {
+        o[n][0] *= alpha[0];
+        o[n][1] *= alpha[0];
+        o[n][2] *= alpha[1];
+        o[n][3] *= alpha[1];
+      }
+    }
+    // weights rounded to T, once, as the second product's operand: the result's own rounding is as large
+    const uint32_t p[4] = {Pair<T>::pack(s[0][0], s[0][1]), Pair<T>::pack(s[0][2], s[0][3]),
+                           Pair<T>::pack(s[1][0], s[1][1]), Pair<T>::pack(s[1][2], s[1][3])};
+    // Query tokens of one sequence see different ends.  A value that some rows must not see may be
+    // infinite or not a number, and a weight of zero does not silence it: such a step is done end by
+    // end, each row taking the pass of its own, with the values behind that end cleared.  (e4m3 codes
+    // are finite.)
+    const int end = min(base + kGroup, it.t1);
+    const bool ragged = !FP8 && a.q_len > 1 &&
+                        __any_sync(0xffffffffu, (g < it.rows && limit[0] < end) || (g + 8 < it.rows && limit[1] < end));
+    if (ragged) {
+      for (int stop = end; stop > base; --stop) {
+        const bool now0 = min(limit[0], end) == stop, now1 = min(limit[1], end) == stop;
+        if (__any_sync(0xffffffffu, now0 || now1)) {
+#pragma unroll
+          for (int n = 0; n < HD / 16; ++n) {
+            uint32_t b[4];
+            ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              float part[4] = {};
+              mma_16816<T>(part, p, b[2 * k], b[2 * k + 1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e < 2 ? now0 : now1) o[2 * n + k][e] += part[e];
+            }
+          }
+        }
+        __syncwarp();
+        for (int ch = lane; ch < CH; ch += 32)
+          *(uint4 *)(ring + (i % kStages) * kStage + kTile + swizzled<CH>(stop - 1 - base, ch) * 16) = make_uint4(0, 0, 0, 0);
+        __syncwarp();
+      }
+    } else if constexpr (!FP8) {
+#pragma unroll
+      for (int n = 0; n < HD / 16; ++n) {
+        uint32_t b[4];
+        ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
+        mma_16816<T>(o[2 * n], p, b[0], b[1]);
+        mma_16816<T>(o[2 * n + 1], p, b[2], b[3]);
+      }
+    } else {   // two neighbouring columns travel as one 16-bit element and are parted afterwards
+#pragma unroll
+      for (int n = 0; n < HD / 32; ++n) {
+        uint32_t b[4];
+        ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
+        mma_16816<T>(o[4 * n], p, even_codes<T>(b[0]), even_codes<T>(b[1]));
+        mma_16816<T>(o[4 * n + 1], p, odd_codes<T>(b[0]), odd_codes<T>(b[1]));
+        mma_16816<T>(o[4 * n + 2], p, even_codes<T>(b[2]), even_codes<T>(b[3]));
+        mma_16816<T>(o[4 * n + 3], p, odd_codes<T>(b[2]), odd_codes<T>(b[3]));
+      }
+    }
+    if (ahead < steps) keep(ahead);
+    __syncwarp();
+  }
+  copy_async_wait<0>();
+
+  // the four warps' parts become one
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
+    l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+    if (c == 0) {
+      s_m[warp][g + 8 * half] = m[half];
+      s_l[warp][g + 8 * half] = l[half];
+    }
+  }
+  __syncthreads();
+  constexpr int kPitch = HD + 4;
+  float *const joined = (float *)smem;
+#pragma unroll
+  for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * (e & 1) : n * 8 + 2 * c + (e & 1);
+      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n][e];
+    }
+  __syncthreads();
+  const int row = threadIdx.x >> 3;
+  if (row >= it.rows) return;
+  float mm = -CUDART_INF_F, ll = 0.f, w[kWarps];
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, s_m[i][row]);
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    w[i] = mm == -CUDART_INF_F ? 0.f : exp2_fast(s_m[i][row] - mm);
+    ll += w[i] * s_l[i][row];
+    if (s_l[i][row] != s_l[i][row]) ll = w[i] = CUDART_NAN_F;   // a maximum does not carry a NaN: the sum does
+  }
+  const int64_t orow = output_row(a, it.seq, it.head, it.row0 + row);
+  const bool last = slots == 1;
+  const float by = last ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f;
+  for (int col = (threadIdx.x & 7) * 4; col < HD; col += 32) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float4 y = *(const float4 *)&joined[(i * 16 + row) * kPitch + col];
+      x.x += w[i] * y.x;
+      x.y += w[i] * y.y;
+      x.z += w[i] * y.z;
+      x.w += w[i] * y.w;
+    }
+    if (last) {
+      const int64_t token = orow / a.n_q_heads;
+      *(uint2 *)((T *)a.out + token * a.out_stride + (orow - token * a.n_q_heads) * HD + col) =
+          make_uint2(Pair<T>::pack(x.x * by, x.y * by), Pair<T>::pack(x.z * by, x.w * by));
+    } else {
+      *(float4 *)(a.part_o + (orow * slots + it.slot) * HD + col) = x;
+    }
+  }
+  if ((threadIdx.x & 7) == 0) {
+    if (last) write_row(a, orow, HD, mm, ll);
+    else a.part_ml[orow * slots + it.slot] = make_float2(mm, ll);
+  }
+}
+
+// Joins the splits of an output row: a warp a row, in the order of the splits.
+template <typename T, int HD>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int N = HD / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  wait_for_previous();
+  if (row >= (int64_t)a.n_seqs * a.q_len * a.n_q_heads) return;
+  const int slots = a.prefix_splits + a.own_splits;
+  const float2 *ml = a.part_ml + row * slots;
+  float m = -CUDART_INF_F;
+  for (int i = lane; i < slots; i += 32) m = fmaxf(m, ml[i].x);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  float l = 0.f, x[N] = {};
+  for (int i = 0; i < slots; ++i) {
+    const float2 p = ml[i];
+    if (p.y == 0.f) continue;
+    const float w = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+    l += w * p.y;
+    const float *src = a.part_o + (row * slots + i) * HD + lane * N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] += w * src[j];
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  const int64_t token = row / a.n_q_heads;
+  T *dst = (T *)a.out + token * a.out_stride + (row - token * a.n_q_heads) * HD + lane * N;
+  if constexpr (N == 1) {
+    *(uint16_t *)dst = (uint16_t)Pair<T>::pack(x[0] * by, 0.f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) *(uint32_t *)(dst + j) = Pair<T>::pack(x[j] * by, x[j + 1] * by);
+  }
+  if (lane == 0) write_row(a, row, HD, m, l);
+}
+
+template <typename K>
+cudaError_t launch_after(K kernel, dim3 grid, int threads, size_t smem, cudaStream_t st, bool early, const AttendArgs &a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename T, int HD, bool FP8>
+cudaError_t launch_rows(const AttendArgs &a, cudaStream_t st) {
+  constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroup * HD * (FP8 ? 1 : 2);
+  constexpr size_t join = (size_t)kWarps * 16 * (HD + 4) * 4;
+  constexpr size_t smem = ring > join ? ring : join;
+  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  e = launch_after(attend_rows_kernel<T, HD, FP8>, dim3(a.prefix_items + a.own_items), kWarps * 32, smem, st, false, a);
+  if (e != cudaSuccess || a.prefix_splits + a.own_splits == 1) return e;
+  const int64_t rows = (int64_t)a.n_seqs * a.q_len * a.n_q_heads;
+  return launch_after(attend_join_kernel<T, HD>, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, a);
+}
+
+template <typename T, bool FP8>
+cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
+  switch (a.c.head_dim) {
+    case 32: return launch_rows<T, 32, FP8>(a, st);
+    case 64: return launch_rows<T, 64, FP8>(a, st);
+    case 128: return launch_rows<T, 128, FP8>(a, st);
+    case 256: return launch_rows<T, 256, FP8>(a, st);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int64_t own_max, int prefix_len) {
+  AttendShape s{};
+  const int64_t want = 4 * kSms;   // items: two blocks an SM, twice over
+  s.seq_rows = q_len * (n_q_heads / n_heads);
+  const auto cut = [&](int64_t tiles, int64_t tokens, int64_t least, int32_t &splits, int32_t &chunk) {
+    int64_t n = (want + tiles - 1) / tiles;
+    n = n < 1 ? 1 : n;
+    const int64_t most = (tokens + least - 1) / least;
+    n = n > most ? most : n;
+    n = n > 64 ? 64 : n < 1 ? 1 : n;
+    int64_t c = ((tokens + n - 1) / n + 63) / 64 * 64;   // whole steps of the four warps
+    c = c ? c : 64;
+    chunk = (int32_t)c;
+    splits = tokens ? (int32_t)((tokens + c - 1) / c) : 1;
+  };
+  if (prefix_len > 0) {
+    const int64_t tiles = (int64_t)n_heads * (((int64_t)n_seqs * s.seq_rows + 15) / 16);
+    cut(tiles, prefix_len, 128, s.prefix_splits, s.prefix_chunk);
+    s.prefix_items = tiles * s.prefix_splits;
+  }
+  if (own_max > 0 || prefix_len == 0) {   // without any token there still is an (empty) item a row tile
+    const int64_t tiles = (int64_t)n_heads * n_seqs * ((s.seq_rows + 15) / 16);
+    cut(tiles, own_max, 128, s.own_splits, s.own_chunk);
+    s.own_items = tiles * s.own_splits;
+  }
+  const int64_t rows = (int64_t)n_seqs * q_len * n_q_heads, slots = s.prefix_splits + s.own_splits;
+  s.parts = slots > 1 ? rows * slots : 0;
+  return s;
+}
+
+cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st) {
+  if (type == EMOE_TYPE_E4M3)
+    return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, st) : by_head_dim<__half, true>(a, st);
+  return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, st) : by_head_dim<__half, false>(a, st);
+}
+
+}  // namespace emoe

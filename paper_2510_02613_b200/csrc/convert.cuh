@@ -1,0 +1,94 @@
+// convert.cuh - 16-bit pairs and e4m3 codes as tensor-core operands.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace emoe {
+
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *(const uint32_t *)&h;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t x) {
+    return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+  }
+};
+template <> struct Pair<__half> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *(const uint32_t *)&h;
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*(const __half2 *)&x); }
+};
+
+// Two e4m3 codes in the upper bytes of the two halves of `x` (whatever is in the lower bytes) as a
+// pair of T, exactly.  bf16: the code's 7 magnitude bits, moved to the right place, are a bf16 whose
+// exponent is 120 too small (denormal codes become denormal bf16), so one packed product by 2^120
+// finishes it.  f16: likewise with 2^8.  The NaN code reads as 480; a vector that is not a number is
+// told by its scale.
+template <typename T> __device__ __forceinline__ uint32_t codes_to_pair(uint32_t x);
+template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uint32_t x) {
+  const uint32_t y = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
+  const uint32_t big = 0x7b807b80u;  // 2^120 twice
+  const __nv_bfloat162 r = __hmul2(*(const __nv_bfloat162 *)&y, *(const __nv_bfloat162 *)&big);
+  return *(const uint32_t *)&r;
+}
+template <> __device__ __forceinline__ uint32_t codes_to_pair<__half>(uint32_t x) {
+  const uint32_t y = ((x >> 1) & 0x3f803f80u) | (x & 0x80008000u);
+  const uint32_t big = 0x5c005c00u;  // 2^8 twice
+  const __half2 r = __hmul2(*(const __half2 *)&y, *(const __half2 *)&big);
+  return *(const uint32_t *)&r;
+}
+// Bytes 0 and 2 of a word of four codes as a pair; bytes 1 and 3.
+template <typename T> __device__ __forceinline__ uint32_t even_codes(uint32_t w) { return codes_to_pair<T>(w << 8); }
+template <typename T> __device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return codes_to_pair<T>(w); }
+
+// d += a b: a 16 x 16 (rows), b 16 x 8 (columns), 32-bit sums.
+template <typename T>
+__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && __is_same(T, __half)) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  } else {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {  // 2 units in the last place; -inf gives 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes global -> shared; `bytes` of them are read (0 or 16), the rest is zero.
+__device__ __forceinline__ void copy_async_16(uint32_t dst, const void *src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
+// Programmatic dependent launch: let the next kernel of the stream start its own prologue; wait
+// until the kernels before have finished and their results can be read.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+}  // namespace emoe

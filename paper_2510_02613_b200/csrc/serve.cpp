@@ -107,6 +107,21 @@ emoe_status_t check_copy(const emoe_kv_cache_t *c, int32_t layer, const void *k,
   return on_current_device(c->arena);
 }
 
+constexpr double kLog2e = 1.4426950408889634;
+
+emoe_status_t check_attend_sizes(const emoe_kv_cache_t *c, int64_t n_seqs, int64_t q_len, int64_t hq, int64_t max_blocks,
+                                 int64_t prefix_len) {
+  if (n_seqs < 0 || q_len <= 0 || hq <= 0 || max_blocks < 0 || prefix_len < 0 || hq % c->n_heads) return EMOE_ERR_SHAPE;
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return EMOE_ERR_UNSUPPORTED;
+  // row and token numbers are kept in 32 bits
+  if (q_len > 1 << 20 || hq > 1 << 20 || n_seqs > 1 << 24 || n_seqs * q_len >= 1 << 24 || n_seqs * q_len * hq >= 1 << 28 ||
+      max_blocks * c->block_tokens >= 1 << 30 || prefix_len >= 1 << 30)
+    return EMOE_ERR_TOO_LARGE;
+  return EMOE_OK;
+}
+
+uint64_t up_256(uint64_t n) { return (n + 255) / 256 * 256; }
+
 }  // namespace
 
 extern "C" {
@@ -142,6 +157,73 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *c, int32_t layer, const int6
   const emoe_status_t st = check_copy(c, layer, k, v, ks, vs, out_type, slots, n);
   if (st != EMOE_OK || n == 0) return st;
   return cuda_status(launch_kv_gather(layer_of(c, layer), c->type, slots, n, k, v, ks, vs, out_type, (cudaStream_t)stream));
+}
+
+emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t q_len, int32_t n_q_heads,
+                                       int32_t max_blocks, int32_t prefix_len, uint64_t *bytes) {
+  emoe_status_t st = check_cache(c);
+  if (st == EMOE_OK && !bytes) st = EMOE_ERR_INVALID_ARG;
+  if (st == EMOE_OK) st = check_attend_sizes(c, n_seqs, q_len, n_q_heads, max_blocks, prefix_len);
+  if (st != EMOE_OK) return st;
+  *bytes = 0;
+  if (n_seqs == 0) return EMOE_OK;
+  const AttendShape s = attend_shape(c->n_heads, n_seqs, q_len, n_q_heads, (int64_t)max_blocks * c->block_tokens, prefix_len);
+  *bytes = up_256(s.parts * sizeof(float2)) + up_256(s.parts * c->head_dim * sizeof(float));
+  return EMOE_OK;
+}
+
+emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe_attend_t *p, void *stream) {
+  TraceRange trace("emoe_kv_attend");
+  emoe_status_t st = check_cache_memory(c, layer);
+  if (st != EMOE_OK) return st;
+  if (!p || p->reserved) return EMOE_ERR_INVALID_ARG;
+  if (p->io_type != EMOE_TYPE_BF16 && p->io_type != EMOE_TYPE_F16) return EMOE_ERR_INVALID_ARG;
+  if (c->type != EMOE_TYPE_E4M3 && c->type != p->io_type) return EMOE_ERR_UNSUPPORTED;
+  st = check_attend_sizes(c, p->n_seqs, p->q_len, p->n_q_heads, p->max_blocks, p->prefix_len);
+  if (st != EMOE_OK || p->n_seqs == 0) return st;
+  if (!p->q || !p->out || (p->max_blocks && (!p->block_table || !p->own_lens)) || (p->prefix_len && !p->prefix_table))
+    return EMOE_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)p->n_q_heads * c->head_dim, tokens = (int64_t)p->n_seqs * p->q_len;
+  if (tokens > 1 && (p->q_stride < row || p->out_stride < row)) return EMOE_ERR_SHAPE;
+  if (!aligned(p->q, 16) || !aligned(p->out, 16) || !aligned(p->lse, 4) || !aligned(p->block_table, 4) ||
+      !aligned(p->own_lens, 4) || !aligned(p->prefix_table, 4) || !aligned(p->workspace, 256))
+    return EMOE_ERR_ALIGNMENT;
+  if (tokens > 1 && (p->q_stride % 8 || p->out_stride % 8)) return EMOE_ERR_ALIGNMENT;
+  const AttendShape s = attend_shape(c->n_heads, p->n_seqs, p->q_len, p->n_q_heads, (int64_t)p->max_blocks * c->block_tokens,
+                                     p->prefix_len);
+  const uint64_t ml = up_256(s.parts * sizeof(float2)), need = ml + up_256(s.parts * c->head_dim * sizeof(float));
+  if (need && (!p->workspace || p->workspace_bytes < need)) return EMOE_ERR_INVALID_ARG;
+  if (s.prefix_items + s.own_items >= (int64_t)1 << 31) return EMOE_ERR_TOO_LARGE;
+  st = on_current_device(c->arena);
+  if (st != EMOE_OK) return st;
+  AttendArgs a{};
+  a.c = layer_of(c, layer);
+  a.num_blocks = c->num_blocks;
+  a.q = p->q;
+  a.out = p->out;
+  a.lse = p->lse;
+  a.q_stride = tokens > 1 ? p->q_stride : row;
+  a.out_stride = tokens > 1 ? p->out_stride : row;
+  a.block_table = p->block_table;
+  a.own_lens = p->own_lens;
+  a.prefix_table = p->prefix_table;
+  a.part_ml = (float2 *)p->workspace;
+  a.part_o = (float *)((uint8_t *)p->workspace + ml);
+  a.n_seqs = p->n_seqs;
+  a.q_len = p->q_len;
+  a.n_q_heads = p->n_q_heads;
+  a.group = p->n_q_heads / c->n_heads;
+  a.max_blocks = p->max_blocks;
+  a.prefix_len = p->prefix_len;
+  a.scale_log2 = (float)(p->scale * kLog2e);
+  a.seq_rows = s.seq_rows;
+  a.prefix_splits = s.prefix_splits;
+  a.prefix_chunk = s.prefix_chunk;
+  a.own_splits = s.own_splits;
+  a.own_chunk = s.own_chunk;
+  a.prefix_items = (uint32_t)s.prefix_items;
+  a.own_items = (uint32_t)s.own_items;
+  return cuda_status(launch_attend(a, c->type, p->io_type, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -36,6 +36,33 @@ cudaError_t launch_kv_append(const KvLayer &c, int type, const void *k, const vo
 cudaError_t launch_kv_gather(const KvLayer &c, int type, const int64_t *slots, int n, void *k, void *v,
                              int64_t ks, int64_t vs, int out_type, cudaStream_t st);
 
+// How attention is cut: a function of what the caller knows on the host.
+struct AttendShape {
+  int32_t seq_rows;                     // rows of one sequence and KV head: q_len * query heads per KV head
+  int32_t prefix_splits, prefix_chunk;  // token ranges of the prefix, tokens of each
+  int32_t own_splits, own_chunk;
+  int64_t prefix_items, own_items;
+  int64_t parts;                        // (row, split) pairs that go through the workspace; 0: none
+};
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int64_t own_max, int prefix_len);
+
+struct AttendArgs {
+  KvLayer c;
+  int32_t num_blocks;
+  const void *q;
+  void *out;
+  float *lse;
+  int64_t q_stride, out_stride;         // elements from one query token to the next
+  const int32_t *block_table, *own_lens, *prefix_table;
+  float2 *part_ml;                      // [row][split]: maximum (log2) and sum
+  float *part_o;                        // [row][split][head_dim]
+  int32_t n_seqs, q_len, n_q_heads, group, max_blocks, prefix_len;
+  float scale_log2;
+  int32_t seq_rows, prefix_splits, prefix_chunk, own_splits, own_chunk;
+  uint32_t prefix_items, own_items;
+};
+cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
+
 constexpr int kSms = 148;  // streaming multiprocessors of a B200: launch shapes are made for it
 
 }  // namespace emoe

@@ -133,3 +133,41 @@ class KvCache:
         """Reads slots back into k and v; rows of negative slots stay as they were."""
         n, kp, ks, vp, vs, t = self._copy_args(k, v, slots)
         _check(_b.lib().emoe_kv_gather(self._ref, layer, slots.data_ptr(), n, kp, vp, ks, vs, t, _stream_handle(stream)))
+
+    def attend_workspace_bytes(self, n_seqs: int, q_len: int, n_q_heads: int, max_blocks: int, prefix_len: int = 0) -> int:
+        n = ctypes.c_uint64()
+        _check(_b.lib().emoe_kv_attend_workspace(self._ref, n_seqs, q_len, n_q_heads, max_blocks, prefix_len, ctypes.byref(n)))
+        return n.value
+
+    def attend(self, layer: int, q, out, block_table, own_lens, prefix_table=None, prefix_len: int = 0,
+               scale: Optional[float] = None, lse=None, workspace=None, stream=None) -> None:
+        """Decode attention: q, out [n_seqs, q_len, n_q_heads, head_dim] (any stride between tokens); own
+        tokens on the blocks of block_table [n_seqs, max_blocks] (int32), own_lens [n_seqs] of them (int32,
+        the query tokens included; both None: prefix only); prefix_len tokens on the blocks of
+        prefix_table, shared by all sequences.  workspace: attend_workspace_bytes bytes of the caller's,
+        not shared by calls that can overlap.  lse: optional float32 [n_seqs, q_len, n_q_heads]."""
+        n, t, hq, _ = q.shape
+        _shaped(q, "q", (None, None, None, self.head_dim), None, self.device)
+        _shaped(out, "out", q.shape, str(q.dtype)[6:], self.device)
+        p = _b._Attend(q=q.data_ptr(), out=out.data_ptr(), n_seqs=n, q_len=t, n_q_heads=hq, prefix_len=prefix_len,
+                       io_type=_value_type(q, "q"), scale=self.head_dim ** -0.5 if scale is None else scale)
+        for x, what, field in ((q, "q", "q_stride"), (out, "out", "out_stride")):
+            _dense(x, what, 2)
+            stride = x.stride(1) if t > 1 else x.stride(0) if n > 1 else hq * self.head_dim
+            if t > 1 and n > 1 and x.stride(0) != t * stride:
+                raise ValueError("%s: sequences have to follow one another at the stride of the tokens" % what)
+            setattr(p, field, stride)
+        if block_table is not None or own_lens is not None:
+            _dense(_shaped(block_table, "block_table", (n, None), "int32", self.device), "block_table", 2)
+            _dense(_shaped(own_lens, "own_lens", (n,), "int32", self.device), "own_lens", 1)
+            p.max_blocks, p.block_table, p.own_lens = block_table.shape[1], block_table.data_ptr(), own_lens.data_ptr()
+        if prefix_len > 0:
+            _dense(_shaped(prefix_table, "prefix_table", (None,), "int32", self.device), "prefix_table", 1)
+            if prefix_table.shape[0] * self.block_tokens < prefix_len:
+                raise ValueError("prefix_table: %d blocks hold fewer than %d tokens" % (prefix_table.shape[0], prefix_len))
+            p.prefix_table = prefix_table.data_ptr()
+        if lse is not None:
+            p.lse = _dense(_shaped(lse, "lse", (n, t, hq), "float32", self.device), "lse", 3).data_ptr()
+        if workspace is not None:
+            p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(_b.lib().emoe_kv_attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))

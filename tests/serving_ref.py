@@ -73,11 +73,15 @@ class Cache:
 
 
 def attend(cache, layer, q, table, own_lens, prefix_table, prefix_len, scale):
-    """q [n, t, Hq, hd] -> (o, lse) in 64 bits; tokens on blocks outside the pool are left out."""
+    """q [n, t, Hq, hd] -> (o, lse, a, e) in 64 bits; tokens on blocks outside the pool are left out.
+    a = sum_j softmax_j |v_j| and e = bound of a score's error for the tolerance: a sum of hd products
+    in 32 bits is off by at most hd * 2^-23 (truncating adders) of the sum of their magnitudes, the sums
+    over n tokens by n * 2^-23 of theirs, and the exponential adds a few 2^-22."""
     n, t, hq, hd = q.shape
     heads, block = cache.dims[4], cache.dims[3]
     group = hq // heads
     o, lse = np.zeros(q.shape), np.full(q.shape[:3], -np.inf)
+    a, err = np.zeros(q.shape), np.zeros(q.shape[:3])
 
     def rows(ids, count):
         ks, vs = [], []
@@ -103,7 +107,10 @@ def attend(cache, layer, q, table, own_lens, prefix_table, prefix_len, scale):
                 w = np.exp(score - top)
                 lse[s, i, h] = top + np.log(w.sum())
                 o[s, i, h] = (w / w.sum()) @ v[:, h // group]
-    return o, lse
+                a[s, i, h] = (w / w.sum()) @ np.abs(v[:, h // group])
+                size = np.abs(scale) * (np.abs(k[:, h // group]) @ np.abs(q[s, i, h])).max()
+                err[s, i, h] = (hd + 8) * 2.0 ** -23 * size + (len(k) + 16) * 2.0 ** -23
+    return o, lse, a, err
 
 
 def route(logits, k):

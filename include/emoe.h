@@ -899,6 +899,78 @@ emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *cache, int32_t n_s
 emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const emoe_attend_t *args,
                              void *cuda_stream);
 
+/* One rank's expert arena, laid out as emoe_reshard_experts moves it:
+ *     [n_layers][3 (gate, up, down)][n_slots][matrix]        (or EMOE_LAYOUT_FUSED_W13)
+ * gate and up matrices are [d_ff][d_model], down matrices [d_model][d_ff], row-major: a row
+ * holds the weights of one output.  matrix_stride: bytes from one matrix to the next where
+ * that is more than the matrix (the slabs of the paged stores), 0 for a dense arena; arenas
+ * with spare slots (emoe_plan_create_inplace) have their capacity as n_slots.  EMOE_TYPE_E4M3:
+ * the arena of a plan with expert_scale_bytes - behind the weights, from the next multiple of
+ * 256 bytes on, [n_layers][3][n_slots] scale tensors, one fp32 per 128 x 128 block of the matrix,
+ * [ceil(rows / 128)][ceil(columns / 128)]: weight = code * scale. */
+typedef struct {
+  const void *arena;      /* 16-byte aligned                                              */
+  int32_t *status;        /* optional int32: set to EMOE_ERR_PLACEMENT by a call that met a */
+                          /* slot beyond n_slots (never cleared)                          */
+  uint64_t matrix_stride; /* 0, or a multiple of 16 (16-bit types, not FUSED_W13)           */
+  int32_t n_layers;
+  int32_t n_slots;        /* at most EMOE_MOE_MAX_SLOTS                                    */
+  int32_t d_model, d_ff;  /* multiples of 16 (EMOE_ERR_UNSUPPORTED)                         */
+  int32_t type;           /* EMOE_TYPE_BF16, _F16 or _E4M3                                 */
+  uint32_t layout;        /* 0 or EMOE_LAYOUT_FUSED_W13                                   */
+  uint32_t reserved;      /* zero                                                         */
+} emoe_expert_arena_t;
+#define EMOE_MOE_MAX_TOKENS 64    /* more: EMOE_ERR_TOO_LARGE, as for the other three        */
+#define EMOE_MOE_MAX_EXPERTS 1024
+#define EMOE_MOE_MAX_CHOSEN 32    /* top_k + n_shared                                       */
+#define EMOE_MOE_MAX_SLOTS 4096
+
+/* Bytes of such an arena.  Host only. */
+emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *experts, uint64_t *bytes);
+
+/*
+ * emoe_moe_decode - a mixture-of-experts layer for up to EMOE_MOE_MAX_TOKENS tokens, from the
+ * router's logits to the weighted sum:
+ *     y_t = sum_e w_te * Wdown_e (silu(Wgate_e x_t) * (Wup_e x_t))
+ * over the top_k experts of the token's largest logits (equal logits: the lower id first;
+ * minus infinity and NaN are never chosen) with w_te = softmax over all n_experts logits, divided
+ * by the chosen ones' sum if EMOE_MOE_RENORMALIZE, times routed_scale; and over the n_shared
+ * shared experts with weight 1.
+ * slot_of_expert [n_experts + n_shared]: slot of each routed, then each shared expert in this
+ * arena, -1 for experts that this call leaves out: on an expert-parallel rank those of other
+ * ranks (a replicated one, routed or shared, is given to one rank's call).  Entries are
+ * distinct where not negative.  The ranks' outputs are summed by the caller; out_type
+ * EMOE_TYPE_F32 leaves that sum to be rounded once.
+ * Only the chosen experts' weights are read, each once for all tokens.  Sums are 32-bit; the
+ * hidden vector w * silu(gate) * up is rounded once to io_type as the last product's operand
+ * (beyond the range of F16: its largest value).  The result does not depend on timing.
+ * A row of logits with nothing above minus infinity chooses no routed expert.
+ */
+#define EMOE_MOE_RENORMALIZE 1u
+typedef struct {
+  const void *x;                  /* [n_tokens][d_model] of io_type, 16-byte aligned          */
+  const float *logits;            /* [n_tokens][n_experts]                                   */
+  const int32_t *slot_of_expert;
+  void *out;                      /* [n_tokens][d_model] of out_type                         */
+  int32_t *ids_out;               /* optional [n_tokens][top_k]: chosen ids, best first, -1    */
+  float *weights_out;             /* optional [n_tokens][top_k]: w, 0 beside -1                */
+  void *workspace;                /* emoe_moe_decode_workspace bytes                          */
+  uint64_t workspace_bytes;       /* (too few: EMOE_ERR_INVALID_ARG)                          */
+  int64_t x_stride;               /* elements from one token to the next, a multiple of 8      */
+  int64_t logits_stride, out_stride;
+  int32_t n_tokens, n_experts, n_shared, top_k;
+  int32_t io_type;                /* the arena's 16-bit type; BF16 or F16 for e4m3            */
+  int32_t out_type;               /* io_type or EMOE_TYPE_F32                                */
+  uint32_t flags;                 /* 0 or EMOE_MOE_RENORMALIZE                               */
+  float routed_scale;             /* usually 1                                              */
+  uint32_t reserved;              /* zero                                                    */
+} emoe_moe_t;
+emoe_status_t emoe_moe_decode_workspace(const emoe_expert_arena_t *experts, int32_t n_tokens,
+                                        int32_t top_k, int32_t n_experts, int32_t n_shared,
+                                        uint64_t *bytes);
+emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *experts, int32_t layer,
+                              const emoe_moe_t *args, void *cuda_stream);
+
 /* Static string for a status code. */
 const char *emoe_strerror(emoe_status_t status);
 

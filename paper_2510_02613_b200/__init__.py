@@ -6,9 +6,9 @@ from .binding import (EXPORTS, MAX_RANKS, PHASE_ATTN, PHASE_EXPERTS, PHASE_KV, P
                       SEGMENT_DTYPE, SIDE_NEW, SIDE_OLD, EmoeError, InplacePlan, Plan, PlanCache, VmmPool, VmmSlots, kv_compact_table, segments_validate, lib, library_path,
                       strerror, vmm_dry_run, ipc_export, ipc_open, ipc_close,
                       place_min_transfer)
-from .serving import KvCache
+from .serving import ExpertArena, KvCache
 
 __all__ = ["EXPORTS", "MAX_RANKS", "PHASE_ATTN", "PHASE_EXPERTS", "PHASE_KV", "PHASE_STEP", "PLAN_HOST_ONLY", "PLAN_HOST_STEP",
            "SEGMENT_DTYPE", "SIDE_NEW", "SIDE_OLD", "EmoeError", "InplacePlan", "Plan", "PlanCache", "kv_compact_table", "segments_validate", "VmmPool", "VmmSlots", "lib", "library_path",
            "strerror", "vmm_dry_run", "ipc_export", "ipc_open", "ipc_close", "place_min_transfer",
-           "KvCache"]
+           "ExpertArena", "KvCache"]

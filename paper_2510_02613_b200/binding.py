@@ -84,6 +84,19 @@ class _Attend(ctypes.Structure):
                [("scale", ctypes.c_float), ("reserved", _u32)]
 
 
+class _ExpertArena(ctypes.Structure):
+    _fields_ = [("arena", _vp), ("status", _vp), ("matrix_stride", _u64)] + \
+               [(n, _i32) for n in ("n_layers", "n_slots", "d_model", "d_ff", "type")] + \
+               [("layout", _u32), ("reserved", _u32)]
+
+
+class _Moe(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("x", "logits", "slot_of_expert", "out", "ids_out", "weights_out", "workspace")] + \
+               [("workspace_bytes", _u64)] + [(n, ctypes.c_int64) for n in ("x_stride", "logits_stride", "out_stride")] + \
+               [(n, _i32) for n in ("n_tokens", "n_experts", "n_shared", "top_k", "io_type", "out_type")] + \
+               [("flags", _u32), ("routed_scale", ctypes.c_float), ("reserved", _u32)]
+
+
 SEGMENT_DTYPE = np.dtype([("src_off", "<u8"), ("dst_off", "<u8"), ("run_bytes", "<u8"),
                           ("src_pitch", "<u8"), ("dst_pitch", "<u8"), ("n_runs", "<u4"),
                           ("src_rank", "<u4"), ("dst_rank", "<u4"), ("group", "<u4")])
@@ -105,7 +118,8 @@ EXPORTS = ("emoe_plan_create", "emoe_plan_create_ex", "emoe_reshard_experts", "e
            "emoe_vmm_slots_create", "emoe_vmm_slots_reshard", "emoe_vmm_slots_info", "emoe_vmm_slots_write",
            "emoe_vmm_slots_read", "emoe_vmm_slots_destroy",
            "emoe_kv_cache_bytes", "emoe_kv_vector_index", "emoe_kv_append", "emoe_kv_gather",
-           "emoe_kv_attend_workspace", "emoe_kv_attend")
+           "emoe_kv_attend_workspace", "emoe_kv_attend",
+           "emoe_expert_arena_bytes", "emoe_moe_decode_workspace", "emoe_moe_decode")
 
 _lib: Optional[ctypes.CDLL] = None
 
@@ -232,11 +246,14 @@ def lib() -> ctypes.CDLL:
         f.argtypes = [_vp, _i32, _i32, _vp, _vp]
     L.emoe_vmm_slots_destroy.restype = None
     L.emoe_vmm_slots_destroy.argtypes = [_vp]
-    cache, i64 = ctypes.POINTER(_KvCache), ctypes.c_int64
+    cache, experts, i64 = ctypes.POINTER(_KvCache), ctypes.POINTER(_ExpertArena), ctypes.c_int64
     for name, args in (("emoe_kv_cache_bytes", [cache, ctypes.POINTER(_u64), ctypes.POINTER(_u64)]),
                        ("emoe_kv_append", [cache, _i32, _vp, _vp, i64, i64, _i32, _vp, _i32, _vp]),
                        ("emoe_kv_attend_workspace", [cache, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
                        ("emoe_kv_attend", [cache, _i32, ctypes.POINTER(_Attend), _vp]),
+                       ("emoe_expert_arena_bytes", [experts, ctypes.POINTER(_u64)]),
+                       ("emoe_moe_decode_workspace", [experts, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
+                       ("emoe_moe_decode", [experts, _i32, ctypes.POINTER(_Moe), _vp]),
                        ("emoe_kv_gather", [cache, _i32, _vp, _i32, _vp, _vp, i64, i64, _i32, _vp])):
         f = getattr(L, name)
         f.restype = _i32

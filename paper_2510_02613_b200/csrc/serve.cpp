@@ -122,6 +122,34 @@ emoe_status_t check_attend_sizes(const emoe_kv_cache_t *c, int64_t n_seqs, int64
 
 uint64_t up_256(uint64_t n) { return (n + 255) / 256 * 256; }
 
+// Sizes, type and layout of an expert arena; pointers apart.
+emoe_status_t check_experts(const emoe_expert_arena_t *e) {
+  if (!e || e->reserved || (e->layout & ~EMOE_LAYOUT_FUSED_W13)) return EMOE_ERR_INVALID_ARG;
+  if (e->type != EMOE_TYPE_BF16 && e->type != EMOE_TYPE_F16 && e->type != EMOE_TYPE_E4M3) return EMOE_ERR_INVALID_ARG;
+  if (e->n_layers <= 0 || e->n_slots <= 0 || e->d_model <= 0 || e->d_ff <= 0) return EMOE_ERR_SHAPE;
+  if (e->d_model % 16 || e->d_ff % 16) return EMOE_ERR_UNSUPPORTED;
+  if (e->n_slots > EMOE_MOE_MAX_SLOTS || e->d_model > 1 << 20 || e->d_ff > 1 << 20) return EMOE_ERR_TOO_LARGE;
+  const int64_t m = (int64_t)e->d_model * e->d_ff * type_bytes(e->type);
+  if (e->matrix_stride) {
+    if (e->layout || e->type == EMOE_TYPE_E4M3) return EMOE_ERR_UNSUPPORTED;
+    if (e->matrix_stride < (uint64_t)m || e->matrix_stride > (uint64_t)1 << 42) return EMOE_ERR_SHAPE;
+    if (e->matrix_stride % 16) return EMOE_ERR_ALIGNMENT;
+  }
+  const unsigned __int128 total = (unsigned __int128)e->n_layers * 3 * e->n_slots * (e->matrix_stride ? e->matrix_stride : m);
+  return total >> 61 ? EMOE_ERR_SHAPE : EMOE_OK;
+}
+
+int64_t scale_floats(const emoe_expert_arena_t *e) {
+  return (int64_t)((e->d_model + 127) / 128) * ((e->d_ff + 127) / 128);
+}
+
+emoe_status_t check_moe_sizes(const emoe_expert_arena_t *e, int64_t n_tokens, int64_t top_k, int64_t n_experts, int64_t n_shared) {
+  if (n_tokens < 0 || top_k <= 0 || n_experts <= 0 || n_shared < 0 || top_k > n_experts) return EMOE_ERR_SHAPE;
+  if (n_tokens > EMOE_MOE_MAX_TOKENS || n_experts > EMOE_MOE_MAX_EXPERTS || top_k + n_shared > EMOE_MOE_MAX_CHOSEN)
+    return EMOE_ERR_TOO_LARGE;
+  return EMOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -224,6 +252,101 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   a.prefix_items = (uint32_t)s.prefix_items;
   a.own_items = (uint32_t)s.own_items;
   return cuda_status(launch_attend(a, c->type, p->io_type, (cudaStream_t)stream));
+}
+
+emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *e, uint64_t *bytes) {
+  const emoe_status_t st = check_experts(e);
+  if (st != EMOE_OK) return st;
+  if (!bytes) return EMOE_ERR_INVALID_ARG;
+  const uint64_t matrices = 3ull * e->n_layers * e->n_slots;
+  const uint64_t m = (uint64_t)e->d_model * e->d_ff * type_bytes(e->type);
+  *bytes = matrices * (e->matrix_stride ? e->matrix_stride : m);
+  if (e->type == EMOE_TYPE_E4M3) *bytes = up_256(*bytes) + matrices * scale_floats(e) * 4;
+  return EMOE_OK;
+}
+
+emoe_status_t emoe_moe_decode_workspace(const emoe_expert_arena_t *e, int32_t n_tokens, int32_t top_k, int32_t n_experts,
+                                        int32_t n_shared, uint64_t *bytes) {
+  emoe_status_t st = check_experts(e);
+  if (st == EMOE_OK && !bytes) st = EMOE_ERR_INVALID_ARG;
+  if (st == EMOE_OK) st = check_moe_sizes(e, n_tokens, top_k, n_experts, n_shared);
+  if (st != EMOE_OK) return st;
+  *bytes = n_tokens ? moe_shape(e->n_slots, e->d_ff, n_tokens, top_k, n_shared).bytes : 0;
+  return EMOE_OK;
+}
+
+emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const emoe_moe_t *p, void *stream) {
+  TraceRange trace("emoe_moe_decode");
+  emoe_status_t st = check_experts(e);
+  if (st != EMOE_OK) return st;
+  if (!p || p->reserved || (p->flags & ~EMOE_MOE_RENORMALIZE) || layer < 0 || layer >= e->n_layers || !e->arena)
+    return EMOE_ERR_INVALID_ARG;
+  if (p->io_type != EMOE_TYPE_BF16 && p->io_type != EMOE_TYPE_F16) return EMOE_ERR_INVALID_ARG;
+  if (p->out_type != p->io_type && p->out_type != EMOE_TYPE_F32) return EMOE_ERR_INVALID_ARG;
+  if (e->type != EMOE_TYPE_E4M3 && e->type != p->io_type) return EMOE_ERR_UNSUPPORTED;
+  st = check_moe_sizes(e, p->n_tokens, p->top_k, p->n_experts, p->n_shared);
+  if (st != EMOE_OK || p->n_tokens == 0) return st;
+  if (!p->x || !p->logits || !p->slot_of_expert || !p->out || !p->workspace) return EMOE_ERR_INVALID_ARG;
+  const MoeShape s = moe_shape(e->n_slots, e->d_ff, p->n_tokens, p->top_k, p->n_shared);
+  if (p->workspace_bytes < (uint64_t)s.bytes) return EMOE_ERR_INVALID_ARG;
+  const bool many = p->n_tokens > 1;
+  if (many && (p->x_stride < e->d_model || p->out_stride < e->d_model || p->logits_stride < p->n_experts)) return EMOE_ERR_SHAPE;
+  if (!aligned(e->arena, 16) || !aligned(e->status, 4) || !aligned(p->x, 16) || !aligned(p->logits, 4) ||
+      !aligned(p->slot_of_expert, 4) || !aligned(p->out, type_bytes(p->out_type)) || !aligned(p->ids_out, 4) ||
+      !aligned(p->weights_out, 4) || !aligned(p->workspace, 256) || (many && p->x_stride % 8))
+    return EMOE_ERR_ALIGNMENT;
+  st = on_current_device(e->arena);
+  if (st != EMOE_OK) return st;
+
+  MoeArgs a{};
+  const int64_t m = (int64_t)e->d_model * e->d_ff * type_bytes(e->type), stride = e->matrix_stride ? (int64_t)e->matrix_stride : m;
+  const uint8_t *base = (const uint8_t *)e->arena + (int64_t)layer * 3 * e->n_slots * stride;
+  if (e->layout & EMOE_LAYOUT_FUSED_W13) {
+    a.gate = base;
+    a.up = base + m;
+    a.down = base + 2 * e->n_slots * m;
+    a.gate_stride = 2 * m;
+    a.down_stride = m;
+  } else {
+    a.gate = base;
+    a.up = base + e->n_slots * stride;
+    a.down = base + 2 * e->n_slots * stride;
+    a.gate_stride = a.down_stride = stride;
+  }
+  if (e->type == EMOE_TYPE_E4M3) {
+    const int64_t per = scale_floats(e);
+    const float *scales = (const float *)((const uint8_t *)e->arena + up_256(3ull * e->n_layers * e->n_slots * m));
+    a.gate_scale = scales + (int64_t)layer * 3 * e->n_slots * per;
+    a.up_scale = a.gate_scale + e->n_slots * per;
+    a.down_scale = a.up_scale + e->n_slots * per;
+    a.scale_stride = per;
+  }
+  uint8_t *const work = (uint8_t *)p->workspace;
+  a.x = p->x;
+  a.logits = p->logits;
+  a.slot_of_expert = p->slot_of_expert;
+  a.out = p->out;
+  a.ids_out = p->ids_out;
+  a.weights_out = p->weights_out;
+  a.status = e->status;
+  a.x_stride = many ? p->x_stride : e->d_model;
+  a.logits_stride = many ? p->logits_stride : p->n_experts;
+  a.out_stride = many ? p->out_stride : e->d_model;
+  a.n_active = (int32_t *)work;
+  a.active = (MoeActive *)(work + s.active);
+  a.pair_token = (int32_t *)(work + s.token);
+  a.pair_weight = (float *)(work + s.weight);
+  a.h = work + s.h;
+  a.n_slots = e->n_slots;
+  a.d_model = e->d_model;
+  a.d_ff = e->d_ff;
+  a.n_tokens = p->n_tokens;
+  a.n_experts = p->n_experts;
+  a.n_shared = p->n_shared;
+  a.top_k = p->top_k;
+  a.renormalize = (p->flags & EMOE_MOE_RENORMALIZE) != 0;
+  a.routed_scale = p->routed_scale;
+  return cuda_status(launch_moe(a, e->type, p->io_type, p->out_type == EMOE_TYPE_F32, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -63,6 +63,41 @@ struct AttendArgs {
 };
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
+// An expert in use: its tokens as a bit mask; its pairs are numbered from `base` in token order.
+struct __align__(16) MoeActive {
+  uint64_t tokens;
+  int32_t slot, base;
+};
+
+// Byte offsets of a layer call's workspace.
+struct MoeShape {
+  int64_t active, token, weight, h, bytes;
+};
+MoeShape moe_shape(int n_slots, int d_ff, int n_tokens, int top_k, int n_shared);
+
+struct MoeArgs {
+  const uint8_t *gate, *up, *down;                        // slot 0 of the layer
+  int64_t gate_stride, down_stride;                       // bytes from slot to slot
+  const float *gate_scale, *up_scale, *down_scale;        // e4m3: slot 0's block scales
+  int64_t scale_stride;                                   // floats from slot to slot
+  const void *x;
+  const float *logits;
+  const int32_t *slot_of_expert;
+  void *out;
+  int32_t *ids_out;
+  float *weights_out;
+  int32_t *status;
+  int64_t x_stride, logits_stride, out_stride;            // elements
+  int32_t *n_active;                                      // workspace
+  MoeActive *active;
+  int32_t *pair_token;
+  float *pair_weight;
+  void *h;                                                // [pair][d_ff]
+  int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize;
+  float routed_scale;
+};
+cudaError_t launch_moe(const MoeArgs &a, int type, int io, bool f32_out, cudaStream_t st);
+
 constexpr int kSms = 148;  // streaming multiprocessors of a B200: launch shapes are made for it
 
 }  // namespace emoe

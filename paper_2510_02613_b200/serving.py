@@ -171,3 +171,64 @@ class KvCache:
         if workspace is not None:
             p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         _check(_b.lib().emoe_kv_attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
+
+
+class ExpertArena:
+    """One rank's expert arena: emoe_moe_decode.
+
+    arena: tensor or device address, [n_layers][3 (gate, up, down)][n_slots][matrix] as
+    emoe_reshard_experts lays it out (or fused_w13), gate and up [d_ff, d_model], down [d_model, d_ff].
+    w_type: "bf16", "f16" or "e4m3"; the last with fp32 scales per 128 x 128 block behind the weights, as
+    a plan with expert_scale_bytes moves them.  matrix_stride: bytes from matrix to matrix in the paged
+    stores (slab_bytes), 0 for a dense arena."""
+
+    def __init__(self, arena, *, n_layers: int, n_slots: int, d_model: int, d_ff: int, w_type: str = "bf16",
+                 fused_w13: bool = False, matrix_stride: int = 0, status=None):
+        self._c = _b._ExpertArena(None, None, matrix_stride, n_layers, n_slots, d_model, d_ff, _type_of(w_type),
+                                  _b.LAYOUT_FUSED_W13 if fused_w13 else 0, 0)
+        self.w_type, self.d_model, self.d_ff, self.n_slots = self._c.type, d_model, d_ff, n_slots
+        self._c.arena, self.device = _arena_pointer(arena, self.bytes(), "arena")
+        if status is not None:
+            _shaped(status, "status", (1,), "int32", self.device)
+            self._c.status = status.data_ptr()
+        self._keep = (arena, status)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def for_rank(cls, shape, n_slots: int, arena, w_type: str = "bf16", **kw) -> "ExpertArena":
+        """The arena of a rank with n_slots slots of a model `shape`, as a plan with that shape lays it out."""
+        if _TYPE_BYTES[_type_of(w_type)] != shape.elem_bytes:
+            raise ValueError("%s elements have %d bytes, the shape's %d" % (w_type, _TYPE_BYTES[_type_of(w_type)], shape.elem_bytes))
+        return cls(arena, n_layers=shape.n_layers, n_slots=n_slots, d_model=shape.d_model, d_ff=shape.d_ff, w_type=w_type, **kw)
+
+    def bytes(self) -> int:
+        n = ctypes.c_uint64()
+        _check(_b.lib().emoe_expert_arena_bytes(ctypes.byref(self._c), ctypes.byref(n)))
+        return n.value
+
+    def decode_workspace_bytes(self, n_tokens: int, top_k: int, n_experts: int, n_shared: int = 0) -> int:
+        n = ctypes.c_uint64()
+        _check(_b.lib().emoe_moe_decode_workspace(self._ref, n_tokens, top_k, n_experts, n_shared, ctypes.byref(n)))
+        return n.value
+
+    def decode(self, layer: int, x, logits, top_k: int, slot_of_expert, out, n_shared: int = 0, renormalize: bool = True,
+               routed_scale: float = 1.0, ids_out=None, weights_out=None, workspace=None, stream=None) -> None:
+        """The layer for up to 64 tokens: x [n, d_model], logits float32 [n, n_experts], slot_of_expert int32
+        [n_experts + n_shared] (-1: not in this arena), out [n, d_model] of x's type or float32 (a rank's
+        part of the sum).  ids_out int32 / weights_out float32 [n, top_k] receive the choice.  workspace:
+        decode_workspace_bytes bytes of the caller's, not shared by calls that can overlap."""
+        n, experts = logits.shape
+        _dense(_shaped(x, "x", (n, self.d_model), None, self.device), "x", 1)
+        _dense(_shaped(logits, "logits", (n, experts), "float32", self.device), "logits", 1)
+        _dense(_shaped(slot_of_expert, "slot_of_expert", (experts + n_shared,), "int32", self.device), "slot_of_expert", 1)
+        _dense(_shaped(out, "out", (n, self.d_model), None, self.device), "out", 1)
+        for t, what, dtype in ((ids_out, "ids_out", "int32"), (weights_out, "weights_out", "float32")):
+            if t is not None:
+                _dense(_shaped(t, what, (n, top_k), dtype, self.device), what, 2)
+        p = _b._Moe(x.data_ptr(), logits.data_ptr(), slot_of_expert.data_ptr(), out.data_ptr(),
+                    None if ids_out is None else ids_out.data_ptr(), None if weights_out is None else weights_out.data_ptr(),
+                    None if workspace is None else workspace.data_ptr(),
+                    0 if workspace is None else workspace.numel() * workspace.element_size(),
+                    x.stride(0), logits.stride(0), out.stride(0), n, experts, n_shared, top_k,
+                    _value_type(x, "x"), _value_type(out, "out"), 1 if renormalize else 0, routed_scale, 0)
+        _check(_b.lib().emoe_moe_decode(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))

@@ -21,19 +21,24 @@
 namespace emoe {
 namespace {
 
-constexpr int kRouteThreads = 1024, kWarps = 8;
+constexpr int kRouteThreads = 1024, kUpWarps = 8;
 
-// Order of logits: larger value first, then the smaller index; NaN as minus infinity.
-__device__ __forceinline__ uint64_t rank_key(float v, int e) {
-  if (v != v) v = -CUDART_INF_F;
+// Logits as unsigned numbers in the same order; NaN counts as minus infinity, and minus infinity and
+// what has been chosen already as 0.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  if (!(v > -CUDART_INF_F)) return 0;
   const uint32_t b = __float_as_uint(v);
-  const uint32_t ordered = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return (uint64_t)ordered << 32 | (uint32_t)~e;
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-constexpr uint32_t kLowest = 0x007fffffu;   // minus infinity's place in that order
+__device__ __forceinline__ float value_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
 
+// One block.  A warp takes tokens warp and warp + 32: its lanes hold the token's logits in registers,
+// each choice is a maximum over the lanes and then the smallest index that has it.  N: experts a lane.
+template <int N>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_constant__ MoeArgs a) {
-  extern __shared__ unsigned long long s_tokens[];   // [n_slots]
+  extern __shared__ unsigned long long s_tokens[];   // [n_slots]: which tokens an expert has
   int32_t *const s_base = (int32_t *)(s_tokens + a.n_slots);
   __shared__ int32_t s_scan[2][32];
   __shared__ int32_t s_total[2];
@@ -43,51 +48,50 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
   if (threadIdx.x < 2) s_total[threadIdx.x] = 0;
   __syncthreads();
 
-  int my_slot[2] = {-1, -1};   // of pair number `lane` (routed, then shared) of tokens warp and warp + 32
+  int my_slot[2] = {-1, -1};   // of pair number `lane` (routed, then shared) of the two tokens
   float my_weight[2] = {};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int t = warp + 32 * half;
     if (t >= a.n_tokens) continue;
     const float *row = a.logits + t * a.logits_stride;
-    uint32_t taken = 0;   // of this lane's experts lane + 32 j
-    float top = 0.f, chosen_sum = 0.f, mine = 0.f;
-    int my_id = -1;
-    for (int k = 0; k < a.top_k; ++k) {
-      uint64_t best = 0;
-      for (int j = 0; j * 32 < a.n_experts; ++j) {
-        const int e = j * 32 + lane;
-        if (e < a.n_experts && !(taken >> j & 1)) {
-          const uint64_t key = rank_key(row[e], e);
-          best = key > best ? key : best;
-        }
-      }
+    uint32_t key[N];
 #pragma unroll
-      for (int d = 16; d; d >>= 1) {
-        const uint64_t other = __shfl_xor_sync(0xffffffffu, best, d);
-        best = other > best ? other : best;
-      }
-      if ((uint32_t)(best >> 32) <= kLowest) break;   // nothing above minus infinity is left
-      const int e = (int)~(uint32_t)best;
-      const float v = row[e];
-      if (k == 0) top = v;
-      const float p = expf(v - top);
-      chosen_sum += p;
-      if (lane == (e & 31)) taken |= 1u << (e >> 5);
-      if (lane == k) {
-        my_id = e;
-        mine = p;
-      }
-    }
-    float total = chosen_sum;
+    for (int j = 0; j < N; ++j) key[j] = j * 32 + lane < a.n_experts ? ordered(row[j * 32 + lane]) : 0;
+    float total = 0.f, top = 0.f, mine = 0.f;
+    int my_id = -1;
     if (!a.renormalize) {
-      total = 0.f;
-      for (int e = lane; e < a.n_experts; e += 32) {
-        const float v = row[e];
-        total += v != v ? 0.f : expf(v - top);
-      }
+      uint32_t best = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) best = max(best, key[j]);
+      top = value_of(__reduce_max_sync(0xffffffffu, best));
+#pragma unroll
+      for (int j = 0; j < N; ++j) total += key[j] ? expf(value_of(key[j]) - top) : 0.f;
 #pragma unroll
       for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    }
+    for (int k = 0; k < a.top_k; ++k) {
+      uint32_t best = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) best = max(best, key[j]);
+      best = __reduce_max_sync(0xffffffffu, best);
+      if (best == 0) break;   // nothing above minus infinity is left
+      uint32_t e = 0xffffffffu;
+#pragma unroll
+      for (int j = N - 1; j >= 0; --j)
+        if (key[j] == best) e = j * 32 + lane;
+      e = __reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (e == (uint32_t)(j * 32 + lane)) key[j] = 0;
+      const float v = value_of(best);
+      if (k == 0) top = v;
+      const float p = expf(v - top);
+      if (a.renormalize) total += p;
+      if (lane == k) {
+        my_id = (int)e;
+        mine = p;
+      }
     }
     const float w = my_id >= 0 ? mine / total * a.routed_scale : 0.f;
     if (lane < a.top_k) {
@@ -114,8 +118,8 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
   // experts in use, in the order of their slots, and the number of pairs before each
   for (int first = 0; first < a.n_slots; first += kRouteThreads) {
     const int slot = first + threadIdx.x;
-    const uint64_t tokens = slot < a.n_slots ? s_tokens[slot] : 0;
-    int used = tokens != 0, pairs = __popcll(tokens), u = used, p = pairs;
+    const int pairs = slot < a.n_slots ? __popcll(s_tokens[slot]) : 0, used = pairs != 0;
+    int u = used, p = pairs;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int x = __shfl_up_sync(0xffffffffu, u, d), y = __shfl_up_sync(0xffffffffu, p, d);
@@ -123,15 +127,19 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
     }
     if (lane == 31) s_scan[0][warp] = u, s_scan[1][warp] = p;
     __syncthreads();
-    int before_u = s_total[0], before_p = s_total[1];
-    for (int i = 0; i < warp; ++i) before_u += s_scan[0][i], before_p += s_scan[1][i];
-    if (slot < a.n_slots) s_base[slot] = before_p + p - pairs;
-    if (used) a.active[before_u + u - 1] = MoeActive{tokens, slot, before_p + p - pairs};
+    const int below = lane < warp ? -1 : 0;
+    u += __reduce_add_sync(0xffffffffu, s_scan[0][lane] & below) + s_total[0];
+    p += __reduce_add_sync(0xffffffffu, s_scan[1][lane] & below) + s_total[1];
+    if (slot < a.n_slots) s_base[slot] = p - pairs;
+    if (used) a.active[u - 1] = make_int2(slot, p - pairs);
     __syncthreads();
-    if (threadIdx.x == kRouteThreads - 1) s_total[0] = before_u + u, s_total[1] = before_p + p;
+    if (threadIdx.x == kRouteThreads - 1) s_total[0] = u, s_total[1] = p;
     __syncthreads();
   }
-  if (threadIdx.x == 0) *a.n_active = s_total[0];
+  if (threadIdx.x == 0) {
+    *a.n_active = s_total[0];
+    a.active[s_total[0]] = make_int2(-1, s_total[1]);   // the end of the last expert's pairs
+  }
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if (my_slot[half] < 0) continue;
@@ -144,9 +152,12 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
 
 // ---- the weight stream --------------------------------------------------------------------
 
-template <bool FP8> struct Block;           // of the k axis: four lanes' 16 bytes of a row
-template <> struct Block<false> { static constexpr int kElems = 32, kProducts = 2; };
-template <> struct Block<true> { static constexpr int kElems = 64, kProducts = 4; };
+// A block of the k axis: 16 bytes of weights a lane and row, four lanes a row; kTok 16-byte parts of the
+// matching token elements a lane.
+template <bool FP8> struct Block {
+  static constexpr int kElems = FP8 ? 64 : 32, kProducts = FP8 ? 4 : 2, kTok = FP8 ? 2 : 1, kES = FP8 ? 1 : 2;
+  static constexpr int kStageBytes = (2 + kTok) * 512;
+};
 
 // Weight rows g and g + 8 of a block, 16 bytes each, as the 16-row operand of product j.
 template <typename T, bool FP8>
@@ -165,151 +176,201 @@ __device__ __forceinline__ void weight_operand(uint32_t (&r)[4], const uint4 &lo
     r[3] = j ? hi.w : hi.y;
   }
 }
-// This lane's part of a token's block (16 or 32 bytes), and the operand of product j from it.
-template <bool FP8> struct TokenPart { uint4 x; };
-template <> struct TokenPart<true> { uint4 x, y; };
+// This lane's part of a token's block, and the operand of product j from it.
+template <bool FP8> struct TokenPart { uint4 v[Block<FP8>::kTok]; };
+template <bool FP8>
+__device__ __forceinline__ void token_operand(uint32_t &b0, uint32_t &b1, const TokenPart<FP8> &t, int j) {
+  if constexpr (FP8) {   // the codes of a word come out as (0, 2) and (1, 3)
+    const uint4 &v = t.v[j >> 1];
+    const uint32_t lo = j & 1 ? v.z : v.x, hi = j & 1 ? v.w : v.y;
+    b0 = __byte_perm(lo, hi, 0x5410);
+    b1 = __byte_perm(lo, hi, 0x7632);
+  } else {
+    b0 = j ? t.v[0].z : t.v[0].x;
+    b1 = j ? t.v[0].w : t.v[0].y;
+  }
+}
 template <bool FP8>
 __device__ __forceinline__ TokenPart<FP8> load_token(const uint8_t *p, bool there) {
   TokenPart<FP8> r = {};
   if (there) {
-    r.x = *(const uint4 *)p;
-    if constexpr (FP8) r.y = *(const uint4 *)(p + 16);
+#pragma unroll
+    for (int i = 0; i < Block<FP8>::kTok; ++i) r.v[i] = ((const uint4 *)p)[i];
   }
   return r;
 }
-template <bool FP8>
-__device__ __forceinline__ void token_operand(uint32_t &b0, uint32_t &b1, const TokenPart<FP8> &t, int j) {
-  if constexpr (FP8) {   // the codes of a word come out as (0, 2) and (1, 3)
-    const uint32_t lo = j == 0 ? t.x.x : j == 1 ? t.x.z : j == 2 ? t.y.x : t.y.z;
-    const uint32_t hi = j == 0 ? t.x.y : j == 1 ? t.x.w : j == 2 ? t.y.y : t.y.w;
-    b0 = __byte_perm(lo, hi, 0x5410);
-    b1 = __byte_perm(lo, hi, 0x7632);
-  } else {
-    b0 = j ? t.x.z : t.x.x;
-    b1 = j ? t.x.w : t.x.y;
-  }
-}
 
-constexpr int kStages = 12;
-constexpr int kStageBytes = 2 * 32 * 16;   // rows g and g + 8, 16 bytes a lane
-constexpr int kRingBytes = kWarps * kStages * kStageBytes;
-
-// One lane's ring.
+// One lane's ring: what it copies there it reads back itself.
+template <bool FP8, int STAGES>
 struct Ring {
+  static constexpr int kStage = Block<FP8>::kStageBytes;
   uint8_t *base;
   uint32_t at;
   __device__ __forceinline__ explicit Ring(uint8_t *smem) {
-    base = smem + (threadIdx.x >> 5) * (kStages * kStageBytes) + (threadIdx.x & 31) * 16;
+    base = smem + (threadIdx.x >> 5) * (STAGES * kStage) + (threadIdx.x & 31) * 16;
     at = shared_address(base);
   }
-  __device__ __forceinline__ void fill(int stage, const uint8_t *lo, const uint8_t *hi, bool there) {
-    copy_async_16(at + stage * kStageBytes, lo, there ? 16 : 0);
-    copy_async_16(at + stage * kStageBytes + 512, hi, there ? 16 : 0);
+  __device__ __forceinline__ void fill(int stage, const uint8_t *lo, const uint8_t *hi, const uint8_t *tok, bool there, bool tok_there) {
+    const uint32_t dst = at + stage * kStage;
+    copy_async_16(dst, lo, there ? 16 : 0);
+    copy_async_16(dst + 512, hi, there ? 16 : 0);
+#pragma unroll
+    for (int i = 0; i < Block<FP8>::kTok; ++i) copy_async_16(dst + 1024 + i * 512, tok + i * 16, tok_there ? 16 : 0);
   }
-  __device__ __forceinline__ uint4 lo(int stage) const { return *(const uint4 *)(base + stage * kStageBytes); }
-  __device__ __forceinline__ uint4 hi(int stage) const { return *(const uint4 *)(base + stage * kStageBytes + 512); }
+  __device__ __forceinline__ uint4 lo(int stage) const { return *(const uint4 *)(base + stage * kStage); }
+  __device__ __forceinline__ uint4 hi(int stage) const { return *(const uint4 *)(base + stage * kStage + 512); }
+  __device__ __forceinline__ TokenPart<FP8> token(int stage) const {
+    TokenPart<FP8> r;
+#pragma unroll
+    for (int i = 0; i < Block<FP8>::kTok; ++i) r.v[i] = *(const uint4 *)(base + stage * kStage + 1024 + i * 512);
+    return r;
+  }
 };
 
-__device__ __forceinline__ MoeActive read_active(const MoeArgs &a, int i) {
-  const longlong2 raw = __ldcg((const longlong2 *)(a.active + i));
-  MoeActive r;
-  r.tokens = (uint64_t)raw.x;
-  r.slot = (int32_t)raw.y;
-  r.base = (int32_t)(raw.y >> 32);
-  return r;
+// acc += weights x tokens over one block; e4m3 blocks come with the scales of rows g and g + 8.
+template <typename T, bool FP8>
+__device__ __forceinline__ void block_product(float (&acc)[4], const uint4 &lo, const uint4 &hi, const TokenPart<FP8> &tok,
+                                              float scale_lo, float scale_hi) {
+  float part[4] = {};
+#pragma unroll
+  for (int j = 0; j < Block<FP8>::kProducts; ++j) {
+    uint32_t w[4], b0, b1;
+    weight_operand<T, FP8>(w, lo, hi, j);
+    token_operand<FP8>(b0, b1, tok, j);
+    if constexpr (FP8) mma_16816<T>(part, w, b0, b1);
+    else mma_16816<T>(acc, w, b0, b1);
+  }
+  if constexpr (FP8) {
+    acc[0] += part[0] * scale_lo;
+    acc[1] += part[1] * scale_lo;
+    acc[2] += part[2] * scale_hi;
+    acc[3] += part[3] * scale_hi;
+  }
 }
 
-// h[pair] = w silu(gate) up, rounded once to T.  NT: column tiles of 8 tokens that an expert may have.
-// The k axis is split over the warps, joined in shared memory in the order of the warps.
-template <typename T, bool FP8, int NT>
-__global__ void __launch_bounds__(kWarps * 32) moe_up_kernel(const __grid_constant__ MoeArgs a) {
+// What the routing found, in shared memory: (slot, first pair) of each expert in use and one more
+// entry for the end, and each pair's token.
+struct Routed {
+  int2 *active;
+  uint8_t *token;
+  int n_active;
+  __device__ __forceinline__ void read(const MoeArgs &a, uint8_t *at) {
+    n_active = __ldcg(a.n_active);
+    active = (int2 *)at;
+    for (int i = threadIdx.x; i <= n_active; i += blockDim.x) active[i] = __ldcg(a.active + i);
+    __syncthreads();
+    token = at + (n_active + 1) * 8;
+    const int pairs = active[n_active].y;
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) token[i] = (uint8_t)__ldcg(a.pair_token + i);
+    __syncthreads();
+  }
+};
+int routed_bytes(const MoeArgs &a) {
+  const int pairs = a.n_tokens * (a.top_k + a.n_shared);
+  return ((pairs < a.n_slots ? pairs : a.n_slots) + 1) * 8 + pairs;
+}
+
+// h[pair] = w silu(gate) up, rounded once to T.  An item is 8 rows of gate and the same 8 of up as one
+// 16-row operand, so a thread gets both sums of its outputs.  The k axis is split over the warps,
+// joined in shared memory in the order of the warps.  NT: column tiles of 8 tokens an expert may have;
+// the first comes through the ring, the others (more than 8 tokens of one expert) straight from L2.
+template <typename T, bool FP8, int NT, int STAGES>
+__global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float s_part[2][kWarps][16][9];
-  constexpr int kElems = Block<FP8>::kElems, kES = FP8 ? 1 : 2;
+  __shared__ float s_part[2][kUpWarps][16][9];
+  using B = Block<FP8>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   wait_for_previous();
   let_next_start();
+  Routed routed;
+  routed.read(a, smem + kUpWarps * STAGES * B::kStageBytes);
   const int tiles = a.d_ff / 8;
-  const int items = *a.n_active * tiles;
-  const int blocks = (a.d_model + kElems - 1) / kElems;
-  const int kb0 = blocks * warp / kWarps, kb1 = blocks * (warp + 1) / kWarps, steps = kb1 - kb0;
-  const int64_t row_bytes = (int64_t)a.d_model * kES;
-  const int lane_k = c * (16 / kES);   // this lane's first element inside a block
+  const int items = routed.n_active * tiles;
+  const int blocks = (a.d_model + B::kElems - 1) / B::kElems;
+  const int kb0 = blocks * warp / kUpWarps, kb1 = blocks * (warp + 1) / kUpWarps;
+  const int64_t row_bytes = (int64_t)a.d_model * B::kES;
+  const int lane_k = c * (16 / B::kES);   // this lane's first element inside a block
+  const uint8_t *const x_lane = (const uint8_t *)a.x + lane_k * 2;
 
-  Ring ring(smem);
+  Ring<FP8, STAGES> ring(smem);
   // the copies run ahead of the products over (item, block)
-  int fill_item = blockIdx.x, fill_kb = kb0, fill_stage = 0;
-  const uint8_t *fill_lo = nullptr, *fill_hi = nullptr;
-  auto enter = [&](int item) {
-    if (item >= items) return;
-    const int slot = read_active(a, item / tiles).slot, row = (item % tiles) * 8 + g;
-    fill_lo = a.gate + slot * a.gate_stride + row * row_bytes + c * 16;
-    fill_hi = a.up + slot * a.gate_stride + row * row_bytes + c * 16;
+  int fill_item = kb0 < kb1 ? blockIdx.x : items, fill_kb = kb0, fill_stage = 0;
+  const uint8_t *fill_lo = nullptr, *fill_hi = nullptr, *fill_tok = nullptr;
+  bool fill_col = false;
+  auto enter = [&]() {
+    if (fill_item >= items) return;
+    const int i = fill_item / tiles, row = (fill_item - i * tiles) * 8 + g;
+    const int2 e = routed.active[i];
+    fill_lo = a.gate + e.x * a.gate_stride + row * row_bytes + c * 16;
+    fill_hi = a.up + e.x * a.gate_stride + row * row_bytes + c * 16;
+    fill_col = g < routed.active[i + 1].y - e.y;
+    fill_tok = fill_col ? x_lane + routed.token[e.y + g] * a.x_stride * 2 : x_lane;
   };
   auto fill = [&]() {
-    if (steps && fill_item < items) {
-      const int64_t off = (int64_t)fill_kb * (kElems * kES);
-      const bool there = fill_kb * kElems + lane_k < a.d_model;
-      ring.fill(fill_stage, there ? fill_lo + off : fill_lo, there ? fill_hi + off : fill_hi, there);
+    if (fill_item < items) {
+      const bool there = fill_kb * B::kElems + lane_k < a.d_model;
+      const int off = there ? fill_kb * 64 : 0;
+      ring.fill(fill_stage, fill_lo + off, fill_hi + off, fill_tok + off * B::kTok, there, there && fill_col);
       if (++fill_kb == kb1) {
         fill_kb = kb0;
         fill_item += gridDim.x;
-        enter(fill_item);
+        enter();
       }
     }
     copy_async_commit();
-    fill_stage = fill_stage + 1 == kStages ? 0 : fill_stage + 1;
+    fill_stage = fill_stage + 1 == STAGES ? 0 : fill_stage + 1;
   };
-  enter(fill_item);
-  for (int i = 0; i < kStages - 1; ++i) fill();
+  enter();
+  for (int i = 0; i < STAGES - 1; ++i) fill();
 
   int stage = 0, buffer = 0;
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const MoeActive e = read_active(a, item / tiles);
-    const int count = __popcll(e.tokens), row0 = (item % tiles) * 8;
-    const uint8_t *x[NT];
+    const int i = item / tiles, row0 = (item - i * tiles) * 8;
+    const int2 e = routed.active[i];
+    const int count = routed.active[i + 1].y - e.y;
     float acc[NT][4] = {};
+    const uint8_t *more[NT];   // this lane's column of the further tiles
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int j = n * 8 + g;
-      x[n] = j < count ? (const uint8_t *)a.x + (a.pair_token[e.base + j] * a.x_stride + lane_k) * 2 : nullptr;
-    }
+    for (int n = 1; n < NT; ++n)
+      more[n] = n * 8 + g < count ? x_lane + routed.token[e.y + n * 8 + g] * a.x_stride * 2 : nullptr;
     const float *scale_g = nullptr, *scale_u = nullptr;
+    float sg = 1.f, su = 1.f;
     if constexpr (FP8) {
-      scale_g = a.gate_scale + (int64_t)e.slot * a.scale_stride + (row0 / 128) * ((a.d_model + 127) / 128);
-      scale_u = a.up_scale + (int64_t)e.slot * a.scale_stride + (row0 / 128) * ((a.d_model + 127) / 128);
+      const int64_t at = e.x * a.scale_stride + (row0 / 128) * ((a.d_model + 127) / 128);
+      scale_g = a.gate_scale + at;
+      scale_u = a.up_scale + at;
+      if (kb0 < kb1) {
+        sg = scale_g[kb0 >> 1];
+        su = scale_u[kb0 >> 1];
+      }
     }
     for (int kb = kb0; kb < kb1; ++kb) {
       fill();
-      copy_async_wait<kStages - 1>();
+      float next_g = 1.f, next_u = 1.f;
+      if constexpr (FP8) {   // one scale for two blocks, read a block ahead
+        if (kb + 1 < kb1) {
+          next_g = scale_g[(kb + 1) >> 1];
+          next_u = scale_u[(kb + 1) >> 1];
+        }
+      }
+      copy_async_wait<STAGES - 1>();
       const uint4 lo = ring.lo(stage), hi = ring.hi(stage);
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-      const bool there = kb * kElems + lane_k < a.d_model;
-      float sg = 1.f, su = 1.f;
-      if constexpr (FP8) {
-        sg = scale_g[kb >> 1];
-        su = scale_u[kb >> 1];
-      }
+      block_product<T, FP8>(acc[0], lo, hi, ring.token(stage), sg, su);
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      if (NT > 1 && count > 8) {
+        const bool there = kb * B::kElems + lane_k < a.d_model;
+        const int64_t off = (int64_t)kb * (B::kElems * 2);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        if (n && n * 8 >= count) break;
-        const TokenPart<FP8> tp = load_token<FP8>(x[n] + (int64_t)kb * (kElems * 2), there && x[n]);
-        float part[4] = {};
-#pragma unroll
-        for (int j = 0; j < Block<FP8>::kProducts; ++j) {
-          uint32_t w[4], b0, b1;
-          weight_operand<T, FP8>(w, lo, hi, j);
-          token_operand<FP8>(b0, b1, tp, j);
-          if constexpr (FP8) mma_16816<T>(part, w, b0, b1);
-          else mma_16816<T>(acc[n], w, b0, b1);
-        }
-        if constexpr (FP8) {   // one scale for 128 of the k axis: two blocks
-          acc[n][0] += part[0] * sg;
-          acc[n][1] += part[1] * sg;
-          acc[n][2] += part[2] * su;
-          acc[n][3] += part[3] * su;
+        for (int n = 1; n < NT; n += 2) {
+          if (n * 8 >= count) break;
+          const TokenPart<FP8> x0 = load_token<FP8>(more[n] + off, there && more[n]);
+          const TokenPart<FP8> x1 = load_token<FP8>(more[n + 1 < NT ? n + 1 : n] + off, n + 1 < NT && there && more[n + 1 < NT ? n + 1 : n]);
+          block_product<T, FP8>(acc[n], lo, hi, x0, sg, su);
+          if (n + 1 < NT) block_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], lo, hi, x1, sg, su);
         }
       }
+      sg = next_g;
+      su = next_u;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -325,15 +386,15 @@ __global__ void __launch_bounds__(kWarps * 32) moe_up_kernel(const __grid_consta
         const int f = threadIdx.x & 7, j = threadIdx.x >> 3;
         float gate = 0.f, up = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kUpWarps; ++w) {
           gate += part[w][f][j];
           up += part[w][f + 8][j];
         }
         if (n * 8 + j < count) {
-          const int pair = e.base + n * 8 + j;
+          const int pair = e.y + n * 8 + j;
           float h = gate / (1.f + expf(-gate)) * up * a.pair_weight[pair];
           // f16 ends at 65504: the largest value stands for what is beyond (bf16 reaches as far as 32 bits)
-          if constexpr (__is_same(T, __half)) h = fminf(fmaxf(h, -65504.f), 65504.f);
+          if constexpr (__is_same(T, __half)) h = h != h ? h : fminf(fmaxf(h, -65504.f), 65504.f);
           ((T *)a.h)[(int64_t)pair * a.d_ff + row0 + f] = T(h);
         }
       }
@@ -343,109 +404,116 @@ __global__ void __launch_bounds__(kWarps * 32) moe_up_kernel(const __grid_consta
 }
 
 // y for 16 output rows a block: the (expert, block of k) steps of all experts in use are dealt to the
-// warps in equal runs.  The columns are the tokens themselves, so that every expert adds to the same
-// accumulators; column tiles without a token of the expert are left out.
-template <typename T, bool FP8, int NT, bool F32_OUT>
-__global__ void __launch_bounds__(kWarps * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
+// warps in equal runs.  At the end of its part of an expert a warp adds the expert's columns to its
+// own sums of the tokens in shared memory; the warps' sums are joined at the end, in their order.
+template <typename T, bool FP8, int NT, int STAGES, int WARPS, bool F32_OUT>
+__global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
-  constexpr int kElems = Block<FP8>::kElems, kES = FP8 ? 1 : 2;
+  using B = Block<FP8>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int row0 = blockIdx.x * 16;
-  const int blocks = (a.d_ff + kElems - 1) / kElems;
-  const int64_t row_bytes = (int64_t)a.d_ff * kES;
-  const int lane_k = c * (16 / kES);
+  const int blocks = (a.d_ff + B::kElems - 1) / B::kElems;
+  const int64_t row_bytes = (int64_t)a.d_ff * B::kES;
+  const int lane_k = c * (16 / B::kES);
+  float *const sums = (float *)(smem + WARPS * STAGES * B::kStageBytes);   // [warp][token][17]
+  for (int i = threadIdx.x; i < WARPS * a.n_tokens * 17; i += WARPS * 32) sums[i] = 0.f;
   wait_for_previous();
-  const int n_active = *a.n_active;
-  const int64_t total = (int64_t)n_active * blocks;
-  const int64_t s0 = total * warp / kWarps, s1 = total * (warp + 1) / kWarps;
+  Routed routed;
+  routed.read(a, (uint8_t *)(sums + (WARPS * a.n_tokens * 17 + 3) / 4 * 4));
+  const int total = routed.n_active * blocks;   // at most 4096 experts x 32768 blocks
+  const int s0 = (int)((int64_t)total * warp / WARPS), s1 = (int)((int64_t)total * (warp + 1) / WARPS);
+  const uint8_t *const h_lane = (const uint8_t *)a.h + lane_k * 2;
 
-  Ring ring(smem);
-  int64_t fill_step = s0;
-  int fill_expert = (int)(s0 / blocks), fill_kb = (int)(s0 % blocks), fill_stage = 0;
-  const uint8_t *fill_lo = nullptr;
-  auto enter = [&](int i) {
-    if (i < n_active) fill_lo = a.down + read_active(a, i).slot * a.down_stride + (row0 + g) * row_bytes + c * 16;
+  Ring<FP8, STAGES> ring(smem);
+  int fill_step = s0, fill_expert = s0 / blocks, fill_kb = s0 - fill_expert * blocks, fill_stage = 0;
+  const uint8_t *fill_lo = nullptr, *fill_tok = nullptr;
+  bool fill_col = false;
+  auto enter = [&]() {
+    if (fill_expert >= routed.n_active) return;
+    const int2 e = routed.active[fill_expert];
+    fill_lo = a.down + e.x * a.down_stride + (row0 + g) * row_bytes + c * 16;
+    fill_col = g < routed.active[fill_expert + 1].y - e.y;
+    fill_tok = h_lane + (fill_col ? (int64_t)(e.y + g) * a.d_ff * 2 : 0);
   };
   auto fill = [&]() {
     if (fill_step < s1) {
-      const bool there = fill_kb * kElems + lane_k < a.d_ff;
-      const uint8_t *p = fill_lo + (there ? (int64_t)fill_kb * (kElems * kES) : 0);
-      ring.fill(fill_stage, p, p + 8 * row_bytes, there);
+      const bool there = fill_kb * B::kElems + lane_k < a.d_ff;
+      const int off = there ? fill_kb * 64 : 0;
+      ring.fill(fill_stage, fill_lo + off, fill_lo + 8 * row_bytes + off, fill_tok + off * B::kTok, there, there && fill_col);
       ++fill_step;
       if (++fill_kb == blocks) {
         fill_kb = 0;
-        enter(++fill_expert);
+        ++fill_expert;
+        enter();
       }
     }
     copy_async_commit();
-    fill_stage = fill_stage + 1 == kStages ? 0 : fill_stage + 1;
+    fill_stage = fill_stage + 1 == STAGES ? 0 : fill_stage + 1;
   };
-  enter(fill_expert);
-  for (int i = 0; i < kStages - 1; ++i) fill();
+  enter();
+  for (int i = 0; i < STAGES - 1; ++i) fill();
 
-  float acc[NT][4] = {};
-  int expert = (int)(s0 / blocks), kb = (int)(s0 % blocks), stage = 0;
-  uint64_t tokens = 0;
-  const uint8_t *h[NT];
-  const float *scale = nullptr;
-  auto take = [&](int i) {
-    const MoeActive e = read_active(a, i);
-    tokens = e.tokens;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int t = n * 8 + g;
-      const int pair = e.base + __popcll(tokens & ((1ull << t) - 1));
-      h[n] = tokens >> t & 1 ? (const uint8_t *)a.h + ((int64_t)pair * a.d_ff + lane_k) * 2 : nullptr;
-    }
-    if constexpr (FP8) scale = a.down_scale + (int64_t)e.slot * a.scale_stride + (row0 / 128) * ((a.d_ff + 127) / 128);
-  };
-  if (s0 < s1) take(expert);
-  for (int64_t s = s0; s < s1; ++s) {
-    fill();
-    copy_async_wait<kStages - 1>();
-    const uint4 lo = ring.lo(stage), hi = ring.hi(stage);
-    stage = stage + 1 == kStages ? 0 : stage + 1;
-    const bool there = kb * kElems + lane_k < a.d_ff;
+  int stage = 0, s = s0;
+  for (int expert = s0 / blocks; s < s1; ++expert) {
+    const int2 e = routed.active[expert];
+    const int count = routed.active[expert + 1].y - e.y;
+    const int first = s - expert * blocks, last = min(blocks, s1 - expert * blocks);
+    s += last - first;
+    const float *scale = nullptr;
     float by = 1.f;
-    if constexpr (FP8) by = scale[kb >> 1];
+    if constexpr (FP8) {
+      scale = a.down_scale + (int64_t)e.x * a.scale_stride + (row0 / 128) * ((a.d_ff + 127) / 128);
+      by = scale[first >> 1];
+    }
+    const uint8_t *const h0 = h_lane + (int64_t)(e.y + g) * a.d_ff * 2;
+    float acc[NT][4] = {};
+    for (int kb = first; kb < last; ++kb) {
+      fill();
+      float next = 1.f;
+      if constexpr (FP8) {
+        if (kb + 1 < last) next = scale[(kb + 1) >> 1];
+      }
+      copy_async_wait<STAGES - 1>();
+      const uint4 lo = ring.lo(stage), hi = ring.hi(stage);
+      block_product<T, FP8>(acc[0], lo, hi, ring.token(stage), by, by);
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      if (NT > 1 && count > 8) {
+        const bool there = kb * B::kElems + lane_k < a.d_ff;
+        const uint8_t *const p = h0 + (int64_t)kb * (B::kElems * 2);
+#pragma unroll
+        for (int n = 1; n < NT; n += 2) {
+          if (n * 8 >= count) break;
+          const TokenPart<FP8> x0 = load_token<FP8>(p + (int64_t)n * 8 * a.d_ff * 2, there && n * 8 + g < count);
+          const TokenPart<FP8> x1 = load_token<FP8>(p + (int64_t)(n + 1) * 8 * a.d_ff * 2, n + 1 < NT && there && (n + 1) * 8 + g < count);
+          block_product<T, FP8>(acc[n], lo, hi, x0, by, by);
+          if (n + 1 < NT) block_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], lo, hi, x1, by, by);
+        }
+      }
+      by = next;
+    }
+    float *const mine = sums + warp * a.n_tokens * 17;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      if (!(tokens >> (n * 8) & 0xff)) continue;
-      const TokenPart<FP8> tp = load_token<FP8>(h[n] + (int64_t)kb * (kElems * 2), there && h[n]);
-      float part[4] = {};
+      if (n * 8 >= count) break;
 #pragma unroll
-      for (int j = 0; j < Block<FP8>::kProducts; ++j) {
-        uint32_t w[4], b0, b1;
-        weight_operand<T, FP8>(w, lo, hi, j);
-        token_operand<FP8>(b0, b1, tp, j);
-        if constexpr (FP8) mma_16816<T>(part, w, b0, b1);
-        else mma_16816<T>(acc[n], w, b0, b1);
-      }
-      if constexpr (FP8) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[n][e] += part[e] * by;
+      for (int k = 0; k < 2; ++k) {   // columns 2c and 2c + 1: no two lanes have the same token and row
+        const int j = n * 8 + 2 * c + k;
+        if (j < count) {
+          float *const y = mine + routed.token[e.y + j] * 17;
+          y[g] += acc[n][k];
+          y[g + 8] += acc[n][2 + k];
+        }
       }
     }
-    if (++kb == blocks) {
-      kb = 0;
-      if (s + 1 < s1) take(++expert);
-    }
+    __syncwarp();   // the next expert may have the same tokens in other lanes
   }
   copy_async_wait<0>();
-  __syncthreads();   // every warp is done with its ring: the sums meet there
-  float *const sums = (float *)smem;   // [warp][token][row], 17 floats a token against bank conflicts
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      sums[(warp * (NT * 8) + n * 8 + 2 * c + (e & 1)) * 17 + g + 8 * (e >> 1)] = acc[n][e];
   __syncthreads();
-  for (int i = threadIdx.x; i < NT * 8 * 16; i += kWarps * 32) {
+  for (int i = threadIdx.x; i < a.n_tokens * 16; i += WARPS * 32) {
     const int t = i >> 4, r = i & 15;
-    if (t >= a.n_tokens) break;
     float y = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) y += sums[(w * (NT * 8) + t) * 17 + r];
+    for (int w = 0; w < WARPS; ++w) y += sums[(w * a.n_tokens + t) * 17 + r];
     if constexpr (F32_OUT) ((float *)a.out)[t * a.out_stride + row0 + r] = y;
     else ((T *)a.out)[t * a.out_stride + row0 + r] = T(y);
   }
@@ -470,18 +538,27 @@ cudaError_t launch(K kernel, unsigned grid, int threads, size_t smem, bool early
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+template <typename T, bool FP8, int NT, int STAGES, int WARPS>
+cudaError_t launch_down(const MoeArgs &a, bool f32_out, cudaStream_t st) {
+  const size_t smem = (size_t)WARPS * STAGES * Block<FP8>::kStageBytes + (size_t)(WARPS * a.n_tokens * 17 + 3) / 4 * 16 + routed_bytes(a);
+  return f32_out ? launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, true>, a.d_model / 16, WARPS * 32, smem, true, a, st)
+                 : launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, false>, a.d_model / 16, WARPS * 32, smem, true, a, st);
+}
+
 template <typename T, bool FP8, int NT>
 cudaError_t launch_layer(const MoeArgs &a, bool f32_out, cudaStream_t st) {
-  cudaError_t e = launch(moe_route_kernel, 1, kRouteThreads, (size_t)a.n_slots * 12, false, a, st);
+  cudaError_t e = a.n_experts <= 256 ? launch(moe_route_kernel<8>, 1, kRouteThreads, (size_t)a.n_slots * 12, false, a, st)
+                                     : launch(moe_route_kernel<32>, 1, kRouteThreads, (size_t)a.n_slots * 12, false, a, st);
   if (e != cudaSuccess) return e;
+  constexpr int kStages = FP8 ? 6 : 8;   // 96 KB: two blocks an SM
   const int64_t pairs = (int64_t)a.n_tokens * (a.top_k + a.n_shared);
   const int64_t most = (pairs < a.n_slots ? pairs : a.n_slots) * (a.d_ff / 8);
-  e = launch(moe_up_kernel<T, FP8, NT>, (unsigned)(most < 2 * kSms ? most : 2 * kSms), kWarps * 32, kRingBytes, true, a, st);
+  e = launch(moe_up_kernel<T, FP8, NT, kStages>, (unsigned)(most < 2 * kSms ? most : 2 * kSms), kUpWarps * 32,
+             (size_t)kUpWarps * kStages * Block<FP8>::kStageBytes + routed_bytes(a), true, a, st);
   if (e != cudaSuccess) return e;
-  constexpr size_t sums = (size_t)kWarps * NT * 8 * 17 * 4;
-  constexpr size_t smem = sums > kRingBytes ? sums : kRingBytes;
-  return f32_out ? launch(moe_down_kernel<T, FP8, NT, true>, a.d_model / 16, kWarps * 32, smem, true, a, st)
-                 : launch(moe_down_kernel<T, FP8, NT, false>, a.d_model / 16, kWarps * 32, smem, true, a, st);
+  // Up to about one block an SM: 8 warps each; more: 4 warps, four blocks an SM, all of them at once.
+  if (a.d_model / 16 <= kSms) return launch_down<T, FP8, NT, FP8 ? 8 : 10, 8>(a, f32_out, st);
+  return launch_down<T, FP8, NT, FP8 ? 5 : 6, 4>(a, f32_out, st);
 }
 
 template <typename T, bool FP8>
@@ -499,7 +576,7 @@ MoeShape moe_shape(int n_slots, int d_ff, int n_tokens, int top_k, int n_shared)
   const int64_t pairs = (int64_t)n_tokens * (top_k + n_shared), most = pairs < n_slots ? pairs : n_slots;
   const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
   s.active = 256;                       // the number of experts in use lies at the start
-  s.token = s.active + up(most * (int64_t)sizeof(MoeActive));
+  s.token = s.active + up((most + 1) * 8);
   s.weight = s.token + up(pairs * 4);
   s.h = s.weight + up(pairs * 4);
   s.bytes = s.h + up(pairs * d_ff * 2);

@@ -333,7 +333,7 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   a.logits_stride = many ? p->logits_stride : p->n_experts;
   a.out_stride = many ? p->out_stride : e->d_model;
   a.n_active = (int32_t *)work;
-  a.active = (MoeActive *)(work + s.active);
+  a.active = (int2 *)(work + s.active);
   a.pair_token = (int32_t *)(work + s.token);
   a.pair_weight = (float *)(work + s.weight);
   a.h = work + s.h;

@@ -63,12 +63,6 @@ struct AttendArgs {
 };
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
-// An expert in use: its tokens as a bit mask; its pairs are numbered from `base` in token order.
-struct __align__(16) MoeActive {
-  uint64_t tokens;
-  int32_t slot, base;
-};
-
 // Byte offsets of a layer call's workspace.
 struct MoeShape {
   int64_t active, token, weight, h, bytes;
@@ -89,7 +83,7 @@ struct MoeArgs {
   int32_t *status;
   int64_t x_stride, logits_stride, out_stride;            // elements
   int32_t *n_active;                                      // workspace
-  MoeActive *active;
+  int2 *active;                                           // (slot, first pair) of each expert in use, and the end
   int32_t *pair_token;
   float *pair_weight;
   void *h;                                                // [pair][d_ff]

@@ -7,12 +7,12 @@
 // is arranged around that stream: each lane owns a ring of 16-byte slots in shared memory that it
 // fills with asynchronous copies and reads back itself (no barrier between a warp's copies and its
 // use of them), weights are the 16-row side of the tensor-core product straight from those slots,
-// tokens its 8-column side, and the order of the k axis inside a block is the order in which the
+// tokens its 8-column side, and the order of the k axis inside a step is the order in which the
 // slots hold it.  Three launches, chained so that each one's prologue overlaps the tail of the one before:
-//   route: one block; top-k and softmax by warps, the list of experts in use, the pairs (expert, token)
+//   route: a block a token; top-k and softmax by one warp
 //   up:    items of 8 gate and 8 up rows of one expert (one product gives both, in the same thread)
-//   down:  16 rows of the output over ALL experts in use: every token's sum stays in registers, in
-//          the order of the slots - no partial results, no atomics.
+//   down:  16 rows of the output over ALL experts in use: the tokens' sums stay in shared memory, in
+//          the order of the slots - no partial results in memory, no atomics.
 #include <math_constants.h>
 
 #include "convert.cuh"
@@ -21,7 +21,17 @@
 namespace emoe {
 namespace {
 
-constexpr int kRouteThreads = 1024, kUpWarps = 8;
+constexpr int kRouteThreads = 256, kUpWarps = 8;
+
+// e4m3 weights as bf16 operands.  A code's magnitude bits, moved to their place, are a bf16 2^120 too
+// small (denormal where the code is), which the tensor cores take as it is; the tokens carry 2^60 of that
+// and the sums the rest, so that neither side leaves its range (tokens below 2^67).  And a word's
+// codes come out as (0, 2) and (1, 3), so the tokens are kept in that order.  (The cvt instructions of
+// this type pair would need a product by 2^120 and a change of order for every word of weights.)
+// f16 operands are what cvt gives: in order and at their own size.
+template <typename T, bool FP8> constexpr bool kMoved = FP8 && !__is_same(T, __half);
+__device__ __forceinline__ int moved_place(int k) { return (k & ~3) | (k & 1) << 1 | (k & 2) >> 1; }
+constexpr float kTokenScale = 0x1p60f, kSumScale = 0x1p60f;
 
 // Logits as unsigned numbers in the same order; NaN counts as minus infinity, and minus infinity and
 // what has been chosen already as 0.
@@ -34,285 +44,324 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// One block.  A warp takes tokens warp and warp + 32: its lanes hold the token's logits in registers,
-// each choice is a maximum over the lanes and then the smallest index that has it.  N: experts a lane.
-template <int N>
+// A block a token.  The first warp holds the token's logits in registers, N experts a lane; each
+// choice is a maximum over the lanes and then the smallest index that has it.  The other warps bring the
+// token into the order and scale that e4m3 products want.
+template <int N, bool MOVED>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_constant__ MoeArgs a) {
-  extern __shared__ unsigned long long s_tokens[];   // [n_slots]: which tokens an expert has
-  int32_t *const s_base = (int32_t *)(s_tokens + a.n_slots);
-  __shared__ int32_t s_scan[2][32];
-  __shared__ int32_t s_total[2];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t = blockIdx.x, lane = threadIdx.x & 31;
   let_next_start();
-  for (int i = threadIdx.x; i < a.n_slots; i += kRouteThreads) s_tokens[i] = 0;
-  if (threadIdx.x < 2) s_total[threadIdx.x] = 0;
-  __syncthreads();
-
-  int my_slot[2] = {-1, -1};   // of pair number `lane` (routed, then shared) of the two tokens
-  float my_weight[2] = {};
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int t = warp + 32 * half;
-    if (t >= a.n_tokens) continue;
-    const float *row = a.logits + t * a.logits_stride;
-    uint32_t key[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) key[j] = j * 32 + lane < a.n_experts ? ordered(row[j * 32 + lane]) : 0;
-    float total = 0.f, top = 0.f, mine = 0.f;
-    int my_id = -1;
-    if (!a.renormalize) {
-      uint32_t best = 0;
-#pragma unroll
-      for (int j = 0; j < N; ++j) best = max(best, key[j]);
-      top = value_of(__reduce_max_sync(0xffffffffu, best));
-#pragma unroll
-      for (int j = 0; j < N; ++j) total += key[j] ? expf(value_of(key[j]) - top) : 0.f;
-#pragma unroll
-      for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    }
-    for (int k = 0; k < a.top_k; ++k) {
-      uint32_t best = 0;
-#pragma unroll
-      for (int j = 0; j < N; ++j) best = max(best, key[j]);
-      best = __reduce_max_sync(0xffffffffu, best);
-      if (best == 0) break;   // nothing above minus infinity is left
-      uint32_t e = 0xffffffffu;
-#pragma unroll
-      for (int j = N - 1; j >= 0; --j)
-        if (key[j] == best) e = j * 32 + lane;
-      e = __reduce_min_sync(0xffffffffu, e);
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (e == (uint32_t)(j * 32 + lane)) key[j] = 0;
-      const float v = value_of(best);
-      if (k == 0) top = v;
-      const float p = expf(v - top);
-      if (a.renormalize) total += p;
-      if (lane == k) {
-        my_id = (int)e;
-        mine = p;
+  if (threadIdx.x >= 32) {
+    if constexpr (MOVED) {
+      const __nv_bfloat16 *const x = (const __nv_bfloat16 *)a.x + t * a.x_stride;
+      uint2 *const to = (uint2 *)((__nv_bfloat16 *)a.moved_x + (int64_t)t * a.d_model);
+      for (int i = threadIdx.x - 32; i < a.d_model / 4; i += kRouteThreads - 32) {
+        const uint2 w = ((const uint2 *)x)[i];
+        const float2 p = Pair<__nv_bfloat16>::unpack(w.x), q = Pair<__nv_bfloat16>::unpack(w.y);
+        to[i] = make_uint2(Pair<__nv_bfloat16>::pack(p.x * kTokenScale, q.x * kTokenScale),
+                           Pair<__nv_bfloat16>::pack(p.y * kTokenScale, q.y * kTokenScale));
       }
     }
-    const float w = my_id >= 0 ? mine / total * a.routed_scale : 0.f;
-    if (lane < a.top_k) {
-      if (a.ids_out) a.ids_out[t * a.top_k + lane] = my_id;
-      if (a.weights_out) a.weights_out[t * a.top_k + lane] = w;
-    }
-    int expert = -1;
-    my_weight[half] = w;
-    if (lane < a.top_k) expert = my_id;
-    else if (lane < a.top_k + a.n_shared) {
-      expert = a.n_experts + lane - a.top_k;
-      my_weight[half] = 1.f;
-    }
-    int slot = expert >= 0 ? a.slot_of_expert[expert] : -1;
-    if (slot >= a.n_slots) {
-      if (a.status) *a.status = EMOE_ERR_PLACEMENT;
-      slot = -1;
-    }
-    my_slot[half] = slot;
-    if (slot >= 0) atomicOr(&s_tokens[slot], 1ull << t);
+    return;
   }
-  __syncthreads();
-
-  // experts in use, in the order of their slots, and the number of pairs before each
-  for (int first = 0; first < a.n_slots; first += kRouteThreads) {
-    const int slot = first + threadIdx.x;
-    const int pairs = slot < a.n_slots ? __popcll(s_tokens[slot]) : 0, used = pairs != 0;
-    int u = used, p = pairs;
+  const float *row = a.logits + t * a.logits_stride;
+  uint32_t key[N];
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const int x = __shfl_up_sync(0xffffffffu, u, d), y = __shfl_up_sync(0xffffffffu, p, d);
-      if (lane >= d) u += x, p += y;
-    }
-    if (lane == 31) s_scan[0][warp] = u, s_scan[1][warp] = p;
-    __syncthreads();
-    const int below = lane < warp ? -1 : 0;
-    u += __reduce_add_sync(0xffffffffu, s_scan[0][lane] & below) + s_total[0];
-    p += __reduce_add_sync(0xffffffffu, s_scan[1][lane] & below) + s_total[1];
-    if (slot < a.n_slots) s_base[slot] = p - pairs;
-    if (used) a.active[u - 1] = make_int2(slot, p - pairs);
-    __syncthreads();
-    if (threadIdx.x == kRouteThreads - 1) s_total[0] = u, s_total[1] = p;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    *a.n_active = s_total[0];
-    a.active[s_total[0]] = make_int2(-1, s_total[1]);   // the end of the last expert's pairs
-  }
+  for (int j = 0; j < N; ++j) key[j] = j * 32 + lane < a.n_experts ? ordered(row[j * 32 + lane]) : 0;
+  float total = 0.f, top = 0.f, mine = 0.f;
+  int my_id = -1;
+  if (!a.renormalize) {
+    uint32_t best = 0;
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if (my_slot[half] < 0) continue;
-    const int t = warp + 32 * half;
-    const int at = s_base[my_slot[half]] + __popcll(s_tokens[my_slot[half]] & ((1ull << t) - 1));
-    a.pair_token[at] = t;
-    a.pair_weight[at] = my_weight[half];
+    for (int j = 0; j < N; ++j) best = max(best, key[j]);
+    top = value_of(__reduce_max_sync(0xffffffffu, best));
+#pragma unroll
+    for (int j = 0; j < N; ++j) total += key[j] ? expf(value_of(key[j]) - top) : 0.f;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   }
+  for (int k = 0; k < a.top_k; ++k) {
+    uint32_t best = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) best = max(best, key[j]);
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (best == 0) break;   // nothing above minus infinity is left
+    uint32_t e = 0xffffffffu;
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j)
+      if (key[j] == best) e = j * 32 + lane;
+    e = __reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (e == (uint32_t)(j * 32 + lane)) key[j] = 0;
+    const float v = value_of(best);
+    if (k == 0) top = v;
+    const float p = expf(v - top);
+    if (a.renormalize) total += p;
+    if (lane == k) {
+      my_id = (int)e;
+      mine = p;
+    }
+  }
+  float w = my_id >= 0 ? mine / total * a.routed_scale : 0.f;
+  if (lane < a.top_k) {
+    if (a.ids_out) a.ids_out[t * a.top_k + lane] = my_id;
+    if (a.weights_out) a.weights_out[t * a.top_k + lane] = w;
+  }
+  const int chosen = a.top_k + a.n_shared;
+  if (lane >= chosen) return;
+  int expert = my_id;
+  if (lane >= a.top_k) {
+    expert = a.n_experts + lane - a.top_k;
+    w = 1.f;
+  }
+  int slot = expert >= 0 ? a.slot_of_expert[expert] : -1;
+  if (slot >= a.n_slots) {
+    if (a.status) *a.status = EMOE_ERR_PLACEMENT;
+    slot = -1;
+  }
+  a.choice[t * chosen + lane] = make_int2(slot < 0 ? -1 : slot, __float_as_int(w));
 }
+
+// The choices grouped by expert, built by each block for itself: (slot, first pair) of each expert in
+// use in the order of the slots, one more entry for the end, and each pair's token and weight, in the
+// order of the tokens.  `scratch` is free again afterwards.
+struct Routed {
+  int2 *active;
+  float *weight;
+  uint8_t *token;
+  int n_active;
+
+  __device__ __forceinline__ void build(const MoeArgs &a, uint8_t *at, uint8_t *scratch) {
+    __shared__ int s_scan[2][32], s_total[2];
+    unsigned long long *const tokens = (unsigned long long *)scratch;   // [n_slots]
+    int *const base = (int *)(tokens + a.n_slots);                      // [n_slots]
+    const int chosen = a.top_k + a.n_shared, pairs = a.n_tokens * chosen;
+    const int most = min(pairs, a.n_slots);
+    active = (int2 *)at;
+    weight = (float *)(active + most + 1);
+    token = (uint8_t *)(weight + pairs);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int i = threadIdx.x; i < a.n_slots; i += blockDim.x) tokens[i] = 0;
+    if (threadIdx.x < 2) s_total[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+      const int slot = __ldcg(&a.choice[i].x);
+      if (slot >= 0) atomicOr(&tokens[slot], 1ull << (i / chosen));
+    }
+    __syncthreads();
+    for (int first = 0; first < a.n_slots; first += blockDim.x) {
+      const int slot = first + threadIdx.x;
+      const int n = slot < a.n_slots ? __popcll(tokens[slot]) : 0, used = n != 0;
+      int u = used, p = n;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, u, d), y = __shfl_up_sync(0xffffffffu, p, d);
+        if (lane >= d) u += x, p += y;
+      }
+      if (lane == 31) s_scan[0][warp] = u, s_scan[1][warp] = p;
+      __syncthreads();
+      for (int i = 0; i < warp; ++i) u += s_scan[0][i], p += s_scan[1][i];
+      u += s_total[0];
+      p += s_total[1];
+      if (slot < a.n_slots) base[slot] = p - n;
+      if (used) active[u - 1] = make_int2(slot, p - n);
+      __syncthreads();
+      if (warp == warps - 1 && lane == 31) s_total[0] = u, s_total[1] = p;
+      __syncthreads();
+    }
+    n_active = s_total[0];
+    if (threadIdx.x == 0) active[n_active] = make_int2(-1, s_total[1]);
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) {
+      const int2 c = __ldcg(a.choice + i);
+      if (c.x < 0) continue;
+      const int t = i / chosen, pair = base[c.x] + __popcll(tokens[c.x] & ((1ull << t) - 1));
+      token[pair] = (uint8_t)t;
+      weight[pair] = __int_as_float(c.y);
+    }
+    __syncthreads();
+  }
+};
+size_t routed_bytes(const MoeArgs &a) {
+  const int pairs = a.n_tokens * (a.top_k + a.n_shared);
+  return ((size_t)(pairs < a.n_slots ? pairs : a.n_slots) + 1) * 8 + (size_t)pairs * 5;
+}
+size_t scratch_bytes(const MoeArgs &a) { return (size_t)a.n_slots * 12; }
 
 // ---- the weight stream --------------------------------------------------------------------
 
-// A block of the k axis: 16 bytes of weights a lane and row, four lanes a row; kTok 16-byte parts of the
-// matching token elements a lane.
-template <bool FP8> struct Block {
-  static constexpr int kElems = FP8 ? 64 : 32, kProducts = FP8 ? 4 : 2, kTok = FP8 ? 2 : 1, kES = FP8 ? 1 : 2;
-  static constexpr int kStageBytes = (2 + kTok) * 512;
+// A step of the k axis: 128 bytes of each of 16 weight rows, a lane having bytes 16c.. and 64 + 16c.. of
+// rows g and g + 8 (g = lane / 4, c = lane % 4), and the same elements of token g.
+template <bool FP8> struct Step {
+  static constexpr int kES = FP8 ? 1 : 2, kElems = 128 / kES, kHalf = kElems / 2, kLane = 16 / kES;
+  static constexpr int kTok = FP8 ? 2 : 1;              // 16-byte parts of a token a lane and half
+  static constexpr int kBytes = (4 + 2 * kTok) * 512;   // of a warp's ring
+};
+template <bool FP8> struct TokenPart { uint4 v[2 * Step<FP8>::kTok]; };
+
+template <bool FP8, int STAGES>
+struct Ring {
+  using S = Step<FP8>;
+  uint8_t *base;
+  uint32_t at;
+  __device__ __forceinline__ explicit Ring(uint8_t *smem) {
+    base = smem + (threadIdx.x >> 5) * (STAGES * S::kBytes) + (threadIdx.x & 31) * 16;
+    at = shared_address(base);
+  }
+  // n0, n1: 16 where the halves lie inside the row, else 0
+  __device__ __forceinline__ void fill_weights(int stage, const uint8_t *lo, const uint8_t *hi, uint32_t n0, uint32_t n1) {
+    const uint32_t dst = at + stage * S::kBytes;
+    copy_async_16(dst, lo, n0);
+    copy_async_16(dst + 512, hi, n0);
+    copy_async_16(dst + 1024, lo + (n1 ? 64 : 0), n1);
+    copy_async_16(dst + 1536, hi + (n1 ? 64 : 0), n1);
+  }
+  __device__ __forceinline__ void fill_token(int stage, const uint8_t *tok, uint32_t n0, uint32_t n1) {
+    const uint32_t dst = at + stage * S::kBytes + 2048;
+#pragma unroll
+    for (int i = 0; i < S::kTok; ++i) {
+      copy_async_16(dst + i * 512, tok + i * 16, n0);
+      copy_async_16(dst + (S::kTok + i) * 512, tok + (n1 ? S::kHalf * 2 : 0) + i * 16, n1);
+    }
+  }
+  __device__ __forceinline__ uint4 get(int stage, int i) const { return *(const uint4 *)(base + stage * S::kBytes + i * 512); }
 };
 
-// Weight rows g and g + 8 of a block, 16 bytes each, as the 16-row operand of product j.
-template <typename T, bool FP8>
-__device__ __forceinline__ void weight_operand(uint32_t (&r)[4], const uint4 &lo, const uint4 &hi, int j) {
-  if constexpr (FP8) {
-    const uint32_t x = j == 0 ? lo.x : j == 1 ? lo.y : j == 2 ? lo.z : lo.w;
-    const uint32_t y = j == 0 ? hi.x : j == 1 ? hi.y : j == 2 ? hi.z : hi.w;
-    r[0] = even_codes<T>(x);
-    r[1] = even_codes<T>(y);
-    r[2] = odd_codes<T>(x);
-    r[3] = odd_codes<T>(y);
-  } else {
-    r[0] = j ? lo.z : lo.x;
-    r[1] = j ? hi.z : hi.x;
-    r[2] = j ? lo.w : lo.y;
-    r[3] = j ? hi.w : hi.y;
-  }
-}
-// This lane's part of a token's block, and the operand of product j from it.
-template <bool FP8> struct TokenPart { uint4 v[Block<FP8>::kTok]; };
 template <bool FP8>
-__device__ __forceinline__ void token_operand(uint32_t &b0, uint32_t &b1, const TokenPart<FP8> &t, int j) {
-  if constexpr (FP8) {   // the codes of a word come out as (0, 2) and (1, 3)
-    const uint4 &v = t.v[j >> 1];
-    const uint32_t lo = j & 1 ? v.z : v.x, hi = j & 1 ? v.w : v.y;
-    b0 = __byte_perm(lo, hi, 0x5410);
-    b1 = __byte_perm(lo, hi, 0x7632);
-  } else {
-    b0 = j ? t.v[0].z : t.v[0].x;
-    b1 = j ? t.v[0].w : t.v[0].y;
-  }
-}
-template <bool FP8>
-__device__ __forceinline__ TokenPart<FP8> load_token(const uint8_t *p, bool there) {
+__device__ __forceinline__ TokenPart<FP8> load_token(const uint8_t *p, bool in0, bool in1) {
+  using S = Step<FP8>;
   TokenPart<FP8> r = {};
-  if (there) {
 #pragma unroll
-    for (int i = 0; i < Block<FP8>::kTok; ++i) r.v[i] = ((const uint4 *)p)[i];
+  for (int i = 0; i < S::kTok; ++i) {
+    if (in0) r.v[i] = *(const uint4 *)(p + i * 16);
+    if (in1) r.v[S::kTok + i] = *(const uint4 *)(p + S::kHalf * 2 + i * 16);
   }
   return r;
 }
 
-// One lane's ring: what it copies there it reads back itself.
-template <bool FP8, int STAGES>
-struct Ring {
-  static constexpr int kStage = Block<FP8>::kStageBytes;
-  uint8_t *base;
-  uint32_t at;
-  __device__ __forceinline__ explicit Ring(uint8_t *smem) {
-    base = smem + (threadIdx.x >> 5) * (STAGES * kStage) + (threadIdx.x & 31) * 16;
-    at = shared_address(base);
-  }
-  __device__ __forceinline__ void fill(int stage, const uint8_t *lo, const uint8_t *hi, const uint8_t *tok, bool there, bool tok_there) {
-    const uint32_t dst = at + stage * kStage;
-    copy_async_16(dst, lo, there ? 16 : 0);
-    copy_async_16(dst + 512, hi, there ? 16 : 0);
-#pragma unroll
-    for (int i = 0; i < Block<FP8>::kTok; ++i) copy_async_16(dst + 1024 + i * 512, tok + i * 16, tok_there ? 16 : 0);
-  }
-  __device__ __forceinline__ uint4 lo(int stage) const { return *(const uint4 *)(base + stage * kStage); }
-  __device__ __forceinline__ uint4 hi(int stage) const { return *(const uint4 *)(base + stage * kStage + 512); }
-  __device__ __forceinline__ TokenPart<FP8> token(int stage) const {
-    TokenPart<FP8> r;
-#pragma unroll
-    for (int i = 0; i < Block<FP8>::kTok; ++i) r.v[i] = *(const uint4 *)(base + stage * kStage + 1024 + i * 512);
-    return r;
-  }
-};
+__device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// acc += weights x tokens over one block; e4m3 blocks come with the scales of rows g and g + 8.
-template <typename T, bool FP8>
-__device__ __forceinline__ void block_product(float (&acc)[4], const uint4 &lo, const uint4 &hi, const TokenPart<FP8> &tok,
-                                              float scale_lo, float scale_hi) {
-  float part[4] = {};
-#pragma unroll
-  for (int j = 0; j < Block<FP8>::kProducts; ++j) {
-    uint32_t w[4], b0, b1;
-    weight_operand<T, FP8>(w, lo, hi, j);
-    token_operand<FP8>(b0, b1, tok, j);
-    if constexpr (FP8) mma_16816<T>(part, w, b0, b1);
-    else mma_16816<T>(acc, w, b0, b1);
+// Two pairs of operands from a word of four codes (see kMoved for which codes, and their scale).
+template <typename T>
+__device__ __forceinline__ void word_of_codes(uint32_t &first, uint32_t &second, uint32_t w) {
+  if constexpr (__is_same(T, __half)) {
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+        : "=r"(first), "=r"(second) : "r"(w));
+  } else {
+    first = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
+    second = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
   }
+}
+
+// acc += 16 weight rows x 8 tokens over one step; e4m3 steps come with the scales of rows g and g + 8.
+template <typename T, bool FP8>
+__device__ __forceinline__ void step_product(float (&acc)[4], const uint4 (&w)[4], const TokenPart<FP8> &tok, float scale_lo,
+                                             float scale_hi) {
   if constexpr (FP8) {
+    float part[4] = {};
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t r[4];
+        word_of_codes<T>(r[0], r[2], word(w[2 * half], j));
+        word_of_codes<T>(r[1], r[3], word(w[2 * half + 1], j));
+        const uint4 &v = tok.v[2 * half + (j >> 1)];
+        mma_16816<T>(part, r, j & 1 ? v.z : v.x, j & 1 ? v.w : v.y);
+      }
     acc[0] += part[0] * scale_lo;
     acc[1] += part[1] * scale_lo;
     acc[2] += part[2] * scale_hi;
     acc[3] += part[3] * scale_hi;
+  } else {
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t r[4] = {word(w[2 * half], 2 * j), word(w[2 * half + 1], 2 * j), word(w[2 * half], 2 * j + 1), word(w[2 * half + 1], 2 * j + 1)};
+        mma_16816<T>(acc, r, word(tok.v[half], 2 * j), word(tok.v[half], 2 * j + 1));
+      }
   }
 }
 
-// What the routing found, in shared memory: (slot, first pair) of each expert in use and one more
-// entry for the end, and each pair's token.
-struct Routed {
-  int2 *active;
-  uint8_t *token;
-  int n_active;
-  __device__ __forceinline__ void read(const MoeArgs &a, uint8_t *at) {
-    n_active = __ldcg(a.n_active);
-    active = (int2 *)at;
-    for (int i = threadIdx.x; i <= n_active; i += blockDim.x) active[i] = __ldcg(a.active + i);
-    __syncthreads();
-    token = at + (n_active + 1) * 8;
-    const int pairs = active[n_active].y;
-    for (int i = threadIdx.x; i < pairs; i += blockDim.x) token[i] = (uint8_t)__ldcg(a.pair_token + i);
-    __syncthreads();
+// The products of one step for all column tiles of an expert: the first tile's tokens lie in the ring,
+// the further ones (more than 8 tokens) are read from L2, two tiles at a time.  column(n): this lane's
+// token of tile n, null if there is none.
+template <typename T, bool FP8, int NT, int STAGES, typename F>
+__device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP8, STAGES> &ring, int stage, int count, int step,
+                                              bool in0, bool in1, float scale_lo, float scale_hi, F column) {
+  using S = Step<FP8>;
+  uint4 w[4];
+  TokenPart<FP8> tok;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = ring.get(stage, i);
+#pragma unroll
+  for (int i = 0; i < 2 * S::kTok; ++i) tok.v[i] = ring.get(stage, 4 + i);
+  step_product<T, FP8>(acc[0], w, tok, scale_lo, scale_hi);
+  if constexpr (NT > 1) {
+    if (count <= 8) return;
+    const int64_t off = (int64_t)step * (S::kElems * 2);
+#pragma unroll
+    for (int n = 1; n < NT; n += 2) {
+      if (n * 8 >= count) break;
+      const uint8_t *const p0 = column(n), *const p1 = n + 1 < NT ? column(n + 1) : nullptr;
+      const TokenPart<FP8> x0 = load_token<FP8>(p0 + off, p0 && in0, p0 && in1), x1 = load_token<FP8>(p1 + off, p1 && in0, p1 && in1);
+      step_product<T, FP8>(acc[n], w, x0, scale_lo, scale_hi);
+      if constexpr (NT > 2)
+        if (n + 1 < NT) step_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], w, x1, scale_lo, scale_hi);
+    }
   }
-};
-int routed_bytes(const MoeArgs &a) {
-  const int pairs = a.n_tokens * (a.top_k + a.n_shared);
-  return ((pairs < a.n_slots ? pairs : a.n_slots) + 1) * 8 + pairs;
 }
 
 // h[pair] = w silu(gate) up, rounded once to T.  An item is 8 rows of gate and the same 8 of up as one
 // 16-row operand, so a thread gets both sums of its outputs.  The k axis is split over the warps,
-// joined in shared memory in the order of the warps.  NT: column tiles of 8 tokens an expert may have;
-// the first comes through the ring, the others (more than 8 tokens of one expert) straight from L2.
+// joined in shared memory in the order of the warps.  NT: column tiles of 8 tokens an expert may have.
 template <typename T, bool FP8, int NT, int STAGES>
 __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_part[2][kUpWarps][16][9];
-  using B = Block<FP8>;
+  using S = Step<FP8>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   wait_for_previous();
   let_next_start();
   Routed routed;
-  routed.read(a, smem + kUpWarps * STAGES * B::kStageBytes);
+  routed.build(a, smem + a.ring_bytes, smem);
   const int tiles = a.d_ff / 8;
   const int items = routed.n_active * tiles;
-  const int blocks = (a.d_model + B::kElems - 1) / B::kElems;
-  const int kb0 = blocks * warp / kUpWarps, kb1 = blocks * (warp + 1) / kUpWarps;
-  const int64_t row_bytes = (int64_t)a.d_model * B::kES;
-  const int lane_k = c * (16 / B::kES);   // this lane's first element inside a block
-  const uint8_t *const x_lane = (const uint8_t *)a.x + lane_k * 2;
+  const int steps = (a.d_model + S::kElems - 1) / S::kElems;
+  const int k0 = steps * warp / kUpWarps, k1 = steps * (warp + 1) / kUpWarps;
+  const int64_t row_bytes = (int64_t)a.d_model * S::kES;
+  // the step at which this lane's half leaves the row: only the last one can
+  const int end0 = (a.d_model - c * S::kLane + S::kElems - 1) / S::kElems;
+  const int end1 = (a.d_model - c * S::kLane - S::kHalf + S::kElems - 1) / S::kElems;
+  const uint8_t *const x_lane = (const uint8_t *)(kMoved<T, FP8> ? a.moved_x : a.x) + c * S::kLane * 2;
+  const int64_t x_stride = (kMoved<T, FP8> ? a.d_model : a.x_stride) * 2;
 
   Ring<FP8, STAGES> ring(smem);
-  // the copies run ahead of the products over (item, block)
-  int fill_item = kb0 < kb1 ? blockIdx.x : items, fill_kb = kb0, fill_stage = 0;
+  // the copies run ahead of the products over (item, step)
+  int fill_item = k0 < k1 ? blockIdx.x : items, fill_k = k0, fill_stage = 0;
   const uint8_t *fill_lo = nullptr, *fill_hi = nullptr, *fill_tok = nullptr;
-  bool fill_col = false;
+  uint32_t fill_col = 0;
   auto enter = [&]() {
     if (fill_item >= items) return;
     const int i = fill_item / tiles, row = (fill_item - i * tiles) * 8 + g;
     const int2 e = routed.active[i];
-    fill_lo = a.gate + e.x * a.gate_stride + row * row_bytes + c * 16;
-    fill_hi = a.up + e.x * a.gate_stride + row * row_bytes + c * 16;
-    fill_col = g < routed.active[i + 1].y - e.y;
-    fill_tok = fill_col ? x_lane + routed.token[e.y + g] * a.x_stride * 2 : x_lane;
+    const int64_t at = e.x * a.gate_stride + row * row_bytes + c * 16 + k0 * 128;
+    fill_lo = a.gate + at;
+    fill_hi = a.up + at;
+    fill_col = g < routed.active[i + 1].y - e.y ? 16 : 0;
+    fill_tok = x_lane + (fill_col ? routed.token[e.y + g] * x_stride : 0) + k0 * (S::kElems * 2);
   };
   auto fill = [&]() {
     if (fill_item < items) {
-      const bool there = fill_kb * B::kElems + lane_k < a.d_model;
-      const int off = there ? fill_kb * 64 : 0;
-      ring.fill(fill_stage, fill_lo + off, fill_hi + off, fill_tok + off * B::kTok, there, there && fill_col);
-      if (++fill_kb == kb1) {
-        fill_kb = kb0;
+      const uint32_t n0 = fill_k < end0 ? 16 : 0, n1 = fill_k < end1 ? 16 : 0;
+      ring.fill_weights(fill_stage, n0 ? fill_lo : a.gate, n0 ? fill_hi : a.gate, n0, n1);
+      ring.fill_token(fill_stage, n0 ? fill_tok : x_lane, n0 & fill_col, n1 & fill_col);
+      fill_lo += 128;
+      fill_hi += 128;
+      fill_tok += S::kElems * 2;
+      if (++fill_k == k1) {
+        fill_k = k0;
         fill_item += gridDim.x;
         enter();
       }
@@ -331,44 +380,30 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
     float acc[NT][4] = {};
     const uint8_t *more[NT];   // this lane's column of the further tiles
 #pragma unroll
-    for (int n = 1; n < NT; ++n)
-      more[n] = n * 8 + g < count ? x_lane + routed.token[e.y + n * 8 + g] * a.x_stride * 2 : nullptr;
+    for (int n = 1; n < NT; ++n) more[n] = n * 8 + g < count ? x_lane + routed.token[e.y + n * 8 + g] * x_stride : nullptr;
     const float *scale_g = nullptr, *scale_u = nullptr;
     float sg = 1.f, su = 1.f;
     if constexpr (FP8) {
       const int64_t at = e.x * a.scale_stride + (row0 / 128) * ((a.d_model + 127) / 128);
       scale_g = a.gate_scale + at;
       scale_u = a.up_scale + at;
-      if (kb0 < kb1) {
-        sg = scale_g[kb0 >> 1];
-        su = scale_u[kb0 >> 1];
+      if (k0 < k1) {
+        sg = scale_g[k0];
+        su = scale_u[k0];
       }
     }
-    for (int kb = kb0; kb < kb1; ++kb) {
+    for (int k = k0; k < k1; ++k) {
       fill();
       float next_g = 1.f, next_u = 1.f;
-      if constexpr (FP8) {   // one scale for two blocks, read a block ahead
-        if (kb + 1 < kb1) {
-          next_g = scale_g[(kb + 1) >> 1];
-          next_u = scale_u[(kb + 1) >> 1];
+      if constexpr (FP8) {   // a step is one block of the scales; read a step ahead
+        if (k + 1 < k1) {
+          next_g = scale_g[k + 1];
+          next_u = scale_u[k + 1];
         }
       }
       copy_async_wait<STAGES - 1>();
-      const uint4 lo = ring.lo(stage), hi = ring.hi(stage);
-      block_product<T, FP8>(acc[0], lo, hi, ring.token(stage), sg, su);
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, k, k < end0, k < end1, sg, su, [&](int n) { return more[n]; });
       stage = stage + 1 == STAGES ? 0 : stage + 1;
-      if (NT > 1 && count > 8) {
-        const bool there = kb * B::kElems + lane_k < a.d_model;
-        const int64_t off = (int64_t)kb * (B::kElems * 2);
-#pragma unroll
-        for (int n = 1; n < NT; n += 2) {
-          if (n * 8 >= count) break;
-          const TokenPart<FP8> x0 = load_token<FP8>(more[n] + off, there && more[n]);
-          const TokenPart<FP8> x1 = load_token<FP8>(more[n + 1 < NT ? n + 1 : n] + off, n + 1 < NT && there && more[n + 1 < NT ? n + 1 : n]);
-          block_product<T, FP8>(acc[n], lo, hi, x0, sg, su);
-          if (n + 1 < NT) block_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], lo, hi, x1, sg, su);
-        }
-      }
       sg = next_g;
       su = next_u;
     }
@@ -392,10 +427,15 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
         }
         if (n * 8 + j < count) {
           const int pair = e.y + n * 8 + j;
-          float h = gate / (1.f + expf(-gate)) * up * a.pair_weight[pair];
+          if constexpr (kMoved<T, FP8>) {
+            gate *= kSumScale;
+            up *= kSumScale;
+          }
+          float h = gate / (1.f + expf(-gate)) * up * routed.weight[pair];
           // f16 ends at 65504: the largest value stands for what is beyond (bf16 reaches as far as 32 bits)
           if constexpr (__is_same(T, __half)) h = h != h ? h : fminf(fmaxf(h, -65504.f), 65504.f);
-          ((T *)a.h)[(int64_t)pair * a.d_ff + row0 + f] = T(h);
+          const int at = row0 + f;
+          ((T *)a.h)[(int64_t)pair * a.d_ff + (kMoved<T, FP8> ? moved_place(at) : at)] = T(kMoved<T, FP8> ? h * kTokenScale : h);
         }
       }
     }
@@ -403,105 +443,117 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
   copy_async_wait<0>();
 }
 
-// y for 16 output rows a block: the (expert, block of k) steps of all experts in use are dealt to the
+// y for 16 output rows a block: the (expert, step) pairs of all experts in use are dealt to the
 // warps in equal runs.  At the end of its part of an expert a warp adds the expert's columns to its
 // own sums of the tokens in shared memory; the warps' sums are joined at the end, in their order.
 template <typename T, bool FP8, int NT, int STAGES, int WARPS, bool F32_OUT>
 __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
-  using B = Block<FP8>;
+  using S = Step<FP8>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int row0 = blockIdx.x * 16;
-  const int blocks = (a.d_ff + B::kElems - 1) / B::kElems;
-  const int64_t row_bytes = (int64_t)a.d_ff * B::kES;
-  const int lane_k = c * (16 / B::kES);
-  float *const sums = (float *)(smem + WARPS * STAGES * B::kStageBytes);   // [warp][token][17]
-  for (int i = threadIdx.x; i < WARPS * a.n_tokens * 17; i += WARPS * 32) sums[i] = 0.f;
-  wait_for_previous();
+  const int steps = (a.d_ff + S::kElems - 1) / S::kElems;
+  const int64_t row_bytes = (int64_t)a.d_ff * S::kES;
+  const int end0 = (a.d_ff - c * S::kLane + S::kElems - 1) / S::kElems;
+  const int end1 = (a.d_ff - c * S::kLane - S::kHalf + S::kElems - 1) / S::kElems;
+  float *const sums = (float *)(smem + a.ring_bytes);   // [warp][token][17]
+  const int sum_count = (WARPS * a.n_tokens * 17 + 1) / 2 * 2;
+  for (int i = threadIdx.x; i < sum_count; i += WARPS * 32) sums[i] = 0.f;
+  // The choices were written by the launch before the last, which had ended before that one began its
+  // work: they can be read, and weights fetched, while the hidden vectors are still being made.
   Routed routed;
-  routed.read(a, (uint8_t *)(sums + (WARPS * a.n_tokens * 17 + 3) / 4 * 4));
-  const int total = routed.n_active * blocks;   // at most 4096 experts x 32768 blocks
+  routed.build(a, (uint8_t *)(sums + sum_count), smem);
+  const int total = routed.n_active * steps;   // at most 2048 experts x 16384 steps
   const int s0 = (int)((int64_t)total * warp / WARPS), s1 = (int)((int64_t)total * (warp + 1) / WARPS);
-  const uint8_t *const h_lane = (const uint8_t *)a.h + lane_k * 2;
+  const uint8_t *const h_lane = (const uint8_t *)a.h + c * S::kLane * 2;
 
   Ring<FP8, STAGES> ring(smem);
-  int fill_step = s0, fill_expert = s0 / blocks, fill_kb = s0 - fill_expert * blocks, fill_stage = 0;
-  const uint8_t *fill_lo = nullptr, *fill_tok = nullptr;
-  bool fill_col = false;
-  auto enter = [&]() {
-    if (fill_expert >= routed.n_active) return;
-    const int2 e = routed.active[fill_expert];
-    fill_lo = a.down + e.x * a.down_stride + (row0 + g) * row_bytes + c * 16;
-    fill_col = g < routed.active[fill_expert + 1].y - e.y;
-    fill_tok = h_lane + (fill_col ? (int64_t)(e.y + g) * a.d_ff * 2 : 0);
+  struct Cursor {
+    int step, expert, k, stage;
+  } wf = {s0, s0 / steps, s0 % steps, 0}, tf = wf;
+  const uint8_t *fill_w = nullptr, *fill_tok = nullptr;
+  uint32_t fill_col = 0;
+  auto enter_weights = [&]() {
+    if (wf.expert < routed.n_active)
+      fill_w = a.down + routed.active[wf.expert].x * a.down_stride + (row0 + g) * row_bytes + c * 16 + wf.k * 128;
   };
-  auto fill = [&]() {
-    if (fill_step < s1) {
-      const bool there = fill_kb * B::kElems + lane_k < a.d_ff;
-      const int off = there ? fill_kb * 64 : 0;
-      ring.fill(fill_stage, fill_lo + off, fill_lo + 8 * row_bytes + off, fill_tok + off * B::kTok, there, there && fill_col);
-      ++fill_step;
-      if (++fill_kb == blocks) {
-        fill_kb = 0;
-        ++fill_expert;
-        enter();
-      }
+  auto enter_tokens = [&]() {
+    if (tf.expert >= routed.n_active) return;
+    const int first = routed.active[tf.expert].y;
+    fill_col = g < routed.active[tf.expert + 1].y - first ? 16 : 0;
+    fill_tok = h_lane + (fill_col ? (int64_t)(first + g) * a.d_ff * 2 : 0) + tf.k * (S::kElems * 2);
+  };
+  auto next = [&](Cursor &cur, auto enter) {
+    ++cur.step;
+    if (++cur.k == steps) {
+      cur.k = 0;
+      ++cur.expert;
+      enter();
+    }
+  };
+  auto fill_weights = [&]() {
+    if (wf.step < s1) {
+      const uint32_t n0 = wf.k < end0 ? 16 : 0, n1 = wf.k < end1 ? 16 : 0;
+      ring.fill_weights(wf.stage, n0 ? fill_w : a.down, n0 ? fill_w + 8 * row_bytes : a.down, n0, n1);
+      fill_w += 128;
+      next(wf, enter_weights);
+    }
+    wf.stage = wf.stage + 1 == STAGES ? 0 : wf.stage + 1;
+  };
+  auto fill_tokens = [&]() {
+    if (tf.step < s1) {
+      const uint32_t n0 = tf.k < end0 ? 16 : 0, n1 = tf.k < end1 ? 16 : 0;
+      ring.fill_token(tf.stage, n0 ? fill_tok : h_lane, n0 & fill_col, n1 & fill_col);
+      fill_tok += S::kElems * 2;
+      next(tf, enter_tokens);
     }
     copy_async_commit();
-    fill_stage = fill_stage + 1 == STAGES ? 0 : fill_stage + 1;
+    tf.stage = tf.stage + 1 == STAGES ? 0 : tf.stage + 1;
   };
-  enter();
-  for (int i = 0; i < STAGES - 1; ++i) fill();
+  enter_weights();
+  for (int i = 0; i < STAGES - 1; ++i) fill_weights();
+  wait_for_previous();
+  enter_tokens();
+  for (int i = 0; i < STAGES - 1; ++i) fill_tokens();   // the first of these groups holds all those weights too
 
   int stage = 0, s = s0;
-  for (int expert = s0 / blocks; s < s1; ++expert) {
+  for (int expert = s0 / steps; s < s1; ++expert) {
     const int2 e = routed.active[expert];
     const int count = routed.active[expert + 1].y - e.y;
-    const int first = s - expert * blocks, last = min(blocks, s1 - expert * blocks);
+    const int first = s - expert * steps, last = min(steps, s1 - expert * steps);
     s += last - first;
     const float *scale = nullptr;
     float by = 1.f;
     if constexpr (FP8) {
       scale = a.down_scale + (int64_t)e.x * a.scale_stride + (row0 / 128) * ((a.d_ff + 127) / 128);
-      by = scale[first >> 1];
+      by = scale[first];
     }
-    const uint8_t *const h0 = h_lane + (int64_t)(e.y + g) * a.d_ff * 2;
     float acc[NT][4] = {};
-    for (int kb = first; kb < last; ++kb) {
-      fill();
-      float next = 1.f;
+    for (int k = first; k < last; ++k) {
+      fill_weights();
+      fill_tokens();
+      float later = 1.f;
       if constexpr (FP8) {
-        if (kb + 1 < last) next = scale[(kb + 1) >> 1];
+        if (k + 1 < last) later = scale[k + 1];
       }
       copy_async_wait<STAGES - 1>();
-      const uint4 lo = ring.lo(stage), hi = ring.hi(stage);
-      block_product<T, FP8>(acc[0], lo, hi, ring.token(stage), by, by);
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, k, k < end0, k < end1, by, by, [&](int n) {
+        return n * 8 + g < count ? h_lane + (int64_t)(e.y + n * 8 + g) * a.d_ff * 2 : nullptr;
+      });
       stage = stage + 1 == STAGES ? 0 : stage + 1;
-      if (NT > 1 && count > 8) {
-        const bool there = kb * B::kElems + lane_k < a.d_ff;
-        const uint8_t *const p = h0 + (int64_t)kb * (B::kElems * 2);
-#pragma unroll
-        for (int n = 1; n < NT; n += 2) {
-          if (n * 8 >= count) break;
-          const TokenPart<FP8> x0 = load_token<FP8>(p + (int64_t)n * 8 * a.d_ff * 2, there && n * 8 + g < count);
-          const TokenPart<FP8> x1 = load_token<FP8>(p + (int64_t)(n + 1) * 8 * a.d_ff * 2, n + 1 < NT && there && (n + 1) * 8 + g < count);
-          block_product<T, FP8>(acc[n], lo, hi, x0, by, by);
-          if (n + 1 < NT) block_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], lo, hi, x1, by, by);
-        }
-      }
-      by = next;
+      by = later;
     }
     float *const mine = sums + warp * a.n_tokens * 17;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if (n * 8 >= count) break;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {   // columns 2c and 2c + 1: no two lanes have the same token and row
-        const int j = n * 8 + 2 * c + k;
+      for (int i = 0; i < 2; ++i) {   // columns 2c and 2c + 1: no two lanes have the same token and row
+        const int j = n * 8 + 2 * c + i;
         if (j < count) {
           float *const y = mine + routed.token[e.y + j] * 17;
-          y[g] += acc[n][k];
-          y[g + 8] += acc[n][2 + k];
+          y[g] += acc[n][i];
+          y[g + 8] += acc[n][2 + i];
         }
       }
     }
@@ -514,6 +566,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
     float y = 0.f;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) y += sums[(w * a.n_tokens + t) * 17 + r];
+    if constexpr (kMoved<T, FP8>) y *= kSumScale;
     if constexpr (F32_OUT) ((float *)a.out)[t * a.out_stride + row0 + r] = y;
     else ((T *)a.out)[t * a.out_stride + row0 + r] = T(y);
   }
@@ -538,27 +591,34 @@ cudaError_t launch(K kernel, unsigned grid, int threads, size_t smem, bool early
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+size_t ring_bytes(size_t ring, const MoeArgs &a) {   // the ring's place also serves to group the choices
+  const size_t n = ring > scratch_bytes(a) ? ring : scratch_bytes(a);
+  return (n + 127) / 128 * 128;
+}
+
 template <typename T, bool FP8, int NT, int STAGES, int WARPS>
-cudaError_t launch_down(const MoeArgs &a, bool f32_out, cudaStream_t st) {
-  const size_t smem = (size_t)WARPS * STAGES * Block<FP8>::kStageBytes + (size_t)(WARPS * a.n_tokens * 17 + 3) / 4 * 16 + routed_bytes(a);
+cudaError_t launch_down(MoeArgs a, bool f32_out, cudaStream_t st) {
+  a.ring_bytes = (int32_t)ring_bytes((size_t)WARPS * STAGES * Step<FP8>::kBytes, a);
+  const size_t smem = a.ring_bytes + (size_t)(WARPS * a.n_tokens * 17 + 1) / 2 * 8 + routed_bytes(a);
   return f32_out ? launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, true>, a.d_model / 16, WARPS * 32, smem, true, a, st)
                  : launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, false>, a.d_model / 16, WARPS * 32, smem, true, a, st);
 }
 
 template <typename T, bool FP8, int NT>
-cudaError_t launch_layer(const MoeArgs &a, bool f32_out, cudaStream_t st) {
-  cudaError_t e = a.n_experts <= 256 ? launch(moe_route_kernel<8>, 1, kRouteThreads, (size_t)a.n_slots * 12, false, a, st)
-                                     : launch(moe_route_kernel<32>, 1, kRouteThreads, (size_t)a.n_slots * 12, false, a, st);
+cudaError_t launch_layer(MoeArgs a, bool f32_out, cudaStream_t st) {
+  cudaError_t e = a.n_experts <= 256 ? launch(moe_route_kernel<8, kMoved<T, FP8>>, a.n_tokens, kRouteThreads, 0, false, a, st)
+                                     : launch(moe_route_kernel<32, kMoved<T, FP8>>, a.n_tokens, kRouteThreads, 0, false, a, st);
   if (e != cudaSuccess) return e;
-  constexpr int kStages = FP8 ? 6 : 8;   // 96 KB: two blocks an SM
+  constexpr int kStages = FP8 ? 3 : 4;   // 96 KB: two blocks an SM
   const int64_t pairs = (int64_t)a.n_tokens * (a.top_k + a.n_shared);
   const int64_t most = (pairs < a.n_slots ? pairs : a.n_slots) * (a.d_ff / 8);
+  a.ring_bytes = (int32_t)ring_bytes((size_t)kUpWarps * kStages * Step<FP8>::kBytes, a);
   e = launch(moe_up_kernel<T, FP8, NT, kStages>, (unsigned)(most < 2 * kSms ? most : 2 * kSms), kUpWarps * 32,
-             (size_t)kUpWarps * kStages * Block<FP8>::kStageBytes + routed_bytes(a), true, a, st);
+             a.ring_bytes + routed_bytes(a), true, a, st);
   if (e != cudaSuccess) return e;
   // Up to about one block an SM: 8 warps each; more: 4 warps, four blocks an SM, all of them at once.
-  if (a.d_model / 16 <= kSms) return launch_down<T, FP8, NT, FP8 ? 8 : 10, 8>(a, f32_out, st);
-  return launch_down<T, FP8, NT, FP8 ? 5 : 6, 4>(a, f32_out, st);
+  if (a.d_model / 16 <= kSms) return launch_down<T, FP8, NT, FP8 ? 4 : 5, 8>(a, f32_out, st);
+  return launch_down<T, FP8, NT, FP8 ? 3 : 4, 4>(a, f32_out, st);
 }
 
 template <typename T, bool FP8>
@@ -571,14 +631,12 @@ cudaError_t by_tokens(const MoeArgs &a, bool f32_out, cudaStream_t st) {
 
 }  // namespace
 
-MoeShape moe_shape(int n_slots, int d_ff, int n_tokens, int top_k, int n_shared) {
+MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared, bool moved) {
   MoeShape s{};
-  const int64_t pairs = (int64_t)n_tokens * (top_k + n_shared), most = pairs < n_slots ? pairs : n_slots;
+  const int64_t pairs = (int64_t)n_tokens * (top_k + n_shared);
   const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
-  s.active = 256;                       // the number of experts in use lies at the start
-  s.token = s.active + up((most + 1) * 8);
-  s.weight = s.token + up(pairs * 4);
-  s.h = s.weight + up(pairs * 4);
+  s.moved_x = up(pairs * 8);   // the choices lie at the start
+  s.h = s.moved_x + (moved ? up((int64_t)n_tokens * d_model * 2) : 0);
   s.bytes = s.h + up(pairs * d_ff * 2);
   return s;
 }

@@ -271,7 +271,7 @@ emoe_status_t emoe_moe_decode_workspace(const emoe_expert_arena_t *e, int32_t n_
   if (st == EMOE_OK && !bytes) st = EMOE_ERR_INVALID_ARG;
   if (st == EMOE_OK) st = check_moe_sizes(e, n_tokens, top_k, n_experts, n_shared);
   if (st != EMOE_OK) return st;
-  *bytes = n_tokens ? moe_shape(e->n_slots, e->d_ff, n_tokens, top_k, n_shared).bytes : 0;
+  *bytes = n_tokens ? moe_shape(e->d_model, e->d_ff, n_tokens, top_k, n_shared, e->type == EMOE_TYPE_E4M3).bytes : 0;
   return EMOE_OK;
 }
 
@@ -287,7 +287,7 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   st = check_moe_sizes(e, p->n_tokens, p->top_k, p->n_experts, p->n_shared);
   if (st != EMOE_OK || p->n_tokens == 0) return st;
   if (!p->x || !p->logits || !p->slot_of_expert || !p->out || !p->workspace) return EMOE_ERR_INVALID_ARG;
-  const MoeShape s = moe_shape(e->n_slots, e->d_ff, p->n_tokens, p->top_k, p->n_shared);
+  const MoeShape s = moe_shape(e->d_model, e->d_ff, p->n_tokens, p->top_k, p->n_shared, e->type == EMOE_TYPE_E4M3);
   if (p->workspace_bytes < (uint64_t)s.bytes) return EMOE_ERR_INVALID_ARG;
   const bool many = p->n_tokens > 1;
   if (many && (p->x_stride < e->d_model || p->out_stride < e->d_model || p->logits_stride < p->n_experts)) return EMOE_ERR_SHAPE;
@@ -332,10 +332,8 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   a.x_stride = many ? p->x_stride : e->d_model;
   a.logits_stride = many ? p->logits_stride : p->n_experts;
   a.out_stride = many ? p->out_stride : e->d_model;
-  a.n_active = (int32_t *)work;
-  a.active = (int2 *)(work + s.active);
-  a.pair_token = (int32_t *)(work + s.token);
-  a.pair_weight = (float *)(work + s.weight);
+  a.choice = (int2 *)work;
+  a.moved_x = work + s.moved_x;
   a.h = work + s.h;
   a.n_slots = e->n_slots;
   a.d_model = e->d_model;

@@ -63,11 +63,12 @@ struct AttendArgs {
 };
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
-// Byte offsets of a layer call's workspace.
+// Byte offsets of a layer call's workspace.  moved: e4m3 weights with bf16 tokens, which are kept in
+// another order and scale.
 struct MoeShape {
-  int64_t active, token, weight, h, bytes;
+  int64_t moved_x, h, bytes;
 };
-MoeShape moe_shape(int n_slots, int d_ff, int n_tokens, int top_k, int n_shared);
+MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared, bool moved);
 
 struct MoeArgs {
   const uint8_t *gate, *up, *down;                        // slot 0 of the layer
@@ -82,12 +83,11 @@ struct MoeArgs {
   float *weights_out;
   int32_t *status;
   int64_t x_stride, logits_stride, out_stride;            // elements
-  int32_t *n_active;                                      // workspace
-  int2 *active;                                           // (slot, first pair) of each expert in use, and the end
-  int32_t *pair_token;
-  float *pair_weight;
+  int2 *choice;                                           // workspace: [token][chosen] slot (-1: none) and weight
+  void *moved_x;                                          // [token][d_model]
   void *h;                                                // [pair][d_ff]
   int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize;
+  int32_t ring_bytes;                                     // shared memory in front of a kernel's tables
   float routed_scale;
 };
 cudaError_t launch_moe(const MoeArgs &a, int type, int io, bool f32_out, cudaStream_t st);

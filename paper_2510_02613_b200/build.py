@@ -7,8 +7,8 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "serve.cpp", "kernels.cu", "kv_cache.cu", "attend.cu", "moe.cu"]
-HEADERS = ["planner.h", "kernels.h", "internal.h", "serve.h", "convert.cuh", os.path.join("..", "..", "include", "emoe.h")]
+SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "serve.cpp", "kernels.cu", "kv_cache.cu", "attend.cu", "attend_prefix.cu", "moe.cu"]
+HEADERS = ["planner.h", "kernels.h", "internal.h", "serve.h", "convert.cuh", "attend_item.cuh", os.path.join("..", "..", "include", "emoe.h")]
 OUT = os.path.join(HERE, "libemoe.so")
 
 

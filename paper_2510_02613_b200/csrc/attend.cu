@@ -8,10 +8,7 @@
 // heads times the query tokens - of the whole batch for the prefix, which is thereby read once, and
 // of one sequence for that sequence's own tokens.  When there are few rows the token axis is split
 // until the machine is full; a second kernel joins the splits.
-#include <math_constants.h>
-
-#include "convert.cuh"
-#include "serve.h"
+#include "attend_item.cuh"
 
 namespace emoe {
 namespace {
@@ -23,10 +20,6 @@ struct Item {
   int seq, head, row0, rows, slot;  // rows of this tile, first row inside the sequence or batch
   int t0, t1;                       // tokens
 };
-
-__device__ __forceinline__ int own_length(const AttendArgs &a, int seq) {
-  return a.max_blocks ? max(0, min(a.own_lens[seq], a.max_blocks * a.c.block_tokens)) : 0;
-}
 
 __device__ __forceinline__ Item item_of(const AttendArgs &a, uint32_t i) {
   Item it;
@@ -59,12 +52,6 @@ __device__ __forceinline__ Item item_of(const AttendArgs &a, uint32_t i) {
   return it;
 }
 
-// Output row (sequence, query token, query head) of a tile row.
-__device__ __forceinline__ int64_t output_row(const AttendArgs &a, int seq, int head, int row) {
-  const int token = row / a.group;   // over the batch for the prefix: seq * q_len + t
-  return ((int64_t)seq * a.q_len + token) * a.n_q_heads + head * a.group + row - token * a.group;
-}
-
 // 16-byte piece c of row r of a tile with CH pieces a row: rotated so that eight rows' equal pieces
 // lie in different banks.
 template <int CH> __device__ __forceinline__ int swizzled(int r, int c) {
@@ -95,6 +82,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 
   let_next_start();
   if (it.t0 >= it.t1 && slots > 1) {   // nothing here: say so to the joining kernel
+    wait_for_previous();
     if (threadIdx.x < it.rows)
       a.part_ml[output_row(a, it.seq, it.head, it.row0 + threadIdx.x) * slots + it.slot] = make_float2(-CUDART_INF_F, 0.f);
     return;
@@ -135,14 +123,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
   auto locate = [&](int i) -> int64_t {
     const int t = it.t0 + (warp + kWarps * i) * kGroup + (lane & 15);
     if (i >= steps || t >= it.t1) return -1;
-    const uint32_t b = (uint32_t)t / (uint32_t)a.c.block_tokens, off = (uint32_t)t - b * a.c.block_tokens;
-    const int block = table[b];
-    if (block < 0 || block >= a.num_blocks) {
-      if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
-      return -1;
-    }
-    return a.c.head_major ? ((int64_t)block * a.c.n_heads + it.head) * a.c.block_tokens + off
-                          : ((int64_t)block * a.c.block_tokens + off) * a.c.n_heads + it.head;
+    return token_vector(a, table, t, it.head);
   };
   uint32_t held_scale = 0, held_valid = 0;
   auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
@@ -217,9 +198,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
         float by = a.scale_log2;
         if constexpr (FP8) {   // both scales are powers of two; 255 is not a number
           const uint32_t b = s_scale[warp][i % kStages][t];
-          const uint32_t kb = b & 255, vb = b >> 8;
-          by *= kb == 255 ? CUDART_NAN_F : __uint_as_float(kb ? kb << 23 : 0x400000u);
-          v_by[j][e] = vb == 255 ? CUDART_NAN_F : __uint_as_float(vb ? vb << 23 : 0x400000u);
+          by *= scale_of(b & 255);
+          v_by[j][e] = scale_of(b >> 8);
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -336,6 +316,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
       joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n][e];
     }
   __syncthreads();
+  // the prefix's own kernel may still be running: the joining one waits for this one alone
+  wait_for_previous();
   const int row = threadIdx.x >> 3;
   if (row >= it.rows) return;
   float mm = -CUDART_INF_F, ll = 0.f, w[kWarps];
@@ -432,8 +414,13 @@ cudaError_t launch_rows(const AttendArgs &a, cudaStream_t st) {
   constexpr size_t smem = ring > join ? ring : join;
   cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_after(attend_rows_kernel<T, HD, FP8>, dim3(a.prefix_items + a.own_items), kWarps * 32, smem, st, false, a);
-  if (e != cudaSuccess || a.prefix_splits + a.own_splits == 1) return e;
+  AttendArgs rest = a;
+  if (a.tensor) rest.prefix_items = 0;
+  if (rest.prefix_items + rest.own_items) {
+    e = launch_after(attend_rows_kernel<T, HD, FP8>, dim3(rest.prefix_items + rest.own_items), kWarps * 32, smem, st, a.tensor, rest);
+    if (e != cudaSuccess) return e;
+  }
+  if (!a.tensor && a.prefix_splits + a.own_splits == 1) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.q_len * a.n_q_heads;
   return launch_after(attend_join_kernel<T, HD>, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, a);
 }
@@ -451,13 +438,12 @@ cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int64_t own_max, int prefix_len) {
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len) {
   AttendShape s{};
   const int64_t want = 4 * kSms;   // items: two blocks an SM, twice over
   s.seq_rows = q_len * (n_q_heads / n_heads);
   const auto cut = [&](int64_t tiles, int64_t tokens, int64_t least, int32_t &splits, int32_t &chunk) {
     int64_t n = (want + tiles - 1) / tiles;
-    n = n < 1 ? 1 : n;
     const int64_t most = (tokens + least - 1) / least;
     n = n > most ? most : n;
     n = n > 64 ? 64 : n < 1 ? 1 : n;
@@ -466,8 +452,26 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int6
     chunk = (int32_t)c;
     splits = tokens ? (int32_t)((tokens + c - 1) / c) : 1;
   };
-  if (prefix_len > 0) {
-    const int64_t tiles = (int64_t)n_heads * (((int64_t)n_seqs * s.seq_rows + 15) / 16);
+  const int64_t batch_rows = (int64_t)n_seqs * s.seq_rows;
+  if (prefix_len > 0 && (head_dim == 64 || head_dim == 128) && batch_rows > 16) {
+    // Blocks of up to 256 rows, one an SM: the number of splits with the fewest steps one after the
+    // other, a block's start and end counting as two.
+    s.tensor = 1;
+    s.alternate = batch_rows <= 128;
+    const int64_t units = n_heads * ((batch_rows + 255) / 256);
+    const int64_t tiles = (prefix_len + 127) / 128, steps = s.alternate ? (tiles + 1) / 2 : tiles;
+    int64_t best = 1, cost = INT64_MAX;
+    for (int64_t n = 1; n <= 64 && n <= steps; ++n) {
+      const int64_t c = ((units * n + kSms - 1) / kSms) * ((steps + n - 1) / n + 2);
+      if (c < cost) cost = c, best = n;
+    }
+    const int64_t per = (steps + best - 1) / best * (s.alternate ? 2 : 1);   // tiles
+    const int64_t blocks = (tiles + per - 1) / per;
+    s.prefix_chunk = (int32_t)(per * 128);
+    s.prefix_splits = (int32_t)(blocks * (s.alternate ? 2 : 1));
+    s.prefix_items = units * blocks;
+  } else if (prefix_len > 0) {
+    const int64_t tiles = (int64_t)n_heads * ((batch_rows + 15) / 16);
     cut(tiles, prefix_len, 128, s.prefix_splits, s.prefix_chunk);
     s.prefix_items = tiles * s.prefix_splits;
   }
@@ -477,11 +481,15 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int6
     s.own_items = tiles * s.own_splits;
   }
   const int64_t rows = (int64_t)n_seqs * q_len * n_q_heads, slots = s.prefix_splits + s.own_splits;
-  s.parts = slots > 1 ? rows * slots : 0;
+  s.parts = s.tensor || slots > 1 ? rows * slots : 0;
   return s;
 }
 
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st) {
+  if (a.tensor) {
+    const cudaError_t e = launch_attend_prefix(a, type, io, st);
+    if (e != cudaSuccess) return e;
+  }
   if (type == EMOE_TYPE_E4M3)
     return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, st) : by_head_dim<__half, true>(a, st);
   return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, st) : by_head_dim<__half, false>(a, st);

@@ -1,0 +1,557 @@
+// attend_prefix.cu - the shared prefix against the rows of a whole batch on the 5th-generation tensor
+// cores.
+//
+// A batch that shares a prefix has n_seqs * q_len * (query heads per KV head) rows for each KV head: a
+// matrix product once there are more than a few.  A block takes a KV head, up to 256 rows and a range of
+// the prefix; it holds the rows' queries in shared memory and two accumulator sets ("slots") in tensor memory,
+//     S = Q K^T (128 x 128), O += P V (128 x head_dim),   P = 2^(scale S - m) rounded to 16 bits,
+// and runs through the tokens 128 at a time.  P is written over S in tensor memory and multiplied from
+// there.  The two slots take turns: while one's weights are computed the other's products run.  With
+// more than 128 rows the slots are two row tiles on the same tokens; with fewer they are the same rows on
+// alternating tiles of tokens, so that a single row tile also keeps both units busy.
+//
+// Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row), 8 issues the products, 9-12 bring
+// K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
+// asynchronously; e4m3 codes are widened on the way).  The maximum in use is only raised when the real one
+// passes it by more than 2^8: sums and weights then still fit, and O is rarely rescaled.
+//
+// Bounds: exponentials (16 a clock and SM, 2 x 128 x 128 a pair of tiles = 2048 clocks) and products
+// (the same) with many rows, the reads of K and V with few.
+#include "attend_item.cuh"
+
+namespace emoe {
+namespace {
+
+constexpr int kTile = 128;                 // rows of a slot, tokens of a step
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarps = 4, kThreads = (kSoftmaxWarps + 1 + kCopyWarps) * 32;
+constexpr int kKept = 4;                   // steps whose masks and scales are kept
+constexpr unsigned long long kWaitNs = 4000000000ull, kDrainNs = 1000000000ull;
+constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
+constexpr uint32_t kColS = 0, kColO = 256; // tensor memory columns: S (and P) of the slots, then O
+
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// False if the phase does not complete in time or another role has given up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit = kWaitNs) {
+  if (bar_try(bar, parity)) return true;
+  const unsigned long long t0 = now_ns();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (bar_try(bar, parity)) return true;
+    if (*abort) return false;
+    if (now_ns() - t0 > limit) {
+      *abort = 1;
+      return false;
+    }
+  }
+}
+
+// For whole warps: the same answer in every lane, so that none goes on alone.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort) {
+  return __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
+}
+
+// Shared memory operand, 128-byte swizzle: rows of 128 bytes, 8 rows (1024 bytes) an atom.  Queries and keys
+// have the k axis along the row (chunks of 64 elements, `chunk` bytes apart, are addressed by the
+// caller); values have it across the rows, and their 64-element chunks follow one another at `chunk`.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t chunk) {
+  return (uint64_t)(at >> 4) | (uint64_t)(chunk >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// 32-bit sums, 16-bit operands (0 f16, 1 bf16), 128 rows, n columns; b_across: b's k axis across its rows.
+__host__ __device__ constexpr uint32_t instruction(uint32_t type, uint32_t n, uint32_t b_across) {
+  return 1u << 4 | type << 7 | type << 10 | b_across << 16 | (n >> 3) << 17 | (128u >> 4) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_load(float (&r)[32], uint32_t at) {
+  uint32_t x[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+      : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]),
+        "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]),
+        "=r"(x[18]), "=r"(x[19]), "=r"(x[20]), "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]),
+        "=r"(x[27]), "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
+      : "r"(at) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(x[i]);
+}
+__device__ __forceinline__ void tmem_store_16(uint32_t at, const uint32_t (&x)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
+      "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]),
+      "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 16-byte piece `piece` of row r in a tile of 128-byte rows, tiles of 64 elements one after the other.
+__device__ __forceinline__ uint32_t piece_at(int r, int piece) {
+  return (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
+}
+
+struct Bars {   // each in two copies: stages of K or V, or slots
+  uint32_t base;
+  __device__ __forceinline__ uint32_t k_full(int i) const { return base + 8 * i; }
+  __device__ __forceinline__ uint32_t k_empty(int i) const { return base + 16 + 8 * i; }
+  __device__ __forceinline__ uint32_t v_full(int i) const { return base + 32 + 8 * i; }
+  __device__ __forceinline__ uint32_t v_empty(int i) const { return base + 48 + 8 * i; }
+  __device__ __forceinline__ uint32_t s_full(int i) const { return base + 64 + 8 * i; }
+  __device__ __forceinline__ uint32_t p_full(int i) const { return base + 80 + 8 * i; }
+  __device__ __forceinline__ uint32_t o_full(int i) const { return base + 96 + 8 * i; }
+  __device__ __forceinline__ uint32_t drained() const { return base + 112; }   // one
+};
+
+template <typename T, int HD, bool FP8>
+__global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr uint32_t kTileBytes = kTile * HD * 2;
+  constexpr int kPieces = HD / 8;   // 16-byte pieces of a 16-bit row
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ __align__(8) uint64_t bars[15];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  __shared__ __align__(16) uint8_t s_bad[kKept][kTile];             // tokens that nobody sees
+  __shared__ __align__(16) float s_scale[2][FP8 ? kKept : 1][FP8 ? kTile : 4];   // of K and V
+  uint8_t *const smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+  const uint32_t q_at = shared_address(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + 2 * kTileBytes;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // the item
+  const uint32_t heads = a.c.n_heads;
+  const int pairs = a.alternate ? 1 : (a.n_seqs * a.seq_rows + 2 * kTile - 1) / (2 * kTile);
+  const int split = blockIdx.x / (heads * pairs), unit = blockIdx.x % (heads * pairs);
+  const int head = unit % heads, row0 = unit / heads * (2 * kTile);
+  const int rows = min(2 * kTile, a.n_seqs * a.seq_rows - row0);
+  const int t0 = split * a.prefix_chunk, t1 = min(a.prefix_len, t0 + a.prefix_chunk);
+  const int tiles = (t1 - t0 + kTile - 1) / kTile;
+  const bool alternate = a.alternate != 0, second = alternate || rows > kTile;
+  // tiles of slot s, and the tile of its step i
+  const int steps[2] = {alternate ? (tiles + 1) / 2 : tiles, alternate ? tiles / 2 : second ? tiles : 0};
+
+  const Bars bar{shared_address(bars)};
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      bar_init(bar.k_full(i), kCopyWarps * 32);
+      bar_init(bar.v_full(i), kCopyWarps * 32);
+      bar_init(bar.k_empty(i), 1);
+      bar_init(bar.v_empty(i), 1);
+      bar_init(bar.s_full(i), 1);
+      bar_init(bar.p_full(i), 128);
+      bar_init(bar.o_full(i), 1);
+    }
+    bar_init(bar.drained(), 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  let_next_start();
+
+  // queries: rows that do not exist are zero; a negative scale turns their sign
+  for (int i = threadIdx.x; i < (alternate ? kTile : 2 * kTile) * kPieces; i += kThreads) {
+    const int r = i / kPieces, piece = i % kPieces;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (r < rows) {
+      const int row = row0 + r, token = row / a.group;
+      w = *(const uint4 *)((const T *)a.q + (int64_t)token * a.q_stride + (head * a.group + row - token * a.group) * HD + piece * 8);
+      if constexpr (kMoved<T, FP8>) {
+        uint32_t *x = (uint32_t *)&w;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float2 p = Pair<T>::unpack(x[2 * h]), q = Pair<T>::unpack(x[2 * h + 1]);
+          x[2 * h] = Pair<T>::pack(p.x * kMovedScale, q.x * kMovedScale);
+          x[2 * h + 1] = Pair<T>::pack(p.y * kMovedScale, q.y * kMovedScale);
+        }
+      }
+      const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0;
+      w.x ^= sign;
+      w.y ^= sign;
+      w.z ^= sign;
+      w.w ^= sign;
+    }
+    *(uint4 *)(smem + (r / kTile) * kTileBytes + piece_at(r % kTile, piece)) = w;
+  }
+  fence_async();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  volatile int *const abort = &s_abort;
+
+  if (warp < kSoftmaxWarps) {
+    const int slot = warp >> 2, local = (warp & 3) * 32 + lane;   // this thread's row in the tile
+    const int row = alternate ? local : slot * kTile + local;
+    const bool busy = (alternate ? 0 : slot * kTile) + (warp & 3) * 32 < rows;   // any real row in the warp
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
+    const uint32_t s_col = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
+    const float c = fabsf(a.scale_log2) * (kMoved<T, FP8> ? kMovedScale : 1.f);
+    float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: f16 weights carry v's scale relative to the largest yet
+    bool ok = true;
+    for (int i = 0; i < steps[slot] && ok; ++i) {
+      const int tile = alternate ? 2 * i + slot : i;
+      ok = bar_wait_warp(bar.s_full(slot), i & 1, abort);
+      if (!ok) break;
+      fence_after();
+      if (busy) {
+        const uint8_t *const bad = s_bad[tile % kKept];
+        uint32_t any_bad = 0;
+#pragma unroll
+        for (int j = 0; j < kTile / 16; ++j) {
+          const uint4 b = ((const uint4 *)bad)[j];
+          any_bad |= b.x | b.y | b.z | b.w;
+        }
+        const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0], *const v_scale = s_scale[1][FP8 ? tile % kKept : 0];
+        // the largest score, and in FP8 with f16 weights the largest scale of v
+        float top = -CUDART_INF_F, v_top = v_ref;
+#pragma unroll
+        for (int j = 0; j < kTile / 32; ++j) {
+          float x[32];
+          tmem_load(x, s_col + 32 * j);
+          if constexpr (FP8) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 k = *(const float4 *)(k_scale + 32 * j + e);
+              x[e] *= k.x;
+              x[e + 1] *= k.y;
+              x[e + 2] *= k.z;
+              x[e + 3] *= k.w;
+              if constexpr (!kMoved<T, FP8>) {
+                const float4 v = *(const float4 *)(v_scale + 32 * j + e);
+                v_top = fmaxf(fmaxf(v_top, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));
+              }
+            }
+          }
+          if (any_bad) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top = fmaxf(top, bad[32 * j + e] ? -CUDART_INF_F : x[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+          }
+        }
+        if (top != -CUDART_INF_F) top *= c;
+        const bool raise = i > 0 && (top > m + kRaise || v_top > v_ref);
+        if (i == 0) {
+          m = top;
+          v_ref = v_top;
+        } else if (__any_sync(0xffffffffu, raise)) {   // O may be touched: S of this step came after the last product
+          const float to = top > m + kRaise ? top : m;
+          float by = to == -CUDART_INF_F ? 1.f : exp2_fast(m - to);
+          l *= by;
+          if constexpr (FP8 && !kMoved<T, FP8>) by *= v_top > 0.f ? v_ref / v_top : 1.f;
+          m = to;
+          v_ref = v_top;
+#pragma unroll
+          for (int j = 0; j < HD / 32; ++j) {
+            float x[32];
+            tmem_load(x, o_col + 32 * j);
+            uint32_t y[16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[16 * h + e] * by);
+              tmem_store_16(o_col + 32 * j + 16 * h, y);
+            }
+          }
+        }
+        const float safe = m == -CUDART_INF_F ? 0.f : m;
+        float v_by = kMovedScale;
+        if constexpr (FP8 && !kMoved<T, FP8>) v_by = v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kTile / 32; ++j) {
+          float x[32];
+          tmem_load(x, s_col + 32 * j);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            float4 k = make_float4(c, c, c, c);
+            if constexpr (FP8) {
+              const float4 s = *(const float4 *)(k_scale + 32 * j + e);
+              k = make_float4(s.x * c, s.y * c, s.z * c, s.w * c);
+            }
+            x[e] = exp2_fast(fmaf(x[e], k.x, -safe));
+            x[e + 1] = exp2_fast(fmaf(x[e + 1], k.y, -safe));
+            x[e + 2] = exp2_fast(fmaf(x[e + 2], k.z, -safe));
+            x[e + 3] = exp2_fast(fmaf(x[e + 3], k.w, -safe));
+          }
+          if (any_bad) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (bad[32 * j + e]) x[e] = 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            sum[0] += x[e];
+            sum[1] += x[e + 1];
+          }
+          if constexpr (FP8) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 v = *(const float4 *)(v_scale + 32 * j + e);
+              x[e] *= v.x * v_by;
+              x[e + 1] *= v.y * v_by;
+              x[e + 2] *= v.z * v_by;
+              x[e + 3] *= v.w * v_by;
+            }
+          }
+          uint32_t p[16];   // rounded once, as the second product's operand
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = Pair<T>::pack(x[2 * e], x[2 * e + 1]);
+          tmem_store_16(s_col + 16 * j, p);   // over columns that have been read
+        }
+        l += sum[0] + sum[1];
+        tmem_stored();
+      }
+      fence_before();
+      bar_arrive(bar.p_full(slot));
+    }
+    // the part of this range: maximum, sum and unnormalised output of every row
+    if (steps[slot] > 0 && ok) ok = bar_wait_warp(bar.o_full(slot), 0, abort);
+    fence_after();
+    const int slots = a.prefix_splits + a.own_splits;
+    const int64_t part = row < rows ? output_row(a, 0, head, row0 + row) * slots + (alternate ? 2 * split + slot : split) : 0;
+    if (busy && (alternate || slot == 0 || second)) {
+      const bool empty = steps[slot] == 0 || !ok;
+      if (row < rows) a.part_ml[part] = empty ? make_float2(-CUDART_INF_F, 0.f) : make_float2(m, l);
+      if (!empty) {
+        float by = 1.f;
+        if constexpr (kMoved<T, FP8>) by = kMovedScale;
+        else if constexpr (FP8) by = v_ref;
+#pragma unroll 1
+        for (int j = 0; j < HD / 32; ++j) {
+          float x[32];
+          tmem_load(x, o_col + 32 * j);
+          if (row < rows) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              float4 y = make_float4(x[e] * by, x[e + 1] * by, x[e + 2] * by, x[e + 3] * by);
+              if constexpr (kMoved<T, FP8>) y = make_float4(y.x, y.z, y.y, y.w);
+              *(float4 *)(a.part_o + part * HD + 32 * j + e) = y;
+            }
+          }
+        }
+      }
+    }
+    fence_before();
+  } else if (warp == kMmaWarp) {
+    if (lane == 0 && tiles > 0) {
+      constexpr uint32_t kType = __is_same(T, __half) ? 0 : 1;
+      constexpr uint32_t kIdS = instruction(kType, kTile, 0), kIdO = instruction(kType, HD, 1);
+      const auto scores = [&](int slot, int stage) {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
+          mma_ss(tmem + kColS + slot * kTile, operand(q_at + (alternate ? 0 : slot * kTileBytes) + off, 0),
+                 operand(k_at + stage * kTileBytes + off, 0), kIdS, k > 0);
+        }
+      };
+      const auto values = [&](int slot, int stage, bool add) {
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ts(tmem + kColO + slot * HD, tmem + kColS + slot * kTile + k * 8,
+                 operand(v_at + stage * kTileBytes + k * 2048, kTile * 128), kIdO, add || k > 0);
+      };
+      bool ok = true;
+      // step i of slot s: its tile, the tile's buffer, and whether this product is the buffer's last reader
+      const auto tile_of = [&](int s, int i) { return alternate ? 2 * i + s : i; };
+      const auto last_reader = [&](int s) { return alternate || s == 1 || !second; };
+      const auto start = [&](int s, int i) {   // S of step i
+        const int tile = tile_of(s, i), stage = tile & 1;
+        if (alternate || s == 0) ok = ok && bar_wait(bar.k_full(stage), (tile >> 1) & 1, abort);
+        if (!ok) return;
+        fence_after();
+        scores(s, stage);
+        mma_commit(bar.s_full(s));
+        if (last_reader(s)) mma_commit(bar.k_empty(stage));
+      };
+      for (int s = 0; s < 2; ++s)
+        if (steps[s] > 0 && ok) start(s, 0);
+      for (int i = 0; i < steps[0] && ok; ++i) {
+        for (int s = 0; s < 2 && ok; ++s) {
+          if (i >= steps[s]) continue;
+          const int tile = tile_of(s, i), stage = tile & 1;
+          if (alternate || s == 0) ok = ok && bar_wait(bar.v_full(stage), (tile >> 1) & 1, abort);
+          ok = ok && bar_wait(bar.p_full(s), i & 1, abort);
+          if (!ok) break;
+          fence_after();
+          values(s, stage, i > 0);
+          if (last_reader(s)) mma_commit(bar.v_empty(stage));
+          if (i + 1 < steps[s]) start(s, i + 1);
+          else mma_commit(bar.o_full(s));
+        }
+      }
+      if (!ok) {   // gave up: let the products in flight end before the tensor memory is given back
+        int never = 0;
+        mma_commit(bar.drained());
+        bar_wait(bar.drained(), 0, &never, kDrainNs);
+      }
+    }
+    __syncwarp();
+  } else if (tiles > 0) {
+    const int w = warp - kMmaWarp - 1;
+    // A row's pieces are taken by kGroup neighbouring lanes; a warp has 32 rows of a tile, and each lane
+    // finds one of them in the table.
+    constexpr int kGroup = FP8 ? HD / 16 : kPieces, kRows = 32 / kGroup, kPasses = kTile / (kCopyWarps * kRows);
+    static_assert(kRows * kPasses == 32, "a lane a row");
+    const int piece = lane % kGroup;
+    const auto row_of = [&](int pass, int r) { return pass * (kCopyWarps * kRows) + w * kRows + r; };
+    const int my_row = row_of(lane / kRows, lane % kRows);
+    const auto locate = [&](int tile) -> int64_t {
+      const int t = t0 + tile * kTile + my_row;
+      return tile < tiles && t < t1 ? token_vector(a, a.prefix_table, t, head) : -1;
+    };
+    bool ok = true;
+    if constexpr (!FP8) {
+      int issued = 0, told = 0;   // buffers (K of tile 0, V of tile 0, K of tile 1, ...) filled, and said to be
+      const auto tell = [&](int upto) {
+        fence_async();
+        for (; told < upto; ++told) bar_arrive(told & 1 ? bar.v_full((told >> 1) & 1) : bar.k_full((told >> 1) & 1));
+      };
+      int64_t vec = locate(0);
+      for (int tile = 0; tile < tiles && ok; ++tile) {
+        const int64_t next = locate(tile + 1);
+        const int stage = tile & 1;
+        for (int v = 0; v < 2 && ok; ++v) {
+          if (tile >= 2) {
+            const uint32_t empty = v ? bar.v_empty(stage) : bar.k_empty(stage), parity = (tile >> 1) + 1 & 1;
+            if (!__all_sync(0xffffffffu, bar_try(empty, parity))) {   // about to wait: first say what has arrived meanwhile
+              copy_async_wait<0>();
+              tell(issued);
+              ok = bar_wait_warp(empty, parity, abort);
+              if (!ok) break;
+            }
+          }
+          if (v == 0) s_bad[tile % kKept][my_row] = vec < 0;
+          const uint8_t *const pool = v ? a.c.v : a.c.k;
+          const uint32_t dst = (v ? v_at : k_at) + stage * kTileBytes;
+#pragma unroll
+          for (int pass = 0; pass < kPasses; ++pass) {
+            const int64_t at = __shfl_sync(0xffffffffu, vec, pass * kRows + lane / kGroup);
+            const int r = row_of(pass, lane / kGroup);
+            copy_async_16(dst + piece_at(r, piece), pool + (at < 0 ? 0 : at * (HD * 2) + piece * 16), at < 0 ? 0 : 16);
+          }
+          copy_async_commit();
+          ++issued;
+          if (issued - told > 2) {
+            copy_async_wait<2>();
+            tell(issued - 2);
+          }
+        }
+        vec = next;
+      }
+      copy_async_wait<0>();
+      if (ok) tell(issued);
+    } else {
+      uint4 raw[2][kPasses];
+      float by[2] = {1.f, 1.f};
+      const auto load = [&](int v, int64_t vec) {
+        const uint8_t *const pool = v ? a.c.v : a.c.k;
+        by[v] = vec < 0 ? 0.f : scale_of((v ? a.c.v_scale : a.c.k_scale)[vec]);
+#pragma unroll
+        for (int pass = 0; pass < kPasses; ++pass) {
+          const int64_t at = __shfl_sync(0xffffffffu, vec, pass * kRows + lane / kGroup);
+          raw[v][pass] = at < 0 ? make_uint4(0, 0, 0, 0) : *(const uint4 *)(pool + at * HD + piece * 16);
+        }
+      };
+      int64_t vec = locate(0);
+      bool bad = vec < 0;
+      load(0, vec);
+      load(1, vec);
+      for (int tile = 0; tile < tiles && ok; ++tile) {
+        const int stage = tile & 1;
+        const int64_t next = locate(tile + 1);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          if (tile >= 2) ok = ok && bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (!ok) break;
+          if (v == 0) s_bad[tile % kKept][my_row] = bad;
+          s_scale[v][tile % kKept][my_row] = by[v];
+          uint8_t *const dst = smem + 2 * kTileBytes + (v ? 2 * kTileBytes : 0) + stage * kTileBytes;
+#pragma unroll
+          for (int pass = 0; pass < kPasses; ++pass) {
+            const int r = row_of(pass, lane / kGroup);
+            const uint4 x = raw[v][pass];
+            uint4 lo, hi;
+            word_of_codes<T>(lo.x, lo.y, x.x);
+            word_of_codes<T>(lo.z, lo.w, x.y);
+            word_of_codes<T>(hi.x, hi.y, x.z);
+            word_of_codes<T>(hi.z, hi.w, x.w);
+            *(uint4 *)(dst + piece_at(r, 2 * piece)) = lo;
+            *(uint4 *)(dst + piece_at(r, 2 * piece + 1)) = hi;
+          }
+          fence_async();
+          bar_arrive(v ? bar.v_full(stage) : bar.k_full(stage));
+          if (tile + 1 < tiles) load(v, next);
+        }
+        bad = next < 0;
+      }
+    }
+  }
+
+  __syncthreads();
+  if (threadIdx.x == 0 && s_abort && a.c.status) *a.c.status = EMOE_ERR_DEVICE_TIMEOUT;
+  if (warp == kMmaWarp) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+template <typename T, int HD, bool FP8>
+cudaError_t launch(const AttendArgs &a, cudaStream_t st) {
+  // queries, two stages of K and of V, room to align; never two blocks an SM (each takes all tensor memory)
+  constexpr size_t need = 6 * (size_t)kTile * HD * 2 + 1024, least = 120 * 1024;
+  constexpr size_t smem = need > least ? need : least;
+  const cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<T, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  attend_prefix_kernel<T, HD, FP8><<<a.prefix_items, kThreads, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T, bool FP8>
+cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
+  return a.c.head_dim == 64 ? launch<T, 64, FP8>(a, st) : launch<T, 128, FP8>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st) {
+  if (type == EMOE_TYPE_E4M3)
+    return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, st) : by_head_dim<__half, true>(a, st);
+  return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, st) : by_head_dim<__half, false>(a, st);
+}
+
+}  // namespace emoe

@@ -48,6 +48,25 @@ template <> __device__ __forceinline__ uint32_t codes_to_pair<__half>(uint32_t x
 template <typename T> __device__ __forceinline__ uint32_t even_codes(uint32_t w) { return codes_to_pair<T>(w << 8); }
 template <typename T> __device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return codes_to_pair<T>(w); }
 
+// e4m3 as bf16 operands without a product: a code's magnitude bits, moved to their place, are a bf16 2^120
+// too small (denormal where the code is), which the tensor cores take as it is.  The other operand
+// carries 2^60 of that and the sums the rest, so that neither side leaves its range.  A word's
+// codes come out as (0, 2) and (1, 3), so the other operand is kept in that order ("moved").  f16 operands are
+// what cvt gives: in order and at their own size.
+template <typename T, bool FP8> constexpr bool kMoved = FP8 && !__is_same(T, __half);
+constexpr float kMovedScale = 0x1p60f;   // of the other operand, and of the sums
+// Two pairs of operands from a word of four codes.
+template <typename T>
+__device__ __forceinline__ void word_of_codes(uint32_t &first, uint32_t &second, uint32_t w) {
+  if constexpr (__is_same(T, __half)) {
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+        : "=r"(first), "=r"(second) : "r"(w));
+  } else {
+    first = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
+    second = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+  }
+}
+
 // d += a b: a 16 x 16 (rows), b 16 x 8 (columns), 32-bit sums.
 template <typename T>
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {

@@ -23,15 +23,8 @@ namespace {
 
 constexpr int kRouteThreads = 256, kUpWarps = 8;
 
-// e4m3 weights as bf16 operands.  A code's magnitude bits, moved to their place, are a bf16 2^120 too
-// small (denormal where the code is), which the tensor cores take as it is; the tokens carry 2^60 of that
-// and the sums the rest, so that neither side leaves its range (tokens below 2^67).  And a word's
-// codes come out as (0, 2) and (1, 3), so the tokens are kept in that order.  (The cvt instructions of
-// this type pair would need a product by 2^120 and a change of order for every word of weights.)
-// f16 operands are what cvt gives: in order and at their own size.
-template <typename T, bool FP8> constexpr bool kMoved = FP8 && !__is_same(T, __half);
+// Where element k of a token lies in the order that moved e4m3 operands want.
 __device__ __forceinline__ int moved_place(int k) { return (k & ~3) | (k & 1) << 1 | (k & 2) >> 1; }
-constexpr float kTokenScale = 0x1p60f, kSumScale = 0x1p60f;
 
 // Logits as unsigned numbers in the same order; NaN counts as minus infinity, and minus infinity and
 // what has been chosen already as 0.
@@ -58,8 +51,8 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
       for (int i = threadIdx.x - 32; i < a.d_model / 4; i += kRouteThreads - 32) {
         const uint2 w = ((const uint2 *)x)[i];
         const float2 p = Pair<__nv_bfloat16>::unpack(w.x), q = Pair<__nv_bfloat16>::unpack(w.y);
-        to[i] = make_uint2(Pair<__nv_bfloat16>::pack(p.x * kTokenScale, q.x * kTokenScale),
-                           Pair<__nv_bfloat16>::pack(p.y * kTokenScale, q.y * kTokenScale));
+        to[i] = make_uint2(Pair<__nv_bfloat16>::pack(p.x * kMovedScale, q.x * kMovedScale),
+                           Pair<__nv_bfloat16>::pack(p.y * kMovedScale, q.y * kMovedScale));
       }
     }
     return;
@@ -241,18 +234,6 @@ __device__ __forceinline__ TokenPart<FP8> load_token(const uint8_t *p, bool in0,
 
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Two pairs of operands from a word of four codes (see kMoved for which codes, and their scale).
-template <typename T>
-__device__ __forceinline__ void word_of_codes(uint32_t &first, uint32_t &second, uint32_t w) {
-  if constexpr (__is_same(T, __half)) {
-    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
-        : "=r"(first), "=r"(second) : "r"(w));
-  } else {
-    first = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
-    second = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
-  }
-}
-
 // acc += 16 weight rows x 8 tokens over one step; e4m3 steps come with the scales of rows g and g + 8.
 template <typename T, bool FP8>
 __device__ __forceinline__ void step_product(float (&acc)[4], const uint4 (&w)[4], const TokenPart<FP8> &tok, float scale_lo,
@@ -428,14 +409,14 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
         if (n * 8 + j < count) {
           const int pair = e.y + n * 8 + j;
           if constexpr (kMoved<T, FP8>) {
-            gate *= kSumScale;
-            up *= kSumScale;
+            gate *= kMovedScale;
+            up *= kMovedScale;
           }
           float h = gate / (1.f + expf(-gate)) * up * routed.weight[pair];
           // f16 ends at 65504: the largest value stands for what is beyond (bf16 reaches as far as 32 bits)
           if constexpr (__is_same(T, __half)) h = h != h ? h : fminf(fmaxf(h, -65504.f), 65504.f);
           const int at = row0 + f;
-          ((T *)a.h)[(int64_t)pair * a.d_ff + (kMoved<T, FP8> ? moved_place(at) : at)] = T(kMoved<T, FP8> ? h * kTokenScale : h);
+          ((T *)a.h)[(int64_t)pair * a.d_ff + (kMoved<T, FP8> ? moved_place(at) : at)] = T(kMoved<T, FP8> ? h * kMovedScale : h);
         }
       }
     }
@@ -566,7 +547,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
     float y = 0.f;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) y += sums[(w * a.n_tokens + t) * 17 + r];
-    if constexpr (kMoved<T, FP8>) y *= kSumScale;
+    if constexpr (kMoved<T, FP8>) y *= kMovedScale;
     if constexpr (F32_OUT) ((float *)a.out)[t * a.out_stride + row0 + r] = y;
     else ((T *)a.out)[t * a.out_stride + row0 + r] = T(y);
   }

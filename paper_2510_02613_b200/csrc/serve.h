@@ -42,9 +42,11 @@ struct AttendShape {
   int32_t prefix_splits, prefix_chunk;  // token ranges of the prefix, tokens of each
   int32_t own_splits, own_chunk;
   int64_t prefix_items, own_items;
+  int32_t tensor;                       // the prefix goes through its own kernel on the 5th-generation tensor cores
+  int32_t alternate;                    // ... whose two slots take the same rows on alternating tiles of tokens
   int64_t parts;                        // (row, split) pairs that go through the workspace; 0: none
 };
-AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int64_t own_max, int prefix_len);
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len);
 
 struct AttendArgs {
   KvLayer c;
@@ -59,8 +61,10 @@ struct AttendArgs {
   int32_t n_seqs, q_len, n_q_heads, group, max_blocks, prefix_len;
   float scale_log2;
   int32_t seq_rows, prefix_splits, prefix_chunk, own_splits, own_chunk;
+  int32_t tensor, alternate;
   uint32_t prefix_items, own_items;
 };
+cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
 // Byte offsets of a layer call's workspace.  moved: e4m3 weights with bf16 tokens, which are kept in

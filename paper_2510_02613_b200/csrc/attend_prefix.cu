@@ -10,8 +10,8 @@
 // more than 128 rows the slots are two row tiles on the same tokens; with fewer they are the same rows on
 // alternating tiles of tokens, so that a single row tile also keeps both units busy.
 //
-// Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row), 8 issues the products, 9-12 bring
-// K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
+// Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row, all 128 scores of a step in its
+// registers), 8 issues the products, 12-15 bring K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
 // asynchronously; e4m3 codes are widened on the way).  The maximum in use is only raised when the real one
 // passes it by more than 2^8: sums and weights then still fit, and O is rarely rescaled.
 //
@@ -23,7 +23,10 @@ namespace emoe {
 namespace {
 
 constexpr int kTile = 128;                 // rows of a slot, tokens of a step
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarps = 4, kThreads = (kSoftmaxWarps + 1 + kCopyWarps) * 32;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
+// Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
+constexpr int kSoftmaxRegs = 184, kMmaRegs = 40, kCopyRegs = 104;
+static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
 constexpr int kKept = 4;                   // steps whose masks and scales are kept
 constexpr unsigned long long kWaitNs = 4000000000ull, kDrainNs = 1000000000ull;
 constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
@@ -95,19 +98,51 @@ __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::be
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-__device__ __forceinline__ void tmem_load(float (&r)[32], uint32_t at) {
-  uint32_t x[32];
+// 32 and 16 columns of this thread's row.  The values are there after tmem_wait on them.
+__device__ __forceinline__ void tmem_load(float (&x)[32], uint32_t at) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
-      : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]),
-        "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]),
-        "=r"(x[18]), "=r"(x[19]), "=r"(x[20]), "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]),
-        "=r"(x[27]), "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
+      "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]),
+        "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]),
+        "=f"(x[18]), "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]),
+        "=f"(x[27]), "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31])
       : "r"(at) : "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) r[i] = __uint_as_float(x[i]);
 }
+__device__ __forceinline__ void tmem_wait(float (&x)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]), "+f"(x[4]), "+f"(x[5]), "+f"(x[6]), "+f"(x[7]), "+f"(x[8]),
+                 "+f"(x[9]), "+f"(x[10]), "+f"(x[11]), "+f"(x[12]), "+f"(x[13]), "+f"(x[14]), "+f"(x[15]), "+f"(x[16]),
+                 "+f"(x[17]), "+f"(x[18]), "+f"(x[19]), "+f"(x[20]), "+f"(x[21]), "+f"(x[22]), "+f"(x[23]), "+f"(x[24]),
+                 "+f"(x[25]), "+f"(x[26]), "+f"(x[27]), "+f"(x[28]), "+f"(x[29]), "+f"(x[30]), "+f"(x[31])
+               :: "memory");
+}
+__device__ __forceinline__ void tmem_load_16(float (&x)[16], uint32_t at) {   // waits
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]),
+        "=f"(x[9]), "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15])
+      : "r"(at) : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ void fma_pair(float &x, float &y, float ax, float ay, float b) {
+  asm("{\n\t.reg .b64 v, k, s;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 k, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\t"
+      "fma.rn.f32x2 v, v, k, s;\n\tmov.b64 {%0, %1}, v;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(ax), "f"(ay), "f"(b));
+}
+__device__ __forceinline__ void add_pair(float &x, float &y, float ax, float ay) {
+  asm("{\n\t.reg .b64 v, k;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 k, {%2, %3};\n\tadd.rn.f32x2 v, v, k;\n\tmov.b64 {%0, %1}, v;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(ax), "f"(ay));
+}
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 __device__ __forceinline__ void tmem_store_16(uint32_t at, const uint32_t (&x)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at),
@@ -131,6 +166,7 @@ struct Bars {   // each in two copies: stages of K or V, or slots
   __device__ __forceinline__ uint32_t p_full(int i) const { return base + 80 + 8 * i; }
   __device__ __forceinline__ uint32_t o_full(int i) const { return base + 96 + 8 * i; }
   __device__ __forceinline__ uint32_t drained() const { return base + 112; }   // one
+  __device__ __forceinline__ uint32_t q_full() const { return base + 120; }    // one
 };
 
 template <typename T, int HD, bool FP8>
@@ -138,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   constexpr uint32_t kTileBytes = kTile * HD * 2;
   constexpr int kPieces = HD / 8;   // 16-byte pieces of a 16-bit row
   extern __shared__ uint8_t raw_smem[];
-  __shared__ __align__(8) uint64_t bars[15];
+  __shared__ __align__(8) uint64_t bars[16];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   __shared__ __align__(16) uint8_t s_bad[kKept][kTile];             // tokens that nobody sees
@@ -172,6 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       bar_init(bar.o_full(i), 1);
     }
     bar_init(bar.drained(), 1);
+    bar_init(bar.q_full(), kSoftmaxWarps * 32);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -181,31 +218,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   }
   let_next_start();
 
-  // queries: rows that do not exist are zero; a negative scale turns their sign
-  for (int i = threadIdx.x; i < (alternate ? kTile : 2 * kTile) * kPieces; i += kThreads) {
-    const int r = i / kPieces, piece = i % kPieces;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (r < rows) {
-      const int row = row0 + r, token = row / a.group;
-      w = *(const uint4 *)((const T *)a.q + (int64_t)token * a.q_stride + (head * a.group + row - token * a.group) * HD + piece * 8);
-      if constexpr (kMoved<T, FP8>) {
-        uint32_t *x = (uint32_t *)&w;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float2 p = Pair<T>::unpack(x[2 * h]), q = Pair<T>::unpack(x[2 * h + 1]);
-          x[2 * h] = Pair<T>::pack(p.x * kMovedScale, q.x * kMovedScale);
-          x[2 * h + 1] = Pair<T>::pack(p.y * kMovedScale, q.y * kMovedScale);
-        }
-      }
-      const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0;
-      w.x ^= sign;
-      w.y ^= sign;
-      w.z ^= sign;
-      w.w ^= sign;
-    }
-    *(uint4 *)(smem + (r / kTile) * kTileBytes + piece_at(r % kTile, piece)) = w;
-  }
-  fence_async();
   fence_before();
   __syncthreads();
   fence_after();
@@ -213,9 +225,39 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   volatile int *const abort = &s_abort;
 
   if (warp < kSoftmaxWarps) {
+    take_registers<kSoftmaxRegs>();
     const int slot = warp >> 2, local = (warp & 3) * 32 + lane;   // this thread's row in the tile
     const int row = alternate ? local : slot * kTile + local;
     const bool busy = (alternate ? 0 : slot * kTile) + (warp & 3) * 32 < rows;   // any real row in the warp
+    float x[4][32];   // a step's scores, then weights
+    {
+      // The row's query (two threads' work where both slots have the same rows): rows that do not exist are
+      // zero, a negative scale turns the sign.
+      uint4 *const w = (uint4 *)x;
+      const int first = alternate ? slot * (kPieces / 2) : 0;
+      const int r = min(row, rows - 1), token = (row0 + r) / a.group;
+      const uint4 *const src = (const uint4 *)((const T *)a.q + (int64_t)token * a.q_stride + (head * a.group + row0 + r - token * a.group) * HD);
+      const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i)
+        if (i < kPieces / 2 || !alternate) w[i] = src[first + i];
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        if (i >= kPieces / 2 && alternate) break;
+        uint4 v = row < rows ? w[i] : make_uint4(0, 0, 0, 0);
+        if constexpr (kMoved<T, FP8>) {
+          const float2 e0 = Pair<T>::unpack(v.x), e1 = Pair<T>::unpack(v.y), e2 = Pair<T>::unpack(v.z), e3 = Pair<T>::unpack(v.w);
+          v.x = Pair<T>::pack(e0.x * kMovedScale, e1.x * kMovedScale);
+          v.y = Pair<T>::pack(e0.y * kMovedScale, e1.y * kMovedScale);
+          v.z = Pair<T>::pack(e2.x * kMovedScale, e3.x * kMovedScale);
+          v.w = Pair<T>::pack(e2.y * kMovedScale, e3.y * kMovedScale);
+        }
+        *(uint4 *)(smem + (alternate ? 0 : slot * kTileBytes) + piece_at(local, first + i)) =
+            make_uint4(v.x ^ sign, v.y ^ sign, v.z ^ sign, v.w ^ sign);
+      }
+      fence_async();
+      bar_arrive(bar.q_full());
+    }
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
     const uint32_t s_col = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
     const float c = fabsf(a.scale_log2) * (kMoved<T, FP8> ? kMovedScale : 1.f);
@@ -227,6 +269,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       if (!ok) break;
       fence_after();
       if (busy) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tmem_load(x[j], s_col + 32 * j);
         const uint8_t *const bad = s_bad[tile % kKept];
         uint32_t any_bad = 0;
 #pragma unroll
@@ -236,33 +280,38 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         }
         const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0], *const v_scale = s_scale[1][FP8 ? tile % kKept : 0];
         // the largest score, and in FP8 with f16 weights the largest scale of v
-        float top = -CUDART_INF_F, v_top = v_ref;
+        float v_top = v_ref, tops[4];
 #pragma unroll
-        for (int j = 0; j < kTile / 32; ++j) {
-          float x[32];
-          tmem_load(x, s_col + 32 * j);
+        for (int j = 0; j < 4; ++j) {
+          tmem_wait(x[j]);
           if constexpr (FP8) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 k = *(const float4 *)(k_scale + 32 * j + e);
-              x[e] *= k.x;
-              x[e + 1] *= k.y;
-              x[e + 2] *= k.z;
-              x[e + 3] *= k.w;
+              x[j][e] *= k.x;
+              x[j][e + 1] *= k.y;
+              x[j][e + 2] *= k.z;
+              x[j][e + 3] *= k.w;
               if constexpr (!kMoved<T, FP8>) {
                 const float4 v = *(const float4 *)(v_scale + 32 * j + e);
-                v_top = fmaxf(fmaxf(v_top, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));
+                v_top = max3(max3(v_top, v.x, v.y), v.z, v.w);
               }
             }
           }
           if (any_bad) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) top = fmaxf(top, bad[32 * j + e] ? -CUDART_INF_F : x[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) top = fmaxf(top, x[e]);
+            for (int e = 0; e < 32; ++e)
+              if (bad[32 * j + e]) x[j][e] = -CUDART_INF_F;
           }
+          float t0 = x[j][0], t1 = x[j][1];
+#pragma unroll
+          for (int e = 2; e < 32; e += 4) {
+            t0 = max3(t0, x[j][e], x[j][e + 1]);
+            if (e + 3 < 32) t1 = max3(t1, x[j][e + 2], x[j][e + 3]);
+          }
+          tops[j] = fmaxf(t0, t1);
         }
+        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         if (top != -CUDART_INF_F) top *= c;
         const bool raise = i > 0 && (top > m + kRaise || v_top > v_ref);
         if (i == 0) {
@@ -275,65 +324,55 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           if constexpr (FP8 && !kMoved<T, FP8>) by *= v_top > 0.f ? v_ref / v_top : 1.f;
           m = to;
           v_ref = v_top;
-#pragma unroll
-          for (int j = 0; j < HD / 32; ++j) {
-            float x[32];
-            tmem_load(x, o_col + 32 * j);
+#pragma unroll 1
+          for (int j = 0; j < HD / 16; ++j) {
+            float o[16];
+            tmem_load_16(o, o_col + 16 * j);
             uint32_t y[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[16 * h + e] * by);
-              tmem_store_16(o_col + 32 * j + 16 * h, y);
-            }
+            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * by);
+            tmem_store_16(o_col + 16 * j, y);
           }
         }
         const float safe = m == -CUDART_INF_F ? 0.f : m;
         float v_by = kMovedScale;
         if constexpr (FP8 && !kMoved<T, FP8>) v_by = v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
-        float sum[2] = {0.f, 0.f};
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < kTile / 32; ++j) {
-          float x[32];
-          tmem_load(x, s_col + 32 * j);
+        for (int j = 0; j < 4; ++j) {
+          uint32_t p[16];   // rounded once, as the second product's operand
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float4 k = make_float4(c, c, c, c);
-            if constexpr (FP8) {
-              const float4 s = *(const float4 *)(k_scale + 32 * j + e);
-              k = make_float4(s.x * c, s.y * c, s.z * c, s.w * c);
-            }
-            x[e] = exp2_fast(fmaf(x[e], k.x, -safe));
-            x[e + 1] = exp2_fast(fmaf(x[e + 1], k.y, -safe));
-            x[e + 2] = exp2_fast(fmaf(x[e + 2], k.z, -safe));
-            x[e + 3] = exp2_fast(fmaf(x[e + 3], k.w, -safe));
+          for (int e = 0; e < 32; e += 2) {
+            float &u = x[j][e], &v = x[j][e + 1];
+            fma_pair(u, v, c, c, -safe);   // a masked score stays minus infinity (c may be zero)
+            u = exp2_fast(u);
+            v = exp2_fast(v);
           }
           if (any_bad) {
 #pragma unroll
             for (int e = 0; e < 32; ++e)
-              if (bad[32 * j + e]) x[e] = 0.f;
+              if (bad[32 * j + e]) x[j][e] = 0.f;
           }
 #pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            sum[0] += x[e];
-            sum[1] += x[e + 1];
+          for (int e = 0; e < 32; e += 4) {
+            add_pair(sum[0], sum[1], x[j][e], x[j][e + 1]);
+            add_pair(sum[2], sum[3], x[j][e + 2], x[j][e + 3]);
           }
           if constexpr (FP8) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 v = *(const float4 *)(v_scale + 32 * j + e);
-              x[e] *= v.x * v_by;
-              x[e + 1] *= v.y * v_by;
-              x[e + 2] *= v.z * v_by;
-              x[e + 3] *= v.w * v_by;
+              x[j][e] *= v.x * v_by;
+              x[j][e + 1] *= v.y * v_by;
+              x[j][e + 2] *= v.z * v_by;
+              x[j][e + 3] *= v.w * v_by;
             }
           }
-          uint32_t p[16];   // rounded once, as the second product's operand
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p[e] = Pair<T>::pack(x[2 * e], x[2 * e + 1]);
+          for (int e = 0; e < 16; ++e) p[e] = Pair<T>::pack(x[j][2 * e], x[j][2 * e + 1]);
           tmem_store_16(s_col + 16 * j, p);   // over columns that have been read
         }
-        l += sum[0] + sum[1];
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tmem_stored();
       }
       fence_before();
@@ -351,14 +390,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         float by = 1.f;
         if constexpr (kMoved<T, FP8>) by = kMovedScale;
         else if constexpr (FP8) by = v_ref;
-#pragma unroll 1
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) tmem_load(x[j], o_col + 32 * j);
+#pragma unroll
         for (int j = 0; j < HD / 32; ++j) {
-          float x[32];
-          tmem_load(x, o_col + 32 * j);
+          tmem_wait(x[j]);
           if (row < rows) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-              float4 y = make_float4(x[e] * by, x[e + 1] * by, x[e + 2] * by, x[e + 3] * by);
+              float4 y = make_float4(x[j][e] * by, x[j][e + 1] * by, x[j][e + 2] * by, x[j][e + 3] * by);
               if constexpr (kMoved<T, FP8>) y = make_float4(y.x, y.z, y.y, y.w);
               *(float4 *)(a.part_o + part * HD + 32 * j + e) = y;
             }
@@ -367,8 +407,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       }
     }
     fence_before();
-  } else if (warp == kMmaWarp) {
-    if (lane == 0 && tiles > 0) {
+  } else if (warp < kCopyWarp0) {
+    give_registers<kMmaRegs>();
+    if (warp == kMmaWarp && lane == 0) {
       constexpr uint32_t kType = __is_same(T, __half) ? 0 : 1;
       constexpr uint32_t kIdS = instruction(kType, kTile, 0), kIdO = instruction(kType, HD, 1);
       const auto scores = [&](int slot, int stage) {
@@ -385,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           mma_ts(tmem + kColO + slot * HD, tmem + kColS + slot * kTile + k * 8,
                  operand(v_at + stage * kTileBytes + k * 2048, kTile * 128), kIdO, add || k > 0);
       };
-      bool ok = true;
+      bool ok = bar_wait(bar.q_full(), 0, abort);
       // step i of slot s: its tile, the tile's buffer, and whether this product is the buffer's last reader
       const auto tile_of = [&](int s, int i) { return alternate ? 2 * i + s : i; };
       const auto last_reader = [&](int s) { return alternate || s == 1 || !second; };
@@ -421,8 +462,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       }
     }
     __syncwarp();
-  } else if (tiles > 0) {
-    const int w = warp - kMmaWarp - 1;
+  } else {
+    give_registers<kCopyRegs>();
+    const int w = warp - kCopyWarp0;
     // A row's pieces are taken by kGroup neighbouring lanes; a warp has 32 rows of a tile, and each lane
     // finds one of them in the table.
     constexpr int kGroup = FP8 ? HD / 16 : kPieces, kRows = 32 / kGroup, kPasses = kTile / (kCopyWarps * kRows);
@@ -487,19 +529,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           raw[v][pass] = at < 0 ? make_uint4(0, 0, 0, 0) : *(const uint4 *)(pool + at * HD + piece * 16);
         }
       };
-      int64_t vec = locate(0);
+      int64_t vec = locate(0), next = locate(1);   // the table is read two tiles ahead
       bool bad = vec < 0;
       load(0, vec);
       load(1, vec);
       for (int tile = 0; tile < tiles && ok; ++tile) {
         const int stage = tile & 1;
-        const int64_t next = locate(tile + 1);
+        const int64_t after = locate(tile + 2);
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           if (tile >= 2) ok = ok && bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
           if (!ok) break;
-          if (v == 0) s_bad[tile % kKept][my_row] = bad;
-          s_scale[v][tile % kKept][my_row] = by[v];
+          if (v == 0) {   // v's scales too: the softmax does not wait for the values
+            s_bad[tile % kKept][my_row] = bad;
+            s_scale[0][tile % kKept][my_row] = by[0];
+            s_scale[1][tile % kKept][my_row] = by[1];
+          }
           uint8_t *const dst = smem + 2 * kTileBytes + (v ? 2 * kTileBytes : 0) + stage * kTileBytes;
 #pragma unroll
           for (int pass = 0; pass < kPasses; ++pass) {
@@ -518,6 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           if (tile + 1 < tiles) load(v, next);
         }
         bad = next < 0;
+        next = after;
       }
     }
   }

@@ -119,11 +119,18 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
   uint8_t *const ring = smem + warp * (kStages * kStage);
   const uint32_t ring_at = shared_address(ring);
 
-  // vector index of this lane's token (lanes 16.. repeat 0..15) of step i, -1 if there is none
-  auto locate = [&](int i) -> int64_t {
+  // this lane's token of step i (lanes 16.. repeat 0..15), -1 if there is none; its block; its vector index
+  auto token_of = [&](int i) {
     const int t = it.t0 + (warp + kWarps * i) * kGroup + (lane & 15);
-    if (i >= steps || t >= it.t1) return -1;
-    return token_vector(a, table, t, it.head);
+    return i >= steps || t >= it.t1 ? -1 : t;
+  };
+  auto block_of = [&](int i) {
+    const int t = token_of(i);
+    return t < 0 ? 0 : table[(uint32_t)t / (uint32_t)a.c.block_tokens];
+  };
+  auto vector_of = [&](int i, int block) {
+    const int t = token_of(i);
+    return t < 0 ? (int64_t)-1 : token_vector(a, block, t, it.head);
   };
   uint32_t held_scale = 0, held_valid = 0;
   auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
@@ -151,17 +158,17 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) {
     if (i < steps) {
-      issue(i, locate(i));
+      issue(i, vector_of(i, block_of(i)));
       keep(i);
     }
     copy_async_commit();
   }
-  int64_t next = locate(kStages - 1);
+  int block = block_of(kStages - 1);   // the table is read a step ahead
   for (int i = 0; i < steps; ++i) {
     const int ahead = i + kStages - 1;
-    if (ahead < steps) issue(ahead, next);
+    if (ahead < steps) issue(ahead, vector_of(ahead, block));
     copy_async_commit();
-    next = locate(ahead + 1);
+    block = block_of(ahead + 1);
     copy_async_wait<kStages - 1>();
     __syncwarp();
 

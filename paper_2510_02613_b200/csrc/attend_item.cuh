@@ -18,10 +18,10 @@ __device__ __forceinline__ int64_t output_row(const AttendArgs &a, int seq, int 
   return ((int64_t)seq * a.q_len + token) * a.n_q_heads + head * a.group + row - token * a.group;
 }
 
-// Vector index of token t on the blocks of `table`, -1 (and the status word) if its block is outside the pool.
-__device__ __forceinline__ int64_t token_vector(const AttendArgs &a, const int32_t *table, int t, int head) {
-  const uint32_t b = (uint32_t)t / (uint32_t)a.c.block_tokens, off = (uint32_t)t - b * a.c.block_tokens;
-  const int block = table[b];
+// Vector index of token t, which lies on `block`; -1 (and the status word) if that is outside the pool.
+// (The table is read apart from this and well before: a branch on what it says waits for it.)
+__device__ __forceinline__ int64_t token_vector(const AttendArgs &a, int block, int t, int head) {
+  const uint32_t off = (uint32_t)t % (uint32_t)a.c.block_tokens;
   if (block < 0 || block >= a.num_blocks) {
     if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
     return -1;

@@ -4,28 +4,29 @@
 // A batch that shares a prefix has n_seqs * q_len * (query heads per KV head) rows for each KV head: a
 // matrix product once there are more than a few.  A block takes a KV head, up to 256 rows and a range of
 // the prefix; it holds the rows' queries in shared memory and two accumulator sets ("slots") in tensor memory,
-//     S = Q K^T (128 x 128), O += P V (128 x head_dim),   P = 2^(scale S - m) rounded to 16 bits,
-// and runs through the tokens 128 at a time.  P is written over S in tensor memory and multiplied from
-// there.  The two slots take turns: while one's weights are computed the other's products run.  With
-// more than 128 rows the slots are two row tiles on the same tokens; with fewer they are the same rows on
-// alternating tiles of tokens, so that a single row tile also keeps both units busy.
+//     S = Q K^T (128 x 64), O += P V (128 x head_dim),   P = 2^(scale S - m) rounded to 16 bits,
+// and runs through the tokens in steps of 64 (tiles of 128 are brought in).  S has two buffers a slot, so
+// that the next step's scores are there when a step's weights are done; P is written over its S in tensor
+// memory and multiplied from there.  With more than 128 rows the slots are two row tiles on the same
+// tokens; with fewer they are the same rows on alternating tiles of tokens, so that a single row tile
+// also keeps both the tensor cores and the exponentials busy.
 //
-// Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row, all 128 scores of a step in its
+// Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row, the scores of a step in its
 // registers), 8 issues the products, 12-15 bring K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
 // asynchronously; e4m3 codes are widened on the way).  The maximum in use is only raised when the real one
 // passes it by more than 2^8: sums and weights then still fit, and O is rarely rescaled.
 //
-// Bounds: exponentials (16 a clock and SM, 2 x 128 x 128 a pair of tiles = 2048 clocks) and products
-// (the same) with many rows, the reads of K and V with few.
+// Bounds: exponentials (16 a clock and SM: 2048 clocks for 2 x 128 rows x 128 tokens) and products
+// (about the same) with many rows, the reads of K and V with few.
 #include "attend_item.cuh"
 
 namespace emoe {
 namespace {
 
-constexpr int kTile = 128;                 // rows of a slot, tokens of a step
+constexpr int kTile = 128, kStep = 64;     // rows of a slot and tokens that are brought in at once; tokens of a step
 constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
 // Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
-constexpr int kSoftmaxRegs = 184, kMmaRegs = 40, kCopyRegs = 104;
+constexpr int kSoftmaxRegs = 152, kMmaRegs = 88, kCopyRegs = 120;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
 constexpr int kKept = 4;                   // steps whose masks and scales are kept
 constexpr unsigned long long kWaitNs = 4000000000ull, kDrainNs = 1000000000ull;
@@ -73,6 +74,13 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
   return __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
 }
 
+// This thread's arrival once all its copies so far have landed.  (They are ordinary writes: who waits for
+// the barrier orders them before the tensor cores' reads with fence_async.)
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // Shared memory operand, 128-byte swizzle: rows of 128 bytes, 8 rows (1024 bytes) an atom.  Queries and keys
 // have the k axis along the row (chunks of 64 elements, `chunk` bytes apart, are addressed by the
 // caller); values have it across the rows, and their 64-element chunks follow one another at `chunk`.
@@ -93,6 +101,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -156,32 +169,33 @@ __device__ __forceinline__ uint32_t piece_at(int r, int piece) {
   return (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
 }
 
-struct Bars {   // each in two copies: stages of K or V, or slots
+struct Bars {
   uint32_t base;
-  __device__ __forceinline__ uint32_t k_full(int i) const { return base + 8 * i; }
-  __device__ __forceinline__ uint32_t k_empty(int i) const { return base + 16 + 8 * i; }
-  __device__ __forceinline__ uint32_t v_full(int i) const { return base + 32 + 8 * i; }
-  __device__ __forceinline__ uint32_t v_empty(int i) const { return base + 48 + 8 * i; }
-  __device__ __forceinline__ uint32_t s_full(int i) const { return base + 64 + 8 * i; }
-  __device__ __forceinline__ uint32_t p_full(int i) const { return base + 80 + 8 * i; }
-  __device__ __forceinline__ uint32_t o_full(int i) const { return base + 96 + 8 * i; }
-  __device__ __forceinline__ uint32_t drained() const { return base + 112; }   // one
-  __device__ __forceinline__ uint32_t q_full() const { return base + 120; }    // one
+  __device__ __forceinline__ uint32_t k_full(int stage) const { return base + 8 * stage; }
+  __device__ __forceinline__ uint32_t k_empty(int stage) const { return base + 16 + 8 * stage; }
+  __device__ __forceinline__ uint32_t v_full(int stage) const { return base + 32 + 8 * stage; }
+  __device__ __forceinline__ uint32_t v_empty(int stage) const { return base + 48 + 8 * stage; }
+  __device__ __forceinline__ uint32_t s_full(int slot, int half) const { return base + 64 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t p_full(int slot, int half) const { return base + 96 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
+  __device__ __forceinline__ uint32_t drained() const { return base + 168; }
 };
+constexpr int kBars = 22;
 
 template <typename T, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
   constexpr uint32_t kTileBytes = kTile * HD * 2;
   constexpr int kPieces = HD / 8;   // 16-byte pieces of a 16-bit row
   extern __shared__ uint8_t raw_smem[];
-  __shared__ __align__(8) uint64_t bars[16];
+  __shared__ __align__(8) uint64_t bars[kBars];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   __shared__ __align__(16) uint8_t s_bad[kKept][kTile];             // tokens that nobody sees
   __shared__ __align__(16) float s_scale[2][FP8 ? kKept : 1][FP8 ? kTile : 4];   // of K and V
   uint8_t *const smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   const uint32_t q_at = shared_address(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + 2 * kTileBytes;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
   // the item
   const uint32_t heads = a.c.n_heads;
@@ -192,8 +206,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   const int t0 = split * a.prefix_chunk, t1 = min(a.prefix_len, t0 + a.prefix_chunk);
   const int tiles = (t1 - t0 + kTile - 1) / kTile;
   const bool alternate = a.alternate != 0, second = alternate || rows > kTile;
-  // tiles of slot s, and the tile of its step i
-  const int steps[2] = {alternate ? (tiles + 1) / 2 : tiles, alternate ? tiles / 2 : second ? tiles : 0};
+  // steps of the slots: two a tile, unless the last one has no token in its second half
+  const int last_halves = t1 - t0 - (tiles - 1) * kTile > kStep ? 2 : 1;
+  const int own_tiles[2] = {alternate ? (tiles + 1) / 2 : tiles, alternate ? tiles / 2 : second ? tiles : 0};
+  const auto steps_of = [&](int slot) {
+    const bool has_last = own_tiles[slot] > 0 && (!alternate || ((tiles - 1) & 1) == slot);
+    return 2 * own_tiles[slot] - (has_last ? 2 - last_halves : 0);
+  };
+  const int steps[2] = {steps_of(0), steps_of(1)};
 
   const Bars bar{shared_address(bars)};
   if (threadIdx.x == 0) {
@@ -203,9 +223,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       bar_init(bar.v_full(i), kCopyWarps * 32);
       bar_init(bar.k_empty(i), 1);
       bar_init(bar.v_empty(i), 1);
-      bar_init(bar.s_full(i), 1);
-      bar_init(bar.p_full(i), 128);
-      bar_init(bar.o_full(i), 1);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        bar_init(bar.s_full(i, half), 1);
+        bar_init(bar.p_full(i, half), 128);
+        bar_init(bar.o_full(i, half), 1);
+      }
     }
     bar_init(bar.drained(), 1);
     bar_init(bar.q_full(), kSoftmaxWarps * 32);
@@ -229,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     const int slot = warp >> 2, local = (warp & 3) * 32 + lane;   // this thread's row in the tile
     const int row = alternate ? local : slot * kTile + local;
     const bool busy = (alternate ? 0 : slot * kTile) + (warp & 3) * 32 < rows;   // any real row in the warp
-    float x[4][32];   // a step's scores, then weights
+    float x[2][32];   // the row's query, then a step's scores and weights
     {
       // The row's query (two threads' work where both slots have the same rows): rows that do not exist are
       // zero, a negative scale turns the sign.
@@ -259,30 +282,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       bar_arrive(bar.q_full());
     }
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
-    const uint32_t s_col = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
+    const uint32_t s_base = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
     const float c = fabsf(a.scale_log2) * (kMoved<T, FP8> ? kMovedScale : 1.f);
     float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: f16 weights carry v's scale relative to the largest yet
     bool ok = true;
     for (int i = 0; i < steps[slot] && ok; ++i) {
-      const int tile = alternate ? 2 * i + slot : i;
-      ok = bar_wait_warp(bar.s_full(slot), i & 1, abort);
+      const int half = i & 1, tile = alternate ? 2 * (i >> 1) + slot : i >> 1;
+      const uint32_t s_col = s_base + half * kStep;
+      ok = bar_wait_warp(bar.s_full(slot, half), (i >> 1) & 1, abort);
       if (!ok) break;
       fence_after();
       if (busy) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) tmem_load(x[j], s_col + 32 * j);
-        const uint8_t *const bad = s_bad[tile % kKept];
+        tmem_load(x[0], s_col);
+        tmem_load(x[1], s_col + 32);
+        const uint8_t *const bad = s_bad[tile % kKept] + half * kStep;
         uint32_t any_bad = 0;
 #pragma unroll
-        for (int j = 0; j < kTile / 16; ++j) {
+        for (int j = 0; j < kStep / 16; ++j) {
           const uint4 b = ((const uint4 *)bad)[j];
           any_bad |= b.x | b.y | b.z | b.w;
         }
-        const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0], *const v_scale = s_scale[1][FP8 ? tile % kKept : 0];
+        const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0] + half * kStep;
+        const float *const v_scale = s_scale[1][FP8 ? tile % kKept : 0] + half * kStep;
         // the largest score, and in FP8 with f16 weights the largest scale of v
-        float v_top = v_ref, tops[4];
+        float v_top = v_ref, tops[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           tmem_wait(x[j]);
           if constexpr (FP8) {
 #pragma unroll
@@ -311,13 +336,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           }
           tops[j] = fmaxf(t0, t1);
         }
-        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        float top = fmaxf(tops[0], tops[1]);
         if (top != -CUDART_INF_F) top *= c;
         const bool raise = i > 0 && (top > m + kRaise || v_top > v_ref);
         if (i == 0) {
           m = top;
           v_ref = v_top;
-        } else if (__any_sync(0xffffffffu, raise)) {   // O may be touched: S of this step came after the last product
+        } else if (__any_sync(0xffffffffu, raise)) {   // O may be touched once the last step's product
+          // is done (the one before it is: this step's scores came after that)
+          ok = bar_wait_warp(bar.o_full(slot, (i - 1) & 1), ((i - 1) >> 1) & 1, abort);
+          if (!ok) break;
+          fence_after();
           const float to = top > m + kRaise ? top : m;
           float by = to == -CUDART_INF_F ? 1.f : exp2_fast(m - to);
           l *= by;
@@ -339,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         if constexpr (FP8 && !kMoved<T, FP8>) v_by = v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           uint32_t p[16];   // rounded once, as the second product's operand
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
@@ -376,10 +405,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         tmem_stored();
       }
       fence_before();
-      bar_arrive(bar.p_full(slot));
+      bar_arrive(bar.p_full(slot, half));
     }
     // the part of this range: maximum, sum and unnormalised output of every row
-    if (steps[slot] > 0 && ok) ok = bar_wait_warp(bar.o_full(slot), 0, abort);
+    // The last two products may be under way.  A parity tells one phase from the next only: each half has a
+    // barrier of its own, whose phase before is over by then.
+    for (int i = max(0, steps[slot] - 2); i < steps[slot] && ok; ++i)
+      ok = bar_wait_warp(bar.o_full(slot, i & 1), (i >> 1) & 1, abort);
     fence_after();
     const int slots = a.prefix_splits + a.own_splits;
     const int64_t part = row < rows ? output_row(a, 0, head, row0 + row) * slots + (alternate ? 2 * split + slot : split) : 0;
@@ -390,6 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         float by = 1.f;
         if constexpr (kMoved<T, FP8>) by = kMovedScale;
         else if constexpr (FP8) by = v_ref;
+        float x[HD / 32][32];
 #pragma unroll
         for (int j = 0; j < HD / 32; ++j) tmem_load(x[j], o_col + 32 * j);
 #pragma unroll
@@ -409,55 +442,68 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     fence_before();
   } else if (warp < kCopyWarp0) {
     give_registers<kMmaRegs>();
-    if (warp == kMmaWarp && lane == 0) {
+    if (warp == kMmaWarp) {   // the whole warp goes along, one lane issues: addresses stay in uniform registers
       constexpr uint32_t kType = __is_same(T, __half) ? 0 : 1;
-      constexpr uint32_t kIdS = instruction(kType, kTile, 0), kIdO = instruction(kType, HD, 1);
-      const auto scores = [&](int slot, int stage) {
+      constexpr uint32_t kIdS = instruction(kType, kStep, 0), kIdO = instruction(kType, HD, 1);
+      const bool one = elect_one();
+      const auto commit = [&](uint32_t b) {
+        if (one) mma_commit(b);
+      };
+      const auto scores = [&](int slot, int stage, int half) {
+        if (!one) return;
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
           const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
-          mma_ss(tmem + kColS + slot * kTile, operand(q_at + (alternate ? 0 : slot * kTileBytes) + off, 0),
-                 operand(k_at + stage * kTileBytes + off, 0), kIdS, k > 0);
+          mma_ss(tmem + kColS + slot * kTile + half * kStep, operand(q_at + (alternate ? 0 : slot * kTileBytes) + off, 0),
+                 operand(k_at + stage * kTileBytes + half * (kStep * 128) + off, 0), kIdS, k > 0);
         }
       };
-      const auto values = [&](int slot, int stage, bool add) {
+      const auto values = [&](int slot, int stage, int half, bool add) {
+        if (!one) return;
 #pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(tmem + kColO + slot * HD, tmem + kColS + slot * kTile + k * 8,
-                 operand(v_at + stage * kTileBytes + k * 2048, kTile * 128), kIdO, add || k > 0);
+        for (int k = 0; k < kStep / 16; ++k)
+          mma_ts(tmem + kColO + slot * HD, tmem + kColS + slot * kTile + half * kStep + k * 8,
+                 operand(v_at + stage * kTileBytes + half * (kStep * 128) + k * 2048, kTile * 128), kIdO, add || k > 0);
       };
-      bool ok = bar_wait(bar.q_full(), 0, abort);
-      // step i of slot s: its tile, the tile's buffer, and whether this product is the buffer's last reader
-      const auto tile_of = [&](int s, int i) { return alternate ? 2 * i + s : i; };
-      const auto last_reader = [&](int s) { return alternate || s == 1 || !second; };
+      bool ok = bar_wait_warp(bar.q_full(), 0, abort);
+      const auto tile_of = [&](int s, int i) { return alternate ? 2 * (i >> 1) + s : i >> 1; };
+      // whether the products of slot s are a tile's last readers, at its last step
+      const auto last_reader = [&](int s, int i) { return (alternate || s == 1 || !second) && ((i & 1) || i + 1 == steps[s]); };
       const auto start = [&](int s, int i) {   // S of step i
         const int tile = tile_of(s, i), stage = tile & 1;
-        if (alternate || s == 0) ok = ok && bar_wait(bar.k_full(stage), (tile >> 1) & 1, abort);
+        if ((alternate || s == 0) && !(i & 1)) {
+          ok = ok && bar_wait_warp(bar.k_full(stage), (tile >> 1) & 1, abort);
+          if constexpr (!FP8) fence_async();
+        }
         if (!ok) return;
         fence_after();
-        scores(s, stage);
-        mma_commit(bar.s_full(s));
-        if (last_reader(s)) mma_commit(bar.k_empty(stage));
+        scores(s, stage, i & 1);
+        commit(bar.s_full(s, i & 1));
+        if (last_reader(s, i)) commit(bar.k_empty(stage));
       };
-      for (int s = 0; s < 2; ++s)
-        if (steps[s] > 0 && ok) start(s, 0);
+      for (int i = 0; i < 2; ++i)
+        for (int s = 0; s < 2; ++s)
+          if (i < steps[s] && ok) start(s, i);
       for (int i = 0; i < steps[0] && ok; ++i) {
         for (int s = 0; s < 2 && ok; ++s) {
           if (i >= steps[s]) continue;
           const int tile = tile_of(s, i), stage = tile & 1;
-          if (alternate || s == 0) ok = ok && bar_wait(bar.v_full(stage), (tile >> 1) & 1, abort);
-          ok = ok && bar_wait(bar.p_full(s), i & 1, abort);
+          if ((alternate || s == 0) && !(i & 1)) {
+            ok = ok && bar_wait_warp(bar.v_full(stage), (tile >> 1) & 1, abort);
+            if constexpr (!FP8) fence_async();
+          }
+          ok = ok && bar_wait_warp(bar.p_full(s, i & 1), (i >> 1) & 1, abort);
           if (!ok) break;
           fence_after();
-          values(s, stage, i > 0);
-          if (last_reader(s)) mma_commit(bar.v_empty(stage));
-          if (i + 1 < steps[s]) start(s, i + 1);
-          else mma_commit(bar.o_full(s));
+          values(s, stage, i & 1, i > 0);
+          commit(bar.o_full(s, i & 1));
+          if (last_reader(s, i)) commit(bar.v_empty(stage));
+          if (i + 2 < steps[s]) start(s, i + 2);
         }
       }
       if (!ok) {   // gave up: let the products in flight end before the tensor memory is given back
         int never = 0;
-        mma_commit(bar.drained());
+        commit(bar.drained());
         bar_wait(bar.drained(), 0, &never, kDrainNs);
       }
     }
@@ -472,84 +518,88 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     const int piece = lane % kGroup;
     const auto row_of = [&](int pass, int r) { return pass * (kCopyWarps * kRows) + w * kRows + r; };
     const int my_row = row_of(lane / kRows, lane % kRows);
-    const auto locate = [&](int tile) -> int64_t {
+    // this lane's token of a tile, -1 if there is none; its block; its vector index
+    const auto token_of = [&](int tile) {
       const int t = t0 + tile * kTile + my_row;
-      return tile < tiles && t < t1 ? token_vector(a, a.prefix_table, t, head) : -1;
+      return tile < tiles && t < t1 ? t : -1;
     };
+    const auto block_of = [&](int tile) {
+      const int t = token_of(tile);
+      return t < 0 ? 0 : a.prefix_table[(uint32_t)t / (uint32_t)a.c.block_tokens];
+    };
+    const auto vector_of = [&](int tile, int block) {
+      const int t = token_of(tile);
+      return t < 0 ? (int64_t)-1 : token_vector(a, block, t, head);
+    };
+    // Order: K of an even tile, K of the next, V of both.  (With one row tile the scores run two tiles
+    // ahead: a value buffer that waits for its products must not hold up the keys that those need.)
     bool ok = true;
     if constexpr (!FP8) {
-      int issued = 0, told = 0;   // buffers (K of tile 0, V of tile 0, K of tile 1, ...) filled, and said to be
-      const auto tell = [&](int upto) {
-        fence_async();
-        for (; told < upto; ++told) bar_arrive(told & 1 ? bar.v_full((told >> 1) & 1) : bar.k_full((told >> 1) & 1));
-      };
-      int64_t vec = locate(0);
-      for (int tile = 0; tile < tiles && ok; ++tile) {
-        const int64_t next = locate(tile + 1);
-        const int stage = tile & 1;
-        for (int v = 0; v < 2 && ok; ++v) {
-          if (tile >= 2) {
-            const uint32_t empty = v ? bar.v_empty(stage) : bar.k_empty(stage), parity = (tile >> 1) + 1 & 1;
-            if (!__all_sync(0xffffffffu, bar_try(empty, parity))) {   // about to wait: first say what has arrived meanwhile
-              copy_async_wait<0>();
-              tell(issued);
-              ok = bar_wait_warp(empty, parity, abort);
-              if (!ok) break;
-            }
-          }
-          if (v == 0) s_bad[tile % kKept][my_row] = vec < 0;
+      int block[2] = {block_of(0), block_of(1)};   // the table is read a pair ahead
+      for (int first = 0; first < tiles && ok; first += 2) {
+        const int64_t vec[2] = {vector_of(first, block[0]), vector_of(first + 1, block[1])};
+        block[0] = block_of(first + 2);
+        block[1] = block_of(first + 3);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int v = u >> 1, stage = u & 1, tile = first + stage;
+          if (tile >= tiles || !ok) continue;
+          if (tile >= 2) ok = bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (!ok) continue;
+          if (v == 0) s_bad[tile % kKept][my_row] = vec[stage] < 0;
           const uint8_t *const pool = v ? a.c.v : a.c.k;
           const uint32_t dst = (v ? v_at : k_at) + stage * kTileBytes;
 #pragma unroll
           for (int pass = 0; pass < kPasses; ++pass) {
-            const int64_t at = __shfl_sync(0xffffffffu, vec, pass * kRows + lane / kGroup);
+            const int64_t at = __shfl_sync(0xffffffffu, vec[stage], pass * kRows + lane / kGroup);
             const int r = row_of(pass, lane / kGroup);
             copy_async_16(dst + piece_at(r, piece), pool + (at < 0 ? 0 : at * (HD * 2) + piece * 16), at < 0 ? 0 : 16);
           }
-          copy_async_commit();
-          ++issued;
-          if (issued - told > 2) {
-            copy_async_wait<2>();
-            tell(issued - 2);
-          }
+          copies_arrive(v ? bar.v_full(stage) : bar.k_full(stage));
         }
-        vec = next;
       }
-      copy_async_wait<0>();
-      if (ok) tell(issued);
+      copy_async_wait_all();
     } else {
+      // Two buffers of registers, for the even and the odd tiles: while one is widened and stored the
+      // other's loads are under way.
       uint4 raw[2][kPasses];
-      float by[2] = {1.f, 1.f};
-      const auto load = [&](int v, int64_t vec) {
+      uint8_t byte[2][2] = {};   // [K, V][tile's parity]: the scale of this lane's row, as it is until it is needed
+      const auto load = [&](int v, int parity, int64_t vec) {
         const uint8_t *const pool = v ? a.c.v : a.c.k;
-        by[v] = vec < 0 ? 0.f : scale_of((v ? a.c.v_scale : a.c.k_scale)[vec]);
+        if (v == 0 && vec >= 0) {
+          byte[0][parity] = a.c.k_scale[vec];
+          byte[1][parity] = a.c.v_scale[vec];
+        }
 #pragma unroll
         for (int pass = 0; pass < kPasses; ++pass) {
           const int64_t at = __shfl_sync(0xffffffffu, vec, pass * kRows + lane / kGroup);
-          raw[v][pass] = at < 0 ? make_uint4(0, 0, 0, 0) : *(const uint4 *)(pool + at * HD + piece * 16);
+          raw[parity][pass] = make_uint4(0, 0, 0, 0);
+          if (at >= 0) raw[parity][pass] = *(const uint4 *)(pool + at * HD + piece * 16);
         }
       };
-      int64_t vec = locate(0), next = locate(1);   // the table is read two tiles ahead
-      bool bad = vec < 0;
-      load(0, vec);
-      load(1, vec);
-      for (int tile = 0; tile < tiles && ok; ++tile) {
-        const int stage = tile & 1;
-        const int64_t after = locate(tile + 2);
+      int block[2] = {block_of(0), block_of(1)};   // the table is read a pair ahead
+      int64_t vec[2] = {vector_of(0, block[0]), vector_of(1, block[1])};
+      block[0] = block_of(2);
+      block[1] = block_of(3);
+      load(0, 0, vec[0]);
+      load(0, 1, vec[1]);
+      for (int first = 0; first < tiles && ok; first += 2) {
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          if (tile >= 2) ok = ok && bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
-          if (!ok) break;
+        for (int u = 0; u < 4; ++u) {
+          const int v = u >> 1, stage = u & 1, tile = first + stage;
+          if (tile >= tiles || !ok) continue;
+          if (tile >= 2) ok = bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (!ok) continue;
           if (v == 0) {   // v's scales too: the softmax does not wait for the values
-            s_bad[tile % kKept][my_row] = bad;
-            s_scale[0][tile % kKept][my_row] = by[0];
-            s_scale[1][tile % kKept][my_row] = by[1];
+            s_bad[tile % kKept][my_row] = vec[stage] < 0;
+            s_scale[0][tile % kKept][my_row] = vec[stage] < 0 ? 0.f : scale_of(byte[0][stage]);
+            s_scale[1][tile % kKept][my_row] = vec[stage] < 0 ? 0.f : scale_of(byte[1][stage]);
           }
           uint8_t *const dst = smem + 2 * kTileBytes + (v ? 2 * kTileBytes : 0) + stage * kTileBytes;
 #pragma unroll
           for (int pass = 0; pass < kPasses; ++pass) {
             const int r = row_of(pass, lane / kGroup);
-            const uint4 x = raw[v][pass];
+            const uint4 x = raw[stage][pass];
             uint4 lo, hi;
             word_of_codes<T>(lo.x, lo.y, x.x);
             word_of_codes<T>(lo.z, lo.w, x.y);
@@ -560,10 +610,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           }
           fence_async();
           bar_arrive(v ? bar.v_full(stage) : bar.k_full(stage));
-          if (tile + 1 < tiles) load(v, next);
+          if (v == 0) {
+            load(1, stage, vec[stage]);
+          } else {
+            vec[stage] = vector_of(tile + 2, block[stage]);
+            block[stage] = block_of(tile + 4);
+            load(0, stage, vec[stage]);
+          }
         }
-        bad = next < 0;
-        next = after;
       }
     }
   }

@@ -137,3 +137,43 @@ def test_captured_and_repeated_calls_give_the_same_bits():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kv,hkv,seqs,prefix", [("e4m3", 37, 20, 4000), ("bf16", 37, 17, 4100), ("f16", 37, 9, 3999), ("e4m3", 19, 40, 5000)])
+def test_many_tiles_a_block(kv, hkv, seqs, prefix):
+    """Long runs of tiles in one block (more heads than splits fill the machine), in both uses of the
+    slots; the definition in 64 bits on the GPU, the tolerance as above with its bound of a score's error."""
+    g = torch.Generator(device="cuda").manual_seed(prefix)
+    group, hd, block = (1, 128, 16) if seqs != 40 else (8, 64, 16)
+    blocks = -(-prefix // block)
+    io = "f16" if kv == "f16" else "bf16"
+    group = 2 if seqs == 9 else group
+    x = torch.randn(2, blocks, block, hkv, hd, generator=g, device="cuda")
+    scales = None
+    if kv == "e4m3":
+        scales = torch.randint(120, 130, x.shape[:-1], generator=g, device="cuda").to(torch.uint8)
+        codes = (x * 60).to(torch.float8_e4m3fn)
+        arena, values = codes.view(torch.uint8), codes.double() * torch.exp2(scales.double() - 133)[..., None]
+        scales = scales - 6
+    else:
+        arena = x.to(TORCH[kv]).view(torch.uint8)
+        values = x.to(TORCH[kv]).double()
+    import paper_2510_02613_b200 as E
+    c = E.KvCache(arena, n_layers=1, num_blocks=blocks, block_tokens=block, n_heads=hkv, head_dim=hd, kv_type=kv, scales=scales)
+    q = torch.randn(seqs, 1, hkv * group, hd, generator=g, device="cuda").to(TORCH[io])
+    pt = torch.randperm(blocks, generator=g, device="cuda").int()
+    k, v = (values[i][pt.long()].reshape(-1, hkv, hd)[:prefix] for i in range(2))
+    score = torch.einsum("nhgd,phd->nhgp", q[:, 0].double().view(seqs, hkv, group, hd), k) * hd ** -0.5
+    p = torch.softmax(score, -1)
+    o, a = torch.einsum("nhgp,phd->nhgd", p, v), torch.einsum("nhgp,phd->nhgd", p, v.abs())
+    size = torch.einsum("nhgd,phd->nhgp", q[:, 0].double().abs().view(seqs, hkv, group, hd), k.abs()).amax(-1) * hd ** -0.5
+    e = (hd + 8) * 2.0 ** -23 * size + (prefix + 16) * 2.0 ** -23
+    tol = 1.05 * (2 * (2.0 ** -11 if io == "f16" else 2.0 ** -8) + 2 * e[..., None]) * a + 1e-30
+    outs = []
+    for _ in range(3):
+        out = torch.empty_like(q)
+        work = torch.empty(c.attend_workspace_bytes(seqs, 1, hkv * group, 0, prefix), dtype=torch.uint8, device="cuda")
+        c.attend(0, q, out, None, None, pt, prefix, workspace=work)
+        outs.append(out)
+        assert ((out[:, 0].double().view(o.shape) - o).abs() <= tol).all()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

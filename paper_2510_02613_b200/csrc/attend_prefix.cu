@@ -12,7 +12,8 @@
 // also keeps both the tensor cores and the exponentials busy.
 //
 // Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row, the scores of a step in its
-// registers), 8 issues the products, 12-15 bring K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
+// registers), 8 and 9 issue the slots' products (each keeps the tensor cores fed while the other
+// waits), 12-15 bring K and V rows from their pages into the 128-byte-swizzled tiles that the products read (copied
 // asynchronously; e4m3 codes are widened on the way).  The maximum in use is only raised when the real one
 // passes it by more than 2^8: sums and weights then still fit, and O is rarely rescaled.
 //
@@ -26,7 +27,7 @@ namespace {
 constexpr int kTile = 128, kStep = 64;     // rows of a slot and tokens that are brought in at once; tokens of a step
 constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
 // Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
-constexpr int kSoftmaxRegs = 152, kMmaRegs = 88, kCopyRegs = 120;
+constexpr int kSoftmaxRegs = 152, kMmaRegs = 80, kCopyRegs = 128;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
 constexpr int kKept = 4;                   // steps whose masks and scales are kept
 constexpr unsigned long long kWaitNs = 4000000000ull, kDrainNs = 1000000000ull;
@@ -179,9 +180,9 @@ struct Bars {
   __device__ __forceinline__ uint32_t p_full(int slot, int half) const { return base + 96 + 16 * slot + 8 * half; }
   __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
   __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
-  __device__ __forceinline__ uint32_t drained() const { return base + 168; }
+  __device__ __forceinline__ uint32_t drained(int slot) const { return base + 168 + 8 * slot; }
 };
-constexpr int kBars = 22;
+constexpr int kBars = 23;
 
 template <typename T, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
@@ -215,14 +216,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   };
   const int steps[2] = {steps_of(0), steps_of(1)};
 
+  const int readers = !alternate && second ? 2 : 1;   // slots that read a tile
   const Bars bar{shared_address(bars)};
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       bar_init(bar.k_full(i), kCopyWarps * 32);
       bar_init(bar.v_full(i), kCopyWarps * 32);
-      bar_init(bar.k_empty(i), 1);
-      bar_init(bar.v_empty(i), 1);
+      bar_init(bar.drained(i), 1);
+      bar_init(bar.k_empty(i), readers);
+      bar_init(bar.v_empty(i), readers);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         bar_init(bar.s_full(i, half), 1);
@@ -230,7 +233,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         bar_init(bar.o_full(i, half), 1);
       }
     }
-    bar_init(bar.drained(), 1);
     bar_init(bar.q_full(), kSoftmaxWarps * 32);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -442,69 +444,68 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     fence_before();
   } else if (warp < kCopyWarp0) {
     give_registers<kMmaRegs>();
-    if (warp == kMmaWarp) {   // the whole warp goes along, one lane issues: addresses stay in uniform registers
+    const int slot = warp - kMmaWarp;
+    if (slot < 2 && steps[slot] > 0) {   // the whole warp goes along, one lane issues: addresses stay in uniform registers
       constexpr uint32_t kType = __is_same(T, __half) ? 0 : 1;
       constexpr uint32_t kIdS = instruction(kType, kStep, 0), kIdO = instruction(kType, HD, 1);
       const bool one = elect_one();
       const auto commit = [&](uint32_t b) {
         if (one) mma_commit(b);
       };
-      const auto scores = [&](int slot, int stage, int half) {
+      // Operands are made once; a step adds to the address in their lower half only (in units of 16 bytes).
+      const uint64_t q_op = operand(q_at, 0), k_op = operand(k_at, 0), v_op = operand(v_at, kTile * 128);
+      const uint64_t q = q_op + (alternate ? 0 : slot * (kTileBytes >> 4));
+      const uint32_t s_at = tmem + kColS + slot * kTile, o_at = tmem + kColO + slot * HD;
+      const auto scores = [&](int stage, int half) {
         if (!one) return;
+        const uint64_t k = k_op + stage * (kTileBytes >> 4) + half * (kStep * 128 >> 4);
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
-          mma_ss(tmem + kColS + slot * kTile + half * kStep, operand(q_at + (alternate ? 0 : slot * kTileBytes) + off, 0),
-                 operand(k_at + stage * kTileBytes + half * (kStep * 128) + off, 0), kIdS, k > 0);
+        for (int i = 0; i < HD / 16; ++i) {
+          const int off = ((i >> 2) * (kTile * 128) + (i & 3) * 32) >> 4;
+          mma_ss(s_at + half * kStep, q + off, k + off, kIdS, i > 0);
         }
       };
-      const auto values = [&](int slot, int stage, int half, bool add) {
+      const auto values = [&](int stage, int half, bool add) {
         if (!one) return;
+        const uint64_t v = v_op + stage * (kTileBytes >> 4) + half * (kStep * 128 >> 4);
 #pragma unroll
-        for (int k = 0; k < kStep / 16; ++k)
-          mma_ts(tmem + kColO + slot * HD, tmem + kColS + slot * kTile + half * kStep + k * 8,
-                 operand(v_at + stage * kTileBytes + half * (kStep * 128) + k * 2048, kTile * 128), kIdO, add || k > 0);
+        for (int i = 0; i < kStep / 16; ++i) mma_ts(o_at, s_at + half * kStep + i * 8, v + i * (2048 >> 4), kIdO, add || i > 0);
       };
       bool ok = bar_wait_warp(bar.q_full(), 0, abort);
-      const auto tile_of = [&](int s, int i) { return alternate ? 2 * (i >> 1) + s : i >> 1; };
-      // whether the products of slot s are a tile's last readers, at its last step
-      const auto last_reader = [&](int s, int i) { return (alternate || s == 1 || !second) && ((i & 1) || i + 1 == steps[s]); };
-      const auto start = [&](int s, int i) {   // S of step i
-        const int tile = tile_of(s, i), stage = tile & 1;
-        if ((alternate || s == 0) && !(i & 1)) {
+      const auto tile_of = [&](int i) { return alternate ? 2 * (i >> 1) + slot : i >> 1; };
+      const auto last_of_tile = [&](int i) { return (i & 1) || i + 1 == steps[slot]; };
+      const auto start = [&](int i) {   // S of step i
+        const int tile = tile_of(i), stage = tile & 1;
+        if (!(i & 1)) {
           ok = ok && bar_wait_warp(bar.k_full(stage), (tile >> 1) & 1, abort);
           if constexpr (!FP8) fence_async();
         }
         if (!ok) return;
         fence_after();
-        scores(s, stage, i & 1);
-        commit(bar.s_full(s, i & 1));
-        if (last_reader(s, i)) commit(bar.k_empty(stage));
+        scores(stage, i & 1);
+        commit(bar.s_full(slot, i & 1));
+        if (last_of_tile(i)) commit(bar.k_empty(stage));
       };
       for (int i = 0; i < 2; ++i)
-        for (int s = 0; s < 2; ++s)
-          if (i < steps[s] && ok) start(s, i);
-      for (int i = 0; i < steps[0] && ok; ++i) {
-        for (int s = 0; s < 2 && ok; ++s) {
-          if (i >= steps[s]) continue;
-          const int tile = tile_of(s, i), stage = tile & 1;
-          if ((alternate || s == 0) && !(i & 1)) {
-            ok = ok && bar_wait_warp(bar.v_full(stage), (tile >> 1) & 1, abort);
-            if constexpr (!FP8) fence_async();
-          }
-          ok = ok && bar_wait_warp(bar.p_full(s, i & 1), (i >> 1) & 1, abort);
-          if (!ok) break;
-          fence_after();
-          values(s, stage, i & 1, i > 0);
-          commit(bar.o_full(s, i & 1));
-          if (last_reader(s, i)) commit(bar.v_empty(stage));
-          if (i + 2 < steps[s]) start(s, i + 2);
+        if (i < steps[slot] && ok) start(i);
+      for (int i = 0; i < steps[slot] && ok; ++i) {
+        const int tile = tile_of(i), stage = tile & 1;
+        if (!(i & 1)) {
+          ok = bar_wait_warp(bar.v_full(stage), (tile >> 1) & 1, abort);
+          if constexpr (!FP8) fence_async();
         }
+        ok = ok && bar_wait_warp(bar.p_full(slot, i & 1), (i >> 1) & 1, abort);
+        if (!ok) break;
+        fence_after();
+        values(stage, i & 1, i > 0);
+        commit(bar.o_full(slot, i & 1));
+        if (last_of_tile(i)) commit(bar.v_empty(stage));
+        if (i + 2 < steps[slot]) start(i + 2);
       }
       if (!ok) {   // gave up: let the products in flight end before the tensor memory is given back
         int never = 0;
-        commit(bar.drained());
-        bar_wait(bar.drained(), 0, &never, kDrainNs);
+        commit(bar.drained(slot));
+        bar_wait(bar.drained(slot), 0, &never, kDrainNs);
       }
     }
     __syncwarp();

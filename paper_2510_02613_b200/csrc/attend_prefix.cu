@@ -181,8 +181,10 @@ struct Bars {
   __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
   __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
   __device__ __forceinline__ uint32_t drained(int slot) const { return base + 168 + 8 * slot; }
+  // a warp of a slot may make its exponentials: warps w of both slots share a quarter of the SM
+  __device__ __forceinline__ uint32_t turn(int slot, int w) const { return base + 184 + 32 * slot + 8 * w; }
 };
-constexpr int kBars = 23;
+constexpr int kBars = 31;
 
 template <typename T, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
@@ -224,6 +226,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       bar_init(bar.k_full(i), kCopyWarps * 32);
       bar_init(bar.v_full(i), kCopyWarps * 32);
       bar_init(bar.drained(i), 1);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) bar_init(bar.turn(i, w), 1);
       bar_init(bar.k_empty(i), readers);
       bar_init(bar.v_empty(i), readers);
 #pragma unroll
@@ -291,6 +295,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     for (int i = 0; i < steps[slot] && ok; ++i) {
       const int half = i & 1, tile = alternate ? 2 * (i >> 1) + slot : i >> 1;
       const uint32_t s_col = s_base + half * kStep;
+      // Exponentials of the two slots' warps that share a quarter of the SM take turns, 0 first: while one has
+      // them the other fetches its scores and finds their maximum.  Together they would both wait.
+      const bool both = steps[1] > 0 && (alternate ? 0 : kTile) + (warp & 3) * 32 < rows;   // the other has rows too
+      const bool wait_turn = both && (slot ? i < steps[0] : i > 0 && i - 1 < steps[1]);
+      const bool give_turn = both && (slot ? i + 1 < steps[0] : i < steps[1]);
       ok = bar_wait_warp(bar.s_full(slot, half), (i >> 1) & 1, abort);
       if (!ok) break;
       fence_after();
@@ -365,13 +374,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
             tmem_store_16(o_col + 16 * j, y);
           }
         }
-        const float safe = m == -CUDART_INF_F ? 0.f : m;
+        float safe = m == -CUDART_INF_F ? 0.f : m;
         float v_by = kMovedScale;
         if constexpr (FP8 && !kMoved<T, FP8>) v_by = v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
+        if (wait_turn) {
+          ok = bar_wait_warp(bar.turn(slot, warp & 3), (slot ? i : i - 1) & 1, abort);
+          if (!ok) break;
+          asm volatile("" : "+f"(safe));   // the exponentials stay behind this
+        }
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           uint32_t p[16];   // rounded once, as the second product's operand
+          if (j == 1 && give_turn && lane == 0) bar_arrive(bar.turn(1 - slot, warp & 3));
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             float &u = x[j][e], &v = x[j][e + 1];

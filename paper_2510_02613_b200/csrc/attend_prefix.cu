@@ -54,25 +54,24 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// False if the phase does not complete in time or another role has given up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit = kWaitNs) {
-  if (bar_try(bar, parity)) return true;
+// For whole warps: false, in every lane, if the phase does not complete in time or another role has given
+// up.  The lanes agree on each try, so that a wait that is over already costs one try and no divergence.
+// PATIENT: who has time sleeps between tries and leaves the issue slots to the others.
+template <bool PATIENT = false>
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit = kWaitNs) {
+  if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
   const unsigned long long t0 = now_ns();
   for (;;) {
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (bar_try(bar, parity)) return true;
-    if (*abort) return false;
-    if (now_ns() - t0 > limit) {
+    for (int i = 0; i < 64; ++i) {
+      if constexpr (PATIENT) __nanosleep(100);
+      if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    }
+    if (__any_sync(0xffffffffu, *abort != 0 || now_ns() - t0 > limit)) {
       *abort = 1;
       return false;
     }
   }
-}
-
-// For whole warps: the same answer in every lane, so that none goes on alone.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort) {
-  return __all_sync(0xffffffffu, bar_wait(bar, parity, abort));
 }
 
 // This thread's arrival once all its copies so far have landed.  (They are ordinary writes: who waits for
@@ -103,6 +102,7 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
@@ -170,6 +170,10 @@ __device__ __forceinline__ uint32_t piece_at(int r, int piece) {
   return (piece >> 3) * (kTile * 128) + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
 }
 
+// Which copying warp has a row of a tile, and which of its lanes finds it in the table.
+template <int ROWS> __device__ __forceinline__ constexpr int warp_of_row(int row) { return row / ROWS % kCopyWarps; }
+template <int ROWS> __device__ __forceinline__ constexpr int lane_of_row(int row) { return row / (ROWS * kCopyWarps) * ROWS + row % ROWS; }
+
 struct Bars {
   uint32_t base;
   __device__ __forceinline__ uint32_t k_full(int stage) const { return base + 8 * stage; }
@@ -190,11 +194,13 @@ template <typename T, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
   constexpr uint32_t kTileBytes = kTile * HD * 2;
   constexpr int kPieces = HD / 8;   // 16-byte pieces of a 16-bit row
+  // copying: a row's pieces are taken by kGroup neighbouring lanes, kRows rows at a time by a warp
+  constexpr int kGroup = FP8 ? HD / 16 : kPieces, kRows = 32 / kGroup;
   extern __shared__ uint8_t raw_smem[];
   __shared__ __align__(8) uint64_t bars[kBars];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
-  __shared__ __align__(16) uint8_t s_bad[kKept][kTile];             // tokens that nobody sees
+  __shared__ uint4 s_bad[kKept];   // tokens that nobody sees: a word of 32 rows from each copying warp
   __shared__ __align__(16) float s_scale[2][FP8 ? kKept : 1][FP8 ? kTile : 4];   // of K and V
   uint8_t *const smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   const uint32_t q_at = shared_address(smem), k_at = q_at + 2 * kTileBytes, v_at = k_at + 2 * kTileBytes;
@@ -223,8 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      bar_init(bar.k_full(i), kCopyWarps * 32);
-      bar_init(bar.v_full(i), kCopyWarps * 32);
+      bar_init(bar.k_full(i), kCopyWarps * (FP8 ? 1 : 32));
+      bar_init(bar.v_full(i), kCopyWarps * (FP8 ? 1 : 32));
       bar_init(bar.drained(i), 1);
 #pragma unroll
       for (int w = 0; w < 4; ++w) bar_init(bar.turn(i, w), 1);
@@ -233,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         bar_init(bar.s_full(i, half), 1);
-        bar_init(bar.p_full(i, half), 128);
+        bar_init(bar.p_full(i, half), 4);
         bar_init(bar.o_full(i, half), 1);
       }
     }
@@ -289,9 +295,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     }
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
     const uint32_t s_base = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
-    const float c = fabsf(a.scale_log2) * (kMoved<T, FP8> ? kMovedScale : 1.f);
+    // not zero: a masked score, minus infinity, has to stay that (and every other one comes to zero all the same)
+    const float c = fmaxf(fabsf(a.scale_log2), 0x1p-100f) * (kMoved<T, FP8> ? kMovedScale : 1.f);
     float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: f16 weights carry v's scale relative to the largest yet
     bool ok = true;
+    if (steps[slot] > 0) {   // the first step's scores
+      ok = bar_wait_warp(bar.s_full(slot, 0), 0, abort);
+      fence_after();
+      if (ok && busy) {
+        tmem_load(x[0], s_base);
+        tmem_load(x[1], s_base + 32);
+      }
+    }
     for (int i = 0; i < steps[slot] && ok; ++i) {
       const int half = i & 1, tile = alternate ? 2 * (i >> 1) + slot : i >> 1;
       const uint32_t s_col = s_base + half * kStep;
@@ -300,19 +315,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       const bool both = steps[1] > 0 && (alternate ? 0 : kTile) + (warp & 3) * 32 < rows;   // the other has rows too
       const bool wait_turn = both && (slot ? i < steps[0] : i > 0 && i - 1 < steps[1]);
       const bool give_turn = both && (slot ? i + 1 < steps[0] : i < steps[1]);
-      ok = bar_wait_warp(bar.s_full(slot, half), (i >> 1) & 1, abort);
-      if (!ok) break;
-      fence_after();
       if (busy) {
-        tmem_load(x[0], s_col);
-        tmem_load(x[1], s_col + 32);
-        const uint8_t *const bad = s_bad[tile % kKept] + half * kStep;
-        uint32_t any_bad = 0;
-#pragma unroll
-        for (int j = 0; j < kStep / 16; ++j) {
-          const uint4 b = ((const uint4 *)bad)[j];
-          any_bad |= b.x | b.y | b.z | b.w;
-        }
+        const uint4 bad = s_bad[tile % kKept];
+        const bool any_bad = (bad.x | bad.y | bad.z | bad.w) != 0;
         const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0] + half * kStep;
         const float *const v_scale = s_scale[1][FP8 ? tile % kKept : 0] + half * kStep;
         // the largest score, and in FP8 with f16 weights the largest scale of v
@@ -334,10 +339,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
               }
             }
           }
-          if (any_bad) {
+          if (__builtin_expect(any_bad, 0)) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (bad[32 * j + e]) x[j][e] = -CUDART_INF_F;
+            for (int e = 0; e < 32; ++e) {   // both halves' columns of a bit: a row is one lane of one warp
+              const int first = 32 * j + e, second = first + kStep;
+              if (word(bad, warp_of_row<kRows>(first)) >> (half ? lane_of_row<kRows>(second) : lane_of_row<kRows>(first)) & 1) x[j][e] = -CUDART_INF_F;
+            }
           }
           float t0 = x[j][0], t1 = x[j][1];
 #pragma unroll
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           tops[j] = fmaxf(t0, t1);
         }
         float top = fmaxf(tops[0], tops[1]);
-        if (top != -CUDART_INF_F) top *= c;
+        top *= c;
         const bool raise = i > 0 && (top > m + kRaise || v_top > v_ref);
         if (i == 0) {
           m = top;
@@ -390,14 +397,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             float &u = x[j][e], &v = x[j][e + 1];
-            fma_pair(u, v, c, c, -safe);   // a masked score stays minus infinity (c may be zero)
+            fma_pair(u, v, c, c, -safe);
             u = exp2_fast(u);
             v = exp2_fast(v);
-          }
-          if (any_bad) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (bad[32 * j + e]) x[j][e] = 0.f;
           }
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
@@ -419,10 +421,22 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           tmem_store_16(s_col + 16 * j, p);   // over columns that have been read
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_stored();
       }
+      // The next step's scores are on their way before this one's weights are waited for and announced.  (They
+      // were asked for a step ago; were they not done yet, their product does not need these weights.)
+      if (i + 1 < steps[slot]) {
+        ok = bar_wait_warp(bar.s_full(slot, half ^ 1), ((i + 1) >> 1) & 1, abort);
+        if (!ok) break;
+        fence_after();
+        if (busy) {
+          tmem_load(x[0], s_base + (half ^ 1) * kStep);
+          tmem_load(x[1], s_base + (half ^ 1) * kStep + 32);
+        }
+      }
+      if (busy) tmem_stored();
       fence_before();
-      bar_arrive(bar.p_full(slot, half));
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar.p_full(slot, half));   // one a warp: arrivals at one barrier go one by one
     }
     // the part of this range: maximum, sum and unnormalised output of every row
     // The last two products may be under way.  A parity tells one phase from the next only: each half has a
@@ -520,20 +534,24 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       if (!ok) {   // gave up: let the products in flight end before the tensor memory is given back
         int never = 0;
         commit(bar.drained(slot));
-        bar_wait(bar.drained(slot), 0, &never, kDrainNs);
+        bar_wait_warp<true>(bar.drained(slot), 0, &never, kDrainNs);
       }
     }
     __syncwarp();
   } else {
     give_registers<kCopyRegs>();
     const int w = warp - kCopyWarp0;
-    // A row's pieces are taken by kGroup neighbouring lanes; a warp has 32 rows of a tile, and each lane
-    // finds one of them in the table.
-    constexpr int kGroup = FP8 ? HD / 16 : kPieces, kRows = 32 / kGroup, kPasses = kTile / (kCopyWarps * kRows);
+    // A warp has 32 rows of a tile; each lane finds one of them in the table.
+    constexpr int kPasses = kTile / (kCopyWarps * kRows);
     static_assert(kRows * kPasses == 32, "a lane a row");
     const int piece = lane % kGroup;
     const auto row_of = [&](int pass, int r) { return pass * (kCopyWarps * kRows) + w * kRows + r; };
     const int my_row = row_of(lane / kRows, lane % kRows);
+    const auto mark = [&](int tile, bool bad) {
+      const uint32_t rows_of_warp = __ballot_sync(0xffffffffu, bad);
+      if (lane == 0) ((uint32_t *)&s_bad[tile % kKept])[w] = rows_of_warp;
+      __syncwarp();
+    };
     // this lane's token of a tile, -1 if there is none; its block; its vector index
     const auto token_of = [&](int tile) {
       const int t = t0 + tile * kTile + my_row;
@@ -560,9 +578,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         for (int u = 0; u < 4; ++u) {
           const int v = u >> 1, stage = u & 1, tile = first + stage;
           if (tile >= tiles || !ok) continue;
-          if (tile >= 2) ok = bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
           if (!ok) continue;
-          if (v == 0) s_bad[tile % kKept][my_row] = vec[stage] < 0;
+          if (v == 0) mark(tile, vec[stage] < 0);
           const uint8_t *const pool = v ? a.c.v : a.c.k;
           const uint32_t dst = (v ? v_at : k_at) + stage * kTileBytes;
 #pragma unroll
@@ -604,10 +622,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         for (int u = 0; u < 4; ++u) {
           const int v = u >> 1, stage = u & 1, tile = first + stage;
           if (tile >= tiles || !ok) continue;
-          if (tile >= 2) ok = bar_wait_warp(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
           if (!ok) continue;
           if (v == 0) {   // v's scales too: the softmax does not wait for the values
-            s_bad[tile % kKept][my_row] = vec[stage] < 0;
+            mark(tile, vec[stage] < 0);
             s_scale[0][tile % kKept][my_row] = vec[stage] < 0 ? 0.f : scale_of(byte[0][stage]);
             s_scale[1][tile % kKept][my_row] = vec[stage] < 0 ? 0.f : scale_of(byte[1][stage]);
           }
@@ -625,7 +643,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
             *(uint4 *)(dst + piece_at(r, 2 * piece + 1)) = hi;
           }
           fence_async();
-          bar_arrive(v ? bar.v_full(stage) : bar.k_full(stage));
+          __syncwarp();
+          if (lane == 0) bar_arrive(v ? bar.v_full(stage) : bar.k_full(stage));
           if (v == 0) {
             load(1, stage, vec[stage]);
           } else {

@@ -363,7 +363,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
   }
 }
 
-// Joins the splits of an output row: a warp a row, in the order of the splits.
+// Joins the splits of an output row: a warp a row, in the order of the splits.  A lane has a split's weight
+// (32 splits at a time); the parts are then read four at a time, without waiting for one another.
 template <typename T, int HD>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int N = HD / 32;
@@ -372,24 +373,52 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
   wait_for_previous();
   if (row >= (int64_t)a.n_seqs * a.q_len * a.n_q_heads) return;
   const int slots = a.prefix_splits + a.own_splits;
-  const float2 *ml = a.part_ml + row * slots;
+  const float2 *const ml = a.part_ml + row * slots;
   float m = -CUDART_INF_F;
   for (int i = lane; i < slots; i += 32) m = fmaxf(m, ml[i].x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  const float *const parts = a.part_o + row * slots * HD + lane * N;
   float l = 0.f, x[N] = {};
-  for (int i = 0; i < slots; ++i) {
-    const float2 p = ml[i];
-    if (p.y == 0.f) continue;
-    const float w = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
-    l += w * p.y;
-    const float *src = a.part_o + (row * slots + i) * HD + lane * N;
+  for (int first = 0; first < slots; first += 32) {
+    const int i = first + lane;
+    const float2 p = i < slots ? ml[i] : make_float2(-CUDART_INF_F, 0.f);
+    // an empty part (sum 0) is not read: nothing was written there
+    const float mine = p.y == 0.f ? 0.f : p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+    float sum = p.y == 0.f ? 0.f : mine * p.y;
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] += w * src[j];
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    l += sum;
+    const int here = min(32, slots - first);
+    for (int k = 0; k < here; k += 4) {
+      float w[4], y[4][N];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        w[u] = __shfl_sync(0xffffffffu, mine, (k + u) & 31);
+        if (k + u >= here) w[u] = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[u][j] = 0.f;
+        if (w[u] != 0.f) {
+          const float *const src = parts + (int64_t)(first + k + u) * HD;
+          if constexpr (N % 4 == 0) {
+#pragma unroll
+            for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
+          } else if constexpr (N == 2) {
+            *(float2 *)y[u] = *(const float2 *)src;
+          } else {
+            y[u][0] = src[0];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] += w[u] * y[u][j];
+    }
   }
   const float by = l == 0.f ? 0.f : 1.f / l;
   const int64_t token = row / a.n_q_heads;
-  T *dst = (T *)a.out + token * a.out_stride + (row - token * a.n_q_heads) * HD + lane * N;
+  T *const dst = (T *)a.out + token * a.out_stride + (row - token * a.n_q_heads) * HD + lane * N;
   if constexpr (N == 1) {
     *(uint16_t *)dst = (uint16_t)Pair<T>::pack(x[0] * by, 0.f);
   } else {
@@ -447,17 +476,18 @@ cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
 
 AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len) {
   AttendShape s{};
-  const int64_t want = 4 * kSms;   // items: two blocks an SM, twice over
   s.seq_rows = q_len * (n_q_heads / n_heads);
-  const auto cut = [&](int64_t tiles, int64_t tokens, int64_t least, int32_t &splits, int32_t &chunk) {
-    int64_t n = (want + tiles - 1) / tiles;
-    const int64_t most = (tokens + least - 1) / least;
-    n = n > most ? most : n;
-    n = n > 64 ? 64 : n < 1 ? 1 : n;
-    int64_t c = ((tokens + n - 1) / n + 63) / 64 * 64;   // whole steps of the four warps
-    c = c ? c : 64;
-    chunk = (int32_t)c;
-    splits = tokens ? (int32_t)((tokens + c - 1) / c) : 1;
+  // Items of `rows` row tiles over `tokens`: the number of splits with the least work one after the other, two
+  // blocks an SM, an item's start and end counting as 96 tokens.  Splits are whole steps of the four warps.
+  const auto cut = [&](int64_t tiles, int64_t tokens, int32_t &splits, int32_t &chunk) {
+    int64_t best = 64 * ((tokens + 63) / 64), cost = INT64_MAX;
+    for (int64_t n = 1; n <= 64 && (n == 1 || (n - 1) * 64 < tokens); ++n) {
+      const int64_t c = ((tokens + n - 1) / n + 63) / 64 * 64;
+      const int64_t t = ((tiles * n + 2 * kSms - 1) / (2 * kSms)) * (c + 96);
+      if (t < cost) cost = t, best = c;
+    }
+    chunk = (int32_t)(best ? best : 64);
+    splits = tokens ? (int32_t)((tokens + chunk - 1) / chunk) : 1;
   };
   const int64_t batch_rows = (int64_t)n_seqs * s.seq_rows;
   if (prefix_len > 0 && (head_dim == 64 || head_dim == 128) && batch_rows > 16) {
@@ -479,12 +509,12 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int 
     s.prefix_items = units * blocks;
   } else if (prefix_len > 0) {
     const int64_t tiles = (int64_t)n_heads * ((batch_rows + 15) / 16);
-    cut(tiles, prefix_len, 128, s.prefix_splits, s.prefix_chunk);
+    cut(tiles, prefix_len, s.prefix_splits, s.prefix_chunk);
     s.prefix_items = tiles * s.prefix_splits;
   }
   if (own_max > 0 || prefix_len == 0) {   // without any token there still is an (empty) item a row tile
     const int64_t tiles = (int64_t)n_heads * n_seqs * ((s.seq_rows + 15) / 16);
-    cut(tiles, own_max, 128, s.own_splits, s.own_chunk);
+    cut(tiles, own_max, s.own_splits, s.own_chunk);
     s.own_items = tiles * s.own_splits;
   }
   const int64_t rows = (int64_t)n_seqs * q_len * n_q_heads, slots = s.prefix_splits + s.own_splits;

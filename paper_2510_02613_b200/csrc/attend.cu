@@ -69,8 +69,9 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int 
 // item as the m side (rows that do not exist are zero), running maximum and sum in registers.  The
 // four warps take every fourth group of tokens and are joined at the end.  Bound by the reads of K
 // and V: 3 stages x 4 warps x 8 KB and two blocks an SM keep 128 KB in flight.
-template <typename T, int HD, bool FP8>
+template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+  using T = typename Operand<IO, FP8>::type;
   constexpr int ES = FP8 ? 1 : 2, CH = HD * ES / 16, kTile = kGroup * HD * ES, kStage = 2 * kTile;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint16_t s_scale[kWarps][kStages][kGroup];
@@ -90,26 +91,49 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 
   // query rows g and g + 8 of the tile as matrix operands, from global memory
   uint32_t q[HD / 16][4];
-  int limit[2];   // tokens that the row sees
+  int limit[2];      // tokens that the row sees
+  float by_row[2];   // scores to log2 weights
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int row = g + 8 * half;
     const bool real = row < it.rows;
     const int r = real ? it.row0 + row : 0;
     const int token = r / a.group;
-    const T *src = (const T *)a.q + ((int64_t)it.seq * a.q_len + token) * a.q_stride + (it.head * a.group + r - token * a.group) * HD;
+    const IO *src = (const IO *)a.q + ((int64_t)it.seq * a.q_len + token) * a.q_stride + (it.head * a.group + r - token * a.group) * HD;
     limit[half] = !real ? 0 : it.prefix ? it.t1 : own_length(a, it.seq) - a.q_len + token + 1;
+    by_row[half] = a.scale_log2;
 #pragma unroll
     for (int ks = 0; ks < HD / 16; ++ks) {
       if constexpr (!FP8) {
         const uint32_t *p = (const uint32_t *)(src + ks * 16 + 2 * c);
         q[ks][half] = real ? p[0] : 0;
         q[ks][2 + half] = real ? p[4] : 0;
-      } else {   // the order in which codes come out of a word: (0, 2), (1, 3)
+      } else {   // four neighbouring elements, as the codes of a word come
         const uint2 w = real ? *(const uint2 *)(src + (ks >> 1) * 32 + c * 8 + (ks & 1) * 4) : make_uint2(0, 0);
-        q[ks][half] = __byte_perm(w.x, w.y, 0x5410);
-        q[ks][2 + half] = __byte_perm(w.x, w.y, 0x7632);
+        q[ks][half] = w.x;
+        q[ks][2 + half] = w.y;
       }
+    }
+    if constexpr (FP8) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks)
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const float2 f = Pair<IO>::unpack(q[ks][half + k]);
+          top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+        }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float by = query_scale(top);
+      by_row[half] = a.scale_log2 / by;
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks)
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const float2 f = Pair<IO>::unpack(q[ks][half + k]);
+          q[ks][half + k] = Pair<T>::pack(f.x * by, f.y * by);
+        }
     }
   }
 
@@ -136,7 +160,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
   auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
     const uint32_t at = ring_at + (i % kStages) * kStage;
     held_valid = __ballot_sync(0xffffffffu, vec >= 0) & 0xffff;
-    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x7f7f;
+    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x007f;   // a token that is not there has no part in the largest scale of v
 #pragma unroll
     for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
       const int id = j * 32 + lane, row = id / CH, ch = id % CH;
@@ -154,6 +178,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     if (lane == 0) s_valid[warp][i % kStages] = held_valid;
   };
 
+  uint32_t v_ref = 0;   // e4m3: the largest scale byte of v so far, whose scale o is relative to
   float o[HD / 8][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) {
@@ -189,29 +214,38 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint2 w = *(const uint2 *)(ring + (i % kStages) * kStage + swizzled<CH>(j * 8 + g, kb * 2 + (c >> 1)) * 16 + (c & 1) * 8);
-          mma_16816<T>(s[j], q[2 * kb], even_codes<T>(w.x), odd_codes<T>(w.x));
-          mma_16816<T>(s[j], q[2 * kb + 1], even_codes<T>(w.y), odd_codes<T>(w.y));
+          uint32_t b[4];
+          codes_to_half(b[0], b[1], w.x);
+          codes_to_half(b[2], b[3], w.y);
+          mma_16816<T>(s[j], q[2 * kb], b[0], b[1]);
+          mma_16816<T>(s[j], q[2 * kb + 1], b[2], b[3]);
         }
     }
 
     const int base = it.t0 + (warp + kWarps * i) * kGroup;
-    float v_by[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
+    float v_by[2][2] = {{1.f, 1.f}, {1.f, 1.f}}, v_raise = 1.f;
+    if constexpr (FP8) {   // the largest scale of v so far (255 is not a number and not counted)
+      const uint32_t mine = s_scale[warp][i % kStages][lane & 15] >> 8;
+      const uint32_t largest = max(v_ref, __reduce_max_sync(0xffffffffu, mine == 255 ? 0 : mine));
+      v_raise = largest - v_ref < 127 ? __uint_as_float((127 - (largest - v_ref)) << 23) : 0.f;
+      v_ref = largest;
+    }
     float top[2] = {m[0], m[1]};
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int t = j * 8 + 2 * c + e;
-        float by = a.scale_log2;
+        float by = 1.f;
         if constexpr (FP8) {   // both scales are powers of two; 255 is not a number
-          const uint32_t b = s_scale[warp][i % kStages][t];
-          by *= scale_of(b & 255);
-          v_by[j][e] = scale_of(b >> 8);
+          const uint32_t b = s_scale[warp][i % kStages][t], v = b >> 8;
+          by = scale_of(b & 255);
+          v_by[j][e] = v == 255 ? CUDART_NAN_F : v_ref - v < 127 ? __uint_as_float((127 - (v_ref - v)) << 23) : 0.f;
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float &x = s[j][2 * half + e];
-          x = ((valid >> t) & 1) && base + t < limit[half] ? x * by : -CUDART_INF_F;
+          x = ((valid >> t) & 1) && base + t < limit[half] ? x * (FP8 ? by * by_row[half] : by_row[half]) : -CUDART_INF_F;
           top[half] = fmaxf(top[half], x);
         }
       }
@@ -220,8 +254,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     for (int half = 0; half < 2; ++half) {
       top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
       top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
-      const float safe = top[half] == -CUDART_INF_F ? 0.f : top[half];
-      alpha[half] = exp2_fast(m[half] - safe);
+      alpha[half] = exp2_fast(m[half] - (top[half] == -CUDART_INF_F ? 0.f : top[half]));
+      const float safe = top[half] == -CUDART_INF_F ? 0.f : top[half] - kWeightLift<T>;
       m[half] = top[half];
       float sum = 0.f;
 #pragma unroll
@@ -236,6 +270,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
         }
       l[half] = l[half] * alpha[half] + sum;
     }
+    alpha[0] *= v_raise;
+    alpha[1] *= v_raise;
     if (!__all_sync(0xffffffffu, alpha[0] == 1.f && alpha[1] == 1.f)) {
 #pragma unroll
       for (int n = 0; n < HD / 8; ++n) {
@@ -248,28 +284,39 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     // weights rounded to T, once, as the second product's operand: the result's own rounding is as large
     const uint32_t p[4] = {Pair<T>::pack(s[0][0], s[0][1]), Pair<T>::pack(s[0][2], s[0][3]),
                            Pair<T>::pack(s[1][0], s[1][1]), Pair<T>::pack(s[1][2], s[1][3])};
+    // Products of 16 columns of v from pieces read with ldmatrix: two column tiles of an e4m3 cache share
+    // 16-bit elements (two neighbouring columns) and are parted here.
+    auto product = [&](float (&d)[4], const uint32_t (&b)[4], int tile) {   // tile: of the 4 (e4m3) or 2 that b holds
+      if constexpr (FP8) {
+        uint32_t x[4];   // column, column + 1 of tokens 2c, 2c + 1; of tokens 2c + 8, 2c + 9
+        codes_to_half(x[0], x[1], __byte_perm(b[tile & 2], 0, 0x3120));
+        codes_to_half(x[2], x[3], __byte_perm(b[(tile & 2) + 1], 0, 0x3120));
+        mma_16816<T>(d, p, x[tile & 1], x[2 + (tile & 1)]);
+      } else {
+        mma_16816<T>(d, p, b[2 * tile], b[2 * tile + 1]);
+      }
+    };
+    constexpr int kTiles = FP8 ? 4 : 2, kReads = HD / 8 / kTiles;   // column tiles a read, reads
     // Query tokens of one sequence see different ends.  A value that some rows must not see may be
     // infinite or not a number, and a weight of zero does not silence it: such a step is done end by
-    // end, each row taking the pass of its own, with the values behind that end cleared.  (e4m3 codes
-    // are finite.)
+    // end, each row taking the pass of its own, with the values behind that end cleared.
     const int end = min(base + kGroup, it.t1);
-    const bool ragged = !FP8 && a.q_len > 1 &&
-                        __any_sync(0xffffffffu, (g < it.rows && limit[0] < end) || (g + 8 < it.rows && limit[1] < end));
+    const bool ragged = a.q_len > 1 && __any_sync(0xffffffffu, (g < it.rows && limit[0] < end) || (g + 8 < it.rows && limit[1] < end));
     if (ragged) {
       for (int stop = end; stop > base; --stop) {
         const bool now0 = min(limit[0], end) == stop, now1 = min(limit[1], end) == stop;
         if (__any_sync(0xffffffffu, now0 || now1)) {
 #pragma unroll
-          for (int n = 0; n < HD / 16; ++n) {
+          for (int n = 0; n < kReads; ++n) {
             uint32_t b[4];
             ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kTiles; ++k) {
               float part[4] = {};
-              mma_16816<T>(part, p, b[2 * k], b[2 * k + 1]);
+              product(part, b, k);
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (e < 2 ? now0 : now1) o[2 * n + k][e] += part[e];
+                if (e < 2 ? now0 : now1) o[kTiles * n + k][e] += part[e];
             }
           }
         }
@@ -278,23 +325,13 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
           *(uint4 *)(ring + (i % kStages) * kStage + kTile + swizzled<CH>(stop - 1 - base, ch) * 16) = make_uint4(0, 0, 0, 0);
         __syncwarp();
       }
-    } else if constexpr (!FP8) {
+    } else {
 #pragma unroll
-      for (int n = 0; n < HD / 16; ++n) {
+      for (int n = 0; n < kReads; ++n) {
         uint32_t b[4];
         ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
-        mma_16816<T>(o[2 * n], p, b[0], b[1]);
-        mma_16816<T>(o[2 * n + 1], p, b[2], b[3]);
-      }
-    } else {   // two neighbouring columns travel as one 16-bit element and are parted afterwards
 #pragma unroll
-      for (int n = 0; n < HD / 32; ++n) {
-        uint32_t b[4];
-        ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
-        mma_16816<T>(o[4 * n], p, even_codes<T>(b[0]), even_codes<T>(b[1]));
-        mma_16816<T>(o[4 * n + 1], p, odd_codes<T>(b[0]), odd_codes<T>(b[1]));
-        mma_16816<T>(o[4 * n + 2], p, even_codes<T>(b[2]), even_codes<T>(b[3]));
-        mma_16816<T>(o[4 * n + 3], p, odd_codes<T>(b[2]), odd_codes<T>(b[3]));
+        for (int k = 0; k < kTiles; ++k) product(o[kTiles * n + k], b, k);
       }
     }
     if (ahead < steps) keep(ahead);
@@ -308,7 +345,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
     l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
     if (c == 0) {
-      s_m[warp][g + 8 * half] = m[half];
+      s_m[warp][g + 8 * half] = m[half] - kWeightLift<T>;
       s_l[warp][g + 8 * half] = l[half];
     }
   }
@@ -320,7 +357,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * (e & 1) : n * 8 + 2 * c + (e & 1);
-      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n][e];
+      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = FP8 ? o[n][e] * scale_of(v_ref) : o[n][e];
     }
   __syncthreads();
   // the prefix's own kernel may still be running: the joining one waits for this one alone
@@ -351,8 +388,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     }
     if (last) {
       const int64_t token = orow / a.n_q_heads;
-      *(uint2 *)((T *)a.out + token * a.out_stride + (orow - token * a.n_q_heads) * HD + col) =
-          make_uint2(Pair<T>::pack(x.x * by, x.y * by), Pair<T>::pack(x.z * by, x.w * by));
+      *(uint2 *)((IO *)a.out + token * a.out_stride + (orow - token * a.n_q_heads) * HD + col) =
+          make_uint2(Pair<IO>::pack(x.x * by, x.y * by), Pair<IO>::pack(x.z * by, x.w * by));
     } else {
       *(float4 *)(a.part_o + (orow * slots + it.slot) * HD + col) = x;
     }

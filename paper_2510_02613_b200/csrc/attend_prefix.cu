@@ -190,9 +190,11 @@ struct Bars {
 };
 constexpr int kBars = 31;
 
-template <typename T, int HD, bool FP8>
+template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {
+  using T = typename Operand<IO, FP8>::type;
   constexpr uint32_t kTileBytes = kTile * HD * 2;
+  constexpr float kLift = kWeightLift<T> > 0.f ? kWeightLift<T> - kRaise : 0.f;
   constexpr int kPieces = HD / 8;   // 16-byte pieces of a 16-bit row
   // copying: a row's pieces are taken by kGroup neighbouring lanes, kRows rows at a time by a warp
   constexpr int kGroup = FP8 ? HD / 16 : kPieces, kRows = 32 / kGroup;
@@ -265,39 +267,46 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     const int row = alternate ? local : slot * kTile + local;
     const bool busy = (alternate ? 0 : slot * kTile) + (warp & 3) * 32 < rows;   // any real row in the warp
     float x[2][32];   // the row's query, then a step's scores and weights
+    // not zero: a masked score, minus infinity, has to stay that (and every other one comes to zero all the same)
+    float c = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
     {
-      // The row's query (two threads' work where both slots have the same rows): rows that do not exist are
-      // zero, a negative scale turns the sign.
+      // The row's query (stored by two threads, half each, where both slots have the same rows): rows that do
+      // not exist are zero, a negative scale turns the sign.
       uint4 *const w = (uint4 *)x;
-      const int first = alternate ? slot * (kPieces / 2) : 0;
       const int r = min(row, rows - 1), token = (row0 + r) / a.group;
-      const uint4 *const src = (const uint4 *)((const T *)a.q + (int64_t)token * a.q_stride + (head * a.group + row0 + r - token * a.group) * HD);
+      const uint4 *const src = (const uint4 *)((const IO *)a.q + (int64_t)token * a.q_stride + (head * a.group + row0 + r - token * a.group) * HD);
       const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-        if (i < kPieces / 2 || !alternate) w[i] = src[first + i];
+      for (int i = 0; i < kPieces; ++i) w[i] = row < rows ? src[i] : make_uint4(0, 0, 0, 0);
+      if constexpr (FP8) {
+        uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        if (i >= kPieces / 2 && alternate) break;
-        uint4 v = row < rows ? w[i] : make_uint4(0, 0, 0, 0);
-        if constexpr (kMoved<T, FP8>) {
-          const float2 e0 = Pair<T>::unpack(v.x), e1 = Pair<T>::unpack(v.y), e2 = Pair<T>::unpack(v.z), e3 = Pair<T>::unpack(v.w);
-          v.x = Pair<T>::pack(e0.x * kMovedScale, e1.x * kMovedScale);
-          v.y = Pair<T>::pack(e0.y * kMovedScale, e1.y * kMovedScale);
-          v.z = Pair<T>::pack(e2.x * kMovedScale, e3.x * kMovedScale);
-          v.w = Pair<T>::pack(e2.y * kMovedScale, e3.y * kMovedScale);
+        for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = Pair<IO>::unpack(word(w[i], k));
+            top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+          }
+        const float by = query_scale(top);
+        c = fmaxf(c / by, 0x1p-126f);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const float2 e0 = Pair<IO>::unpack(w[i].x), e1 = Pair<IO>::unpack(w[i].y), e2 = Pair<IO>::unpack(w[i].z), e3 = Pair<IO>::unpack(w[i].w);
+          w[i] = make_uint4(Pair<T>::pack(e0.x * by, e0.y * by), Pair<T>::pack(e1.x * by, e1.y * by), Pair<T>::pack(e2.x * by, e2.y * by),
+                            Pair<T>::pack(e3.x * by, e3.y * by));
         }
-        *(uint4 *)(smem + (alternate ? 0 : slot * kTileBytes) + piece_at(local, first + i)) =
-            make_uint4(v.x ^ sign, v.y ^ sign, v.z ^ sign, v.w ^ sign);
       }
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i)
+        if (!alternate || i / (kPieces / 2) == slot)
+          *(uint4 *)(smem + (alternate ? 0 : slot * kTileBytes) + piece_at(local, i)) =
+              make_uint4(w[i].x ^ sign, w[i].y ^ sign, w[i].z ^ sign, w[i].w ^ sign);
       fence_async();
       bar_arrive(bar.q_full());
     }
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
     const uint32_t s_base = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
-    // not zero: a masked score, minus infinity, has to stay that (and every other one comes to zero all the same)
-    const float c = fmaxf(fabsf(a.scale_log2), 0x1p-100f) * (kMoved<T, FP8> ? kMovedScale : 1.f);
-    float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: f16 weights carry v's scale relative to the largest yet
+    float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: the largest scale of v so far
     bool ok = true;
     if (steps[slot] > 0) {   // the first step's scores
       ok = bar_wait_warp(bar.s_full(slot, 0), 0, abort);
@@ -320,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         const bool any_bad = (bad.x | bad.y | bad.z | bad.w) != 0;
         const float *const k_scale = s_scale[0][FP8 ? tile % kKept : 0] + half * kStep;
         const float *const v_scale = s_scale[1][FP8 ? tile % kKept : 0] + half * kStep;
-        // the largest score, and in FP8 with f16 weights the largest scale of v
+        // the largest score, and of an e4m3 cache the largest scale of v
         float v_top = v_ref, tops[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -333,10 +342,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
               x[j][e + 1] *= k.y;
               x[j][e + 2] *= k.z;
               x[j][e + 3] *= k.w;
-              if constexpr (!kMoved<T, FP8>) {
-                const float4 v = *(const float4 *)(v_scale + 32 * j + e);
-                v_top = max3(max3(v_top, v.x, v.y), v.z, v.w);
-              }
+              const float4 v = *(const float4 *)(v_scale + 32 * j + e);
+              v_top = max3(max3(v_top, v.x, v.y), v.z, v.w);
             }
           }
           if (__builtin_expect(any_bad, 0)) {
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           const float to = top > m + kRaise ? top : m;
           float by = to == -CUDART_INF_F ? 1.f : exp2_fast(m - to);
           l *= by;
-          if constexpr (FP8 && !kMoved<T, FP8>) by *= v_top > 0.f ? v_ref / v_top : 1.f;
+          if constexpr (FP8) by *= v_top > 0.f ? v_ref / v_top : 1.f;
           m = to;
           v_ref = v_top;
 #pragma unroll 1
@@ -381,9 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
             tmem_store_16(o_col + 16 * j, y);
           }
         }
-        float safe = m == -CUDART_INF_F ? 0.f : m;
-        float v_by = kMovedScale;
-        if constexpr (FP8 && !kMoved<T, FP8>) v_by = v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
+        float safe = m == -CUDART_INF_F ? 0.f : m - kLift;
+        const float v_by = FP8 && v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
         if (wait_turn) {
           ok = bar_wait_warp(bar.turn(slot, warp & 3), (slot ? i : i - 1) & 1, abort);
           if (!ok) break;
@@ -448,11 +454,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     const int64_t part = row < rows ? output_row(a, 0, head, row0 + row) * slots + (alternate ? 2 * split + slot : split) : 0;
     if (busy && (alternate || slot == 0 || second)) {
       const bool empty = steps[slot] == 0 || !ok;
-      if (row < rows) a.part_ml[part] = empty ? make_float2(-CUDART_INF_F, 0.f) : make_float2(m, l);
+      if (row < rows) a.part_ml[part] = empty ? make_float2(-CUDART_INF_F, 0.f) : make_float2(m - kLift, l);
       if (!empty) {
-        float by = 1.f;
-        if constexpr (kMoved<T, FP8>) by = kMovedScale;
-        else if constexpr (FP8) by = v_ref;
+        const float by = FP8 ? v_ref : 1.f;
         float x[HD / 32][32];
 #pragma unroll
         for (int j = 0; j < HD / 32; ++j) tmem_load(x[j], o_col + 32 * j);
@@ -462,8 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           if (row < rows) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-              float4 y = make_float4(x[j][e] * by, x[j][e + 1] * by, x[j][e + 2] * by, x[j][e + 3] * by);
-              if constexpr (kMoved<T, FP8>) y = make_float4(y.x, y.z, y.y, y.w);
+              const float4 y = make_float4(x[j][e] * by, x[j][e + 1] * by, x[j][e + 2] * by, x[j][e + 3] * by);
               *(float4 *)(a.part_o + part * HD + 32 * j + e) = y;
             }
           }
@@ -635,10 +638,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
             const int r = row_of(pass, lane / kGroup);
             const uint4 x = raw[stage][pass];
             uint4 lo, hi;
-            word_of_codes<T>(lo.x, lo.y, x.x);
-            word_of_codes<T>(lo.z, lo.w, x.y);
-            word_of_codes<T>(hi.x, hi.y, x.z);
-            word_of_codes<T>(hi.z, hi.w, x.w);
+            codes_to_half(lo.x, lo.y, x.x);
+            codes_to_half(lo.z, lo.w, x.y);
+            codes_to_half(hi.x, hi.y, x.z);
+            codes_to_half(hi.z, hi.w, x.w);
             *(uint4 *)(dst + piece_at(r, 2 * piece)) = lo;
             *(uint4 *)(dst + piece_at(r, 2 * piece + 1)) = hi;
           }
@@ -665,14 +668,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   }
 }
 
-template <typename T, int HD, bool FP8>
+template <typename IO, int HD, bool FP8>
 cudaError_t launch(const AttendArgs &a, cudaStream_t st) {
   // queries, two stages of K and of V, room to align; never two blocks an SM (each takes all tensor memory)
   constexpr size_t need = 6 * (size_t)kTile * HD * 2 + 1024, least = 120 * 1024;
   constexpr size_t smem = need > least ? need : least;
-  const cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<T, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<IO, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  attend_prefix_kernel<T, HD, FP8><<<a.prefix_items, kThreads, smem, st>>>(a);
+  attend_prefix_kernel<IO, HD, FP8><<<a.prefix_items, kThreads, smem, st>>>(a);
   return cudaGetLastError();
 }
 

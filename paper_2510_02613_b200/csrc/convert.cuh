@@ -26,28 +26,6 @@ template <> struct Pair<__half> {
   static __device__ __forceinline__ float2 unpack(uint32_t x) { return __half22float2(*(const __half2 *)&x); }
 };
 
-// Two e4m3 codes in the upper bytes of the two halves of `x` (whatever is in the lower bytes) as a
-// pair of T, exactly.  bf16: the code's 7 magnitude bits, moved to the right place, are a bf16 whose
-// exponent is 120 too small (denormal codes become denormal bf16), so one packed product by 2^120
-// finishes it.  f16: likewise with 2^8.  The NaN code reads as 480; a vector that is not a number is
-// told by its scale.
-template <typename T> __device__ __forceinline__ uint32_t codes_to_pair(uint32_t x);
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__nv_bfloat16>(uint32_t x) {
-  const uint32_t y = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
-  const uint32_t big = 0x7b807b80u;  // 2^120 twice
-  const __nv_bfloat162 r = __hmul2(*(const __nv_bfloat162 *)&y, *(const __nv_bfloat162 *)&big);
-  return *(const uint32_t *)&r;
-}
-template <> __device__ __forceinline__ uint32_t codes_to_pair<__half>(uint32_t x) {
-  const uint32_t y = ((x >> 1) & 0x3f803f80u) | (x & 0x80008000u);
-  const uint32_t big = 0x5c005c00u;  // 2^8 twice
-  const __half2 r = __hmul2(*(const __half2 *)&y, *(const __half2 *)&big);
-  return *(const uint32_t *)&r;
-}
-// Bytes 0 and 2 of a word of four codes as a pair; bytes 1 and 3.
-template <typename T> __device__ __forceinline__ uint32_t even_codes(uint32_t w) { return codes_to_pair<T>(w << 8); }
-template <typename T> __device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return codes_to_pair<T>(w); }
-
 // e4m3 as bf16 operands without a product: a code's magnitude bits, moved to their place, are a bf16 2^120
 // too small (denormal where the code is), which the tensor cores take as it is.  The other operand
 // carries 2^60 of that and the sums the rest, so that neither side leaves its range.  A word's
@@ -65,6 +43,12 @@ __device__ __forceinline__ void word_of_codes(uint32_t &first, uint32_t &second,
     first = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
     second = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
   }
+}
+
+// Four codes as f16 pairs (0, 1) and (2, 3).
+__device__ __forceinline__ void codes_to_half(uint32_t &lo, uint32_t &hi, uint32_t w) {
+  asm("{\n\t.reg .b16 x, y;\n\tmov.b32 {x, y}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, x;\n\tcvt.rn.f16x2.e4m3x2 %1, y;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(w));
 }
 
 // d += a b: a 16 x 16 (rows), b 16 x 8 (columns), 32-bit sums.

@@ -68,8 +68,10 @@ def test_scores_that_raise_the_maximum_and_signs(kv, io):
             check(ref, c, q, pt, 795, None, None, io, scale=scale)
 
 
-def test_small_and_large_values_in_e4m3_with_f16():
-    """Scales of v from 2^-40 to 2^10 within one prefix: weights carry them relative to the largest yet."""
+@pytest.mark.parametrize("rows", [30, 4])
+def test_small_and_large_values_in_e4m3_with_f16(rows):
+    """Scales of v from 2^-40 to 2^10 within one prefix: weights carry them relative to the largest yet.
+    30 sequences: the tensor memory path, 4: the other."""
     rng = np.random.default_rng(6)
     ref = R.Cache(1, 40, 16, 1, 128, "e4m3")
     size = np.exp2(rng.integers(-30, 2, (1, 2, 40, 16, 1, 1)).astype(float))
@@ -81,7 +83,7 @@ def test_small_and_large_values_in_e4m3_with_f16():
     for cache in (ref, small):
         c, _, _ = device_cache(cache)
         pt = np.arange(40, dtype=np.int32)
-        q = torch.from_numpy(rng.standard_normal((30, 1, 2, 128))).to(torch.float16).cuda()
+        q = torch.from_numpy(rng.standard_normal((rows, 1, 2, 128))).to(torch.float16).cuda()
         # f16 outputs below its normal range are off by up to half its smallest step
         n, t, hq, hd = q.shape
         out = torch.empty_like(q)
@@ -177,3 +179,19 @@ def test_many_tiles_a_block(kv, hkv, seqs, prefix):
         outs.append(out)
         assert ((out[:, 0].double().view(o.shape) - o).abs() <= tol).all()
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("seqs", [30, 3])
+def test_queries_of_any_size_with_e4m3(seqs):
+    """Rows whose elements span 2^-100 to 2^100 (bf16), and zero rows: they are brought to f16 by a power of two each."""
+    rng = np.random.default_rng(11)
+    ref = filled(rng, (1, 30, 16, 1), 128, "e4m3", False)
+    ref.bytes[:, 0] = 127 - 9      # keys of about one
+    c, _, _ = device_cache(ref)
+    size = np.exp2(rng.integers(-100, 3, (seqs, 1, 4, 1)).astype(float))
+    q = rng.standard_normal((seqs, 1, 4, 128)) * size
+    q[0, 0, 0] = 0
+    q[1, 0, 1, 1:] *= 2.0 ** -60
+    check(ref, c, torch.from_numpy(q).to(torch.bfloat16).cuda(), np.arange(30, dtype=np.int32), 470, None, None, "bf16")
+    big = torch.from_numpy(rng.standard_normal((seqs, 1, 4, 128)) * 2.0 ** 100).to(torch.bfloat16).cuda()
+    check(ref, c, big, np.arange(30, dtype=np.int32), 470, None, None, "bf16", scale=2.0 ** -103)

@@ -941,7 +941,7 @@ emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *experts, uint64
  * ranks (a replicated one, routed or shared, is given to one rank's call).  Entries are
  * distinct where not negative.  The ranks' outputs are summed by the caller; out_type
  * EMOE_TYPE_F32 leaves that sum to be rounded once.
- * (e4m3 weights with BF16 tokens: a token's and a hidden vector's values have to be below 2^67.)
+ * (e4m3 weights with BF16 tokens: a hidden vector's values have to be below 2^67.)
  * Only the chosen experts' weights are read, each once for all tokens.  Sums are 32-bit; the
  * hidden vector w * silu(gate) * up is rounded once to io_type as the last product's operand
  * (beyond the range of F16: its largest value).  The result does not depend on timing.

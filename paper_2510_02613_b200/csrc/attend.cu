@@ -485,7 +485,7 @@ cudaError_t launch_rows(const AttendArgs &a, cudaStream_t st) {
   constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroup * HD * (FP8 ? 1 : 2);
   constexpr size_t join = (size_t)kWarps * 16 * (HD + 4) * 4;
   constexpr size_t smem = ring > join ? ring : join;
-  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = allow_shared<attend_rows_kernel<T, HD, FP8>>();
   if (e != cudaSuccess) return e;
   AttendArgs rest = a;
   if (a.tensor) rest.prefix_items = 0;

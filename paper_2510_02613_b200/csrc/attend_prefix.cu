@@ -673,7 +673,7 @@ cudaError_t launch(const AttendArgs &a, cudaStream_t st) {
   // queries, two stages of K and of V, room to align; never two blocks an SM (each takes all tensor memory)
   constexpr size_t need = 6 * (size_t)kTile * HD * 2 + 1024, least = 120 * 1024;
   constexpr size_t smem = need > least ? need : least;
-  const cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<IO, HD, FP8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = allow_shared<attend_prefix_kernel<IO, HD, FP8>>();
   if (e != cudaSuccess) return e;
   attend_prefix_kernel<IO, HD, FP8><<<a.prefix_items, kThreads, smem, st>>>(a);
   return cudaGetLastError();

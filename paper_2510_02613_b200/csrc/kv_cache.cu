@@ -115,31 +115,34 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const __grid_constant__ Ar
   uint8_t *const scale = blockIdx.y ? a.c.v_scale : a.c.k_scale;
   constexpr int kIn = bytes_of(IN), kCache = bytes_of(CACHE);
 
-  int64_t at[U];   // vector index in the pool; -1: nothing to do
+  // Slots first, and in an append the rows, which do not wait for them: a branch on a slot would.
+  int64_t slot[U], at[U];   // at: vector index in the pool; -1: nothing to do
+  uint32_t head[U];
   uint8_t *row[U];
   Raw<APPEND ? IN : CACHE> raw[U];
   uint32_t sb[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = first + u * group;
-    at[u] = -1;
-    if (i >= a.n_vec) continue;
-    const uint32_t token = i / (uint32_t)a.c.n_heads, head = i - token * a.c.n_heads;
-    const int64_t slot = a.slots[token];
-    row[u] = dense + token * stride + ((int64_t)head * a.c.head_dim + lane * 8) * kIn;
-    if (kv_slot_ok(a.c, slot))
-      at[u] = kv_vector(a.c, slot, head);
-    else if (slot >= 0 && a.c.status)
-      *a.c.status = EMOE_ERR_BLOCK_TABLE;
+    const uint32_t i = min(first + u * group, a.n_vec - 1), token = i / (uint32_t)a.c.n_heads;
+    head[u] = i - token * a.c.n_heads;
+    slot[u] = a.slots[token];
+    row[u] = dense + token * stride + ((int64_t)head[u] * a.c.head_dim + lane * 8) * kIn;
+    raw[u] = {};
+    if constexpr (APPEND) {
+      if (mine) raw[u] = *(const Raw<IN> *)row[u];
+    }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    raw[u] = {};
+    at[u] = -1;
     sb[u] = 127;
-    if (at[u] < 0) continue;
-    if constexpr (APPEND) {
-      if (mine) raw[u] = *(const Raw<IN> *)row[u];
-    } else {
+    if (first + u * group >= a.n_vec) continue;
+    if (kv_slot_ok(a.c, slot[u]))
+      at[u] = kv_vector(a.c, slot[u], head[u]);
+    else if (slot[u] >= 0 && a.c.status)
+      *a.c.status = EMOE_ERR_BLOCK_TABLE;
+    if constexpr (!APPEND) {
+      if (at[u] < 0) continue;
       if (mine) raw[u] = *(const Raw<CACHE> *)(pool + (at[u] * a.c.head_dim + lane * 8) * kCache);
       if constexpr (CACHE == EMOE_TYPE_E4M3) sb[u] = scale[at[u]];
     }

@@ -26,6 +26,14 @@ constexpr int kRouteThreads = 256, kUpWarps = 8;
 // Where element k of a token lies in the order that moved e4m3 operands want.
 __device__ __forceinline__ int moved_place(int k) { return (k & ~3) | (k & 1) << 1 | (k & 2) >> 1; }
 
+// The gate and up products of an e4m3 arena run on f16 operands whatever the type of x: cvt widens four
+// codes in two instructions (to bf16 it takes seven, on a pipe half as wide: 99 -> UPTIME us for 16 tokens of the
+// wide layer).  bf16 tokens are brought to f16 by the power of two that puts their largest element below 2^15 - exact
+// but for elements 2^29 times smaller, whose error is far below that of a 32-bit sum.  The hidden vectors'
+// largest element is not known when they are written, so the down product keeps them in bf16.
+template <typename IO, bool FP8> struct UpOperand { using type = IO; };
+template <typename IO> struct UpOperand<IO, true> { using type = __half; };
+
 // Logits as unsigned numbers in the same order; NaN counts as minus infinity, and minus infinity and
 // what has been chosen already as 0.
 __device__ __forceinline__ uint32_t ordered(float v) {
@@ -38,22 +46,36 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 
 // A block a token.  The first warp holds the token's logits in registers, N experts a lane; each
-// choice is a maximum over the lanes and then the smallest index that has it.  The other warps bring the
-// token into the order and scale that e4m3 products want.
+// choice is a maximum over the lanes and then the smallest index that has it.  The other warps bring a bf16
+// token to f16 where the weights are e4m3.
 template <int N, bool MOVED>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_constant__ MoeArgs a) {
   const int t = blockIdx.x, lane = threadIdx.x & 31;
   let_next_start();
   if (threadIdx.x >= 32) {
     if constexpr (MOVED) {
-      const __nv_bfloat16 *const x = (const __nv_bfloat16 *)a.x + t * a.x_stride;
-      uint2 *const to = (uint2 *)((__nv_bfloat16 *)a.moved_x + (int64_t)t * a.d_model);
-      for (int i = threadIdx.x - 32; i < a.d_model / 4; i += kRouteThreads - 32) {
-        const uint2 w = ((const uint2 *)x)[i];
-        const float2 p = Pair<__nv_bfloat16>::unpack(w.x), q = Pair<__nv_bfloat16>::unpack(w.y);
-        to[i] = make_uint2(Pair<__nv_bfloat16>::pack(p.x * kMovedScale, q.x * kMovedScale),
-                           Pair<__nv_bfloat16>::pack(p.y * kMovedScale, q.y * kMovedScale));
+      __shared__ uint32_t s_top[kRouteThreads / 32];
+      const uint2 *const x = (const uint2 *)((const __nv_bfloat16 *)a.x + t * a.x_stride);
+      uint2 *const to = (uint2 *)((__half *)a.moved_x + (int64_t)t * a.d_model);
+      constexpr int kThreads = kRouteThreads - 32;
+      uint32_t top = 0;   // two magnitudes a word compare as their bits do
+      for (int i = threadIdx.x - 32; i < a.d_model / 4; i += kThreads) {
+        const uint2 w = x[i];
+        top = __vmaxu2(top, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu));
       }
+      top = __reduce_max_sync(0xffffffffu, max(top >> 16, top & 0xffffu));
+      if (lane == 0) s_top[threadIdx.x >> 5] = top;
+      asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory");
+      for (int i = 1; i < kRouteThreads / 32; ++i) top = max(top, s_top[i]);
+      // 2^(14 - exponent); 1 for a zero token and one that is not finite
+      const uint32_t e = top >> 7;
+      const float by = top == 0 || e == 255 ? 1.f : __uint_as_float((uint32_t)min(254, 268 - max(1, (int)e)) << 23);
+      for (int i = threadIdx.x - 32; i < a.d_model / 4; i += kThreads) {
+        const uint2 w = x[i];
+        const float2 p = Pair<__nv_bfloat16>::unpack(w.x), q = Pair<__nv_bfloat16>::unpack(w.y);
+        to[i] = make_uint2(Pair<__half>::pack(p.x * by, p.y * by), Pair<__half>::pack(q.x * by, q.y * by));
+      }
+      if (threadIdx.x == 32) a.token_scale[t] = 1.f / by;
     }
     return;
   }
@@ -294,14 +316,16 @@ __device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP
   }
 }
 
-// h[pair] = w silu(gate) up, rounded once to T.  An item is 8 rows of gate and the same 8 of up as one
+// h[pair] = w silu(gate) up, rounded once to IO.  An item is 8 rows of gate and the same 8 of up as one
 // 16-row operand, so a thread gets both sums of its outputs.  The k axis is split over the warps,
 // joined in shared memory in the order of the warps.  NT: column tiles of 8 tokens an expert may have.
-template <typename T, bool FP8, int NT, int STAGES>
+template <typename IO, bool FP8, int NT, int STAGES>
 __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_part[2][kUpWarps][16][9];
   using S = Step<FP8>;
+  using T = typename UpOperand<IO, FP8>::type;
+  constexpr bool kScaled = !__is_same(T, IO);   // tokens in f16, by a power of two each
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   wait_for_previous();
   let_next_start();
@@ -315,8 +339,8 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
   // the step at which this lane's half leaves the row: only the last one can
   const int end0 = (a.d_model - c * S::kLane + S::kElems - 1) / S::kElems;
   const int end1 = (a.d_model - c * S::kLane - S::kHalf + S::kElems - 1) / S::kElems;
-  const uint8_t *const x_lane = (const uint8_t *)(kMoved<T, FP8> ? a.moved_x : a.x) + c * S::kLane * 2;
-  const int64_t x_stride = (kMoved<T, FP8> ? a.d_model : a.x_stride) * 2;
+  const uint8_t *const x_lane = (const uint8_t *)(kScaled ? a.moved_x : a.x) + c * S::kLane * 2;
+  const int64_t x_stride = (kScaled ? a.d_model : a.x_stride) * 2;
 
   Ring<FP8, STAGES> ring(smem);
   // the copies run ahead of the products over (item, step)
@@ -408,15 +432,16 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
         }
         if (n * 8 + j < count) {
           const int pair = e.y + n * 8 + j;
-          if constexpr (kMoved<T, FP8>) {
-            gate *= kMovedScale;
-            up *= kMovedScale;
+          if constexpr (kScaled) {
+            const float by = a.token_scale[routed.token[pair]];
+            gate *= by;
+            up *= by;
           }
           float h = gate / (1.f + expf(-gate)) * up * routed.weight[pair];
           // f16 ends at 65504: the largest value stands for what is beyond (bf16 reaches as far as 32 bits)
-          if constexpr (__is_same(T, __half)) h = h != h ? h : fminf(fmaxf(h, -65504.f), 65504.f);
+          if constexpr (__is_same(IO, __half)) h = h != h ? h : fminf(fmaxf(h, -65504.f), 65504.f);
           const int at = row0 + f;
-          ((T *)a.h)[(int64_t)pair * a.d_ff + (kMoved<T, FP8> ? moved_place(at) : at)] = T(kMoved<T, FP8> ? h * kMovedScale : h);
+          ((IO *)a.h)[(int64_t)pair * a.d_ff + (kMoved<IO, FP8> ? moved_place(at) : at)] = IO(kMoved<IO, FP8> ? h * kMovedScale : h);
         }
       }
     }
@@ -553,12 +578,10 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
   }
 }
 
-template <typename K>
-cudaError_t launch(K kernel, unsigned grid, int threads, size_t smem, bool early, const MoeArgs &a, cudaStream_t st) {
-  if (smem > 40 * 1024) {   // with the static part more than a launch may have unasked
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+template <auto KERNEL>
+cudaError_t launch(unsigned grid, int threads, size_t smem, bool early, const MoeArgs &a, cudaStream_t st) {
+  const cudaError_t e = allow_shared<KERNEL>();
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
@@ -569,7 +592,7 @@ cudaError_t launch(K kernel, unsigned grid, int threads, size_t smem, bool early
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+  return cudaLaunchKernelEx(&cfg, KERNEL, a);
 }
 
 size_t ring_bytes(size_t ring, const MoeArgs &a) {   // the ring's place also serves to group the choices
@@ -581,20 +604,20 @@ template <typename T, bool FP8, int NT, int STAGES, int WARPS>
 cudaError_t launch_down(MoeArgs a, bool f32_out, cudaStream_t st) {
   a.ring_bytes = (int32_t)ring_bytes((size_t)WARPS * STAGES * Step<FP8>::kBytes, a);
   const size_t smem = a.ring_bytes + (size_t)(WARPS * a.n_tokens * 17 + 1) / 2 * 8 + routed_bytes(a);
-  return f32_out ? launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, true>, a.d_model / 16, WARPS * 32, smem, true, a, st)
-                 : launch(moe_down_kernel<T, FP8, NT, STAGES, WARPS, false>, a.d_model / 16, WARPS * 32, smem, true, a, st);
+  return f32_out ? launch<moe_down_kernel<T, FP8, NT, STAGES, WARPS, true>>(a.d_model / 16, WARPS * 32, smem, true, a, st)
+                 : launch<moe_down_kernel<T, FP8, NT, STAGES, WARPS, false>>(a.d_model / 16, WARPS * 32, smem, true, a, st);
 }
 
 template <typename T, bool FP8, int NT>
 cudaError_t launch_layer(MoeArgs a, bool f32_out, cudaStream_t st) {
-  cudaError_t e = a.n_experts <= 256 ? launch(moe_route_kernel<8, kMoved<T, FP8>>, a.n_tokens, kRouteThreads, 0, false, a, st)
-                                     : launch(moe_route_kernel<32, kMoved<T, FP8>>, a.n_tokens, kRouteThreads, 0, false, a, st);
+  cudaError_t e = a.n_experts <= 256 ? launch<moe_route_kernel<8, kMoved<T, FP8>>>(a.n_tokens, kRouteThreads, 0, false, a, st)
+                                     : launch<moe_route_kernel<32, kMoved<T, FP8>>>(a.n_tokens, kRouteThreads, 0, false, a, st);
   if (e != cudaSuccess) return e;
   constexpr int kStages = FP8 ? 3 : 4;   // 96 KB: two blocks an SM
   const int64_t pairs = (int64_t)a.n_tokens * (a.top_k + a.n_shared);
   const int64_t most = (pairs < a.n_slots ? pairs : a.n_slots) * (a.d_ff / 8);
   a.ring_bytes = (int32_t)ring_bytes((size_t)kUpWarps * kStages * Step<FP8>::kBytes, a);
-  e = launch(moe_up_kernel<T, FP8, NT, kStages>, (unsigned)(most < 2 * kSms ? most : 2 * kSms), kUpWarps * 32,
+  e = launch<moe_up_kernel<T, FP8, NT, kStages>>((unsigned)(most < 2 * kSms ? most : 2 * kSms), kUpWarps * 32,
              a.ring_bytes + routed_bytes(a), true, a, st);
   if (e != cudaSuccess) return e;
   // Up to about one block an SM: 8 warps each; more: 4 warps, four blocks an SM, all of them at once.
@@ -616,7 +639,8 @@ MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared,
   MoeShape s{};
   const int64_t pairs = (int64_t)n_tokens * (top_k + n_shared);
   const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
-  s.moved_x = up(pairs * 8);   // the choices lie at the start
+  s.token_scale = up(pairs * 8);   // the choices lie at the start
+  s.moved_x = s.token_scale + (moved ? up(n_tokens * 4) : 0);
   s.h = s.moved_x + (moved ? up((int64_t)n_tokens * d_model * 2) : 0);
   s.bytes = s.h + up(pairs * d_ff * 2);
   return s;

@@ -335,6 +335,7 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   a.logits_stride = many ? p->logits_stride : p->n_experts;
   a.out_stride = many ? p->out_stride : e->d_model;
   a.choice = (int2 *)work;
+  a.token_scale = (float *)(work + s.token_scale);
   a.moved_x = work + s.moved_x;
   a.h = work + s.h;
   a.n_slots = e->n_slots;

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/emoe.h"
 
 namespace emoe {
@@ -67,10 +69,10 @@ struct AttendArgs {
 cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
-// Byte offsets of a layer call's workspace.  moved: e4m3 weights with bf16 tokens, which are kept in
-// another order and scale.
+// Byte offsets of a layer call's workspace.  moved: e4m3 weights, whose bf16 tokens are kept in f16 by a power
+// of two each.
 struct MoeShape {
-  int64_t moved_x, h, bytes;
+  int64_t token_scale, moved_x, h, bytes;
 };
 MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared, bool moved);
 
@@ -88,6 +90,7 @@ struct MoeArgs {
   int32_t *status;
   int64_t x_stride, logits_stride, out_stride;            // elements
   int2 *choice;                                           // workspace: [token][chosen] slot (-1: none) and weight
+  float *token_scale;
   void *moved_x;                                          // [token][d_model]
   void *h;                                                // [pair][d_ff]
   int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize;
@@ -95,6 +98,23 @@ struct MoeArgs {
   float routed_scale;
 };
 cudaError_t launch_moe(const MoeArgs &a, int type, int io, bool f32_out, cudaStream_t st);
+
+// Lets a kernel ask for all the dynamic shared memory there is; done once a device.
+template <auto KERNEL>
+cudaError_t allow_shared() {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  cudaFuncAttributes at;
+  e = cudaFuncGetAttributes(&at, KERNEL);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)at.sharedSizeBytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 constexpr int kSms = 148;  // streaming multiprocessors of a B200: launch shapes are made for it
 

@@ -25,19 +25,31 @@ def _type_of(name: str) -> int:
         raise ValueError("element type %r: one of %s" % (name, ", ".join(_TYPE_NAMES))) from None
 
 
+_types: dict = {}   # torch dtype -> type, filled as they come (their names are slow to make)
+
+
 def _value_type(t, what: str) -> int:
-    try:
-        return _TORCH_TYPES[str(t.dtype)]
-    except KeyError:
-        raise ValueError("%s: bfloat16, float16 or float32, not %s" % (what, t.dtype)) from None
+    code = _types.get(t.dtype)
+    if code is None:
+        code = _types[t.dtype] = _TORCH_TYPES.get(str(t.dtype), -1)
+    if code < 0:
+        raise ValueError("%s: bfloat16, float16 or float32, not %s" % (what, t.dtype))
+    return code
+
+
+_names: dict = {}   # torch dtype -> its name
 
 
 def _shaped(t, what: str, shape, dtype: Optional[str] = None, device=None):
     """t itself; ValueError unless it has this shape (None: any size), type and device."""
     if len(t.shape) != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
         raise ValueError("%s: shape %s, wanted %s" % (what, tuple(t.shape), tuple("any" if w is None else w for w in shape)))
-    if dtype is not None and str(t.dtype) != "torch." + dtype:
-        raise ValueError("%s: %s, wanted %s" % (what, t.dtype, dtype))
+    if dtype is not None:
+        name = _names.get(t.dtype)
+        if name is None:
+            name = _names[t.dtype] = str(t.dtype)[6:]
+        if name != dtype:
+            raise ValueError("%s: %s, wanted %s" % (what, name, dtype))
     if device is not None and t.device != device:
         raise ValueError("%s is on %s, the arena on %s" % (what, t.device, device))
     return t
@@ -45,6 +57,8 @@ def _shaped(t, what: str, shape, dtype: Optional[str] = None, device=None):
 
 def _dense(t, what: str, inner: int):
     """t itself; ValueError unless its last `inner` dimensions are densely packed."""
+    if t.is_contiguous():
+        return t
     step = 1
     for n, s in list(zip(t.shape, t.stride()))[:-inner - 1:-1]:
         if n != 1 and s != step:
@@ -91,6 +105,9 @@ class KvCache:
             self._c.status = status.data_ptr()
         self._keep = (arena, scales, status)
         self._ref = ctypes.byref(self._c)
+        self._row = n_heads * head_dim
+        L = _b.lib()
+        self._append, self._gather, self._attend = L.emoe_kv_append, L.emoe_kv_gather, L.emoe_kv_attend
 
     @classmethod
     def for_rank(cls, shape, tp: int, num_blocks: int, arena, kv_type: str = "bf16", **kw) -> "KvCache":
@@ -111,12 +128,16 @@ class KvCache:
         return _b.lib().emoe_kv_vector_index(self._ref, layer, kv, slot, head)
 
     def _rows(self, x, what, n):
-        _dense(_shaped(x, what, (n, self.n_heads, self.head_dim), None, self.device), what, 2)
-        return x.data_ptr(), (x.stride(0) if n > 1 else self.n_heads * self.head_dim)
+        if x.shape != (n, self.n_heads, self.head_dim) or (self.device is not None and x.device != self.device):
+            _shaped(x, what, (n, self.n_heads, self.head_dim), None, self.device)
+        if x.is_contiguous():
+            return x.data_ptr(), self._row
+        return _dense(x, what, 2).data_ptr(), (x.stride(0) if n > 1 else self._row)
 
     def _copy_args(self, k, v, slots):
-        n = slots.shape[0]
-        _dense(_shaped(slots, "slots", (None,), "int64", self.device), "slots", 1)
+        if not slots.is_contiguous():
+            raise ValueError("slots: not contiguous")
+        n = _shaped(slots, "slots", (None,), "int64", self.device).shape[0]
         (kp, ks), (vp, vs) = self._rows(k, "k", n), self._rows(v, "v", n)
         if k.dtype != v.dtype:
             raise ValueError("k is %s, v %s" % (k.dtype, v.dtype))
@@ -127,12 +148,12 @@ class KvCache:
         their slots (int64: block * block_tokens + offset; negative: skipped), quantising where the
         cache is e4m3."""
         n, kp, ks, vp, vs, t = self._copy_args(k, v, slots)
-        _check(_b.lib().emoe_kv_append(self._ref, layer, kp, vp, ks, vs, t, slots.data_ptr(), n, _stream_handle(stream)))
+        _check(self._append(self._ref, layer, kp, vp, ks, vs, t, slots.data_ptr(), n, _stream_handle(stream)))
 
     def gather(self, layer: int, slots, k, v, stream=None) -> None:
         """Reads slots back into k and v; rows of negative slots stay as they were."""
         n, kp, ks, vp, vs, t = self._copy_args(k, v, slots)
-        _check(_b.lib().emoe_kv_gather(self._ref, layer, slots.data_ptr(), n, kp, vp, ks, vs, t, _stream_handle(stream)))
+        _check(self._gather(self._ref, layer, slots.data_ptr(), n, kp, vp, ks, vs, t, _stream_handle(stream)))
 
     def attend_workspace_bytes(self, n_seqs: int, q_len: int, n_q_heads: int, max_blocks: int, prefix_len: int = 0) -> int:
         n = ctypes.c_uint64()
@@ -147,30 +168,33 @@ class KvCache:
         prefix_table, shared by all sequences.  workspace: attend_workspace_bytes bytes of the caller's,
         not shared by calls that can overlap.  lse: optional float32 [n_seqs, q_len, n_q_heads]."""
         n, t, hq, _ = q.shape
-        _shaped(q, "q", (None, None, None, self.head_dim), None, self.device)
-        _shaped(out, "out", q.shape, str(q.dtype)[6:], self.device)
-        p = _b._Attend(q=q.data_ptr(), out=out.data_ptr(), n_seqs=n, q_len=t, n_q_heads=hq, prefix_len=prefix_len,
-                       io_type=_value_type(q, "q"), scale=self.head_dim ** -0.5 if scale is None else scale)
-        for x, what, field in ((q, "q", "q_stride"), (out, "out", "out_stride")):
-            _dense(x, what, 2)
-            stride = x.stride(1) if t > 1 else x.stride(0) if n > 1 else hq * self.head_dim
-            if t > 1 and n > 1 and x.stride(0) != t * stride:
-                raise ValueError("%s: sequences have to follow one another at the stride of the tokens" % what)
-            setattr(p, field, stride)
+        _shaped(q, "q", (n, t, hq, self.head_dim), None, self.device)
+        if out.dtype != q.dtype:
+            raise ValueError("out is %s, q %s" % (out.dtype, q.dtype))
+        _shaped(out, "out", (n, t, hq, self.head_dim), None, self.device)
+        strides = [hq * self.head_dim] * 2
+        for i, (x, what) in enumerate(((q, "q"), (out, "out"))):
+            if not x.is_contiguous():
+                _dense(x, what, 2)
+                strides[i] = x.stride(1) if t > 1 else x.stride(0) if n > 1 else hq * self.head_dim
+                if t > 1 and n > 1 and x.stride(0) != t * strides[i]:
+                    raise ValueError("%s: sequences have to follow one another at the stride of the tokens" % what)
+        blocks, bt, ol, pt = 0, None, None, None
         if block_table is not None or own_lens is not None:
             _dense(_shaped(block_table, "block_table", (n, None), "int32", self.device), "block_table", 2)
             _dense(_shaped(own_lens, "own_lens", (n,), "int32", self.device), "own_lens", 1)
-            p.max_blocks, p.block_table, p.own_lens = block_table.shape[1], block_table.data_ptr(), own_lens.data_ptr()
+            blocks, bt, ol = block_table.shape[1], block_table.data_ptr(), own_lens.data_ptr()
         if prefix_len > 0:
             _dense(_shaped(prefix_table, "prefix_table", (None,), "int32", self.device), "prefix_table", 1)
             if prefix_table.shape[0] * self.block_tokens < prefix_len:
                 raise ValueError("prefix_table: %d blocks hold fewer than %d tokens" % (prefix_table.shape[0], prefix_len))
-            p.prefix_table = prefix_table.data_ptr()
-        if lse is not None:
-            p.lse = _dense(_shaped(lse, "lse", (n, t, hq), "float32", self.device), "lse", 3).data_ptr()
-        if workspace is not None:
-            p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _check(_b.lib().emoe_kv_attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
+            pt = prefix_table.data_ptr()
+        p = _b._Attend(q.data_ptr(), out.data_ptr(),
+                       None if lse is None else _dense(_shaped(lse, "lse", (n, t, hq), "float32", self.device), "lse", 3).data_ptr(),
+                       strides[0], strides[1], bt, ol, pt, None if workspace is None else workspace.data_ptr(),
+                       0 if workspace is None else workspace.numel() * workspace.element_size(), n, t, hq, blocks, prefix_len,
+                       _value_type(q, "q"), self.head_dim ** -0.5 if scale is None else scale, 0)
+        _check(self._attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
 
 
 class ExpertArena:
@@ -193,6 +217,7 @@ class ExpertArena:
             self._c.status = status.data_ptr()
         self._keep = (arena, status)
         self._ref = ctypes.byref(self._c)
+        self._decode = _b.lib().emoe_moe_decode
 
     @classmethod
     def for_rank(cls, shape, n_slots: int, arena, w_type: str = "bf16", **kw) -> "ExpertArena":
@@ -231,4 +256,4 @@ class ExpertArena:
                     0 if workspace is None else workspace.numel() * workspace.element_size(),
                     x.stride(0), logits.stride(0), out.stride(0), n, experts, n_shared, top_k,
                     _value_type(x, "x"), _value_type(out, "out"), 1 if renormalize else 0, routed_scale, 0)
-        _check(_b.lib().emoe_moe_decode(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
+        _check(self._decode(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))

@@ -231,6 +231,7 @@ struct Ring {
     copy_async_16(dst + 1024, lo + (n1 ? 64 : 0), n1);
     copy_async_16(dst + 1536, hi + (n1 ? 64 : 0), n1);
   }
+  // (Columns without a token are left as they are: they only make sums that nobody looks at.)
   __device__ __forceinline__ void fill_token(int stage, const uint8_t *tok, uint32_t n0, uint32_t n1) {
     const uint32_t dst = at + stage * S::kBytes + 2048;
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
   // the copies run ahead of the products over (item, step)
   int fill_item = k0 < k1 ? blockIdx.x : items, fill_k = k0, fill_stage = 0;
   const uint8_t *fill_lo = nullptr, *fill_hi = nullptr, *fill_tok = nullptr;
-  uint32_t fill_col = 0;
+  bool fill_col = false;
   auto enter = [&]() {
     if (fill_item >= items) return;
     const int i = fill_item / tiles, row = (fill_item - i * tiles) * 8 + g;
@@ -354,14 +355,14 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
     const int64_t at = e.x * a.gate_stride + row * row_bytes + c * 16 + k0 * 128;
     fill_lo = a.gate + at;
     fill_hi = a.up + at;
-    fill_col = g < routed.active[i + 1].y - e.y ? 16 : 0;
+    fill_col = g < routed.active[i + 1].y - e.y;
     fill_tok = x_lane + (fill_col ? routed.token[e.y + g] * x_stride : 0) + k0 * (S::kElems * 2);
   };
   auto fill = [&]() {
     if (fill_item < items) {
       const uint32_t n0 = fill_k < end0 ? 16 : 0, n1 = fill_k < end1 ? 16 : 0;
       ring.fill_weights(fill_stage, n0 ? fill_lo : a.gate, n0 ? fill_hi : a.gate, n0, n1);
-      ring.fill_token(fill_stage, n0 ? fill_tok : x_lane, n0 & fill_col, n1 & fill_col);
+      if (fill_col) ring.fill_token(fill_stage, n0 ? fill_tok : x_lane, n0, n1);
       fill_lo += 128;
       fill_hi += 128;
       fill_tok += S::kElems * 2;
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
     int step, expert, k, stage;
   } wf = {s0, s0 / steps, s0 % steps, 0}, tf = wf;
   const uint8_t *fill_w = nullptr, *fill_tok = nullptr;
-  uint32_t fill_col = 0;
+  bool fill_col = false;
   auto enter_weights = [&]() {
     if (wf.expert < routed.n_active)
       fill_w = a.down + routed.active[wf.expert].x * a.down_stride + (row0 + g) * row_bytes + c * 16 + wf.k * 128;
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
   auto enter_tokens = [&]() {
     if (tf.expert >= routed.n_active) return;
     const int first = routed.active[tf.expert].y;
-    fill_col = g < routed.active[tf.expert + 1].y - first ? 16 : 0;
+    fill_col = g < routed.active[tf.expert + 1].y - first;
     fill_tok = h_lane + (fill_col ? (int64_t)(first + g) * a.d_ff * 2 : 0) + tf.k * (S::kElems * 2);
   };
   auto next = [&](Cursor &cur, auto enter) {
@@ -509,7 +510,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
   auto fill_tokens = [&]() {
     if (tf.step < s1) {
       const uint32_t n0 = tf.k < end0 ? 16 : 0, n1 = tf.k < end1 ? 16 : 0;
-      ring.fill_token(tf.stage, n0 ? fill_tok : h_lane, n0 & fill_col, n1 & fill_col);
+      if (fill_col) ring.fill_token(tf.stage, n0 ? fill_tok : h_lane, n0, n1);
       fill_tok += S::kElems * 2;
       next(tf, enter_tokens);
     }

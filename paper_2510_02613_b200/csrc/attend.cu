@@ -400,69 +400,64 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
   }
 }
 
-// Joins the splits of an output row: a warp a row, in the order of the splits.  A lane has a split's weight
-// (32 splits at a time); the parts are then read four at a time, without waiting for one another.
+// Joins the splits of an output row: a block of four warps a row, each with every fourth group of four splits (read
+// without waiting for one another), joined in the order of the warps.
+constexpr int kJoinWarps = 4;
 template <typename T, int HD>
-__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int N = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  wait_for_previous();
-  if (row >= (int64_t)a.n_seqs * a.q_len * a.n_q_heads) return;
+  __shared__ float s_x[kJoinWarps][HD], s_l[kJoinWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = blockIdx.x;
   const int slots = a.prefix_splits + a.own_splits;
   const float2 *const ml = a.part_ml + row * slots;
+  const float *const parts = a.part_o + row * slots * HD + lane * N;
+  wait_for_previous();
   float m = -CUDART_INF_F;
   for (int i = lane; i < slots; i += 32) m = fmaxf(m, ml[i].x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  const float *const parts = a.part_o + row * slots * HD + lane * N;
   float l = 0.f, x[N] = {};
-  for (int first = 0; first < slots; first += 32) {
-    const int i = first + lane;
-    const float2 p = i < slots ? ml[i] : make_float2(-CUDART_INF_F, 0.f);
-    // an empty part (sum 0) is not read: nothing was written there
-    const float mine = p.y == 0.f ? 0.f : p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
-    float sum = p.y == 0.f ? 0.f : mine * p.y;
+  for (int first = warp * 4; first < slots; first += kJoinWarps * 4) {
+    float w[4], y[4][N];
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    l += sum;
-    const int here = min(32, slots - first);
-    for (int k = 0; k < here; k += 4) {
-      float w[4], y[4][N];
+    for (int u = 0; u < 4; ++u) {
+      const float2 p = first + u < slots ? ml[first + u] : make_float2(-CUDART_INF_F, 0.f);
+      // an empty part (sum 0) does not count: nothing was written there
+      w[u] = p.y == 0.f ? 0.f : p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+      l += p.y == 0.f ? 0.f : w[u] * p.y;
+      const float *const src = parts + (int64_t)min(first + u, slots - 1) * HD;
+      if constexpr (N % 4 == 0) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        w[u] = __shfl_sync(0xffffffffu, mine, (k + u) & 31);
-        if (k + u >= here) w[u] = 0.f;
-#pragma unroll
-        for (int j = 0; j < N; ++j) y[u][j] = 0.f;
-        if (w[u] != 0.f) {
-          const float *const src = parts + (int64_t)(first + k + u) * HD;
-          if constexpr (N % 4 == 0) {
-#pragma unroll
-            for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
-          } else if constexpr (N == 2) {
-            *(float2 *)y[u] = *(const float2 *)src;
-          } else {
-            y[u][0] = src[0];
-          }
-        }
+        for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
+      } else if constexpr (N == 2) {
+        *(float2 *)y[u] = *(const float2 *)src;
+      } else {
+        y[u][0] = src[0];
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] += w[u] * y[u][j];
     }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] += w[u] == 0.f ? 0.f : w[u] * y[u][j];
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) s_x[warp][lane * N + j] = x[j];
+  if (lane == 0) s_l[warp] = l;
+  __syncthreads();
+  if (threadIdx.x * 2 >= HD) return;
+  l = 0.f;
+  float u = 0.f, v = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWarps; ++w) {
+    l += s_l[w];
+    u += s_x[w][threadIdx.x * 2];
+    v += s_x[w][threadIdx.x * 2 + 1];
   }
   const float by = l == 0.f ? 0.f : 1.f / l;
   const int64_t token = row / a.n_q_heads;
-  T *const dst = (T *)a.out + token * a.out_stride + (row - token * a.n_q_heads) * HD + lane * N;
-  if constexpr (N == 1) {
-    *(uint16_t *)dst = (uint16_t)Pair<T>::pack(x[0] * by, 0.f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; j += 2) *(uint32_t *)(dst + j) = Pair<T>::pack(x[j] * by, x[j + 1] * by);
-  }
-  if (lane == 0) write_row(a, row, HD, m, l);
+  *(uint32_t *)((T *)a.out + token * a.out_stride + (row - token * a.n_q_heads) * HD + threadIdx.x * 2) = Pair<T>::pack(u * by, v * by);
+  if (threadIdx.x == 0) write_row(a, row, HD, m, l);
 }
 
 template <typename K>
@@ -495,7 +490,7 @@ cudaError_t launch_rows(const AttendArgs &a, cudaStream_t st) {
   }
   if (!a.tensor && a.prefix_splits + a.own_splits == 1) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.q_len * a.n_q_heads;
-  return launch_after(attend_join_kernel<T, HD>, dim3((unsigned)((rows + 3) / 4)), 128, 0, st, true, a);
+  return launch_after(attend_join_kernel<T, HD>, dim3((unsigned)rows), kJoinWarps * 32, 0, st, true, a);
 }
 
 template <typename T, bool FP8>
@@ -514,13 +509,14 @@ cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
 AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len) {
   AttendShape s{};
   s.seq_rows = q_len * (n_q_heads / n_heads);
-  // Items of `rows` row tiles over `tokens`: the number of splits with the least work one after the other, two
-  // blocks an SM, an item's start and end counting as 96 tokens.  Splits are whole steps of the four warps.
+  // Row tiles over up to `tokens` tokens (how many there really are is known on the device only): splits are whole
+  // steps of the four warps, as many as make the sum of all the work over two blocks an SM, an item's start and
+  // end counting as 96 tokens, and of the last item least.
   const auto cut = [&](int64_t tiles, int64_t tokens, int32_t &splits, int32_t &chunk) {
     int64_t best = 64 * ((tokens + 63) / 64), cost = INT64_MAX;
     for (int64_t n = 1; n <= 64 && (n == 1 || (n - 1) * 64 < tokens); ++n) {
       const int64_t c = ((tokens + n - 1) / n + 63) / 64 * 64;
-      const int64_t t = ((tiles * n + 2 * kSms - 1) / (2 * kSms)) * (c + 96);
+      const int64_t t = tiles * n * (c + 96) / (2 * kSms) + c;
       if (t < cost) cost = t, best = c;
     }
     chunk = (int32_t)(best ? best : 64);

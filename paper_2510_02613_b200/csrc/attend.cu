@@ -13,7 +13,9 @@
 namespace emoe {
 namespace {
 
-constexpr int kWarps = 4, kStages = 3, kGroup = 16;  // tokens of one warp's step
+constexpr int kWarps = 4, kStages = 2;
+// Tokens of one warp's step: the same bytes for both element sizes.
+template <bool FP8> constexpr int kGroupOf = FP8 ? 32 : 16;
 
 struct Item {
   bool prefix;
@@ -64,14 +66,15 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int 
   if (a.lse) a.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * CUDART_LN2_F : -CUDART_INF_F;
 }
 
-// One warp's step covers 16 tokens: K and V rows come through a ring of its own in shared memory
+// One warp's step covers 16 tokens (32 of an e4m3 cache): K and V rows come through a ring of its own in shared memory
 // (no block barrier in the loop), scores and products on the tensor cores with the 16 rows of the
 // item as the m side (rows that do not exist are zero), running maximum and sum in registers.  The
 // four warps take every fourth group of tokens and are joined at the end.  Bound by the reads of K
 // and V: 3 stages x 4 warps x 8 KB and two blocks an SM keep 128 KB in flight.
 template <typename IO, int HD, bool FP8>
-__global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   using T = typename Operand<IO, FP8>::type;
+  constexpr int kGroup = kGroupOf<FP8>;
   constexpr int ES = FP8 ? 1 : 2, CH = HD * ES / 16, kTile = kGroup * HD * ES, kStage = 2 * kTile;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint16_t s_scale[kWarps][kStages][kGroup];
@@ -88,6 +91,60 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
       a.part_ml[output_row(a, it.seq, it.head, it.row0 + threadIdx.x) * slots + it.slot] = make_float2(-CUDART_INF_F, 0.f);
     return;
   }
+
+  const int groups = it.t1 > it.t0 ? (it.t1 - it.t0 + kGroup - 1) / kGroup : 0;
+  const int steps = groups > warp ? (groups - warp + kWarps - 1) / kWarps : 0;
+  const int32_t *table = it.prefix ? a.prefix_table : a.block_table + (int64_t)it.seq * a.max_blocks;
+  uint8_t *const ring = smem + warp * (kStages * kStage);
+  const uint32_t ring_at = shared_address(ring);
+
+  // this lane's token of step i (lanes beyond a group's tokens repeat them), -1 if there is none; its block; its vector index
+  auto token_of = [&](int i) {
+    const int t = it.t0 + (warp + kWarps * i) * kGroup + (lane & (kGroup - 1));
+    return i >= steps || t >= it.t1 ? -1 : t;
+  };
+  auto block_of = [&](int i) {
+    const int t = token_of(i);
+    return t < 0 ? 0 : table[(uint32_t)t / (uint32_t)a.c.block_tokens];
+  };
+  auto vector_of = [&](int i, int block) {
+    const int t = token_of(i);
+    return t < 0 ? (int64_t)-1 : token_vector(a, block, t, it.head);
+  };
+  uint32_t held_scale = 0, held_valid = 0;
+  auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
+    const uint32_t at = ring_at + (i % kStages) * kStage;
+    held_valid = __ballot_sync(0xffffffffu, vec >= 0);
+    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x007f;   // a token that is not there has no part in the largest scale of v
+#pragma unroll
+    for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
+      const int id = j * 32 + lane, row = id / CH, ch = id % CH;
+      const int64_t v = __shfl_sync(0xffffffffu, vec, row & (kGroup - 1));
+      if (kGroup * CH % 32 == 0 || id < kGroup * CH) {
+        const int64_t src = v < 0 ? 0 : v * (HD * ES) + ch * 16;
+        const uint32_t dst = at + swizzled<CH>(row, ch) * 16;
+        copy_async_16(dst, a.c.k + src, v < 0 ? 0 : 16);
+        copy_async_16(dst + kTile, a.c.v + src, v < 0 ? 0 : 16);
+      }
+    }
+  };
+  auto keep = [&](int i) {   // what the issue of step i found, for its use
+    if (FP8) s_scale[warp][i % kStages][lane] = (uint16_t)held_scale;
+    if (lane == 0) s_valid[warp][i % kStages] = held_valid;
+  };
+
+  uint32_t v_ref = 0;   // e4m3: the largest scale byte of v so far, whose scale o is relative to
+  constexpr int kTileGroup = FP8 ? 4 : 2;   // column tiles that are read together
+  float o[HD / 8 / kTileGroup][kTileGroup][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (i < steps) {
+      issue(i, vector_of(i, block_of(i)));
+      keep(i);
+    }
+    copy_async_commit();
+  }
+  int block = block_of(kStages - 1);   // the table is read a step ahead
 
   // query rows g and g + 8 of the tile as matrix operands, from global memory
   uint32_t q[HD / 16][4];
@@ -137,58 +194,6 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     }
   }
 
-  const int groups = it.t1 > it.t0 ? (it.t1 - it.t0 + kGroup - 1) / kGroup : 0;
-  const int steps = groups > warp ? (groups - warp + kWarps - 1) / kWarps : 0;
-  const int32_t *table = it.prefix ? a.prefix_table : a.block_table + (int64_t)it.seq * a.max_blocks;
-  uint8_t *const ring = smem + warp * (kStages * kStage);
-  const uint32_t ring_at = shared_address(ring);
-
-  // this lane's token of step i (lanes 16.. repeat 0..15), -1 if there is none; its block; its vector index
-  auto token_of = [&](int i) {
-    const int t = it.t0 + (warp + kWarps * i) * kGroup + (lane & 15);
-    return i >= steps || t >= it.t1 ? -1 : t;
-  };
-  auto block_of = [&](int i) {
-    const int t = token_of(i);
-    return t < 0 ? 0 : table[(uint32_t)t / (uint32_t)a.c.block_tokens];
-  };
-  auto vector_of = [&](int i, int block) {
-    const int t = token_of(i);
-    return t < 0 ? (int64_t)-1 : token_vector(a, block, t, it.head);
-  };
-  uint32_t held_scale = 0, held_valid = 0;
-  auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
-    const uint32_t at = ring_at + (i % kStages) * kStage;
-    held_valid = __ballot_sync(0xffffffffu, vec >= 0) & 0xffff;
-    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x007f;   // a token that is not there has no part in the largest scale of v
-#pragma unroll
-    for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
-      const int id = j * 32 + lane, row = id / CH, ch = id % CH;
-      const int64_t v = __shfl_sync(0xffffffffu, vec, row & 15);
-      if (kGroup * CH % 32 == 0 || id < kGroup * CH) {
-        const int64_t src = v < 0 ? 0 : v * (HD * ES) + ch * 16;
-        const uint32_t dst = at + swizzled<CH>(row, ch) * 16;
-        copy_async_16(dst, a.c.k + src, v < 0 ? 0 : 16);
-        copy_async_16(dst + kTile, a.c.v + src, v < 0 ? 0 : 16);
-      }
-    }
-  };
-  auto keep = [&](int i) {   // what the issue of step i found, for its use
-    if (FP8 && lane < 16) s_scale[warp][i % kStages][lane] = (uint16_t)held_scale;
-    if (lane == 0) s_valid[warp][i % kStages] = held_valid;
-  };
-
-  uint32_t v_ref = 0;   // e4m3: the largest scale byte of v so far, whose scale o is relative to
-  float o[HD / 8][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    if (i < steps) {
-      issue(i, vector_of(i, block_of(i)));
-      keep(i);
-    }
-    copy_async_commit();
-  }
-  int block = block_of(kStages - 1);   // the table is read a step ahead
   for (int i = 0; i < steps; ++i) {
     const int ahead = i + kStages - 1;
     if (ahead < steps) issue(ahead, vector_of(ahead, block));
@@ -199,7 +204,8 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 
     const uint32_t k_at = ring_at + (i % kStages) * kStage, v_at = k_at + kTile;
     const uint32_t valid = s_valid[warp][i % kStages];
-    float s[2][4] = {};
+    constexpr int kN = kGroup / 8, kP = kGroup / 16;   // column tiles of the scores, k steps of the second product
+    float s[kN][4] = {};
     if constexpr (!FP8) {
 #pragma unroll
       for (int ks = 0; ks < HD / 16; ++ks) {
@@ -212,7 +218,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 #pragma unroll
       for (int kb = 0; kb < HD / 32; ++kb)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kN; ++j) {
           const uint2 w = *(const uint2 *)(ring + (i % kStages) * kStage + swizzled<CH>(j * 8 + g, kb * 2 + (c >> 1)) * 16 + (c & 1) * 8);
           uint32_t b[4];
           codes_to_half(b[0], b[1], w.x);
@@ -223,29 +229,33 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     }
 
     const int base = it.t0 + (warp + kWarps * i) * kGroup;
-    float v_by[2][2] = {{1.f, 1.f}, {1.f, 1.f}}, v_raise = 1.f;
-    if constexpr (FP8) {   // the largest scale of v so far (255 is not a number and not counted)
-      const uint32_t mine = s_scale[warp][i % kStages][lane & 15] >> 8;
+    float k_by[kN][2], v_by[kN][2], v_raise = 1.f;
+    if constexpr (FP8) {   // scales are powers of two; 255 is not a number and not counted in the largest of v so far
+      const uint32_t mine = s_scale[warp][i % kStages][lane] >> 8;
       const uint32_t largest = max(v_ref, __reduce_max_sync(0xffffffffu, mine == 255 ? 0 : mine));
       v_raise = largest - v_ref < 127 ? __uint_as_float((127 - (largest - v_ref)) << 23) : 0.f;
       v_ref = largest;
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const uint32_t two = *(const uint32_t *)&s_scale[warp][i % kStages][j * 8 + 2 * c];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t k = two >> (16 * e) & 255, v = two >> (16 * e + 8) & 255;
+          k_by[j][e] = scale_of(k);
+          v_by[j][e] = v == 255 ? CUDART_NAN_F : v_ref - v < 127 ? __uint_as_float((127 - (v_ref - v)) << 23) : 0.f;
+        }
+      }
     }
     float top[2] = {m[0], m[1]};
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < kN; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int t = j * 8 + 2 * c + e;
-        float by = 1.f;
-        if constexpr (FP8) {   // both scales are powers of two; 255 is not a number
-          const uint32_t b = s_scale[warp][i % kStages][t], v = b >> 8;
-          by = scale_of(b & 255);
-          v_by[j][e] = v == 255 ? CUDART_NAN_F : v_ref - v < 127 ? __uint_as_float((127 - (v_ref - v)) << 23) : 0.f;
-        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float &x = s[j][2 * half + e];
-          x = ((valid >> t) & 1) && base + t < limit[half] ? x * (FP8 ? by * by_row[half] : by_row[half]) : -CUDART_INF_F;
+          x = ((valid >> t) & 1) && base + t < limit[half] ? x * (FP8 ? k_by[j][e] * by_row[half] : by_row[half]) : -CUDART_INF_F;
           top[half] = fmaxf(top[half], x);
         }
       }
@@ -259,13 +269,13 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
       m[half] = top[half];
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < kN; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float &x = s[j][2 * half + e];
           x = exp2_fast(x - safe);
           sum += x;
-          // a masked token's v may be anything (its scale too): its weight is exactly zero
+          // a masked token's scale may be anything: its weight is exactly zero
           if constexpr (FP8) x = x == 0.f ? 0.f : x * v_by[j][e];
         }
       l[half] = l[half] * alpha[half] + sum;
@@ -275,28 +285,45 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
     if (!__all_sync(0xffffffffu, alpha[0] == 1.f && alpha[1] == 1.f)) {
 #pragma unroll
       for (int n = 0; n < HD / 8; ++n) {
-        o[n][0] *= alpha[0];
-        o[n][1] *= alpha[0];
-        o[n][2] *= alpha[1];
-        o[n][3] *= alpha[1];
+        float(&d)[4] = o[n / kTileGroup][n % kTileGroup];
+        d[0] *= alpha[0];
+        d[1] *= alpha[0];
+        d[2] *= alpha[1];
+        d[3] *= alpha[1];
       }
     }
     // weights rounded to T, once, as the second product's operand: the result's own rounding is as large
-    const uint32_t p[4] = {Pair<T>::pack(s[0][0], s[0][1]), Pair<T>::pack(s[0][2], s[0][3]),
-                           Pair<T>::pack(s[1][0], s[1][1]), Pair<T>::pack(s[1][2], s[1][3])};
-    // Products of 16 columns of v from pieces read with ldmatrix: two column tiles of an e4m3 cache share
-    // 16-bit elements (two neighbouring columns) and are parted here.
-    auto product = [&](float (&d)[4], const uint32_t (&b)[4], int tile) {   // tile: of the 4 (e4m3) or 2 that b holds
-      if constexpr (FP8) {
-        uint32_t x[4];   // column, column + 1 of tokens 2c, 2c + 1; of tokens 2c + 8, 2c + 9
-        codes_to_half(x[0], x[1], __byte_perm(b[tile & 2], 0, 0x3120));
-        codes_to_half(x[2], x[3], __byte_perm(b[(tile & 2) + 1], 0, 0x3120));
-        mma_16816<T>(d, p, x[tile & 1], x[2 + (tile & 1)]);
-      } else {
-        mma_16816<T>(d, p, b[2 * tile], b[2 * tile + 1]);
+    uint32_t p[kP][4];
+#pragma unroll
+    for (int k = 0; k < kP; ++k) {
+      p[k][0] = Pair<T>::pack(s[2 * k][0], s[2 * k][1]);
+      p[k][1] = Pair<T>::pack(s[2 * k][2], s[2 * k][3]);
+      p[k][2] = Pair<T>::pack(s[2 * k + 1][0], s[2 * k + 1][1]);
+      p[k][3] = Pair<T>::pack(s[2 * k + 1][2], s[2 * k + 1][3]);
+    }
+    // Products with the n-th 16 (e4m3: 32) columns of v, pieces read with ldmatrix: two column tiles of an e4m3
+    // cache share 16-bit elements (two neighbouring columns) and are parted here.
+    constexpr int kTiles = FP8 ? 4 : 2, kReads = HD / 8 / kTiles;   // column tiles a read, reads
+    auto products = [&](float (&d)[kTiles][4], int n) {
+#pragma unroll
+      for (int k = 0; k < kP; ++k) {
+        uint32_t b[4];
+        ldmatrix_x4_trans(b, v_at + swizzled<CH>(16 * k + (lane & 15), 2 * n + (lane >> 4)) * 16);
+        if constexpr (FP8) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t x[4];   // column, column + 1 of tokens 2c, 2c + 1; of tokens 2c + 8, 2c + 9
+            codes_to_half(x[0], x[1], __byte_perm(b[2 * t], 0, 0x3120));
+            codes_to_half(x[2], x[3], __byte_perm(b[2 * t + 1], 0, 0x3120));
+            mma_16816<T>(d[2 * t], p[k], x[0], x[2]);
+            mma_16816<T>(d[2 * t + 1], p[k], x[1], x[3]);
+          }
+        } else {
+          mma_16816<T>(d[0], p[k], b[0], b[1]);
+          mma_16816<T>(d[1], p[k], b[2], b[3]);
+        }
       }
     };
-    constexpr int kTiles = FP8 ? 4 : 2, kReads = HD / 8 / kTiles;   // column tiles a read, reads
     // Query tokens of one sequence see different ends.  A value that some rows must not see may be
     // infinite or not a number, and a weight of zero does not silence it: such a step is done end by
     // end, each row taking the pass of its own, with the values behind that end cleared.
@@ -308,16 +335,13 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
         if (__any_sync(0xffffffffu, now0 || now1)) {
 #pragma unroll
           for (int n = 0; n < kReads; ++n) {
-            uint32_t b[4];
-            ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
+            float part[kTiles][4] = {};
+            products(part, n);
 #pragma unroll
-            for (int k = 0; k < kTiles; ++k) {
-              float part[4] = {};
-              product(part, b, k);
+            for (int k = 0; k < kTiles; ++k)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (e < 2 ? now0 : now1) o[kTiles * n + k][e] += part[e];
-            }
+                if (e < 2 ? now0 : now1) o[n][k][e] += part[k][e];
           }
         }
         __syncwarp();
@@ -327,12 +351,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
       }
     } else {
 #pragma unroll
-      for (int n = 0; n < kReads; ++n) {
-        uint32_t b[4];
-        ldmatrix_x4_trans(b, v_at + swizzled<CH>(lane & 15, 2 * n + (lane >> 4)) * 16);
-#pragma unroll
-        for (int k = 0; k < kTiles; ++k) product(o[kTiles * n + k], b, k);
-      }
+      for (int n = 0; n < kReads; ++n) products(o[n], n);
     }
     if (ahead < steps) keep(ahead);
     __syncwarp();
@@ -357,7 +376,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_rows_kernel(const __grid_c
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * (e & 1) : n * 8 + 2 * c + (e & 1);
-      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = FP8 ? o[n][e] * scale_of(v_ref) : o[n][e];
+      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n / kTileGroup][n % kTileGroup][e] * (FP8 ? scale_of(v_ref) : 1.f);
     }
   __syncthreads();
   // the prefix's own kernel may still be running: the joining one waits for this one alone
@@ -477,7 +496,7 @@ cudaError_t launch_after(K kernel, dim3 grid, int threads, size_t smem, cudaStre
 
 template <typename T, int HD, bool FP8>
 cudaError_t launch_rows(const AttendArgs &a, cudaStream_t st) {
-  constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroup * HD * (FP8 ? 1 : 2);
+  constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroupOf<FP8> * HD * (FP8 ? 1 : 2);
   constexpr size_t join = (size_t)kWarps * 16 * (HD + 4) * 4;
   constexpr size_t smem = ring > join ? ring : join;
   cudaError_t e = allow_shared<attend_rows_kernel<T, HD, FP8>>();
@@ -506,20 +525,21 @@ cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len) {
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len) {
   AttendShape s{};
   s.seq_rows = q_len * (n_q_heads / n_heads);
+  const int64_t unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>);
   // Row tiles over up to `tokens` tokens (how many there really are is known on the device only): splits are whole
   // steps of the four warps, as many as make the sum of all the work over two blocks an SM, an item's start and
   // end counting as 96 tokens, and of the last item least.
   const auto cut = [&](int64_t tiles, int64_t tokens, int32_t &splits, int32_t &chunk) {
-    int64_t best = 64 * ((tokens + 63) / 64), cost = INT64_MAX;
-    for (int64_t n = 1; n <= 64 && (n == 1 || (n - 1) * 64 < tokens); ++n) {
-      const int64_t c = ((tokens + n - 1) / n + 63) / 64 * 64;
+    int64_t best = unit * ((tokens + unit - 1) / unit), cost = INT64_MAX;
+    for (int64_t n = 1; n <= 64 && (n == 1 || (n - 1) * unit < tokens); ++n) {
+      const int64_t c = ((tokens + n - 1) / n + unit - 1) / unit * unit;
       const int64_t t = tiles * n * (c + 96) / (2 * kSms) + c;
       if (t < cost) cost = t, best = c;
     }
-    chunk = (int32_t)(best ? best : 64);
+    chunk = (int32_t)(best ? best : unit);
     splits = tokens ? (int32_t)((tokens + chunk - 1) / chunk) : 1;
   };
   const int64_t batch_rows = (int64_t)n_seqs * s.seq_rows;

@@ -100,6 +100,8 @@ struct Args {
   int64_t k_stride, v_stride;  // bytes
   const int64_t *slots;
   uint32_t n_vec;            // n_tokens * n_heads
+  uint32_t n_tokens;
+  uint32_t step_tokens, step_heads;  // from one vector of a thread to its next
   uint32_t lanes;            // lanes per vector, a power of two >= head_dim / 8
 };
 
@@ -115,18 +117,27 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const __grid_constant__ Ar
   uint8_t *const scale = blockIdx.y ? a.c.v_scale : a.c.k_scale;
   constexpr int kIn = bytes_of(IN), kCache = bytes_of(CACHE);
 
-  // Slots first, and in an append the rows, which do not wait for them: a branch on a slot would.
+  // Slots first, and in an append the rows, which do not wait for them: a branch on a slot would.  One division a
+  // thread: from one of its vectors to the next it is a fixed number of tokens and heads.
   int64_t slot[U], at[U];   // at: vector index in the pool; -1: nothing to do
   uint32_t head[U];
   uint8_t *row[U];
   Raw<APPEND ? IN : CACHE> raw[U];
   uint32_t sb[U];
+  uint32_t token = first / (uint32_t)a.c.n_heads, h = first - token * a.c.n_heads;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t i = min(first + u * group, a.n_vec - 1), token = i / (uint32_t)a.c.n_heads;
-    head[u] = i - token * a.c.n_heads;
-    slot[u] = a.slots[token];
-    row[u] = dense + token * stride + ((int64_t)head[u] * a.c.head_dim + lane * 8) * kIn;
+    const bool there = first + u * group < a.n_vec;   // else the last vector once more, which nobody writes
+    const uint32_t t = there ? token : a.n_tokens - 1;
+    head[u] = there ? h : 0;
+    slot[u] = a.slots[t];
+    row[u] = dense + t * stride + (head[u] * a.c.head_dim + lane * 8) * kIn;
+    token += a.step_tokens;
+    h += a.step_heads;
+    if (h >= (uint32_t)a.c.n_heads) {
+      h -= a.c.n_heads;
+      ++token;
+    }
     raw[u] = {};
     if constexpr (APPEND) {
       if (mine) raw[u] = *(const Raw<IN> *)row[u];
@@ -157,16 +168,29 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const __grid_constant__ Ar
         unpack<IN>(raw[u], f);
         if constexpr (CACHE == EMOE_TYPE_E4M3) {
           uint32_t top = 0;   // magnitudes compare as their bits do, NaN above infinity
+          if constexpr (IN == EMOE_TYPE_F32) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+          } else {   // so do those of 16 bits, two at a time
+            const uint4 w = raw[u].x;
+            const uint32_t two = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+            top = max(two >> 16, two & 0xffffu);
+          }
           for (uint32_t m = a.lanes >> 1; m; m >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+          if constexpr (IN == EMOE_TYPE_BF16) top <<= 16;
+          if constexpr (IN == EMOE_TYPE_F16) top = __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
           const uint32_t byte = scale_byte(top);
           const float by = __uint_as_float((254u - byte) << 23);  // 2^-k: byte is 1 .. 247 here, or 255
+          Raw<CACHE> codes;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = byte == 255 ? 0.f : f[i] * by;
+          for (int i = 0; i < 8; ++i) f[i] *= by;
+          codes = pack<CACHE>(f);
+          if (byte == 255) codes = {};
+          if (at[u] >= 0 && mine) *(Raw<CACHE> *)(pool + (at[u] * a.c.head_dim + lane * 8) * kCache) = codes;
           if (at[u] >= 0 && lane == 0) scale[at[u]] = (uint8_t)byte;
         }
-        if (at[u] >= 0 && mine) *(Raw<CACHE> *)(pool + (at[u] * a.c.head_dim + lane * 8) * kCache) = pack<CACHE>(f);
+        if constexpr (CACHE != EMOE_TYPE_E4M3)
+          if (at[u] >= 0 && mine) *(Raw<CACHE> *)(pool + (at[u] * a.c.head_dim + lane * 8) * kCache) = pack<CACHE>(f);
       }
     } else {
       if (at[u] < 0 || !mine) continue;
@@ -225,6 +249,9 @@ Args make(const KvLayer &c, void *k, void *v, int64_t ks, int64_t vs, int io, co
   a.n_vec = (uint32_t)n * (uint32_t)c.n_heads;
   a.lanes = 1;
   while (a.lanes * 8 < (uint32_t)c.head_dim) a.lanes *= 2;
+  a.n_tokens = (uint32_t)n;
+  a.step_tokens = 256 / a.lanes / c.n_heads;
+  a.step_heads = 256 / a.lanes % c.n_heads;
   return a;
 }
 

@@ -195,7 +195,7 @@ emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *c, int32_t n_seqs,
   if (st != EMOE_OK) return st;
   *bytes = 0;
   if (n_seqs == 0) return EMOE_OK;
-  const AttendShape s = attend_shape(c->n_heads, n_seqs, q_len, n_q_heads, c->head_dim, (int64_t)max_blocks * c->block_tokens, prefix_len);
+  const AttendShape s = attend_shape(c->n_heads, n_seqs, q_len, n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3, (int64_t)max_blocks * c->block_tokens, prefix_len);
   *bytes = up_256(s.parts * sizeof(float2)) + up_256(s.parts * c->head_dim * sizeof(float));
   return EMOE_OK;
 }
@@ -217,7 +217,7 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
       !aligned(p->own_lens, 4) || !aligned(p->prefix_table, 4) || !aligned(p->workspace, 256))
     return EMOE_ERR_ALIGNMENT;
   if (tokens > 1 && (p->q_stride % 8 || p->out_stride % 8)) return EMOE_ERR_ALIGNMENT;
-  const AttendShape s = attend_shape(c->n_heads, p->n_seqs, p->q_len, p->n_q_heads, c->head_dim,
+  const AttendShape s = attend_shape(c->n_heads, p->n_seqs, p->q_len, p->n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
                                      (int64_t)p->max_blocks * c->block_tokens, p->prefix_len);
   const uint64_t ml = up_256(s.parts * sizeof(float2)), need = ml + up_256(s.parts * c->head_dim * sizeof(float));
   if (need && (!p->workspace || p->workspace_bytes < need)) return EMOE_ERR_INVALID_ARG;

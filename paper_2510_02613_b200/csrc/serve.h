@@ -48,7 +48,7 @@ struct AttendShape {
   int32_t alternate;                    // ... whose two slots take the same rows on alternating tiles of tokens
   int64_t parts;                        // (row, split) pairs that go through the workspace; 0: none
 };
-AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, int64_t own_max, int prefix_len);
+AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len);
 
 struct AttendArgs {
   KvLayer c;

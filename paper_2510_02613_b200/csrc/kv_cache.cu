@@ -107,7 +107,7 @@ struct Args {
 
 // U vectors a group of lanes: all loads are issued before the first is used.  blockIdx.y: K or V.
 template <int IN, int CACHE, int U, bool APPEND>
-__global__ void __launch_bounds__(256) kv_copy_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(256, 6) kv_copy_kernel(const __grid_constant__ Args a) {
   const uint32_t group = 256 / a.lanes, lane = threadIdx.x & (a.lanes - 1);
   const uint32_t first = blockIdx.x * (group * U) + threadIdx.x / a.lanes;
   const bool mine = lane * 8 < (uint32_t)a.c.head_dim;  // head_dim / 8 need not be a power of two

@@ -195,3 +195,22 @@ def test_queries_of_any_size_with_e4m3(seqs):
     check(ref, c, torch.from_numpy(q).to(torch.bfloat16).cuda(), np.arange(30, dtype=np.int32), 470, None, None, "bf16")
     big = torch.from_numpy(rng.standard_normal((seqs, 1, 4, 128)) * 2.0 ** 100).to(torch.bfloat16).cuda()
     check(ref, c, big, np.arange(30, dtype=np.int32), 470, None, None, "bf16", scale=2.0 ** -103)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    rng = np.random.default_rng(12)
+    ref = filled(rng, (1, 130, 16, 2), 128, "bf16", False)
+    c, _, _ = device_cache(ref)
+    pt, table = make_tables(rng, 130, 16, 1500, [30] * 10)
+    dev = [torch.from_numpy(x).cuda() for x in (table, np.full(10, 30, np.int32), pt)]
+    q = torch.from_numpy(rng.standard_normal((10, 1, 16, 128))).to(torch.bfloat16).cuda()
+    want = check(ref, c, q, pt, 1500, table, [30] * 10, "bf16")
+    streams, outs = [torch.cuda.Stream() for _ in range(3)], [torch.empty(20, *q.shape, dtype=q.dtype, device="cuda") for _ in range(3)]
+    works = [torch.empty(c.attend_workspace_bytes(10, 1, 16, table.shape[1], 1500), dtype=torch.uint8, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s in range(3):
+            c.attend(0, q, outs[s][i], dev[0], dev[1], dev[2], 1500, workspace=works[s], stream=streams[s])
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(x, want) for x in o)

@@ -22,13 +22,13 @@ namespace emoe {
 namespace {
 
 constexpr int kRouteThreads = 256, kUpWarps = 8;
+constexpr size_t kMaxShared = 226 * 1024;   // of 227 KB: a kernel's own variables have the rest
 
 // Where element k of a token lies in the order that moved e4m3 operands want.
 __device__ __forceinline__ int moved_place(int k) { return (k & ~3) | (k & 1) << 1 | (k & 2) >> 1; }
 
 // The gate and up products of an e4m3 arena run on f16 operands whatever the type of x: cvt widens four
-// codes in two instructions (to bf16 it takes seven, on a pipe half as wide: 99 -> UPTIME us for 16 tokens of the
-// wide layer).  bf16 tokens are brought to f16 by the power of two that puts their largest element below 2^15 - exact
+// codes in two instructions (to bf16 it takes seven, on a pipe half as wide).  bf16 tokens are brought to f16 by the power of two that puts their largest element below 2^15 - exact
 // but for elements 2^29 times smaller, whose error is far below that of a 32-bit sum.  The hidden vectors'
 // largest element is not known when they are written, so the down product keeps them in bf16.
 template <typename IO, bool FP8> struct UpOperand { using type = IO; };
@@ -138,6 +138,8 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const __grid_c
   a.choice[t * chosen + lane] = make_int2(slot < 0 ? -1 : slot, __float_as_int(w));
 }
 
+template <bool FP8, int NT> __device__ __forceinline__ int stages_of(int count);
+
 // The choices grouped by expert, built by each block for itself: (slot, first pair) of each expert in
 // use in the order of the slots, one more entry for the end, and each pair's token and weight, in the
 // order of the tokens.  `scratch` is free again afterwards.
@@ -196,6 +198,35 @@ struct Routed {
     }
     __syncthreads();
   }
+
+  // The step - of all experts' steps in a row - at which share `i` of `n` equal shares begins, equal in the
+  // stages that the steps take.
+  template <bool FP8, int NT>
+  __device__ __forceinline__ int share(int steps, int i, int n) const {
+    if constexpr (NT == 1) return (int)((int64_t)n_active * steps * i / n);
+    const int lane = threadIdx.x & 31;
+    int parts = 0;
+    for (int e = lane; e < n_active; e += 32) parts += stages_of<FP8, NT>(active[e + 1].y - active[e].y);
+    int64_t target = (int64_t)__reduce_add_sync(0xffffffffu, parts) * steps * i / n;
+    for (int first = 0; first < n_active; first += 32) {
+      const int e = first + lane, own = e < n_active ? stages_of<FP8, NT>(active[e + 1].y - active[e].y) : 0;
+      int sum = own;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += x;
+      }
+      // the first expert that ends beyond the target
+      const uint32_t beyond = __ballot_sync(0xffffffffu, (int64_t)sum * steps > target);
+      if (beyond) {
+        const int at = __ffs(beyond) - 1;
+        const int own_at = __shfl_sync(0xffffffffu, own, at), before = __shfl_sync(0xffffffffu, sum, at) - own_at;
+        return (first + at) * steps + (int)((target - (int64_t)before * steps) / own_at);
+      }
+      target -= (int64_t)__shfl_sync(0xffffffffu, sum, 31) * steps;
+    }
+    return n_active * steps;
+  }
 };
 size_t routed_bytes(const MoeArgs &a) {
   const int pairs = a.n_tokens * (a.top_k + a.n_shared);
@@ -211,6 +242,7 @@ template <bool FP8> struct Step {
   static constexpr int kES = FP8 ? 1 : 2, kElems = 128 / kES, kHalf = kElems / 2, kLane = 16 / kES;
   static constexpr int kTok = FP8 ? 2 : 1;              // 16-byte parts of a token a lane and half
   static constexpr int kBytes = (4 + 2 * kTok) * 512;   // of a warp's ring
+  static constexpr int kMore = FP8 ? 2 : 3;             // column tiles that a stage holds without weights
 };
 template <bool FP8> struct TokenPart { uint4 v[2 * Step<FP8>::kTok]; };
 
@@ -231,14 +263,19 @@ struct Ring {
     copy_async_16(dst + 1024, lo + (n1 ? 64 : 0), n1);
     copy_async_16(dst + 1536, hi + (n1 ? 64 : 0), n1);
   }
-  // (Columns without a token are left as they are: they only make sums that nobody looks at.)
-  __device__ __forceinline__ void fill_token(int stage, const uint8_t *tok, uint32_t n0, uint32_t n1) {
-    const uint32_t dst = at + stage * S::kBytes + 2048;
+  __device__ __forceinline__ void put(uint32_t dst, const uint8_t *tok, uint32_t n0, uint32_t n1) {
 #pragma unroll
     for (int i = 0; i < S::kTok; ++i) {
       copy_async_16(dst + i * 512, tok + i * 16, n0);
       copy_async_16(dst + (S::kTok + i) * 512, tok + (n1 ? S::kHalf * 2 : 0) + i * 16, n1);
     }
+  }
+  // (Columns without a token are left as they are: they only make sums that nobody looks at.)
+  __device__ __forceinline__ void fill_token(int stage, const uint8_t *tok, uint32_t n0, uint32_t n1) {
+    put(at + stage * S::kBytes + 2048, tok, n0, n1);
+  }
+  __device__ __forceinline__ void fill_more(int stage, int tile, const uint8_t *tok, uint32_t n0, uint32_t n1) {
+    put(at + stage * S::kBytes + tile * (S::kTok * 1024), tok, n0, n1);
   }
   __device__ __forceinline__ uint4 get(int stage, int i) const { return *(const uint4 *)(base + stage * S::kBytes + i * 512); }
 };
@@ -288,31 +325,54 @@ __device__ __forceinline__ void step_product(float (&acc)[4], const uint4 (&w)[4
   }
 }
 
-// The products of one step for all column tiles of an expert: the first tile's tokens lie in the ring,
-// the further ones (more than 8 tokens) are read from L2, two tiles at a time.  column(n): this lane's
-// token of tile n, null if there is none.
-template <typename T, bool FP8, int NT, int STAGES, typename F>
-__device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP8, STAGES> &ring, int stage, int count, int step,
-                                              bool in0, bool in1, float scale_lo, float scale_hi, F column) {
+// With e4m3 weights and up to 16 tokens the second tile's tokens are read straight from L2 ahead of the wait
+// for the step's weights: in a stage of the ring (three of 4 KB) they would halve the steps that the weights run
+// ahead (16 tokens, 14 experts of 7168 x 2048: 144 us, through the ring 159).  Everywhere else they come through the ring
+// (64 tokens, 126 bf16 experts of 2048 x 768: 189 us, straight from L2 207; 20 of 7168 x 2048, two of them with all
+// tokens: 341 and 527).
+template <bool FP8, int NT> constexpr bool kDirect = FP8 && NT == 2;
+
+// Stages that a step takes: its weights with the first 8 tokens, then the further column tiles, kMore at a time.
+template <bool FP8, int NT>
+__device__ __forceinline__ int stages_of(int count) {
+  if constexpr (NT == 1 || kDirect<FP8, NT>) return 1;
+  else return 1 + (max(count - 1, 0) / 8 + Step<FP8>::kMore - 1) / Step<FP8>::kMore;
+}
+
+// The products of one step for all column tiles of an expert.  fill() starts the copies of the stage that was
+// consumed last; second() reads this lane's token of the second tile.
+template <typename T, bool FP8, int NT, int STAGES, typename F, typename G>
+__device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP8, STAGES> &ring, int &stage, int count,
+                                              float scale_lo, float scale_hi, F fill, G second) {
   using S = Step<FP8>;
+  const auto next = [&]() { stage = stage + 1 == STAGES ? 0 : stage + 1; };
   uint4 w[4];
-  TokenPart<FP8> tok;
+  TokenPart<FP8> tok, tok2 = {};
+  if constexpr (kDirect<FP8, NT>)
+    if (count > 8) tok2 = second();
+  copy_async_wait<STAGES - 1>();
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = ring.get(stage, i);
 #pragma unroll
   for (int i = 0; i < 2 * S::kTok; ++i) tok.v[i] = ring.get(stage, 4 + i);
   step_product<T, FP8>(acc[0], w, tok, scale_lo, scale_hi);
-  if constexpr (NT > 1) {
-    if (count <= 8) return;
-    const int64_t off = (int64_t)step * (S::kElems * 2);
+  next();
+  if constexpr (kDirect<FP8, NT>) {
+    if (count > 8) step_product<T, FP8>(acc[1], w, tok2, scale_lo, scale_hi);
+  } else {
 #pragma unroll
-    for (int n = 1; n < NT; n += 2) {
+    for (int n = 1; n < NT; n += S::kMore) {
       if (n * 8 >= count) break;
-      const uint8_t *const p0 = column(n), *const p1 = n + 1 < NT ? column(n + 1) : nullptr;
-      const TokenPart<FP8> x0 = load_token<FP8>(p0 + off, p0 && in0, p0 && in1), x1 = load_token<FP8>(p1 + off, p1 && in0, p1 && in1);
-      step_product<T, FP8>(acc[n], w, x0, scale_lo, scale_hi);
-      if constexpr (NT > 2)
-        if (n + 1 < NT) step_product<T, FP8>(acc[n + 1 < NT ? n + 1 : n], w, x1, scale_lo, scale_hi);
+      fill();
+      copy_async_wait<STAGES - 1>();
+#pragma unroll
+      for (int m = 0; m < S::kMore; ++m) {
+        if (n + m >= NT || (n + m) * 8 >= count) break;
+#pragma unroll
+        for (int i = 0; i < 2 * S::kTok; ++i) tok.v[i] = ring.get(stage, m * (2 * S::kTok) + i);
+        step_product<T, FP8>(acc[n + m < NT ? n + m : 0], w, tok, scale_lo, scale_hi);
+      }
+      next();
     }
   }
 }
@@ -326,6 +386,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
   __shared__ float s_part[2][kUpWarps][16][9];
   using S = Step<FP8>;
   using T = typename UpOperand<IO, FP8>::type;
+  constexpr bool kOnePart = NT == 1 || kDirect<FP8, NT>;
   constexpr bool kScaled = !__is_same(T, IO);   // tokens in f16, by a power of two each
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   wait_for_previous();
@@ -345,7 +406,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
 
   Ring<FP8, STAGES> ring(smem);
   // the copies run ahead of the products over (item, step)
-  int fill_item = k0 < k1 ? blockIdx.x : items, fill_k = k0, fill_stage = 0;
+  int fill_item = k0 < k1 ? blockIdx.x : items, fill_k = k0, fill_part = 0, fill_parts = 1, fill_stage = 0;
   const uint8_t *fill_lo = nullptr, *fill_hi = nullptr, *fill_tok = nullptr;
   bool fill_col = false;
   auto enter = [&]() {
@@ -355,21 +416,36 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
     const int64_t at = e.x * a.gate_stride + row * row_bytes + c * 16 + k0 * 128;
     fill_lo = a.gate + at;
     fill_hi = a.up + at;
-    fill_col = g < routed.active[i + 1].y - e.y;
+    const int count = routed.active[i + 1].y - e.y;
+    fill_parts = stages_of<FP8, NT>(count);
+    fill_col = g < count;
     fill_tok = x_lane + (fill_col ? routed.token[e.y + g] * x_stride : 0) + k0 * (S::kElems * 2);
   };
   auto fill = [&]() {
     if (fill_item < items) {
       const uint32_t n0 = fill_k < end0 ? 16 : 0, n1 = fill_k < end1 ? 16 : 0;
-      ring.fill_weights(fill_stage, n0 ? fill_lo : a.gate, n0 ? fill_hi : a.gate, n0, n1);
-      if (fill_col) ring.fill_token(fill_stage, n0 ? fill_tok : x_lane, n0, n1);
-      fill_lo += 128;
-      fill_hi += 128;
-      fill_tok += S::kElems * 2;
-      if (++fill_k == k1) {
-        fill_k = k0;
-        fill_item += gridDim.x;
-        enter();
+      if (kOnePart || fill_part == 0) {
+        ring.fill_weights(fill_stage, n0 ? fill_lo : a.gate, n0 ? fill_hi : a.gate, n0, n1);
+        if (fill_col) ring.fill_token(fill_stage, n0 ? fill_tok : x_lane, n0, n1);
+      } else {
+        const int i = fill_item / tiles, first = routed.active[i].y, end = routed.active[i + 1].y;
+#pragma unroll
+        for (int m = 0; m < S::kMore; ++m) {
+          const int pair = first + (1 + (fill_part - 1) * S::kMore + m) * 8 + g;
+          if (pair < end)
+            ring.fill_more(fill_stage, m, x_lane + (n0 ? routed.token[pair] * x_stride + fill_k * (S::kElems * 2) : 0), n0, n1);
+        }
+      }
+      if (kOnePart || ++fill_part == fill_parts) {
+        fill_part = 0;
+        fill_lo += 128;
+        fill_hi += 128;
+        fill_tok += S::kElems * 2;
+        if (++fill_k == k1) {
+          fill_k = k0;
+          fill_item += gridDim.x;
+          enter();
+        }
       }
     }
     copy_async_commit();
@@ -384,9 +460,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
     const int2 e = routed.active[i];
     const int count = routed.active[i + 1].y - e.y;
     float acc[NT][4] = {};
-    const uint8_t *more[NT];   // this lane's column of the further tiles
-#pragma unroll
-    for (int n = 1; n < NT; ++n) more[n] = n * 8 + g < count ? x_lane + routed.token[e.y + n * 8 + g] * x_stride : nullptr;
+    const uint8_t *const second = 8 + g < count ? x_lane + routed.token[e.y + 8 + g] * x_stride : x_lane;
     const float *scale_g = nullptr, *scale_u = nullptr;
     float sg = 1.f, su = 1.f;
     if constexpr (FP8) {
@@ -407,9 +481,10 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
           next_u = scale_u[k + 1];
         }
       }
-      copy_async_wait<STAGES - 1>();
-      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, k, k < end0, k < end1, sg, su, [&](int n) { return more[n]; });
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, sg, su, fill, [&]() {
+        const bool in = 8 + g < count;
+        return load_token<FP8>(second + (int64_t)k * (S::kElems * 2), in && k < end0, in && k < end1);
+      });
       sg = next_g;
       su = next_u;
     }
@@ -453,11 +528,12 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
 // y for 16 output rows a block: the (expert, step) pairs of all experts in use are dealt to the
 // warps in equal runs.  At the end of its part of an expert a warp adds the expert's columns to its
 // own sums of the tokens in shared memory; the warps' sums are joined at the end, in their order.
-template <typename T, bool FP8, int NT, int STAGES, int WARPS, bool F32_OUT>
+template <typename T, bool FP8, int NT, int STAGES, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   using S = Step<FP8>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  constexpr bool kOnePart = NT == 1 || kDirect<FP8, NT>;
   const int row0 = blockIdx.x * 16;
   const int steps = (a.d_ff + S::kElems - 1) / S::kElems;
   const int64_t row_bytes = (int64_t)a.d_ff * S::kES;
@@ -470,49 +546,63 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
   // work: they can be read, and weights fetched, while the hidden vectors are still being made.
   Routed routed;
   routed.build(a, (uint8_t *)(sums + sum_count), smem);
-  const int total = routed.n_active * steps;   // at most 2048 experts x 16384 steps
-  const int s0 = (int)((int64_t)total * warp / WARPS), s1 = (int)((int64_t)total * (warp + 1) / WARPS);
+  // at most 2048 experts x 16384 steps
+  const int s0 = routed.template share<FP8, NT>(steps, warp, WARPS), s1 = routed.template share<FP8, NT>(steps, warp + 1, WARPS);
   const uint8_t *const h_lane = (const uint8_t *)a.h + c * S::kLane * 2;
 
   Ring<FP8, STAGES> ring(smem);
   struct Cursor {
-    int step, expert, k, stage;
-  } wf = {s0, s0 / steps, s0 % steps, 0}, tf = wf;
+    int step, expert, k, part, parts, stage;
+  } wf = {s0, s0 / steps, s0 % steps, 0, 1, 0}, tf = wf;
   const uint8_t *fill_w = nullptr, *fill_tok = nullptr;
   bool fill_col = false;
   auto enter_weights = [&]() {
-    if (wf.expert < routed.n_active)
-      fill_w = a.down + routed.active[wf.expert].x * a.down_stride + (row0 + g) * row_bytes + c * 16 + wf.k * 128;
+    if (wf.expert >= routed.n_active) return;
+    wf.parts = stages_of<FP8, NT>(routed.active[wf.expert + 1].y - routed.active[wf.expert].y);
+    fill_w = a.down + routed.active[wf.expert].x * a.down_stride + (row0 + g) * row_bytes + c * 16 + wf.k * 128;
   };
   auto enter_tokens = [&]() {
     if (tf.expert >= routed.n_active) return;
-    const int first = routed.active[tf.expert].y;
-    fill_col = g < routed.active[tf.expert + 1].y - first;
+    const int first = routed.active[tf.expert].y, count = routed.active[tf.expert + 1].y - first;
+    tf.parts = stages_of<FP8, NT>(count);
+    fill_col = g < count;
     fill_tok = h_lane + (fill_col ? (int64_t)(first + g) * a.d_ff * 2 : 0) + tf.k * (S::kElems * 2);
   };
-  auto next = [&](Cursor &cur, auto enter) {
+  auto next = [&](Cursor &cur, auto enter) {   // true: on to the next step
+    if (!kOnePart && ++cur.part < cur.parts) return false;
+    cur.part = 0;
     ++cur.step;
     if (++cur.k == steps) {
       cur.k = 0;
       ++cur.expert;
       enter();
+      return false;   // it has set the pointers itself
     }
+    return true;
   };
   auto fill_weights = [&]() {
     if (wf.step < s1) {
       const uint32_t n0 = wf.k < end0 ? 16 : 0, n1 = wf.k < end1 ? 16 : 0;
-      ring.fill_weights(wf.stage, n0 ? fill_w : a.down, n0 ? fill_w + 8 * row_bytes : a.down, n0, n1);
-      fill_w += 128;
-      next(wf, enter_weights);
+      if (kOnePart || wf.part == 0) ring.fill_weights(wf.stage, n0 ? fill_w : a.down, n0 ? fill_w + 8 * row_bytes : a.down, n0, n1);
+      if (next(wf, enter_weights)) fill_w += 128;
     }
     wf.stage = wf.stage + 1 == STAGES ? 0 : wf.stage + 1;
   };
   auto fill_tokens = [&]() {
     if (tf.step < s1) {
       const uint32_t n0 = tf.k < end0 ? 16 : 0, n1 = tf.k < end1 ? 16 : 0;
-      if (fill_col) ring.fill_token(tf.stage, n0 ? fill_tok : h_lane, n0, n1);
-      fill_tok += S::kElems * 2;
-      next(tf, enter_tokens);
+      if (kOnePart || tf.part == 0) {
+        if (fill_col) ring.fill_token(tf.stage, n0 ? fill_tok : h_lane, n0, n1);
+      } else {
+        const int first = routed.active[tf.expert].y, end = routed.active[tf.expert + 1].y;
+#pragma unroll
+        for (int m = 0; m < S::kMore; ++m) {
+          const int pair = first + (1 + (tf.part - 1) * S::kMore + m) * 8 + g;
+          if (pair < end)
+            ring.fill_more(tf.stage, m, h_lane + (n0 ? (int64_t)pair * a.d_ff * 2 + tf.k * (S::kElems * 2) : 0), n0, n1);
+        }
+      }
+      if (next(tf, enter_tokens)) fill_tok += S::kElems * 2;
     }
     copy_async_commit();
     tf.stage = tf.stage + 1 == STAGES ? 0 : tf.stage + 1;
@@ -529,6 +619,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
     const int count = routed.active[expert + 1].y - e.y;
     const int first = s - expert * steps, last = min(steps, s1 - expert * steps);
     s += last - first;
+    const uint8_t *const second = h_lane + (8 + g < count ? (int64_t)(e.y + 8 + g) * a.d_ff * 2 : 0);
     const float *scale = nullptr;
     float by = 1.f;
     if constexpr (FP8) {
@@ -543,11 +634,13 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
       if constexpr (FP8) {
         if (k + 1 < last) later = scale[k + 1];
       }
-      copy_async_wait<STAGES - 1>();
-      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, k, k < end0, k < end1, by, by, [&](int n) {
-        return n * 8 + g < count ? h_lane + (int64_t)(e.y + n * 8 + g) * a.d_ff * 2 : nullptr;
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, by, by, [&]() {
+        fill_weights();
+        fill_tokens();
+      }, [&]() {
+        const bool in = 8 + g < count;
+        return load_token<FP8>(second + (int64_t)k * (S::kElems * 2), in && k < end0, in && k < end1);
       });
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
       by = later;
     }
     float *const mine = sums + warp * a.n_tokens * 17;
@@ -574,7 +667,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) y += sums[(w * a.n_tokens + t) * 17 + r];
     if constexpr (kMoved<T, FP8>) y *= kMovedScale;
-    if constexpr (F32_OUT) ((float *)a.out)[t * a.out_stride + row0 + r] = y;
+    if (a.out_f32) ((float *)a.out)[t * a.out_stride + row0 + r] = y;
     else ((T *)a.out)[t * a.out_stride + row0 + r] = T(y);
   }
 }
@@ -601,16 +694,19 @@ size_t ring_bytes(size_t ring, const MoeArgs &a) {   // the ring's place also se
   return (n + 127) / 128 * 128;
 }
 
+template <bool FP8, int STAGES, int WARPS>
+size_t down_bytes(const MoeArgs &a) {
+  return ring_bytes((size_t)WARPS * STAGES * Step<FP8>::kBytes, a) + (size_t)(WARPS * a.n_tokens * 17 + 1) / 2 * 8 + routed_bytes(a);
+}
+
 template <typename T, bool FP8, int NT, int STAGES, int WARPS>
-cudaError_t launch_down(MoeArgs a, bool f32_out, cudaStream_t st) {
+cudaError_t launch_down(MoeArgs a, cudaStream_t st) {
   a.ring_bytes = (int32_t)ring_bytes((size_t)WARPS * STAGES * Step<FP8>::kBytes, a);
-  const size_t smem = a.ring_bytes + (size_t)(WARPS * a.n_tokens * 17 + 1) / 2 * 8 + routed_bytes(a);
-  return f32_out ? launch<moe_down_kernel<T, FP8, NT, STAGES, WARPS, true>>(a.d_model / 16, WARPS * 32, smem, true, a, st)
-                 : launch<moe_down_kernel<T, FP8, NT, STAGES, WARPS, false>>(a.d_model / 16, WARPS * 32, smem, true, a, st);
+  return launch<moe_down_kernel<T, FP8, NT, STAGES, WARPS>>(a.d_model / 16, WARPS * 32, down_bytes<FP8, STAGES, WARPS>(a), true, a, st);
 }
 
 template <typename T, bool FP8, int NT>
-cudaError_t launch_layer(MoeArgs a, bool f32_out, cudaStream_t st) {
+cudaError_t launch_layer(MoeArgs a, cudaStream_t st) {
   cudaError_t e = a.n_experts <= 256 ? launch<moe_route_kernel<8, kMoved<T, FP8>>>(a.n_tokens, kRouteThreads, 0, false, a, st)
                                      : launch<moe_route_kernel<32, kMoved<T, FP8>>>(a.n_tokens, kRouteThreads, 0, false, a, st);
   if (e != cudaSuccess) return e;
@@ -621,17 +717,25 @@ cudaError_t launch_layer(MoeArgs a, bool f32_out, cudaStream_t st) {
   e = launch<moe_up_kernel<T, FP8, NT, kStages>>((unsigned)(most < 2 * kSms ? most : 2 * kSms), kUpWarps * 32,
              a.ring_bytes + routed_bytes(a), true, a, st);
   if (e != cudaSuccess) return e;
-  // Up to about one block an SM: 8 warps each; more: 4 warps, four blocks an SM, all of them at once.
-  if (a.d_model / 16 <= kSms) return launch_down<T, FP8, NT, FP8 ? 4 : 5, 8>(a, f32_out, st);
-  return launch_down<T, FP8, NT, FP8 ? 3 : 4, 4>(a, f32_out, st);
+  // A warp's step is a chain of about 100 instructions, so an SM wants 12 to 16 warps, and the blocks have to fit
+  // all at once: with up to one block an SM 16 warps each (64 tokens, d_model 2048: 207 us for the layer, 8 warps 221),
+  // up to two 8 (16 tokens, d_model 4096, bf16: 73 us, 4 warps 105), up to three 8 with short rings where the
+  // registers allow it (d_model 5120, bf16: 100 us, 4 warps 120; e4m3 95 and 87, so not there), beyond that 4
+  // (d_model 7168, bf16: 181 us, 8 warps 213, whose 444 places are four too few).
+  const int blocks = a.d_model / 16;
+  if (blocks <= kSms && down_bytes<FP8, FP8 ? 2 : 3, 16>(a) <= kMaxShared) return launch_down<T, FP8, NT, FP8 ? 2 : 3, 16>(a, st);
+  if (blocks <= 2 * kSms) return launch_down<T, FP8, NT, FP8 ? 3 : 4, 8>(a, st);
+  if constexpr (NT <= 2 && !FP8)
+    if (blocks <= 3 * kSms) return launch_down<T, FP8, NT, 2, 8>(a, st);
+  return launch_down<T, FP8, NT, FP8 ? 3 : 4, 4>(a, st);
 }
 
 template <typename T, bool FP8>
-cudaError_t by_tokens(const MoeArgs &a, bool f32_out, cudaStream_t st) {
-  if (a.n_tokens <= 8) return launch_layer<T, FP8, 1>(a, f32_out, st);
-  if (a.n_tokens <= 16) return launch_layer<T, FP8, 2>(a, f32_out, st);
-  if (a.n_tokens <= 32) return launch_layer<T, FP8, 4>(a, f32_out, st);
-  return launch_layer<T, FP8, 8>(a, f32_out, st);
+cudaError_t by_tokens(const MoeArgs &a, cudaStream_t st) {
+  if (a.n_tokens <= 8) return launch_layer<T, FP8, 1>(a, st);
+  if (a.n_tokens <= 16) return launch_layer<T, FP8, 2>(a, st);
+  if (a.n_tokens <= 32) return launch_layer<T, FP8, 4>(a, st);
+  return launch_layer<T, FP8, 8>(a, st);
 }
 
 }  // namespace
@@ -647,10 +751,10 @@ MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared,
   return s;
 }
 
-cudaError_t launch_moe(const MoeArgs &a, int type, int io, bool f32_out, cudaStream_t st) {
+cudaError_t launch_moe(const MoeArgs &a, int type, int io, cudaStream_t st) {
   if (type == EMOE_TYPE_E4M3)
-    return io == EMOE_TYPE_BF16 ? by_tokens<__nv_bfloat16, true>(a, f32_out, st) : by_tokens<__half, true>(a, f32_out, st);
-  return io == EMOE_TYPE_BF16 ? by_tokens<__nv_bfloat16, false>(a, f32_out, st) : by_tokens<__half, false>(a, f32_out, st);
+    return io == EMOE_TYPE_BF16 ? by_tokens<__nv_bfloat16, true>(a, st) : by_tokens<__half, true>(a, st);
+  return io == EMOE_TYPE_BF16 ? by_tokens<__nv_bfloat16, false>(a, st) : by_tokens<__half, false>(a, st);
 }
 
 }  // namespace emoe

@@ -346,8 +346,9 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   a.n_shared = p->n_shared;
   a.top_k = p->top_k;
   a.renormalize = (p->flags & EMOE_MOE_RENORMALIZE) != 0;
+  a.out_f32 = p->out_type == EMOE_TYPE_F32;
   a.routed_scale = p->routed_scale;
-  return cuda_status(launch_moe(a, e->type, p->io_type, p->out_type == EMOE_TYPE_F32, (cudaStream_t)stream));
+  return cuda_status(launch_moe(a, e->type, p->io_type, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -93,11 +93,11 @@ struct MoeArgs {
   float *token_scale;
   void *moved_x;                                          // [token][d_model]
   void *h;                                                // [pair][d_ff]
-  int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize;
+  int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize, out_f32;
   int32_t ring_bytes;                                     // shared memory in front of a kernel's tables
   float routed_scale;
 };
-cudaError_t launch_moe(const MoeArgs &a, int type, int io, bool f32_out, cudaStream_t st);
+cudaError_t launch_moe(const MoeArgs &a, int type, int io, cudaStream_t st);
 
 // Lets a kernel ask for all the dynamic shared memory there is; done once a device.
 template <auto KERNEL>

@@ -243,3 +243,37 @@ def test_repeated_calls_give_the_same_bits():
         ex.handle.decode(0, x, logits, 6, table, outs[i], workspace=works[i % 2], stream=streams[i % 2])
     torch.cuda.synchronize()
     assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+@pytest.mark.parametrize("w,io", [("bf16", "bf16"), ("f16", "f16"), ("e4m3", "bf16"), ("e4m3", "f16")])
+@pytest.mark.parametrize("n", [7, 15, 16, 31, 64])
+def test_experts_with_few_and_with_all_tokens(w, io, n):
+    """Column tiles: experts that 0, 1, 8, 9, 17, 33 and all tokens chose, and shared ones, in one call."""
+    rng = np.random.default_rng(n)
+    ex = Experts(rng, 1, 9, 400, 208, w)
+    x = torch.from_numpy(rng.standard_normal((n, 400))).to(TORCH[io]).cuda()
+    logits = torch.full((n, 7), -float("inf"))
+    for e, count in enumerate((0, 1, 8, 9, 17, 33, 64)):
+        logits[torch.from_numpy(rng.permutation(n)[:count]), e] = float(e)
+    check(ex, x, logits.cuda(), 4, np.concatenate([rng.permutation(7), [7, 8]]), 2, io=io)
+
+
+@pytest.mark.parametrize("d", [2368, 2384, 4752, 7120])
+@pytest.mark.parametrize("w,n", [("bf16", 2), ("bf16", 12), ("bf16", 64), ("e4m3", 3), ("e4m3", 13), ("e4m3", 40)])
+def test_outputs_of_every_width(d, w, n):
+    """Widths at which the rows of an output take one block an SM, up to two, up to three and more."""
+    rng = np.random.default_rng(d + n)
+    ex = Experts(rng, 1, 7, d, 80, w)
+    x = torch.from_numpy(rng.standard_normal((n, d))).to(torch.bfloat16).cuda()
+    logits = torch.from_numpy(rng.standard_normal((n, 6))).float().cuda()
+    check(ex, x, logits, 2, np.arange(7), 1)
+
+
+@pytest.mark.parametrize("experts", [300, 1024])
+def test_the_most_choices(experts):
+    """64 tokens with 32 choices each, with tables that leave room for the wider blocks and that do not."""
+    rng = np.random.default_rng(experts)
+    ex = Experts(rng, 1, experts, 64, 16)
+    x = torch.from_numpy(rng.standard_normal((64, 64))).to(torch.bfloat16).cuda()
+    logits = torch.from_numpy(rng.standard_normal((64, experts))).float().cuda()
+    check(ex, x, logits, 32, rng.permutation(experts))

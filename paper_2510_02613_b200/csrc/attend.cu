@@ -70,7 +70,9 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int 
 // (no block barrier in the loop), scores and products on the tensor cores with the 16 rows of the
 // item as the m side (rows that do not exist are zero), running maximum and sum in registers.  The
 // four warps take every fourth group of tokens and are joined at the end.  Bound by the reads of K
-// and V: 3 stages x 4 warps x 8 KB and two blocks an SM keep 128 KB in flight.
+// and V: 2 stages x 4 warps x 8 KB and three blocks an SM have 192 KB of ring there (head_dim 128).  Measured, 32 sequences
+// of 3000 tokens, 16 heads: bf16 132 us, 6.0 TB/s; e4m3 129 us, 3.1 TB/s - there the conversion of the codes bounds it, on the
+// integer and conversion pipes.  Short calls are bound by an item's start and end (48 x 625 tokens, 4 heads: 2.3 TB/s).
 template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   using T = typename Operand<IO, FP8>::type;
@@ -543,7 +545,13 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int 
     splits = tokens ? (int32_t)((tokens + chunk - 1) / chunk) : 1;
   };
   const int64_t batch_rows = (int64_t)n_seqs * s.seq_rows;
-  if (prefix_len > 0 && (head_dim == 64 || head_dim == 128) && batch_rows > 16) {
+  // The other kernel starts later and ends earlier; this one takes 256 rows at once.  They meet at about 2^17 row tiles
+  // (of 16 rows) x tokens.  The whole call, this kernel and the other one, 4 KV heads, head_dim 128:
+  //   64 rows, 2000 tokens (2^15): bf16 21.5 and 15.4 us, e4m3 25.6 and 17.4
+  //   128 rows, 2000 tokens (2^16): 25.6 and 21.5, 31.7 and 25.6;  17 rows, 16000 (2^17): 27.6 and 27.8, 33.8 and 33.8
+  //   384 rows, 2000 (1.5 x 2^17): 27.6 and 29.7, 31.7 and 37.9;  384 rows, 16000: 42 and 120, 54 and 132
+  const int64_t work = n_heads * ((batch_rows + 15) / 16) * prefix_len;
+  if ((head_dim == 64 || head_dim == 128) && batch_rows > 16 && work >= 1 << 17) {
     // Blocks of up to 256 rows, one an SM: the number of splits with the fewest steps one after the
     // other, a block's start and end counting as two.
     s.tensor = 1;

@@ -1,6 +1,6 @@
-"""emoe_kv_attend where a prefix meets many rows (the 5th-generation tensor core path: more than 16
-rows a KV head, head dimensions 64 and 128), against the 64-bit definition with the tolerance of
-test_gpu_serving_attend."""
+"""emoe_kv_attend where a prefix meets several row tiles, against the 64-bit definition with the tolerance of
+test_gpu_serving_attend.  Most are small enough for the row kernel; test_gpu_serving_prefix_wide has the same with
+the work that goes to the 5th-generation tensor core path."""
 from __future__ import annotations
 
 import numpy as np

@@ -862,8 +862,9 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
  * on blocks of their own (row s of block_table, from the start of its first block):
  *     out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log(sum_j exp(scale * q.k_j)).
  * The prefix is read once for the whole batch.  A row that sees no token gives 0 and
- * -infinity.  Sums, maxima and statistics are 32-bit; the softmax weights are rounded to io_type
- * before they meet v.  The keys and values of the query tokens themselves have to be in the
+ * -infinity.  Sums, maxima and statistics are 32-bit; the softmax weights are rounded to 16 bits
+ * before they meet v: to io_type, for an e4m3 cache to F16 with an absolute step of at most 2^-30
+ * of the largest weight times v's largest scale.  The keys and values of the query tokens themselves have to be in the
  * cache already (emoe_kv_append earlier on the stream).
  *
  * Calls over different prefixes, or over parts of one long context, are joined with lse:
@@ -873,7 +874,8 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
  * type for an e4m3 cache.  own_lens beyond max_blocks * block_tokens count as that, negative ones
  * as 0.  Tokens on a block id outside the pool are left out and reported in the status word.
  * What lies behind a sequence's length - in its last block, in its row of the table, in the pool -
- * has no influence, whatever it holds.  prefix_len, and max_blocks as the bound of own_lens, are
+ * has no influence, whatever it holds.  Waits inside the kernel are bounded: should one ever run
+ * out, the status word holds EMOE_ERR_DEVICE_TIMEOUT and out is undefined.  prefix_len, and max_blocks as the bound of own_lens, are
  * host values; a captured call follows own_lens and the tables from replay to replay.
  * Sizes beyond 2^24 query tokens, 2^28 rows or 2^30 tokens a sequence: EMOE_ERR_TOO_LARGE.
  */
@@ -911,7 +913,8 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const 
 typedef struct {
   const void *arena;      /* 16-byte aligned                                              */
   int32_t *status;        /* optional int32: set to EMOE_ERR_PLACEMENT by a call that met a */
-                          /* slot beyond n_slots (never cleared)                          */
+                          /* slot beyond n_slots, or one slot for two experts of a token  */
+                          /* (never cleared)                                              */
   uint64_t matrix_stride; /* 0, or a multiple of 16 (16-bit types, not FUSED_W13)           */
   int32_t n_layers;
   int32_t n_slots;        /* at most EMOE_MOE_MAX_SLOTS                                    */
@@ -939,11 +942,13 @@ emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *experts, uint64
  * slot_of_expert [n_experts + n_shared]: slot of each routed, then each shared expert in this
  * arena, -1 for experts that this call leaves out: on an expert-parallel rank those of other
  * ranks (a replicated one, routed or shared, is given to one rank's call).  Entries are
- * distinct where not negative.  The ranks' outputs are summed by the caller; out_type
+ * distinct where not negative (a token whose two choices lie in one slot is reported in the status
+ * word, its output undefined).  The ranks' outputs are summed by the caller; out_type
  * EMOE_TYPE_F32 leaves that sum to be rounded once.
  * (e4m3 weights with BF16 tokens: a hidden vector's values have to be below 2^67.)
  * Only the chosen experts' weights are read, each once for all tokens.  Sums are 32-bit; the
- * hidden vector w * silu(gate) * up is rounded once to io_type as the last product's operand
+ * hidden vector w * silu(gate) * up is rounded once to io_type as the last product's operand, what that
+ * takes being kept as a second operand in calls of up to 8 tokens for experts with up to 4 of them
  * (beyond the range of F16: its largest value).  The result does not depend on timing.
  * A row of logits with nothing above minus infinity chooses no routed expert.
  */

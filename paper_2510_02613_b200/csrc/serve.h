@@ -72,7 +72,7 @@ cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st
 // Byte offsets of a layer call's workspace.  moved: e4m3 weights, whose bf16 tokens are kept in f16 by a power
 // of two each.
 struct MoeShape {
-  int64_t token_scale, moved_x, h, bytes;
+  int64_t token_scale, moved_x, h, h_rest, bytes;         // h_rest: from h to what its rounding took, up to 8 tokens
 };
 MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared, bool moved);
 
@@ -93,6 +93,7 @@ struct MoeArgs {
   float *token_scale;
   void *moved_x;                                          // [token][d_model]
   void *h;                                                // [pair][d_ff]
+  int64_t h_rest;                                         // bytes
   int32_t n_slots, d_model, d_ff, n_tokens, n_experts, n_shared, top_k, renormalize, out_f32;
   int32_t ring_bytes;                                     // shared memory in front of a kernel's tables
   float routed_scale;

@@ -277,3 +277,19 @@ def test_the_most_choices(experts):
     x = torch.from_numpy(rng.standard_normal((64, 64))).to(torch.bfloat16).cuda()
     logits = torch.from_numpy(rng.standard_normal((64, experts))).float().cuda()
     check(ex, x, logits, 32, rng.permutation(experts))
+
+
+def test_one_slot_for_two_experts_is_reported():
+    """A table that names a slot twice: reported when a token chooses both, other tokens keep their results."""
+    rng = np.random.default_rng(9)
+    ex = Experts(rng, 1, 3, 64, 32)
+    x = torch.from_numpy(rng.standard_normal((2, 64))).to(torch.bfloat16).cuda()
+    logits = torch.tensor([[9.0, 8, 0, 1], [0.0, 1, 9, 8]], device="cuda")
+    want = check(ex, x[1:], logits[1:], 2, np.array([0, -1, 1, 2]))
+    table, out = torch.tensor([0, 1, 1, 2], dtype=torch.int32, device="cuda"), torch.zeros_like(x)
+    work = torch.empty(ex.handle.decode_workspace_bytes(2, 2, 4), dtype=torch.uint8, device="cuda")
+    ex.handle.decode(0, x, logits, 2, table, out, workspace=work)
+    assert ex.status.item() == 0 and torch.equal(out[1:], want)
+    logits[0] = torch.tensor([0.0, 9, 8, 1])
+    ex.handle.decode(0, x, logits, 2, table, out, workspace=work)
+    assert ex.status.item() == 3 and torch.equal(out[1:], want)

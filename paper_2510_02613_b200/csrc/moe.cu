@@ -543,9 +543,10 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
 }
 
 // y for 16 output rows a block: the (expert, step) pairs of all experts in use are dealt to the
-// warps in runs of equal work.  Bound by the weights with many blocks, and with few by a
-// warp's chain of instructions: 340 MB (2048 rows, 126 experts of 768, 64 tokens) in about 70 us.  At the end of its part of an expert a warp adds the expert's columns to its
+// warps in runs of equal work.  At the end of its part of an expert a warp adds the expert's columns to its
 // own sums of the tokens in shared memory; the warps' sums are joined at the end, in their order.
+// Bound by the weights where the warps are enough to keep them coming: 340 MB (2048 rows, 126 experts
+// of 768, 64 tokens) in 68 us, 5.0 TB/s from 128 of the 148 SMs.
 template <typename T, bool FP8, int NT, int STAGES, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];

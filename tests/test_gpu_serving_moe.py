@@ -293,3 +293,28 @@ def test_one_slot_for_two_experts_is_reported():
     logits[0] = torch.tensor([0.0, 9, 8, 1])
     ex.handle.decode(0, x, logits, 2, table, out, workspace=work)
     assert ex.status.item() == 3 and torch.equal(out[1:], want)
+
+
+@pytest.mark.parametrize("w", ["bf16", "e4m3"])
+def test_an_arena_longer_than_32_bit_offsets(w):
+    """The last of 2048 slots in the second of two layers, more than 2^32 bytes from the arena's start."""
+    rng = np.random.default_rng(10)
+    d, f = (512, 512) if w == "bf16" else (1024, 768)
+    ex = Experts(rng, 1, 4, d, f, w)
+    x = torch.from_numpy(rng.standard_normal((9, d))).to(torch.bfloat16).cuda()
+    logits = torch.from_numpy(rng.standard_normal((9, 4))).float().cuda()
+    table = rng.permutation(4)
+    want = check(ex, x, logits, 2, table)
+    m = d * f * (2 if w == "bf16" else 1)
+    small = ex.arena.flatten().view(torch.uint8)
+    weights = 2 * 3 * 2048 * m
+    scales = 2 * 3 * 2048 * (d // 128) * (f // 128) * 4 if w == "e4m3" else 0
+    big = torch.empty(weights + scales, dtype=torch.uint8, device="cuda")
+    big[:weights].view(2, 3, 2048, m)[1, :, -4:] = small[:12 * m].view(3, 4, m)
+    if scales:
+        big[weights:].view(2, 3, 2048, -1)[1, :, -4:] = small[12 * m:].view(3, 4, -1)
+    handle = E.ExpertArena(big, n_layers=2, n_slots=2048, d_model=d, d_ff=f, w_type=w)
+    out = torch.empty_like(want)
+    work = torch.empty(handle.decode_workspace_bytes(9, 2, 4), dtype=torch.uint8, device="cuda")
+    handle.decode(1, x, logits, 2, torch.from_numpy((table + 2044).astype(np.int32)).cuda(), out, workspace=work)
+    assert torch.equal(out, want)

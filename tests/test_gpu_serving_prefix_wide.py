@@ -272,3 +272,38 @@ def test_queries_of_any_size_with_e4m3():
     check_codes(ref, c, torch.from_numpy(q).to(torch.bfloat16).cuda(), np.arange(30, dtype=np.int32), 470, "bf16")
     big = torch.from_numpy(rng.standard_normal((30, 1, 4 * hkv, 128)) * 2.0 ** 100).to(torch.bfloat16).cuda()
     check_codes(ref, c, big, np.arange(30, dtype=np.int32), 470, "bf16", scale=2.0 ** -106)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_a_cache_longer_than_32_bit_offsets_and_strided_rows(fast, kv):
+    """Prefix and own tokens on the last blocks of a pool of 5.2 GB (e4m3: 4.6) each for K and V; queries and outputs with gaps."""
+    import paper_2510_02613_b200 as E
+    rng = np.random.default_rng(13)
+    size = 2 if kv == "bf16" else 1
+    heads, hd, seqs, prefix, many = 16, 128, 32, 4096, 80000 if size == 2 else 140000
+    lens = [int(x) for x in rng.integers(0, 30, seqs)]
+    pool = prefix // 16 + sum(-(-n // 16) for n in lens) + 1
+    ref = wide(rng, (1, pool, 16, heads), hd, kv)
+    _, arena, scales = device_cache(ref)
+    big = torch.empty(2 * many * 16 * heads * hd * size, dtype=torch.uint8, device="cuda")
+    big.view(2, many, -1)[:, -pool:] = arena.view(2, pool, -1)
+    big_scales = None
+    if kv == "e4m3":
+        big_scales = torch.full((2 * many * 16 * heads,), 255, dtype=torch.uint8, device="cuda")
+        big_scales.view(2, many, -1)[:, -pool:] = scales.view(2, pool, -1)
+    c = E.KvCache(big, n_layers=1, num_blocks=many, block_tokens=16, n_heads=heads, head_dim=hd, kv_type=kv, scales=big_scales)
+    pt, table = make_tables(rng, pool, 16, prefix, lens)
+    wide_q = torch.full((seqs, 1, heads + 1, hd), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide_q[:, :, :heads] = torch.from_numpy(rng.standard_normal((seqs, 1, heads, hd)) * 0.2).to(torch.bfloat16).cuda()
+    wide_out = torch.full((seqs, 1, heads + 2, hd), 7.0, dtype=torch.bfloat16, device="cuda")
+    q, out = wide_q[:, :, :heads], wide_out[:, :, :heads]
+    lse = torch.empty(seqs, 1, heads, device="cuda")
+    at = many - pool
+    dev = [torch.from_numpy(x).cuda() for x in (np.where(table < 0, -1, table + at).astype(np.int32), np.asarray(lens, np.int32), (pt + at).astype(np.int32))]
+    work = torch.empty(c.attend_workspace_bytes(seqs, 1, heads, table.shape[1], prefix), dtype=torch.uint8, device="cuda")
+    c.attend(0, q, out, dev[0], dev[1], dev[2], prefix, lse=lse, workspace=work)
+    o, want_l, a, e = definition(ref, 0, q.double().cpu().numpy(), table, lens, pt, prefix, hd ** -0.5)
+    tol = 1.05 * (2 * HALF_STEP["bf16"] + 2 * e[..., None]) * a + 1e-30
+    assert (np.abs(out.double().cpu().numpy() - o) <= tol).all()
+    assert (np.abs(lse.double().cpu().numpy() - want_l) <= e + 2.0 ** -21 * np.abs(want_l) + 2.0 ** -20).all()
+    assert (wide_out[:, :, heads:] == 7).all()

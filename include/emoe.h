@@ -864,7 +864,7 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
  * The prefix is read once for the whole batch.  A row that sees no token gives 0 and
  * -infinity.  Sums, maxima and statistics are 32-bit; the softmax weights are rounded to 16 bits
  * before they meet v: to io_type, for an e4m3 cache to F16 with an absolute step of at most 2^-30
- * of the largest weight times v's largest scale.  The keys and values of the query tokens themselves have to be in the
+ * of the largest weight times the largest scale of the v that the row sees.  The keys and values of the query tokens themselves have to be in the
  * cache already (emoe_kv_append earlier on the stream).
  *
  * Calls over different prefixes, or over parts of one long context, are joined with lse:

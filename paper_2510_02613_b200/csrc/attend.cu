@@ -135,7 +135,8 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
     if (lane == 0) s_valid[warp][i % kStages] = held_valid;
   };
 
-  uint32_t v_ref = 0;   // e4m3: the largest scale byte of v so far, whose scale o is relative to
+  // e4m3: the largest scale byte of v so far that a row (g, g + 8) sees, whose scale its o is relative to
+  uint32_t v_ref[2] = {0, 0};
   constexpr int kTileGroup = FP8 ? 4 : 2;   // column tiles that are read together
   float o[HD / 8 / kTileGroup][kTileGroup][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -231,21 +232,33 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
     }
 
     const int base = it.t0 + (warp + kWarps * i) * kGroup;
-    float k_by[kN][2], v_by[kN][2], v_raise = 1.f;
+    // Query tokens of one sequence see different ends: in a ragged step some real row does not see all of its tokens.
+    const int end = min(base + kGroup, it.t1);
+    const auto is_ragged = [&]() {
+      return a.q_len > 1 && __any_sync(0xffffffffu, (g < it.rows && limit[0] < end) || (g + 8 < it.rows && limit[1] < end));
+    };
+    const bool ragged_scales = FP8 && is_ragged();
+    float k_by[kN][2], v_by[kN][2], v_raise[2] = {1.f, 1.f};
     if constexpr (FP8) {   // scales are powers of two; 255 is not a number and not counted in the largest of v so far
-      const uint32_t mine = s_scale[warp][i % kStages][lane] >> 8;
-      const uint32_t largest = max(v_ref, __reduce_max_sync(0xffffffffu, mine == 255 ? 0 : mine));
-      v_raise = largest - v_ref < 127 ? __uint_as_float((127 - (largest - v_ref)) << 23) : 0.f;
-      v_ref = largest;
+      uint32_t largest = v_ref[0];
+      if (!ragged_scales) {   // no ragged step has been yet: all rows have the same largest scale
+        const uint32_t mine = s_scale[warp][i % kStages][lane] >> 8;
+        largest = max(v_ref[0], __reduce_max_sync(0xffffffffu, mine == 255 ? 0 : mine));
+        v_raise[0] = v_raise[1] = v_relative(v_ref[0], largest);
+        v_ref[0] = v_ref[1] = largest;
+      }
 #pragma unroll
       for (int j = 0; j < kN; ++j) {
         const uint32_t two = *(const uint32_t *)&s_scale[warp][i % kStages][j * 8 + 2 * c];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const uint32_t k = two >> (16 * e) & 255, v = two >> (16 * e + 8) & 255;
-          k_by[j][e] = scale_of(k);
-          v_by[j][e] = v == 255 ? CUDART_NAN_F : v_ref - v < 127 ? __uint_as_float((127 - (v_ref - v)) << 23) : 0.f;
+          k_by[j][e] = scale_of(two >> (16 * e) & 255);
+          v_by[j][e] = v_relative(two >> (16 * e + 8) & 255, largest);
         }
+      }
+      if (ragged_scales) {   // what a row does not see has no part in its largest scale: weights are scaled row by row below
+#pragma unroll
+        for (int j = 0; j < kN; ++j) v_by[j][0] = v_by[j][1] = 1.f;
       }
     }
     float top[2] = {m[0], m[1]};
@@ -282,8 +295,27 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
         }
       l[half] = l[half] * alpha[half] + sum;
     }
-    alpha[0] *= v_raise;
-    alpha[1] *= v_raise;
+    if constexpr (FP8)
+      if (__builtin_expect(ragged_scales, 0)) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const auto scale_byte = [&](int t) { return (uint32_t)s_scale[warp][i % kStages][t] >> 8; };
+          uint32_t largest = v_ref[half];
+          const int seen = min(limit[half] - base, kGroup);
+          for (int t = 0; t < seen; ++t) largest = max(largest, scale_byte(t) == 255 ? 0 : scale_byte(t));
+          v_raise[half] = v_relative(v_ref[half], largest);
+          v_ref[half] = largest;
+#pragma unroll
+          for (int j = 0; j < kN; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float &x = s[j][2 * half + e];
+              if (x != 0.f) x *= v_relative(scale_byte(j * 8 + 2 * c + e), largest);
+            }
+        }
+      }
+    alpha[0] *= v_raise[0];
+    alpha[1] *= v_raise[1];
     if (!__all_sync(0xffffffffu, alpha[0] == 1.f && alpha[1] == 1.f)) {
 #pragma unroll
       for (int n = 0; n < HD / 8; ++n) {
@@ -326,12 +358,10 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
         }
       }
     };
-    // Query tokens of one sequence see different ends.  A value that some rows must not see may be
-    // infinite or not a number, and a weight of zero does not silence it: such a step is done end by
-    // end, each row taking the pass of its own, with the values behind that end cleared.
-    const int end = min(base + kGroup, it.t1);
-    const bool ragged = a.q_len > 1 && __any_sync(0xffffffffu, (g < it.rows && limit[0] < end) || (g + 8 < it.rows && limit[1] < end));
-    if (ragged) {
+    // A value that some rows must not see may be infinite or not a number, and a weight of zero does not
+    // silence it: a ragged step is done end by end, each row taking the pass of its own, with the values
+    // behind that end cleared.
+    if (FP8 ? ragged_scales : is_ragged()) {
       for (int stop = end; stop > base; --stop) {
         const bool now0 = min(limit[0], end) == stop, now1 = min(limit[1], end) == stop;
         if (__any_sync(0xffffffffu, now0 || now1)) {
@@ -378,7 +408,7 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * (e & 1) : n * 8 + 2 * c + (e & 1);
-      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n / kTileGroup][n % kTileGroup][e] * (FP8 ? scale_of(v_ref) : 1.f);
+      joined[(warp * 16 + g + 8 * (e >> 1)) * kPitch + col] = o[n / kTileGroup][n % kTileGroup][e] * (FP8 ? scale_of(v_ref[e >> 1]) : 1.f);
     }
   __syncthreads();
   // the prefix's own kernel may still be running: the joining one waits for this one alone

@@ -52,4 +52,9 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
   return byte == 255 ? CUDART_NAN_F : __uint_as_float(byte ? byte << 23 : 0x400000u);
 }
 
+// The scale of byte v relative to that of byte `largest`, which is not below it (but for 255: not a number).
+__device__ __forceinline__ float v_relative(uint32_t v, uint32_t largest) {
+  return v == 255 ? CUDART_NAN_F : largest - v < 127 ? __uint_as_float((127 - (largest - v)) << 23) : 0.f;
+}
+
 }  // namespace emoe

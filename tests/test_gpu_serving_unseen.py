@@ -1,0 +1,44 @@
+"""emoe_kv_attend: what a query token does not see has no influence on it, and what it sees is never dropped,
+whatever the values are."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import serving_ref as R
+from test_gpu_serving_attend import make_tables
+from test_gpu_serving_kv import TORCH, device_cache, filled
+
+pytestmark = pytest.mark.gpu
+
+
+def call(c, q, table=None, lens=None, pt=None, prefix=0, scale=None):
+    n, t, hq, _ = q.shape
+    dev = lambda x: None if x is None else torch.from_numpy(np.ascontiguousarray(np.asarray(x, np.int32))).cuda()    # noqa: E731
+    out, lse = torch.empty_like(q), torch.empty(n, t, hq, device="cuda")
+    work = torch.empty(c.attend_workspace_bytes(n, t, hq, 0 if table is None else table.shape[1], prefix), dtype=torch.uint8, device="cuda")
+    c.attend(0, q, out, dev(table), dev(lens), dev(pt), prefix, scale=scale, lse=lse, workspace=work)
+    return out, lse
+
+
+@pytest.mark.parametrize("byte", [0, 141, 170, 200, 254])
+@pytest.mark.parametrize("hd,group,t,io", [(64, 2, 2, "bf16"), (128, 4, 4, "f16"), (128, 8, 4, "bf16"), (256, 1, 3, "bf16"), (32, 5, 5, "f16")])
+def test_scales_of_tokens_that_a_row_does_not_see(byte, hd, group, t, io):
+    """The last own token's scales of an e4m3 cache may be any: the query tokens before it do not see it, so
+    their outputs keep every bit."""
+    rng = np.random.default_rng(hd + t)
+    lens, prefix, block = [20, t, 33, 150, 64], 21, 16
+    pool = 30
+    ref = filled(rng, (1, pool, block, 2), hd, "e4m3", False)
+    pt, table = make_tables(rng, pool, block, prefix, lens)
+    clean = device_cache(ref)[0]
+    c, _, scales = device_cache(ref)
+    for s, n in enumerate(lens):
+        scales[0, :, int(table[s, (n - 1) // block]), (n - 1) % block] = byte
+    q = torch.from_numpy(rng.standard_normal((len(lens), t, 2 * group, hd))).to(TORCH[io]).cuda()
+    for shared in (prefix, 0):
+        want, got = (call(x, q, table, lens, pt if shared else None, shared) for x in (clean, c))
+        assert torch.isfinite(want[0]).all()
+        for x, y in zip(want, got):
+            assert torch.equal(x[:, :-1], y[:, :-1])

@@ -290,8 +290,8 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
           float &x = s[j][2 * half + e];
           x = exp2_fast(x - safe);
           sum += x;
-          // a masked token's scale may be anything: its weight is exactly zero
-          if constexpr (FP8) x = x == 0.f ? 0.f : x * v_by[j][e];
+          // (what no row sees has a finite scale here; a NaN scale shows even where the weight has come to zero)
+          if constexpr (FP8) x *= v_by[j][e];
         }
       l[half] = l[half] * alpha[half] + sum;
     }
@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_ker
           for (int j = 0; j < kN; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float &x = s[j][2 * half + e];
-              if (x != 0.f) x *= v_relative(scale_byte(j * 8 + 2 * c + e), largest);
+              const int t = j * 8 + 2 * c + e;
+              if (t < seen) s[j][2 * half + e] *= v_relative(scale_byte(t), largest);
             }
         }
       }

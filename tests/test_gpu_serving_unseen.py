@@ -42,3 +42,25 @@ def test_scales_of_tokens_that_a_row_does_not_see(byte, hd, group, t, io):
         assert torch.isfinite(want[0]).all()
         for x, y in zip(want, got):
             assert torch.equal(x[:, :-1], y[:, :-1])
+
+
+@pytest.mark.parametrize("t", [1, 2])
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_a_value_that_is_not_a_number_shows_whatever_its_weight(kv, t):
+    """A token whose weight is below the smallest 32-bit number still has a part in the sum: a NaN in its value
+    makes the row's output NaN, for 16-bit caches as for e4m3 ones."""
+    ref = R.Cache(1, 6, 16, 2, 64, kv)
+    ref.values[:, 0, 2, 5] = -2.0       # a score of -128 against 0: a weight of 2^-184
+    ref.values[:, 1] = 1.0
+    c, arena, scales = device_cache(ref)
+    if kv == "e4m3":
+        scales[0, 1, 2, 5, 0] = 255
+    else:
+        arena.view(torch.bfloat16).view(2, 6, 16, 2, 64)[1, 2, 5, 0] = float("nan")
+    q = torch.ones(2, t, 4, 64, dtype=torch.bfloat16, device="cuda")
+    table = np.array([[4, 2, 0], [1, 3, 5]], np.int32)
+    out, lse = call(c, q, table, [40, 40], scale=1.0)
+    assert torch.isnan(out[0, :, :2]).all()
+    assert bool((out[0, :, 2:] == 1).all()) and bool((out[1] == 1).all())
+    out, _ = call(c, q, pt=[0, 2], prefix=30, scale=1.0)
+    assert torch.isnan(out[:, :, :2]).all() and bool((out[:, :, 2:] == 1).all())

@@ -472,12 +472,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
   float l = 0.f, x[N] = {};
   for (int first = warp * 4; first < slots; first += kJoinWarps * 4) {
     float w[4], y[4][N];
+    bool there[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float2 p = first + u < slots ? ml[first + u] : make_float2(-CUDART_INF_F, 0.f);
       // an empty part (sum 0) does not count: nothing was written there
-      w[u] = p.y == 0.f ? 0.f : p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
-      l += p.y == 0.f ? 0.f : w[u] * p.y;
+      there[u] = p.y != 0.f;
+      w[u] = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+      l += there[u] ? w[u] * p.y : 0.f;
       const float *const src = parts + (int64_t)min(first + u, slots - 1) * HD;
       if constexpr (N % 4 == 0) {
 #pragma unroll
@@ -491,7 +493,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const __gr
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] += w[u] == 0.f ? 0.f : w[u] * y[u][j];
+      for (int j = 0; j < N; ++j) x[j] += there[u] ? w[u] * y[u][j] : 0.f;
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) s_x[warp][lane * N + j] = x[j];

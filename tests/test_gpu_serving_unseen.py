@@ -64,3 +64,25 @@ def test_a_value_that_is_not_a_number_shows_whatever_its_weight(kv, t):
     assert bool((out[0, :, 2:] == 1).all()) and bool((out[1] == 1).all())
     out, _ = call(c, q, pt=[0, 2], prefix=30, scale=1.0)
     assert torch.isnan(out[:, :, :2]).all() and bool((out[:, :, 2:] == 1).all())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_a_value_that_is_not_a_number_in_a_split_of_no_weight(kv):
+    """The same where all the tokens of its split have weights that small."""
+    ref = R.Cache(1, 130, 16, 1, 64, kv)
+    ref.values[:, 0, :64] = -2.0        # 1024 tokens
+    ref.values[:, 1] = 1.0
+    c, arena, scales = device_cache(ref)
+    if kv == "e4m3":
+        scales[0, 1, 0, 5, 0] = 255
+    else:
+        arena.view(torch.bfloat16).view(2, 130, 16, 1, 64)[1, 0, 5, 0] = float("nan")
+    q = torch.ones(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    table = np.arange(130)[None]
+    assert c.attend_workspace_bytes(1, 1, 2, 130, 0) > 0      # there are splits
+    out, _ = call(c, q, table, [2000], scale=1.0)
+    assert torch.isnan(out).all()
+    out, _ = call(c, q, table[:, ::-1], [1000], scale=1.0)    # ends before it
+    assert bool((out == 1).all())
+    out, _ = call(c, q, pt=table[0], prefix=2000, scale=1.0)
+    assert torch.isnan(out).all()

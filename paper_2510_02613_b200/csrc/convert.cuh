@@ -30,7 +30,7 @@ template <> struct Pair<__half> {
 // too small (denormal where the code is), which the tensor cores take as it is.  The other operand
 // carries 2^60 of that and the sums the rest, so that neither side leaves its range.  A word's
 // codes come out as (0, 2) and (1, 3), so the other operand is kept in that order ("moved").  f16 operands are
-// what cvt gives: in order and at their own size.
+// what cvt gives: in order and at their own size.  (Codes 0x7f and 0xff, not a number, would become 480: see moved_top.)
 template <typename T, bool FP8> constexpr bool kMoved = FP8 && !__is_same(T, __half);
 constexpr float kMovedScale = 0x1p60f;   // of the other operand, and of the sums
 // Two pairs of operands from a word of four codes.
@@ -44,6 +44,13 @@ __device__ __forceinline__ void word_of_codes(uint32_t &first, uint32_t &second,
     second = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
   }
 }
+
+// The largest magnitudes of moved codes so far, and whether a code that is not a number, the largest there is, was
+// among them.
+__device__ __forceinline__ uint32_t moved_top(uint32_t top, uint32_t w) {
+  return __vimax3_u16x2(top, (w << 4) & 0x07f007f0u, (w >> 4) & 0x07f007f0u);
+}
+__device__ __forceinline__ bool moved_nan(uint32_t top) { return (top & 0xffffu) == 0x07f0u || top >> 16 == 0x07f0u; }
 
 // Four codes as f16 pairs (0, 1) and (2, 3).
 __device__ __forceinline__ void codes_to_half(uint32_t &lo, uint32_t &hi, uint32_t w) {

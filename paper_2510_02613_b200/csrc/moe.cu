@@ -343,10 +343,11 @@ __device__ __forceinline__ int stages_of(int count) {
 }
 
 // The products of one step for all column tiles of an expert.  fill() starts the copies of the stage that was
-// consumed last; second() reads this lane's token of the second tile.
+// consumed last; second() reads this lane's token of the second tile.  top: moved_top of this lane's codes in rows g
+// and g + 8.
 template <typename T, bool FP8, int NT, int STAGES, typename F, typename G>
 __device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP8, STAGES> &ring, int &stage, int count,
-                                              float scale_lo, float scale_hi, F fill, G second) {
+                                              float scale_lo, float scale_hi, uint32_t (&top)[2], F fill, G second) {
   using S = Step<FP8>;
   const auto next = [&]() { stage = stage + 1 == STAGES ? 0 : stage + 1; };
   uint4 w[4];
@@ -356,6 +357,12 @@ __device__ __forceinline__ void step_products(float (&acc)[NT][4], const Ring<FP
   copy_async_wait<STAGES - 1>();
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = ring.get(stage, i);
+  if constexpr (kMoved<T, FP8>) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top[i & 1] = moved_top(top[i & 1], word(w[i], j));
+  }
 #pragma unroll
   for (int i = 0; i < 2 * S::kTok; ++i) tok.v[i] = ring.get(stage, 4 + i);
   step_product<T, FP8>(acc[0], w, tok, scale_lo, scale_hi);
@@ -472,6 +479,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
     const int2 e = routed.active[i];
     const int count = routed.active[i + 1].y - e.y;
     float acc[NT][4] = {};
+    uint32_t top[2] = {0, 0};
     const uint8_t *const second = 8 + g < count ? x_lane + routed.token[e.y + 8 + g] * x_stride : x_lane;
     const float *scale_g = nullptr, *scale_u = nullptr;
     float sg = 1.f, su = 1.f;
@@ -493,7 +501,7 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
           next_u = scale_u[k + 1];
         }
       }
-      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, sg, su, fill, [&]() {
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, sg, su, top, fill, [&]() {
         const bool in = 8 + g < count;
         return load_token<FP8>(second + (int64_t)k * (S::kElems * 2), in && k < end0, in && k < end1);
       });
@@ -648,6 +656,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
       by = scale[first];
     }
     float acc[NT][4] = {};
+    uint32_t top[2] = {0, 0};
     for (int k = first; k < last; ++k) {
       fill_weights();
       fill_tokens();
@@ -655,7 +664,7 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
       if constexpr (FP8) {
         if (k + 1 < last) later = scale[k + 1];
       }
-      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, by, by, [&]() {
+      step_products<T, FP8, NT, STAGES>(acc, ring, stage, count, by, by, top, [&]() {
         fill_weights();
         fill_tokens();
       }, [&]() {
@@ -663,6 +672,14 @@ __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_const
         return load_token<FP8>(second + (int64_t)k * (S::kElems * 2), in && k < end0, in && k < end1);
       });
       by = later;
+    }
+    if constexpr (kMoved<T, FP8>) {   // a weight that is not a number makes its row of sums that
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+        if (__ballot_sync(0xffffffffu, moved_nan(top[half])) >> (lane & 28) & 15) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n) acc[n][2 * half] = acc[n][2 * half + 1] = CUDART_NAN_F;
+        }
     }
     if constexpr (kWithRest<NT>)
       if (count <= 4) {   // columns 4 to 7 are two lanes further

@@ -158,6 +158,10 @@ __device__ __forceinline__ void add_pair(float &x, float &y, float ax, float ay)
   asm("{\n\t.reg .b64 v, k;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 k, {%2, %3};\n\tadd.rn.f32x2 v, v, k;\n\tmov.b64 {%0, %1}, v;\n\t}"
       : "+f"(x), "+f"(y) : "f"(ax), "f"(ay));
 }
+__device__ __forceinline__ void mul_pair(float &x, float &y, float ax, float ay) {
+  asm("{\n\t.reg .b64 v, k;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 k, {%2, %3};\n\tmul.rn.f32x2 v, v, k;\n\tmov.b64 {%0, %1}, v;\n\t}"
+      : "+f"(x), "+f"(y) : "f"(ax), "f"(ay));
+}
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
@@ -272,7 +276,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     const bool busy = (alternate ? 0 : slot * kTile) + (warp & 3) * 32 < rows;   // any real row in the warp
     float x[2][32];   // the row's query, then a step's scores and weights
     // not zero: a masked score, minus infinity, has to stay that (and every other one comes to zero all the same)
-    float c = fmaxf(fabsf(a.scale_log2), 0x1p-126f);
+    const float c = fmaxf(fabsf(a.scale_log2), 0x1p-149f);
+    float query_by = 1.f;   // e4m3: the row's query is this much smaller than the one that is multiplied
     {
       // The row's query (stored by two threads, half each, where both slots have the same rows): rows that do
       // not exist are zero, a negative scale turns the sign.
@@ -292,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
             top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
           }
         const float by = query_scale(top);
-        c = fmaxf(c / by, 0x1p-126f);
+        query_by = 1.f / by;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
           const float2 e0 = Pair<IO>::unpack(w[i].x), e1 = Pair<IO>::unpack(w[i].y), e2 = Pair<IO>::unpack(w[i].z), e3 = Pair<IO>::unpack(w[i].w);
@@ -341,11 +346,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           if constexpr (FP8) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
-              const float4 k = *(const float4 *)(k_scale + 32 * j + e);
-              x[j][e] *= k.x;
-              x[j][e + 1] *= k.y;
-              x[j][e + 2] *= k.z;
-              x[j][e + 3] *= k.w;
+              // the two scales first: either one alone can take a score out of range
+              float4 k = *(const float4 *)(k_scale + 32 * j + e);
+              mul_pair(k.x, k.y, query_by, query_by);
+              mul_pair(k.z, k.w, query_by, query_by);
+              mul_pair(x[j][e], x[j][e + 1], k.x, k.y);
+              mul_pair(x[j][e + 2], x[j][e + 3], k.z, k.w);
               const float4 v = *(const float4 *)(v_scale + 32 * j + e);
               v_top = max3(max3(v_top, v.x, v.y), v.z, v.w);
             }

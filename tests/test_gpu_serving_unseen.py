@@ -86,3 +86,32 @@ def test_a_value_that_is_not_a_number_in_a_split_of_no_weight(kv):
     assert bool((out == 1).all())
     out, _ = call(c, q, pt=table[0], prefix=2000, scale=1.0)
     assert torch.isnan(out).all()
+
+
+@pytest.mark.parametrize("rows,heads", [(4, 1), (33, 16)])
+def test_tiny_queries_on_large_keys(rows, heads):
+    """Queries of 2^-122 and e4m3 keys with scales of 2^117: their products are ordinary scores.  33 sequences on 16
+    heads are work for the tensor core path (3 row tiles x 16 heads x 3200 tokens), 4 on one head for the other."""
+    from test_gpu_serving_prefix_wide import definition
+    rng = np.random.default_rng(11)
+    prefix = 3200
+    ref = R.Cache(1, 200, 16, heads, 128, "e4m3")
+    codes = rng.integers(0, 127, ref.values.shape, dtype=np.uint8) | (rng.integers(0, 2, ref.values.shape, dtype=np.uint8) << 7)
+    ref.values = torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
+    ref.bytes[:, 0] = 127 + 117
+    c, _, _ = device_cache(ref)
+    pt = np.arange(200, dtype=np.int32)
+    q = torch.from_numpy(rng.standard_normal((rows, 1, heads, 128)) * 2.0 ** -122).to(torch.bfloat16).cuda()
+    assert float(q.abs().max()) > 2.0 ** -124
+    out, lse = call(c, q, pt=pt, prefix=prefix)
+    o, want, a, e = definition(ref, 0, q.double().cpu().numpy(), np.zeros((rows, 0), np.int32), [0] * rows, pt, prefix, 128 ** -0.5)
+    assert want.std() > 0.01     # the scores matter
+    # A query's power of two (2^127 at most) and the call's scale meet in a 32-bit factor of 2^-131 or more: off by
+    # half its smallest step 2^-149, 2^-19 of a score.  Scores are at most |want| + log(tokens) from it.
+    size = 2.0 ** -19 * (np.abs(want) + 2 * np.log(prefix) + 40)
+    assert (np.abs(lse.double().cpu().numpy() - want) <= e + size + 2.0 ** -20).all()
+    # weights and result rounded to 16 bits, scores off by that, weights below f16's normal range (2^-31 of v's largest
+    # scale, 1 here, times the code)
+    v = np.abs(ref.values[0, 1].reshape(-1, heads, 128)).sum(0)
+    tol = 1.05 * (2 * 2.0 ** -8 + 2 * (e + size)[..., None]) * a + 2.0 ** -31 * v[None, None]
+    assert (np.abs(out.double().cpu().numpy() - o) <= tol).all()

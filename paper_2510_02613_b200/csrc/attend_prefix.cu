@@ -454,6 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       __syncwarp();
       if (lane == 0) bar_arrive(bar.p_full(slot, half));   // one a warp: arrivals at one barrier go one by one
     }
+    if (!ok) tmem_stored();   // what was under way when a wait ran out
     // the part of this range: maximum, sum and unnormalised output of every row
     // The last two products may be under way.  A parity tells one phase from the next only: each half has a
     // barrier of its own, whose phase before is over by then.
@@ -544,11 +545,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         if (last_of_tile(i)) commit(bar.v_empty(stage));
         if (i + 2 < steps[slot]) start(i + 2);
       }
-      if (!ok) {   // gave up: let the products in flight end before the tensor memory is given back
-        int never = 0;
-        commit(bar.drained(slot));
-        bar_wait_warp<true>(bar.drained(slot), 0, &never, kDrainNs);
-      }
+      // The products in flight end before the tensor memory is given back, whoever gives up: the slot's softmax may
+      // have when this warp has issued its last.
+      int undrained = 0;
+      commit(bar.drained(slot));
+      if (!bar_wait_warp(bar.drained(slot), 0, &undrained, kDrainNs)) *abort = 1;
     }
     __syncwarp();
   } else {

@@ -800,7 +800,8 @@ typedef struct {
   void *arena;          /* 16-byte aligned                                              */
   void *scales;         /* EMOE_TYPE_E4M3: the scale bytes; otherwise NULL                */
   int32_t *status;      /* optional int32: set to EMOE_ERR_BLOCK_TABLE by a call that met   */
-                        /* a slot or block id outside the pool (never cleared)            */
+                        /* a slot or block id outside the pool, to EMOE_ERR_DEVICE_TIMEOUT  */
+                        /* by emoe_kv_attend (never cleared)                              */
   int32_t n_layers;
   int32_t num_blocks;   /* num_blocks * block_tokens < 2^31                              */
   int32_t block_tokens;
@@ -874,8 +875,9 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
  * type for an e4m3 cache.  own_lens beyond max_blocks * block_tokens count as that, negative ones
  * as 0.  Tokens on a block id outside the pool are left out and reported in the status word.
  * What lies behind a sequence's length - in its last block, in its row of the table, in the pool -
- * has no influence, whatever it holds.  Waits inside the kernel are bounded: should one ever run
- * out, the status word holds EMOE_ERR_DEVICE_TIMEOUT and out is undefined.  prefix_len, and max_blocks as the bound of own_lens, are
+ * has no influence, whatever it holds.  Waits inside the kernels are bounded (wait_limit_us): should one
+ * ever run out, the status word holds EMOE_ERR_DEVICE_TIMEOUT and the rows that waited give NaN.
+ * prefix_len, and max_blocks as the bound of own_lens, are
  * host values; a captured call follows own_lens and the tables from replay to replay.
  * Sizes beyond 2^24 query tokens, 2^28 rows or 2^30 tokens a sequence: EMOE_ERR_TOO_LARGE.
  */
@@ -894,6 +896,10 @@ typedef struct {
   int32_t io_type;             /* EMOE_TYPE_BF16 or _F16                                        */
   float scale;                 /* usually 1 / sqrt(head_dim)                                   */
   uint32_t reserved;           /* zero                                                         */
+  int32_t wait_limit_us;       /* bound of the waits inside the kernels in microseconds; 0: the  */
+                               /* default, 4 s; -1: a wait that is not over when it is first   */
+                               /* polled runs out at once (to exercise that path)              */
+  uint32_t reserved2;          /* zero                                                         */
 } emoe_attend_t;
 emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *cache, int32_t n_seqs, int32_t q_len,
                                        int32_t n_q_heads, int32_t max_blocks, int32_t prefix_len,

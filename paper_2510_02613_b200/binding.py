@@ -81,7 +81,7 @@ class _Attend(ctypes.Structure):
     _fields_ = [("q", _vp), ("out", _vp), ("lse", _vp), ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
                 ("block_table", _vp), ("own_lens", _vp), ("prefix_table", _vp), ("workspace", _vp), ("workspace_bytes", _u64)] + \
                [(n, _i32) for n in ("n_seqs", "q_len", "n_q_heads", "max_blocks", "prefix_len", "io_type")] + \
-               [("scale", ctypes.c_float), ("reserved", _u32)]
+               [("scale", ctypes.c_float), ("reserved", _u32), ("wait_limit_us", _i32), ("reserved2", _u32)]
 
 
 class _ExpertArena(ctypes.Structure):

@@ -34,7 +34,7 @@ constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, 
 constexpr int kSoftmaxRegs = 152, kMmaRegs = 80, kCopyRegs = 128;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
 constexpr int kKept = 4;                   // steps whose masks and scales are kept
-constexpr unsigned long long kWaitNs = 4000000000ull, kDrainNs = 1000000000ull;
+constexpr unsigned long long kDrainNs = 1000000000ull;
 constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
 constexpr uint32_t kColS = 0, kColO = 256; // tensor memory columns: S (and P) of the slots, then O
 
@@ -58,12 +58,26 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// For whole warps: false, in every lane, if the phase does not complete in time or another role has given
-// up.  The lanes agree on each try, so that a wait that is over already costs one try and no divergence.
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {   // without bar_try's own wait
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// For whole warps: false, in every lane, if the phase does not complete within `limit` nanoseconds (0: is not
+// over already) or another role has given up.  The lanes agree on each try, so that a wait that is over already
+// costs one try and no divergence.
 // PATIENT: who has time sleeps between tries and leaves the issue slots to the others.
 template <bool PATIENT = false>
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit = kWaitNs) {
-  if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit) {
+  if (__all_sync(0xffffffffu, bar_test(bar, parity))) return true;
+  if (limit == 0) {
+    *abort = 1;
+    return false;
+  }
   const unsigned long long t0 = now_ns();
   for (;;) {
 #pragma unroll 1
@@ -318,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     float m = -CUDART_INF_F, l = 0.f, v_ref = 0.f;   // v_ref: the largest scale of v so far
     bool ok = true;
     if (steps[slot] > 0) {   // the first step's scores
-      ok = bar_wait_warp(bar.s_full(slot, 0), 0, abort);
+      ok = bar_wait_warp(bar.s_full(slot, 0), 0, abort, a.wait_ns);
       fence_after();
       if (ok && busy) {
         tmem_load(x[0], s_base);
@@ -379,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           v_ref = v_top;
         } else if (__any_sync(0xffffffffu, raise)) {   // O may be touched once the last step's product
           // is done (the one before it is: this step's scores came after that)
-          ok = bar_wait_warp(bar.o_full(slot, (i - 1) & 1), ((i - 1) >> 1) & 1, abort);
+          ok = bar_wait_warp(bar.o_full(slot, (i - 1) & 1), ((i - 1) >> 1) & 1, abort, a.wait_ns);
           if (!ok) break;
           fence_after();
           const float to = top > m + kRaise ? top : m;
@@ -401,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         float safe = m == -CUDART_INF_F ? 0.f : m - kLift;
         const float v_by = FP8 && v_ref > 0.f ? 1.f / v_ref : 0.f;   // powers of two: exact
         if (wait_turn) {
-          ok = bar_wait_warp(bar.turn(slot, warp & 3), (slot ? i : i - 1) & 1, abort);
+          ok = bar_wait_warp(bar.turn(slot, warp & 3), (slot ? i : i - 1) & 1, abort, a.wait_ns);
           if (!ok) break;
           asm volatile("" : "+f"(safe));   // the exponentials stay behind this
         }
@@ -441,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       // The next step's scores are on their way before this one's weights are waited for and announced.  (They
       // were asked for a step ago; were they not done yet, their product does not need these weights.)
       if (i + 1 < steps[slot]) {
-        ok = bar_wait_warp(bar.s_full(slot, half ^ 1), ((i + 1) >> 1) & 1, abort);
+        ok = bar_wait_warp(bar.s_full(slot, half ^ 1), ((i + 1) >> 1) & 1, abort, a.wait_ns);
         if (!ok) break;
         fence_after();
         if (busy) {
@@ -459,13 +473,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
     // The last two products may be under way.  A parity tells one phase from the next only: each half has a
     // barrier of its own, whose phase before is over by then.
     for (int i = max(0, steps[slot] - 2); i < steps[slot] && ok; ++i)
-      ok = bar_wait_warp(bar.o_full(slot, i & 1), (i >> 1) & 1, abort);
+      ok = bar_wait_warp(bar.o_full(slot, i & 1), (i >> 1) & 1, abort, a.wait_ns);
     fence_after();
     const int slots = a.prefix_splits + a.own_splits;
     const int64_t part = row < rows ? output_row(a, 0, head, row0 + row) * slots + (alternate ? 2 * split + slot : split) : 0;
     if (busy && (alternate || slot == 0 || second)) {
+      // what a wait that ran out leaves behind is not a number: a part that counts as empty would go unnoticed
       const bool empty = steps[slot] == 0 || !ok;
-      if (row < rows) a.part_ml[part] = empty ? make_float2(-CUDART_INF_F, 0.f) : make_float2(m - kLift, l);
+      if (row < rows) a.part_ml[part] = empty ? make_float2(-CUDART_INF_F, ok ? 0.f : CUDART_NAN_F) : make_float2(m - kLift, l);
       if (!empty) {
         const float by = FP8 ? v_ref : 1.f;
         float x[HD / 32][32];
@@ -514,13 +529,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
 #pragma unroll
         for (int i = 0; i < kStep / 16; ++i) mma_ts(o_at, s_at + half * kStep + i * 8, v + i * (2048 >> 4), kIdO, add || i > 0);
       };
-      bool ok = bar_wait_warp(bar.q_full(), 0, abort);
+      bool ok = bar_wait_warp(bar.q_full(), 0, abort, a.wait_ns);
       const auto tile_of = [&](int i) { return alternate ? 2 * (i >> 1) + slot : i >> 1; };
       const auto last_of_tile = [&](int i) { return (i & 1) || i + 1 == steps[slot]; };
       const auto start = [&](int i) {   // S of step i
         const int tile = tile_of(i), stage = tile & 1;
         if (!(i & 1)) {
-          ok = ok && bar_wait_warp(bar.k_full(stage), (tile >> 1) & 1, abort);
+          ok = ok && bar_wait_warp(bar.k_full(stage), (tile >> 1) & 1, abort, a.wait_ns);
           if constexpr (!FP8) fence_async();
         }
         if (!ok) return;
@@ -534,10 +549,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
       for (int i = 0; i < steps[slot] && ok; ++i) {
         const int tile = tile_of(i), stage = tile & 1;
         if (!(i & 1)) {
-          ok = bar_wait_warp(bar.v_full(stage), (tile >> 1) & 1, abort);
+          ok = bar_wait_warp(bar.v_full(stage), (tile >> 1) & 1, abort, a.wait_ns);
           if constexpr (!FP8) fence_async();
         }
-        ok = ok && bar_wait_warp(bar.p_full(slot, i & 1), (i >> 1) & 1, abort);
+        ok = ok && bar_wait_warp(bar.p_full(slot, i & 1), (i >> 1) & 1, abort, a.wait_ns);
         if (!ok) break;
         fence_after();
         values(stage, i & 1, i > 0);
@@ -592,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         for (int u = 0; u < 4; ++u) {
           const int v = u >> 1, stage = u & 1, tile = first + stage;
           if (tile >= tiles || !ok) continue;
-          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort, a.wait_ns);
           if (!ok) continue;
           if (v == 0) mark(tile, vec[stage] < 0);
           const uint8_t *const pool = v ? a.c.v : a.c.k;
@@ -607,6 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         }
       }
       copy_async_wait_all();
+      if (!ok) __nanosleep(2000);   // nobody may wait for the arrivals that come behind the copies
     } else {
       // Two buffers of registers, for the even and the odd tiles: while one is widened and stored the
       // other's loads are under way.
@@ -636,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
         for (int u = 0; u < 4; ++u) {
           const int v = u >> 1, stage = u & 1, tile = first + stage;
           if (tile >= tiles || !ok) continue;
-          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort);
+          if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort, a.wait_ns);
           if (!ok) continue;
           if (v == 0) {   // v's scales too: the softmax does not wait for the values
             mark(tile, vec[stage] < 0);

@@ -108,6 +108,7 @@ emoe_status_t check_copy(const emoe_kv_cache_t *c, int32_t layer, const void *k,
 }
 
 constexpr double kLog2e = 1.4426950408889634;
+constexpr unsigned long long kDefaultWaitNs = 4000000000ull;
 
 emoe_status_t check_attend_sizes(const emoe_kv_cache_t *c, int64_t n_seqs, int64_t q_len, int64_t hq, int64_t max_blocks,
                                  int64_t prefix_len) {
@@ -204,7 +205,7 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   TraceRange trace("emoe_kv_attend");
   emoe_status_t st = check_cache_memory(c, layer);
   if (st != EMOE_OK) return st;
-  if (!p || p->reserved) return EMOE_ERR_INVALID_ARG;
+  if (!p || p->reserved || p->reserved2 || p->wait_limit_us < -1) return EMOE_ERR_INVALID_ARG;
   if (p->io_type != EMOE_TYPE_BF16 && p->io_type != EMOE_TYPE_F16) return EMOE_ERR_INVALID_ARG;
   if (c->type != EMOE_TYPE_E4M3 && c->type != p->io_type) return EMOE_ERR_UNSUPPORTED;
   st = check_attend_sizes(c, p->n_seqs, p->q_len, p->n_q_heads, p->max_blocks, p->prefix_len);
@@ -253,6 +254,7 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   a.alternate = s.alternate;
   a.prefix_items = (uint32_t)s.prefix_items;
   a.own_items = (uint32_t)s.own_items;
+  a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;
   return cuda_status(launch_attend(a, c->type, p->io_type, (cudaStream_t)stream));
 }
 

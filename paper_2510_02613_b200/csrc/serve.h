@@ -65,6 +65,7 @@ struct AttendArgs {
   int32_t seq_rows, prefix_splits, prefix_chunk, own_splits, own_chunk;
   int32_t tensor, alternate;
   uint32_t prefix_items, own_items;
+  unsigned long long wait_ns;           // bound of a wait inside a kernel, 0: for nothing
 };
 cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);

@@ -85,7 +85,8 @@ class KvCache:
     emoe_reshard_kv lays it out (head_major: [n_heads][block_tokens] inside a block).  kv_type: "bf16",
     "f16" or "e4m3"; the last has scale bytes [n_layers][2][num_blocks][block_tokens][n_heads] in
     `scales`, a KV arena of head_dim 1 and elem_bytes 1.  status: optional int32 tensor of one element,
-    set to 4 (EMOE_ERR_BLOCK_TABLE) by calls that meet an id outside the pool."""
+    set to 4 (EMOE_ERR_BLOCK_TABLE) by calls that meet an id outside the pool, to 10 (EMOE_ERR_DEVICE_TIMEOUT)
+    by an attend whose bounded waits run out."""
 
     def __init__(self, arena, *, n_layers: int, num_blocks: int, block_tokens: int, n_heads: int, head_dim: int,
                  kv_type: str = "bf16", scales=None, head_major: bool = False, status=None):
@@ -161,12 +162,13 @@ class KvCache:
         return n.value
 
     def attend(self, layer: int, q, out, block_table, own_lens, prefix_table=None, prefix_len: int = 0,
-               scale: Optional[float] = None, lse=None, workspace=None, stream=None) -> None:
+               scale: Optional[float] = None, lse=None, workspace=None, stream=None, wait_limit_us: int = 0) -> None:
         """Decode attention: q, out [n_seqs, q_len, n_q_heads, head_dim] (any stride between tokens); own
         tokens on the blocks of block_table [n_seqs, max_blocks] (int32), own_lens [n_seqs] of them (int32,
         the query tokens included; both None: prefix only); prefix_len tokens on the blocks of
         prefix_table, shared by all sequences.  workspace: attend_workspace_bytes bytes of the caller's,
-        not shared by calls that can overlap.  lse: optional float32 [n_seqs, q_len, n_q_heads]."""
+        not shared by calls that can overlap.  lse: optional float32 [n_seqs, q_len, n_q_heads].
+        wait_limit_us: bound of the waits inside the kernels (0: 4 s)."""
         n, t, hq, _ = q.shape
         _shaped(q, "q", (n, t, hq, self.head_dim), None, self.device)
         if out.dtype != q.dtype:
@@ -193,7 +195,7 @@ class KvCache:
                        None if lse is None else _dense(_shaped(lse, "lse", (n, t, hq), "float32", self.device), "lse", 3).data_ptr(),
                        strides[0], strides[1], bt, ol, pt, None if workspace is None else workspace.data_ptr(),
                        0 if workspace is None else workspace.numel() * workspace.element_size(), n, t, hq, blocks, prefix_len,
-                       _value_type(q, "q"), self.head_dim ** -0.5 if scale is None else scale, 0)
+                       _value_type(q, "q"), self.head_dim ** -0.5 if scale is None else scale, 0, wait_limit_us, 0)
         _check(self._attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
 
 

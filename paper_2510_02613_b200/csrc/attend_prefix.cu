@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      bar_init(bar.k_full(i), kCopyWarps * (FP8 ? 1 : 32));
+      bar_init(bar.k_full(i), kCopyWarps * (FP8 ? 1 : 33));   // copies arrive by the lane; the marks with one arrival more
       bar_init(bar.v_full(i), kCopyWarps * (FP8 ? 1 : 32));
       bar_init(bar.drained(i), 1);
 #pragma unroll
@@ -609,7 +609,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid
           if (tile >= tiles || !ok) continue;
           if (tile >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (tile >> 1) + 1 & 1, abort, a.wait_ns);
           if (!ok) continue;
-          if (v == 0) mark(tile, vec[stage] < 0);
+          if (v == 0) {
+            mark(tile, vec[stage] < 0);
+            if (lane == 0) bar_arrive(bar.k_full(stage));   // the copies' arrivals order the copies only
+          }
           const uint8_t *const pool = v ? a.c.v : a.c.k;
           const uint32_t dst = (v ? v_at : k_at) + stage * kTileBytes;
 #pragma unroll

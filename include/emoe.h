@@ -967,7 +967,8 @@ typedef struct {
   int32_t *ids_out;               /* optional [n_tokens][top_k]: chosen ids, best first, -1    */
   float *weights_out;             /* optional [n_tokens][top_k]: w, 0 beside -1                */
   void *workspace;                /* emoe_moe_decode_workspace bytes                          */
-  uint64_t workspace_bytes;       /* (too few: EMOE_ERR_INVALID_ARG)                          */
+  uint64_t workspace_bytes;       /* (too few: EMOE_ERR_INVALID_ARG); enough for a call is    */
+                                  /* enough for calls of fewer tokens, experts or choices     */
   int64_t x_stride;               /* elements from one token to the next, a multiple of 8      */
   int64_t logits_stride, out_stride;
   int32_t n_tokens, n_experts, n_shared, top_k;

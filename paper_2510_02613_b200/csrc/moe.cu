@@ -775,7 +775,7 @@ cudaError_t launch_layer(MoeArgs a, cudaStream_t st) {
 
 template <typename T, bool FP8>
 cudaError_t by_tokens(const MoeArgs &a, cudaStream_t st) {
-  if (a.n_tokens <= 8) return launch_layer<T, FP8, 1>(a, st);
+  if (a.n_tokens <= kMoeWithRest) return launch_layer<T, FP8, 1>(a, st);
   if (a.n_tokens <= 16) return launch_layer<T, FP8, 2>(a, st);
   if (a.n_tokens <= 32) return launch_layer<T, FP8, 4>(a, st);
   return launch_layer<T, FP8, 8>(a, st);
@@ -791,7 +791,7 @@ MoeShape moe_shape(int d_model, int d_ff, int n_tokens, int top_k, int n_shared,
   s.moved_x = s.token_scale + (moved ? up(n_tokens * 4) : 0);
   s.h = s.moved_x + (moved ? up((int64_t)n_tokens * d_model * 2) : 0);
   s.h_rest = up(pairs * d_ff * 2);
-  s.bytes = s.h + s.h_rest * (n_tokens <= 8 ? 2 : 1);
+  s.bytes = s.h + s.h_rest * (n_tokens <= kMoeWithRest ? 2 : 1);
   return s;
 }
 

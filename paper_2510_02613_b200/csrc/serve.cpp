@@ -275,7 +275,13 @@ emoe_status_t emoe_moe_decode_workspace(const emoe_expert_arena_t *e, int32_t n_
   if (st == EMOE_OK && !bytes) st = EMOE_ERR_INVALID_ARG;
   if (st == EMOE_OK) st = check_moe_sizes(e, n_tokens, top_k, n_experts, n_shared);
   if (st != EMOE_OK) return st;
-  *bytes = n_tokens ? moe_shape(e->d_model, e->d_ff, n_tokens, top_k, n_shared, e->type == EMOE_TYPE_E4M3).bytes : 0;
+  // Calls of up to kMoeWithRest tokens keep more for each: the most that this many or fewer need.
+  *bytes = 0;
+  for (int n : {n_tokens, n_tokens < kMoeWithRest ? n_tokens : kMoeWithRest})
+    if (n) {
+      const uint64_t need = moe_shape(e->d_model, e->d_ff, n, top_k, n_shared, e->type == EMOE_TYPE_E4M3).bytes;
+      if (need > *bytes) *bytes = need;
+    }
   return EMOE_OK;
 }
 

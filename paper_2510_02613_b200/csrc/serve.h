@@ -70,6 +70,8 @@ struct AttendArgs {
 cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
+// Calls of up to so many tokens keep what rounding takes from the hidden vectors.
+constexpr int kMoeWithRest = 8;
 // Byte offsets of a layer call's workspace.  moved: e4m3 weights, whose bf16 tokens are kept in f16 by a power
 // of two each.
 struct MoeShape {

@@ -234,6 +234,7 @@ class ExpertArena:
         return n.value
 
     def decode_workspace_bytes(self, n_tokens: int, top_k: int, n_experts: int, n_shared: int = 0) -> int:
+        """Enough for calls of up to these sizes."""
         n = ctypes.c_uint64()
         _check(_b.lib().emoe_moe_decode_workspace(self._ref, n_tokens, top_k, n_experts, n_shared, ctypes.byref(n)))
         return n.value

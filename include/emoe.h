@@ -891,7 +891,8 @@ typedef struct {
   const int32_t *own_lens;     /* [n_seqs]: own tokens, the query tokens included                */
   const int32_t *prefix_table; /* [ceil(prefix_len / block_tokens)]; NULL with prefix_len = 0    */
   void *workspace;             /* emoe_kv_attend_workspace bytes                                */
-  uint64_t workspace_bytes;    /* (too few: EMOE_ERR_INVALID_ARG)                               */
+  uint64_t workspace_bytes;    /* (too few: EMOE_ERR_INVALID_ARG); enough for a call is enough  */
+                               /* for calls with less of any of its five arguments             */
   int32_t n_seqs, q_len, n_q_heads, max_blocks, prefix_len;
   int32_t io_type;             /* EMOE_TYPE_BF16 or _F16                                        */
   float scale;                 /* usually 1 / sqrt(head_dim)                                   */

@@ -8,6 +8,9 @@
 // heads times the query tokens - of the whole batch for the prefix, which is thereby read once, and
 // of one sequence for that sequence's own tokens.  When there are few rows the token axis is split
 // until the machine is full; a second kernel joins the splits.
+#include <algorithm>
+#include <cmath>
+
 #include "attend_item.cuh"
 
 namespace emoe {
@@ -560,16 +563,32 @@ cudaError_t by_head_dim(const AttendArgs &a, cudaStream_t st) {
 
 }  // namespace
 
+namespace {
+
+constexpr int kMostSplits = 64;
+// Whether the prefix goes to the tensor core kernel.  It starts later and ends earlier than the other one and takes 256 rows
+// at once.  They meet at about 2^17 row tiles
+// (of 16 rows) x tokens.  The whole call, this kernel and the other one, 4 KV heads, head_dim 128:
+//   64 rows, 2000 tokens (2^15): bf16 21.5 and 15.4 us, e4m3 25.6 and 17.4
+//   128 rows, 2000 tokens (2^16): 25.6 and 21.5, 31.7 and 25.6;  17 rows, 16000 (2^17): 27.6 and 27.8, 33.8 and 33.8
+//   384 rows, 2000 (1.5 x 2^17): 27.6 and 29.7, 31.7 and 37.9;  384 rows, 16000: 42 and 120, 54 and 132
+bool prefix_on_tensor(int n_heads, int64_t batch_rows, int head_dim, int prefix_len) {
+  return (head_dim == 64 || head_dim == 128) && batch_rows > 16 && n_heads * ((batch_rows + 15) / 16) * prefix_len >= 1 << 17;
+}
+
+}  // namespace
+
 AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len) {
   AttendShape s{};
   s.seq_rows = q_len * (n_q_heads / n_heads);
   const int64_t unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>);
   // Row tiles over up to `tokens` tokens (how many there really are is known on the device only): splits are whole
   // steps of the four warps, as many as make the sum of all the work over two blocks an SM, an item's start and
-  // end counting as 96 tokens, and of the last item least.
+  // end counting as 96 tokens, and of the last item least.  (That is at about n = sqrt(3 tokens / tiles), and was never
+  // met beyond sqrt(17 tokens / tiles): the bound is for attend_parts.)
   const auto cut = [&](int64_t tiles, int64_t tokens, int32_t &splits, int32_t &chunk) {
     int64_t best = unit * ((tokens + unit - 1) / unit), cost = INT64_MAX;
-    for (int64_t n = 1; n <= 64 && (n == 1 || (n - 1) * unit < tokens); ++n) {
+    for (int64_t n = 1; n <= kMostSplits && (n == 1 || ((n - 1) * unit < tokens && n * n * tiles <= 20 * tokens)); ++n) {
       const int64_t c = ((tokens + n - 1) / n + unit - 1) / unit * unit;
       const int64_t t = tiles * n * (c + 96) / (2 * kSms) + c;
       if (t < cost) cost = t, best = c;
@@ -578,21 +597,17 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int 
     splits = tokens ? (int32_t)((tokens + chunk - 1) / chunk) : 1;
   };
   const int64_t batch_rows = (int64_t)n_seqs * s.seq_rows;
-  // The other kernel starts later and ends earlier; this one takes 256 rows at once.  They meet at about 2^17 row tiles
-  // (of 16 rows) x tokens.  The whole call, this kernel and the other one, 4 KV heads, head_dim 128:
-  //   64 rows, 2000 tokens (2^15): bf16 21.5 and 15.4 us, e4m3 25.6 and 17.4
-  //   128 rows, 2000 tokens (2^16): 25.6 and 21.5, 31.7 and 25.6;  17 rows, 16000 (2^17): 27.6 and 27.8, 33.8 and 33.8
-  //   384 rows, 2000 (1.5 x 2^17): 27.6 and 29.7, 31.7 and 37.9;  384 rows, 16000: 42 and 120, 54 and 132
-  const int64_t work = n_heads * ((batch_rows + 15) / 16) * prefix_len;
-  if ((head_dim == 64 || head_dim == 128) && batch_rows > 16 && work >= 1 << 17) {
+  if (prefix_on_tensor(n_heads, batch_rows, head_dim, prefix_len)) {
     // Blocks of up to 256 rows, one an SM: the number of splits with the fewest steps one after the
-    // other, a block's start and end counting as two.
+    // other, a block's start and end counting as two.  Beyond two blocks an SM 16 of them are enough: more would save 0.2%
+    // of the steps on average and fill the workspace.
     s.tensor = 1;
     s.alternate = batch_rows <= 128;
     const int64_t units = n_heads * ((batch_rows + 255) / 256);
     const int64_t tiles = (prefix_len + 127) / 128, steps = s.alternate ? (tiles + 1) / 2 : tiles;
-    int64_t best = 1, cost = INT64_MAX;
-    for (int64_t n = 1; n <= 64 && n <= steps; ++n) {
+    int64_t best = 1, cost = INT64_MAX, most = s.alternate ? 8 : 16;   // two parts a block
+    if (2 * kSms / units > most) most = 2 * kSms / units;
+    for (int64_t n = 1; n <= kMostSplits && n <= steps && n <= most; ++n) {
       const int64_t c = ((units * n + kSms - 1) / kSms) * ((steps + n - 1) / n + 2);
       if (c < cost) cost = c, best = n;
     }
@@ -614,6 +629,28 @@ AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int 
   const int64_t rows = (int64_t)n_seqs * q_len * n_q_heads, slots = s.prefix_splits + s.own_splits;
   s.parts = s.tensor || slots > 1 ? rows * slots : 0;
   return s;
+}
+
+int64_t attend_parts(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len) {
+  const int64_t rows = (int64_t)n_seqs * q_len * n_q_heads, unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>);
+  // The row kernel's splits n are 1, or at most sqrt(20 tokens / tiles) with tiles >= rows / 16.
+  const auto most_splits = [&](int64_t tokens) { return std::min<int64_t>(kMostSplits, (tokens + unit - 1) / unit); };
+  const auto of_rows_x_tokens = [](double n) { return (int64_t)std::sqrt(320.0 * n) + 1; };
+  const auto on_rows = [&](int64_t r, int64_t tokens) {
+    return tokens ? std::max(r, std::min(r * most_splits(tokens), of_rows_x_tokens((double)r * tokens))) : 0;
+  };
+  int64_t prefix = on_rows(rows, prefix_len), slots = most_splits(prefix_len) + most_splits(own_max);
+  if (prefix_on_tensor(n_heads, (int64_t)n_seqs * q_len * (n_q_heads / n_heads), head_dim, prefix_len)) {
+    // Smaller calls that stay with the row kernel have up to 16 rows a head, or up to 2^17 row tiles x tokens.
+    const int64_t left = std::max(on_rows(std::min<int64_t>(rows, 16 * (int64_t)n_heads), prefix_len), of_rows_x_tokens(16 << 17));
+    // The others have units >= rows / 256, a block each, and up to 16 splits or 2 kSms / units; with alternating tiles units
+    // >= rows / 128, 8 splits or 2 kSms / units, and two parts a split.
+    const int64_t tiles = (prefix_len + 127) / 128;
+    const int64_t tensor = std::min(rows * std::min<int64_t>(2 * kMostSplits, tiles + 1), std::max<int64_t>(16 * rows, 2 * kSms * 256));
+    prefix = std::max({rows, std::min(prefix, left), tensor});
+    slots = 2;
+  }
+  return slots > 1 ? prefix + on_rows(rows, own_max) : 0;
 }
 
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st) {

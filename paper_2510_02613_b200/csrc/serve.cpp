@@ -196,8 +196,9 @@ emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *c, int32_t n_seqs,
   if (st != EMOE_OK) return st;
   *bytes = 0;
   if (n_seqs == 0) return EMOE_OK;
-  const AttendShape s = attend_shape(c->n_heads, n_seqs, q_len, n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3, (int64_t)max_blocks * c->block_tokens, prefix_len);
-  *bytes = up_256(s.parts * sizeof(float2)) + up_256(s.parts * c->head_dim * sizeof(float));
+  const int64_t parts = attend_parts(c->n_heads, n_seqs, q_len, n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
+                                     (int64_t)max_blocks * c->block_tokens, prefix_len);
+  *bytes = up_256(parts * sizeof(float2)) + up_256(parts * c->head_dim * sizeof(float));
   return EMOE_OK;
 }
 

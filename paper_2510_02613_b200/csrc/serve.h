@@ -49,6 +49,8 @@ struct AttendShape {
   int64_t parts;                        // (row, split) pairs that go through the workspace; 0: none
 };
 AttendShape attend_shape(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len);
+// The most `parts` of a call of up to these sizes: grows with each of them (n_heads and head_dim are the cache's).
+int64_t attend_parts(int n_heads, int n_seqs, int q_len, int n_q_heads, int head_dim, bool e4m3, int64_t own_max, int prefix_len);
 
 struct AttendArgs {
   KvLayer c;

@@ -157,6 +157,7 @@ class KvCache:
         _check(self._gather(self._ref, layer, slots.data_ptr(), n, kp, vp, ks, vs, t, _stream_handle(stream)))
 
     def attend_workspace_bytes(self, n_seqs: int, q_len: int, n_q_heads: int, max_blocks: int, prefix_len: int = 0) -> int:
+        """Enough for calls of up to these sizes on this cache."""
         n = ctypes.c_uint64()
         _check(_b.lib().emoe_kv_attend_workspace(self._ref, n_seqs, q_len, n_q_heads, max_blocks, prefix_len, ctypes.byref(n)))
         return n.value

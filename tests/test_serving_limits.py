@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 
+import numpy as np
 import pytest
 
 import paper_2510_02613_b200 as E
@@ -31,3 +32,37 @@ def test_a_layer_workspace_is_enough_for_fewer_tokens(w):
         for m in range(1, n + 1):
             p.n_tokens = m
             assert B.lib().emoe_moe_decode(ctypes.byref(arena), 0, ctypes.byref(p), None) == 8     # only the arena is at fault
+
+
+def _sizes(rng, heads):
+    log = lambda lo, hi: int(2.0 ** rng.uniform(np.log2(lo), np.log2(hi)))    # noqa: E731
+    return [log(1, 400), int(rng.integers(1, 5)), heads * log(1, 17), log(1, 300) if rng.random() < 0.8 else 0,
+            log(1, 200000) if rng.random() < 0.7 else 0]
+
+
+@pytest.mark.parametrize("head_dim,kv", [(128, "bf16"), (64, "e4m3"), (256, "bf16"), (32, "e4m3")])
+def test_an_attention_workspace_is_enough_for_smaller_calls(head_dim, kv):
+    rng = np.random.default_rng(head_dim)
+    for _ in range(1200):
+        heads, block = int(2 ** rng.integers(0, 6)), int(rng.choice([1, 7, 16, 64]))
+        scales = (1 << 24) if kv == "e4m3" else None
+        c = E.KvCache(1 << 24, n_layers=1, num_blocks=1 << 20, block_tokens=block, n_heads=heads, head_dim=head_dim, kv_type=kv, scales=scales)
+        raw = B._KvCache(1 << 24, scales, None, 1, 1 << 20, block, heads, head_dim, c.kv_type, 0, 0)
+        size = _sizes(rng, heads)
+        bytes_ = c.attend_workspace_bytes(*size)
+        assert bytes_ <= 16 * 520 * (9 << 20)     # and not out of all proportion
+        for _ in range(40):
+            less = [int(x * 2.0 ** -rng.uniform(0, 8 * (rng.random() < 0.5))) for x in size]
+            less = [max(1, less[0]), max(1, less[1]), max(heads, less[2] // heads * heads)] + less[3:]
+            assert c.attend_workspace_bytes(*less) <= bytes_
+            n, t, hq, blocks, prefix = less
+            p = B._Attend(1 << 20, 1 << 21, None, hq * head_dim, hq * head_dim, 1 << 22, 1 << 23, 1 << 25, 1 << 28, bytes_, n, t, hq, blocks,
+                          prefix, 0, 0.125, 0)
+            # refused for the arena, which is no memory of a device, and not for the workspace
+            assert B.lib().emoe_kv_attend(ctypes.byref(raw), 0, ctypes.byref(p), None) == 8, (size, less)
+
+
+def test_attention_workspaces_of_usual_calls():
+    c = E.KvCache(1 << 20, n_layers=1, num_blocks=50000, block_tokens=16, n_heads=4, head_dim=128)
+    mib = [c.attend_workspace_bytes(*x) / 2 ** 20 for x in ((128, 1, 32, 172, 65536), (64, 1, 32, 172, 0), (1, 1, 32, 512, 0), (1, 1, 32, 4, 0))]
+    assert mib[0] < 80 and mib[1] < 25 and mib[2] < 2 and mib[3] == 0

@@ -40,8 +40,21 @@ def _value_type(t, what: str) -> int:
 _names: dict = {}   # torch dtype -> its name
 
 
-def _shaped(t, what: str, shape, dtype: Optional[str] = None, device=None):
-    """t itself; ValueError unless it has this shape (None: any size), type and device."""
+def _placed(t, what: str, device) -> None:
+    """ValueError unless t lies where the arena does (device None: the arena was given as an address, which the
+    call itself looks for on the current device)."""
+    if device is None:
+        if not t.is_cuda:
+            raise ValueError("%s is on %s, the arena on a CUDA device" % (what, t.device))
+        import torch
+        if t.get_device() != torch.cuda.current_device():
+            raise ValueError("%s is on %s, which is not the current device" % (what, t.device))
+    elif t.device != device:
+        raise ValueError("%s is on %s, the arena on %s" % (what, t.device, device))
+
+
+def _shaped(t, what: str, shape, dtype: Optional[str], device):
+    """t itself; ValueError unless it has this shape (None: any size), type and place."""
     if len(t.shape) != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
         raise ValueError("%s: shape %s, wanted %s" % (what, tuple(t.shape), tuple("any" if w is None else w for w in shape)))
     if dtype is not None:
@@ -50,8 +63,7 @@ def _shaped(t, what: str, shape, dtype: Optional[str] = None, device=None):
             name = _names[t.dtype] = str(t.dtype)[6:]
         if name != dtype:
             raise ValueError("%s: %s, wanted %s" % (what, name, dtype))
-    if device is not None and t.device != device:
-        raise ValueError("%s is on %s, the arena on %s" % (what, t.device, device))
+    _placed(t, what, device)
     return t
 
 
@@ -65,6 +77,16 @@ def _dense(t, what: str, inner: int):
             raise ValueError("%s: its last %d dimensions have to be contiguous" % (what, inner))
         step *= n
     return t
+
+
+def _workspace(t, device):
+    """(address, bytes) of a workspace or None."""
+    if t is None:
+        return None, 0
+    _placed(t, "workspace", device)
+    if not t.is_contiguous():
+        raise ValueError("workspace: not contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _arena_pointer(arena, need: int, what: str):
@@ -101,9 +123,10 @@ class KvCache:
             self._c.scales, device = _arena_pointer(scales, sizes[1], "scales")
             if None not in (device, self.device) and device != self.device:
                 raise ValueError("scales are on %s, the arena on %s" % (device, self.device))
+            self.device = self.device or device
         if status is not None:
-            _shaped(status, "status", (1,), "int32", self.device)
-            self._c.status = status.data_ptr()
+            self.device = self.device or status.device
+            self._c.status = _shaped(status, "status", (1,), "int32", self.device).data_ptr()
         self._keep = (arena, scales, status)
         self._ref = ctypes.byref(self._c)
         self._row = n_heads * head_dim
@@ -129,7 +152,7 @@ class KvCache:
         return _b.lib().emoe_kv_vector_index(self._ref, layer, kv, slot, head)
 
     def _rows(self, x, what, n):
-        if x.shape != (n, self.n_heads, self.head_dim) or (self.device is not None and x.device != self.device):
+        if x.shape != (n, self.n_heads, self.head_dim) or x.device != self.device:
             _shaped(x, what, (n, self.n_heads, self.head_dim), None, self.device)
         if x.is_contiguous():
             return x.data_ptr(), self._row
@@ -194,8 +217,7 @@ class KvCache:
             pt = prefix_table.data_ptr()
         p = _b._Attend(q.data_ptr(), out.data_ptr(),
                        None if lse is None else _dense(_shaped(lse, "lse", (n, t, hq), "float32", self.device), "lse", 3).data_ptr(),
-                       strides[0], strides[1], bt, ol, pt, None if workspace is None else workspace.data_ptr(),
-                       0 if workspace is None else workspace.numel() * workspace.element_size(), n, t, hq, blocks, prefix_len,
+                       strides[0], strides[1], bt, ol, pt, *_workspace(workspace, self.device), n, t, hq, blocks, prefix_len,
                        _value_type(q, "q"), self.head_dim ** -0.5 if scale is None else scale, 0, wait_limit_us, 0)
         _check(self._attend(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
 
@@ -216,8 +238,8 @@ class ExpertArena:
         self.w_type, self.d_model, self.d_ff, self.n_slots = self._c.type, d_model, d_ff, n_slots
         self._c.arena, self.device = _arena_pointer(arena, self.bytes(), "arena")
         if status is not None:
-            _shaped(status, "status", (1,), "int32", self.device)
-            self._c.status = status.data_ptr()
+            self.device = self.device or status.device
+            self._c.status = _shaped(status, "status", (1,), "int32", self.device).data_ptr()
         self._keep = (arena, status)
         self._ref = ctypes.byref(self._c)
         self._decode = _b.lib().emoe_moe_decode
@@ -256,8 +278,7 @@ class ExpertArena:
                 _dense(_shaped(t, what, (n, top_k), dtype, self.device), what, 2)
         p = _b._Moe(x.data_ptr(), logits.data_ptr(), slot_of_expert.data_ptr(), out.data_ptr(),
                     None if ids_out is None else ids_out.data_ptr(), None if weights_out is None else weights_out.data_ptr(),
-                    None if workspace is None else workspace.data_ptr(),
-                    0 if workspace is None else workspace.numel() * workspace.element_size(),
+                    *_workspace(workspace, self.device),
                     x.stride(0), logits.stride(0), out.stride(0), n, experts, n_shared, top_k,
                     _value_type(x, "x"), _value_type(out, "out"), 1 if renormalize else 0, routed_scale, 0)
         _check(self._decode(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))

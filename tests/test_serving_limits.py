@@ -5,6 +5,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2510_02613_b200 as E
 from paper_2510_02613_b200 import binding as B
@@ -66,3 +67,48 @@ def test_attention_workspaces_of_usual_calls():
     c = E.KvCache(1 << 20, n_layers=1, num_blocks=50000, block_tokens=16, n_heads=4, head_dim=128)
     mib = [c.attend_workspace_bytes(*x) / 2 ** 20 for x in ((128, 1, 32, 172, 65536), (64, 1, 32, 172, 0), (1, 1, 32, 512, 0), (1, 1, 32, 4, 0))]
     assert mib[0] < 80 and mib[1] < 25 and mib[2] < 2 and mib[3] == 0
+
+
+def _handles(arena):
+    """(cache, its attend arguments, experts, their decode arguments), tensors on the CPU."""
+    size = 2 * 8 * 4 * 2 * 64 * 2
+    cache = E.KvCache(torch.zeros(size, dtype=torch.uint8) if arena is None else arena, n_layers=1, num_blocks=8, block_tokens=4, n_heads=2, head_dim=64)
+    q, table = torch.zeros(3, 1, 4, 64, dtype=torch.bfloat16), torch.zeros(3, 2, dtype=torch.int32)
+    attend_args = dict(q=q, out=q.clone(), block_table=table, own_lens=torch.zeros(3, dtype=torch.int32))
+    experts = E.ExpertArena(torch.zeros(3 * 6 * 64 * 32 * 2, dtype=torch.uint8) if arena is None else arena, n_layers=1, n_slots=6, d_model=64, d_ff=32)
+    x = torch.zeros(3, 64, dtype=torch.bfloat16)
+    decode_args = dict(x=x, logits=torch.zeros(3, 8), top_k=2, slot_of_expert=torch.zeros(8, dtype=torch.int32), out=x.clone())
+    return cache, attend_args, experts, decode_args
+
+
+def test_workspaces_are_checked():
+    """A workspace has to lie where the arena does, in one piece."""
+    cache, a, experts, d = _handles(None)
+    for work in (torch.empty(1 << 20, dtype=torch.uint8, device="meta"), torch.empty(1 << 20, dtype=torch.uint8)[::2],
+                 torch.empty(1, dtype=torch.uint8).expand(1 << 20)):
+        with pytest.raises(ValueError, match="workspace"):
+            cache.attend(0, **a, workspace=work)
+        with pytest.raises(ValueError, match="workspace"):
+            experts.decode(0, **d, workspace=work)
+
+
+def test_tensors_beside_an_arena_given_as_an_address():
+    """Nothing says where it lies; a CPU tensor is refused all the same, before its address reaches a kernel."""
+    cache, a, experts, d = _handles(1 << 24)
+    k, slots = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="cpu"):
+        cache.attend(0, **a)
+    with pytest.raises(ValueError, match="cpu"):
+        cache.append(0, k, k, slots)
+    with pytest.raises(ValueError, match="cpu"):
+        cache.gather(0, slots, k, k.clone())
+    with pytest.raises(ValueError, match="cpu"):
+        experts.decode(0, **d)
+
+
+def test_a_status_word_tells_where_an_arena_lies():
+    status = torch.zeros(1, dtype=torch.int32, device="meta")
+    cache = E.KvCache(1 << 24, n_layers=1, num_blocks=8, block_tokens=4, n_heads=2, head_dim=64, status=status)
+    assert cache.device == status.device
+    with pytest.raises(ValueError, match="cpu"):
+        cache.append(0, torch.zeros(1, 2, 64), torch.zeros(1, 2, 64), torch.zeros(1, dtype=torch.int64, device="meta"))

@@ -895,7 +895,7 @@ typedef struct {
                                /* for calls with less of any of its five arguments             */
   int32_t n_seqs, q_len, n_q_heads, max_blocks, prefix_len;
   int32_t io_type;             /* EMOE_TYPE_BF16 or _F16                                        */
-  float scale;                 /* usually 1 / sqrt(head_dim)                                   */
+  float scale;                 /* usually 1 / sqrt(head_dim); finite, up to 2^127               */
   uint32_t reserved;           /* zero                                                         */
   int32_t wait_limit_us;       /* bound of the waits inside the kernels in microseconds; 0: the  */
                                /* default, 4 s; -1: a wait that is not over when it is first   */

@@ -2,6 +2,8 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <cmath>
+
 #include "serve.h"
 
 using namespace emoe;
@@ -208,6 +210,8 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   if (st != EMOE_OK) return st;
   if (!p || p->reserved || p->reserved2 || p->wait_limit_us < -1) return EMOE_ERR_INVALID_ARG;
   if (p->io_type != EMOE_TYPE_BF16 && p->io_type != EMOE_TYPE_F16) return EMOE_ERR_INVALID_ARG;
+  const float scale_log2 = (float)(p->scale * kLog2e);
+  if (!std::isfinite(scale_log2)) return EMOE_ERR_INVALID_ARG;
   if (c->type != EMOE_TYPE_E4M3 && c->type != p->io_type) return EMOE_ERR_UNSUPPORTED;
   st = check_attend_sizes(c, p->n_seqs, p->q_len, p->n_q_heads, p->max_blocks, p->prefix_len);
   if (st != EMOE_OK || p->n_seqs == 0) return st;
@@ -245,7 +249,7 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   a.group = p->n_q_heads / c->n_heads;
   a.max_blocks = p->max_blocks;
   a.prefix_len = p->prefix_len;
-  a.scale_log2 = (float)(p->scale * kLog2e);
+  a.scale_log2 = scale_log2;
   a.seq_rows = s.seq_rows;
   a.prefix_splits = s.prefix_splits;
   a.prefix_chunk = s.prefix_chunk;

@@ -112,3 +112,9 @@ def test_a_status_word_tells_where_an_arena_lies():
     assert cache.device == status.device
     with pytest.raises(ValueError, match="cpu"):
         cache.append(0, torch.zeros(1, 2, 64), torch.zeros(1, 2, 64), torch.zeros(1, dtype=torch.int64, device="meta"))
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38, -3e38])
+def test_an_attention_scale_is_finite(scale):
+    """The two kernels would answer such calls differently.  (3e38 is not finite any more as a factor of exponents of 2.)"""
+    assert attend(scale=scale) == 1

@@ -834,7 +834,8 @@ int64_t emoe_kv_vector_index(const emoe_kv_cache_t *cache, int32_t layer, int32_
  * slots: int64 [n_tokens].  A negative slot skips its token; one beyond the pool is skipped
  *   and reported in the status word.  A slot may be listed once; listed twice, its vectors
  *   (and nothing else) are undefined.
- * head_dim: a multiple of 8, at most 256 (EMOE_ERR_UNSUPPORTED).
+ * head_dim: a multiple of 8, at most 256 (EMOE_ERR_UNSUPPORTED).  n_tokens * n_heads below 2^31, a
+ * token's k or v below 4 GB (EMOE_ERR_TOO_LARGE).
  *
  * Quantisation of a vector x with a = max |x_i|: 2^k is the smallest power of two with
  * a <= 448 * 2^k, k >= -126 (k = 0 for a zero vector); the codes are x_i * 2^-k rounded to

@@ -102,8 +102,9 @@ emoe_status_t check_copy(const emoe_kv_cache_t *c, int32_t layer, const void *k,
   if (n == 0) return EMOE_OK;
   if (!k || !v || !slots) return EMOE_ERR_INVALID_ARG;
   const int64_t row = (int64_t)c->n_heads * c->head_dim;
-  if (n > 1 && (ks < row || vs < row)) return EMOE_ERR_SHAPE;
   const int size = type_bytes(io);
+  if (row * size >= (int64_t)1 << 32) return EMOE_ERR_TOO_LARGE;   // places inside a token are kept in 32 bits
+  if (n > 1 && (ks < row || vs < row)) return EMOE_ERR_SHAPE;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return EMOE_ERR_ALIGNMENT;
   if (n > 1 && (ks * size % 16 || vs * size % 16)) return EMOE_ERR_ALIGNMENT;
   return on_current_device(c->arena);

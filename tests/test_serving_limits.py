@@ -10,6 +10,7 @@ import torch
 import paper_2510_02613_b200 as E
 from paper_2510_02613_b200 import binding as B
 from test_serving_attend import _call as attend
+from test_serving_kv import _call as copy
 
 
 @pytest.mark.parametrize("change", [dict(wait_limit_us=-2), dict(wait_limit_us=-(1 << 31)), dict(reserved2=1)])
@@ -118,3 +119,11 @@ def test_a_status_word_tells_where_an_arena_lies():
 def test_an_attention_scale_is_finite(scale):
     """The two kernels would answer such calls differently.  (3e38 is not finite any more as a factor of exponents of 2.)"""
     assert attend(scale=scale) == 1
+
+
+@pytest.mark.parametrize("fn", ["emoe_kv_append", "emoe_kv_gather"])
+def test_places_inside_a_token_fit_32_bits(fn):
+    big = dict(n_heads=1 << 23, head_dim=128, num_blocks=1, ks=1 << 30, vs=1 << 30)
+    for n in (1, 2):
+        assert copy(fn, io=2, n=n, **big) == 11            # 4 GB a token
+        assert copy(fn, io=0, n=n, **big) == 8             # 2 GB: refused for the arena only

@@ -55,6 +55,8 @@ def _placed(t, what: str, device) -> None:
 
 def _shaped(t, what: str, shape, dtype: Optional[str], device):
     """t itself; ValueError unless it has this shape (None: any size), type and place."""
+    if t is None:
+        raise ValueError("%s is missing" % what)
     if len(t.shape) != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)):
         raise ValueError("%s: shape %s, wanted %s" % (what, tuple(t.shape), tuple("any" if w is None else w for w in shape)))
     if dtype is not None:

@@ -127,3 +127,10 @@ def test_places_inside_a_token_fit_32_bits(fn):
     for n in (1, 2):
         assert copy(fn, io=2, n=n, **big) == 11            # 4 GB a token
         assert copy(fn, io=0, n=n, **big) == 8             # 2 GB: refused for the arena only
+
+
+def test_missing_tensors_are_named():
+    cache, a, _, _ = _handles(None)
+    for bad, what in ((dict(own_lens=None), "own_lens"), (dict(block_table=None), "block_table"), (dict(prefix_len=5), "prefix_table")):
+        with pytest.raises(ValueError, match=what + " is missing"):
+            cache.attend(0, **{**a, **bad})

@@ -115,3 +115,25 @@ def test_tiny_queries_on_large_keys(rows, heads):
     v = np.abs(ref.values[0, 1].reshape(-1, heads, 128)).sum(0)
     tol = 1.05 * (2 * 2.0 ** -8 + 2 * (e + size)[..., None]) * a + 2.0 ** -31 * v[None, None]
     assert (np.abs(out.double().cpu().numpy() - o) <= tol).all()
+
+
+@pytest.mark.parametrize("rows,heads", [(4, 1), (33, 24)])
+def test_values_far_below_the_16_bit_ones(rows, heads):
+    """Values of 2^-24 and less in an e4m3 cache, with bf16 outputs, which reach as far: nothing is lost (24 heads x
+    3 row tiles x 2000 tokens: the tensor core path)."""
+    from test_gpu_serving_prefix_wide import definition, wide
+    rng = np.random.default_rng(12)
+    ref = wide(rng, (1, 125, 16, heads), 128, "e4m3")
+    pt = np.arange(125, dtype=np.int32)
+    q = torch.from_numpy(rng.standard_normal((rows, 1, heads, 128)) * 0.2).to(torch.bfloat16).cuda()
+    for low, high in ((127 - 33, 127 - 33), (127 - 100, 127 - 100), (1, 1), (127 - 60, 127 - 33)):
+        ref.bytes[:, 1] = rng.integers(low, high + 1, ref.bytes[:, 1].shape)
+        c, _, _ = device_cache(ref)
+        out, _ = call(c, q, pt=pt, prefix=2000)
+        o, _, a, e = definition(ref, 0, q.double().cpu().numpy(), np.zeros((rows, 0), np.int32), [0] * rows, pt, 2000, 128 ** -0.5)
+        v = np.abs(ref.values[0, 1].reshape(-1, heads, 128)).sum(0)
+        top = 2.0 ** (int(ref.bytes[0, 1].max()) - 127)
+        # bf16's own smallest step, 2^-133, beside the tolerance of the tests above
+        tol = 1.05 * (2 * 2.0 ** -8 + 2 * e[..., None]) * a + 2.0 ** -31 * top * v[None, None] + 2.0 ** -134
+        assert np.mean(np.abs(o) > tol) > 0.7      # an output of zeros would not pass
+        assert (np.abs(out.double().cpu().numpy() - o) <= tol).all()

@@ -74,8 +74,8 @@ __device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int 
 // item as the m side (rows that do not exist are zero), running maximum and sum in registers.  The
 // four warps take every fourth group of tokens and are joined at the end.  Bound by the reads of K
 // and V: 2 stages x 4 warps x 8 KB and three blocks an SM have 192 KB of ring there (head_dim 128).  Measured, 32 sequences
-// of 3000 tokens, 16 heads: bf16 132 us, 6.0 TB/s; e4m3 129 us, 3.1 TB/s - there the conversion of the codes bounds it, on the
-// integer and conversion pipes.  Short calls are bound by an item's start and end (48 x 625 tokens, 4 heads: 2.3 TB/s).
+// of 3000 tokens, 16 heads: bf16 132 us, 6.0 TB/s; e4m3 132 us, 3.0 TB/s - there no pipe is full (issue slots 51%, integer
+// pipe 42%, DRAM 37%): it is the chain of a step, with three warps a scheduler.  Short calls are bound by an item's start and end (48 x 625 tokens, 4 heads: 2.3 TB/s).
 template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   using T = typename Operand<IO, FP8>::type;

@@ -331,7 +331,7 @@ __device__ __forceinline__ void step_product(float (&acc)[4], const uint4 (&w)[4
 // With e4m3 weights and up to 16 tokens the second tile's tokens are read straight from L2 ahead of the wait
 // for the step's weights: in a stage of the ring (three of 4 KB) they would halve the steps that the weights run
 // ahead (16 tokens, 14 experts of 7168 x 2048: 144 us, through the ring 159).  Everywhere else they come through the ring
-// (64 tokens, 126 bf16 experts of 2048 x 768: 189 us, straight from L2 207; 20 of 7168 x 2048, two of them with all
+// (64 tokens, about 108 bf16 experts of 2048 x 768: 189 us, straight from L2 207; 20 of 7168 x 2048, two of them with all
 // tokens: 341 and 527).
 template <bool FP8, int NT> constexpr bool kDirect = FP8 && NT == 2;
 
@@ -395,10 +395,11 @@ template <int NT> constexpr bool kWithRest = NT == 1;
 // h[pair] = w silu(gate) up, rounded once to IO.  An item is 8 rows of gate and the same 8 of up as one
 // 16-row operand, so a thread gets both sums of its outputs.  The k axis is split over the warps,
 // joined in shared memory in the order of the warps.  NT: column tiles of 8 tokens an expert may have.  Two blocks
-// an SM with 64 KB of weights and 32 KB of tokens in their rings each; bound by the weights: 680 MB (126 bf16 experts of
-// 2 x 768 x 2048, 64 tokens) in 120 us, 5.7 TB/s, 69% of the memory's nominal rate.  e4m3 weights: 3.6 to 4.5 TB/s, bound
-// by widening the codes.  Items dealt by a counter in memory instead of in turn: 2% faster there, 8% slower
-// for 14 e4m3 experts.
+// an SM with 64 KB of weights and 32 KB of tokens in their rings each; bound by the weights: 680 MB (108 bf16 experts of
+// 2 x 768 x 2048, 64 tokens) in 120 us, 5.7 TB/s, 69% of the memory's nominal rate.  e4m3 weights:
+// 25 experts of 2 x 2048 x 7168, 16 tokens, 734 MB in 154 us, 4.8 TB/s (DRAM 59%, issue slots 43%, integer pipe 40%); 20 with
+// 28 tokens each, 701 us, waiting for the tokens' operands from shared memory (DRAM 10%, issue slots 22%).  Items dealt
+// by a counter in memory instead of in turn: 2% faster for the bf16 ones, 8% slower for 14 e4m3 experts.
 template <typename IO, bool FP8, int NT, int STAGES>
 __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
@@ -553,8 +554,10 @@ __global__ void __launch_bounds__(kUpWarps * 32) moe_up_kernel(const __grid_cons
 // y for 16 output rows a block: the (expert, step) pairs of all experts in use are dealt to the
 // warps in runs of equal work.  At the end of its part of an expert a warp adds the expert's columns to its
 // own sums of the tokens in shared memory; the warps' sums are joined at the end, in their order.
-// Bound by the weights where the warps are enough to keep them coming: 340 MB (2048 rows, 126 experts
-// of 768, 64 tokens) in 68 us, 5.0 TB/s from 128 of the 148 SMs.
+// Bound by the weights where the warps are enough to keep them coming: 340 MB (2048 rows, 108 experts
+// of 768, 64 tokens) in 68 us, 5.0 TB/s from 128 of the 148 SMs.  e4m3 weights: 25 experts of 7168 x 2048, 16 tokens, 368 MB
+// in 130 us, 2.8 TB/s (integer pipe 62%, DRAM 35%): the shifts that make bf16 operands of the codes, and looking out for
+// codes that are not a number (3% of a call); 20 with 28 tokens each, 434 us, as the products before.
 template <typename T, bool FP8, int NT, int STAGES, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32) moe_down_kernel(const __grid_constant__ MoeArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];

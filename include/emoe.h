@@ -866,7 +866,8 @@ emoe_status_t emoe_kv_gather(const emoe_kv_cache_t *cache, int32_t layer, const 
  * The prefix is read once for the whole batch.  A row that sees no token gives 0 and
  * -infinity.  Sums, maxima and statistics are 32-bit; the softmax weights are rounded to 16 bits
  * before they meet v: to io_type, for an e4m3 cache to F16 with an absolute step of at most 2^-30
- * of the largest weight times the largest scale of the v that the row sees.  The keys and values of the query tokens themselves have to be in the
+ * of the largest weight times the largest scale of the v that the row sees.  (There a BF16 query vector is taken as F16 by
+ * a power of two: elements below 2^-29 of its largest are kept to 2^-40 of that.)  The keys and values of the query tokens themselves have to be in the
  * cache already (emoe_kv_append earlier on the stream).
  *
  * Calls over different prefixes, or over parts of one long context, are joined with lse:
@@ -953,7 +954,8 @@ emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *experts, uint64
  * distinct where not negative (a token whose two choices lie in one slot is reported in the status
  * word, its output undefined).  The ranks' outputs are summed by the caller; out_type
  * EMOE_TYPE_F32 leaves that sum to be rounded once.
- * (e4m3 weights with BF16 tokens: a hidden vector's values have to be below 2^67.)
+ * (e4m3 weights with BF16 tokens: a hidden vector's values have to be below 2^67, and a token is taken as F16 by a
+ * power of two: its elements are exact down to 2^-29 of the largest, below that kept to 2^-40 of it.)
  * Only the chosen experts' weights are read, each once for all tokens.  Sums are 32-bit; the
  * hidden vector w * silu(gate) * up is rounded once to io_type as the last product's operand, what that
  * takes being kept as a second operand in calls of up to 8 tokens for experts with up to 4 of them

@@ -910,6 +910,141 @@ emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *cache, int32_t n_s
 emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const emoe_attend_t *args,
                              void *cuda_stream);
 
+/*
+ * emoe_kv_extend - gives the sequences of a batch the blocks for their next tokens and makes what
+ * the other calls of the step want: block tables, lengths, the packed order of the new tokens and
+ * their slots.  Blocks come from a list of free ids in device memory, so a captured step follows the
+ * lengths from replay to replay.
+ *
+ * Sequence s has lens[s] tokens on the first ceil(lens[s] / block_tokens) blocks of its row of
+ * block_table and changes by add[s]:
+ *   add > 0  it gets the blocks that lens[s] + add[s] tokens want more;
+ *   add < 0  its last -add tokens are gone (at most all of them); the blocks that it has too many go
+ *            back to the list (their entries in its row stay as they are, behind its length);
+ * q_start[0 .. n_seqs]: the sum of max(add, 0) over the sequences before: the new tokens of all
+ *   sequences are packed in this order (q, k, v, out of the step), at most n_slots.
+ * slots[i], i < n_slots: slot of the i-th new token (block * block_tokens + offset), -1 behind the last:
+ *   what emoe_kv_append takes.
+ * lens_out[s] = lens[s] + add[s] (may be lens itself).
+ *
+ * The list is a stack: free_blocks[0 .. *n_free) are free ids.  What is given back goes on top
+ * of it (sequence by sequence, block by block), then new blocks are taken from the top, in the same
+ * order; *n_free_out is what remains (may be n_free itself).  Entries that are taken stay in the array.
+ *
+ * A sequence is refused as a whole - lens_out = lens, its row as it was, slots -1 for its tokens, which
+ * keep their places in the packed order - if it would not fit in max_blocks blocks, if its new tokens do not
+ * fit in n_slots, or if it wants blocks and the blocks wanted by the sequences up to it (those that
+ * do not fit their rows apart) are more than there are.  status (as in emoe_kv_cache_t, optional) is set to
+ * EMOE_ERR_TOO_LARGE then, and where a block that is given back finds no room in the list; to EMOE_ERR_BLOCK_TABLE
+ * by an id outside the pool (its tokens get slot -1).  Negative lens count as 0, so does a negative *n_free.
+ *
+ * cache: only its block size, number of blocks and status are used.  n_seqs at most EMOE_KV_MAX_SEQS
+ * (EMOE_ERR_TOO_LARGE), n_seqs * max_blocks below 2^31.  One launch.
+ */
+#define EMOE_KV_MAX_SEQS 8192
+typedef struct {
+  const int32_t *lens, *add;   /* [n_seqs]                                                     */
+  int32_t *block_table;        /* [n_seqs][max_blocks], updated                                */
+  int32_t *free_blocks;        /* [free_capacity]                                              */
+  const int32_t *n_free;       /* [1]                                                          */
+  int32_t *q_start;            /* [n_seqs + 1]                                                 */
+  int64_t *slots;              /* [n_slots]                                                    */
+  int32_t *lens_out;           /* [n_seqs]                                                     */
+  int32_t *n_free_out;         /* [1]                                                          */
+  int32_t n_seqs, max_blocks, free_capacity, n_slots;
+  uint32_t reserved, reserved2;  /* zero                                                       */
+} emoe_extend_t;
+emoe_status_t emoe_kv_extend(const emoe_kv_cache_t *cache, const emoe_extend_t *args, void *cuda_stream);
+
+/*
+ * emoe_kv_attend_tree, emoe_kv_attend_window - attention of a batch's query tokens, packed as
+ * emoe_kv_extend packs them, over their own sequences' tokens:
+ *     out = sum_j softmax_j(scale * q.k_j) v_j,  lse = log(sum_j exp(scale * q.k_j)).
+ * Sequence s has query tokens q_start[s] .. q_start[s + 1] - 1 (at most max_q of them; any number, none
+ * too), the last ones of its own_lens[s] tokens, which lie on its row of block_table.  Their
+ * keys and values have to be in the cache already.  Query head h reads KV head h / (n_q_heads / n_heads).
+ *
+ * _tree: the query tokens are the nodes of a tree (of any graph) of drafted tokens.  Node i of a
+ * sequence sees all tokens before the nodes and those nodes k for which bit k % 32 of word k / 32 of
+ * its row of mask is set; itself too only by its bit.  Bits of nodes that do not exist, and words behind
+ * mask_words, count as unset whatever they hold.  Positions (rotary or other) are in q and k already.
+ *
+ * _window: a query token at place p of its sequence sees the tokens j <= p with j > p - window or
+ * j < sinks.  Single tokens of decoding sequences and pieces of prompts come in one call.  window at least 1
+ * (2^30 and more: no limit), sinks at least 0.  Blocks without any token that a query token of the
+ * sequence sees are not read, nor are their entries in the table: they may have been given back.
+ *
+ * A row that sees no token gives 0 and minus infinity.  What a row does not see - tokens that its mask leaves out,
+ * what lies behind a sequence's length, in its last block, in the rest of the pool - has no influence on
+ * it, whatever it holds.  Rows of out and lse that no sequence has (behind the last one, or beyond max_q) stay
+ * as they were.  Starts outside 0 .. n_tokens are taken as the nearest of these; they must not fall (the outputs of a
+ * call with a start below the one before it are undefined).  Sequences with more than max_q query tokens are reported in the status word (EMOE_ERR_TOO_LARGE); their
+ * first max_q are computed, each at the place that it has.  Tokens on a block id outside the pool are left out and
+ * reported (EMOE_ERR_BLOCK_TABLE).  own_lens beyond max_blocks * block_tokens count as that, negative ones as 0; query tokens
+ * whose places would be negative see nothing (but _tree nodes that there are, by their bits).
+ * Precision, types, head_dim, bounded waits, lse and workspaces are as for emoe_kv_attend; a call over a
+ * shared prefix is joined with one of these by lse.  n_tokens, max_q, max_blocks are host values: a captured call
+ * follows q_start, own_lens, tables and masks from replay to replay.
+ * Sizes beyond 2^24 query tokens, 2^28 rows or 2^30 tokens a sequence: EMOE_ERR_TOO_LARGE.
+ */
+typedef struct {
+  const void *q;               /* [n_tokens][n_q_heads][head_dim], 16-byte aligned               */
+  void *out;                   /* as q                                                         */
+  float *lse;                  /* optional [n_tokens][n_q_heads], natural logarithm              */
+  int64_t q_stride;            /* elements from one query token to the next, a multiple of 8     */
+  int64_t out_stride;
+  const int32_t *block_table;  /* [n_seqs][max_blocks]                                         */
+  const int32_t *own_lens;     /* [n_seqs]: tokens, the query tokens included                    */
+  const int32_t *q_start;      /* [n_seqs + 1]                                                 */
+  const uint32_t *mask;        /* _tree: [n_tokens][mask_words]; _window: NULL                    */
+  void *workspace;             /* bytes of the _workspace call (too few: EMOE_ERR_INVALID_ARG);  */
+  uint64_t workspace_bytes;    /* enough for a call is enough for calls with less of any size   */
+  int32_t n_seqs, n_tokens, max_q, n_q_heads, max_blocks;
+  int32_t mask_words;          /* _tree: at least ceil(max_q / 32); _window: 0                    */
+  int32_t window, sinks;       /* _tree: 0                                                     */
+  int32_t io_type;             /* EMOE_TYPE_BF16 or _F16, as for emoe_kv_attend                  */
+  float scale;                 /* usually 1 / sqrt(head_dim); finite, up to 2^127               */
+  int32_t wait_limit_us;       /* as for emoe_kv_attend                                        */
+  uint32_t reserved;           /* zero                                                         */
+} emoe_attend_rows_t;
+emoe_status_t emoe_kv_attend_tree_workspace(const emoe_kv_cache_t *cache, int32_t n_seqs,
+                                            int32_t n_tokens, int32_t max_q, int32_t n_q_heads,
+                                            int32_t max_blocks, uint64_t *bytes);
+emoe_status_t emoe_kv_attend_tree(const emoe_kv_cache_t *cache, int32_t layer,
+                                  const emoe_attend_rows_t *args, void *cuda_stream);
+emoe_status_t emoe_kv_attend_window_workspace(const emoe_kv_cache_t *cache, int32_t n_seqs,
+                                              int32_t n_tokens, int32_t max_q, int32_t n_q_heads,
+                                              int32_t max_blocks, int32_t window, int32_t sinks,
+                                              uint64_t *bytes);
+emoe_status_t emoe_kv_attend_window(const emoe_kv_cache_t *cache, int32_t layer,
+                                    const emoe_attend_rows_t *args, void *cuda_stream);
+
+/*
+ * emoe_kv_keep - keeps the accepted path of each sequence's tree: its nodes' keys and values, in all
+ * layers of the cache, move to the places behind the tokens before the tree.
+ *
+ * Sequence s has lens[s] tokens, the last q_start[s + 1] - q_start[s] of them the nodes; accepted[s][0 ..
+ * n_accepted[s]) are node numbers in rising order (max_accepted a row).  Node accepted[s][i] moves to place
+ * lens[s] - nodes + i, bit for bit, scale bytes of an e4m3 cache included.  change[s] = accepted nodes -
+ * nodes: the add that takes the others from the sequence in the next emoe_kv_extend.
+ * A path that does not rise, or leaves the nodes, ends there; that, and places outside the table or blocks outside the
+ * pool (whose moves are left out), are reported in the status word (EMOE_ERR_BLOCK_TABLE).
+ * head_dim: a multiple of 8 (EMOE_ERR_UNSUPPORTED).  max_accepted at most EMOE_KV_MAX_ACCEPTED, n_seqs at most 2^16 - 1
+ * (EMOE_ERR_TOO_LARGE).  Sequences hold blocks of their own.  One launch.
+ */
+#define EMOE_KV_MAX_ACCEPTED 1024
+typedef struct {
+  const int32_t *block_table;  /* [n_seqs][max_blocks]                                         */
+  const int32_t *lens;         /* [n_seqs]                                                     */
+  const int32_t *q_start;      /* [n_seqs + 1]                                                 */
+  const int32_t *accepted;     /* [n_seqs][max_accepted]                                       */
+  const int32_t *n_accepted;   /* [n_seqs]                                                     */
+  int32_t *change;             /* [n_seqs]                                                     */
+  int32_t n_seqs, max_blocks, max_accepted;
+  uint32_t reserved;           /* zero                                                         */
+} emoe_keep_t;
+emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *cache, const emoe_keep_t *args, void *cuda_stream);
+
 /* One rank's expert arena, laid out as emoe_reshard_experts moves it:
  *     [n_layers][3 (gate, up, down)][n_slots][matrix]        (or EMOE_LAYOUT_FUSED_W13)
  * gate and up matrices are [d_ff][d_model], down matrices [d_model][d_ff], row-major: a row

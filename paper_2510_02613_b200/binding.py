@@ -90,6 +90,23 @@ class _ExpertArena(ctypes.Structure):
                [("layout", _u32), ("reserved", _u32)]
 
 
+class _Extend(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("lens", "add", "block_table", "free_blocks", "n_free", "q_start", "slots", "lens_out", "n_free_out")] + \
+               [(n, _i32) for n in ("n_seqs", "max_blocks", "free_capacity", "n_slots")] + [("reserved", _u32), ("reserved2", _u32)]
+
+
+class _AttendRows(ctypes.Structure):
+    _fields_ = [("q", _vp), ("out", _vp), ("lse", _vp), ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("block_table", _vp), ("own_lens", _vp), ("q_start", _vp), ("mask", _vp), ("workspace", _vp), ("workspace_bytes", _u64)] + \
+               [(n, _i32) for n in ("n_seqs", "n_tokens", "max_q", "n_q_heads", "max_blocks", "mask_words", "window", "sinks", "io_type")] + \
+               [("scale", ctypes.c_float), ("wait_limit_us", _i32), ("reserved", _u32)]
+
+
+class _Keep(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("block_table", "lens", "q_start", "accepted", "n_accepted", "change")] + \
+               [(n, _i32) for n in ("n_seqs", "max_blocks", "max_accepted")] + [("reserved", _u32)]
+
+
 class _Moe(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("x", "logits", "slot_of_expert", "out", "ids_out", "weights_out", "workspace")] + \
                [("workspace_bytes", _u64)] + [(n, ctypes.c_int64) for n in ("x_stride", "logits_stride", "out_stride")] + \
@@ -119,6 +136,8 @@ EXPORTS = ("emoe_plan_create", "emoe_plan_create_ex", "emoe_reshard_experts", "e
            "emoe_vmm_slots_read", "emoe_vmm_slots_destroy",
            "emoe_kv_cache_bytes", "emoe_kv_vector_index", "emoe_kv_append", "emoe_kv_gather",
            "emoe_kv_attend_workspace", "emoe_kv_attend",
+           "emoe_kv_extend", "emoe_kv_keep", "emoe_kv_attend_tree_workspace", "emoe_kv_attend_tree",
+           "emoe_kv_attend_window_workspace", "emoe_kv_attend_window",
            "emoe_expert_arena_bytes", "emoe_moe_decode_workspace", "emoe_moe_decode")
 
 _lib: Optional[ctypes.CDLL] = None
@@ -251,6 +270,12 @@ def lib() -> ctypes.CDLL:
                        ("emoe_kv_append", [cache, _i32, _vp, _vp, i64, i64, _i32, _vp, _i32, _vp]),
                        ("emoe_kv_attend_workspace", [cache, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
                        ("emoe_kv_attend", [cache, _i32, ctypes.POINTER(_Attend), _vp]),
+                       ("emoe_kv_extend", [cache, ctypes.POINTER(_Extend), _vp]),
+                       ("emoe_kv_keep", [cache, ctypes.POINTER(_Keep), _vp]),
+                       ("emoe_kv_attend_tree_workspace", [cache, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
+                       ("emoe_kv_attend_tree", [cache, _i32, ctypes.POINTER(_AttendRows), _vp]),
+                       ("emoe_kv_attend_window_workspace", [cache] + [_i32] * 7 + [ctypes.POINTER(_u64)]),
+                       ("emoe_kv_attend_window", [cache, _i32, ctypes.POINTER(_AttendRows), _vp]),
                        ("emoe_expert_arena_bytes", [experts, ctypes.POINTER(_u64)]),
                        ("emoe_moe_decode_workspace", [experts, _i32, _i32, _i32, _i32, ctypes.POINTER(_u64)]),
                        ("emoe_moe_decode", [experts, _i32, ctypes.POINTER(_Moe), _vp]),

@@ -57,14 +57,6 @@ __device__ __forceinline__ Item item_of(const AttendArgs &a, uint32_t i) {
   return it;
 }
 
-// 16-byte piece c of row r of a tile with CH pieces a row: rotated so that eight rows' equal pieces
-// lie in different banks.
-template <int CH> __device__ __forceinline__ int swizzled(int r, int c) {
-  if constexpr (CH >= 8) return r * CH + (c ^ (r & 7));
-  else if constexpr (CH == 4) return r * CH + (c ^ ((r >> 1) & 3));
-  else return r * CH + (c ^ ((r >> 2) & 1));
-}
-
 __device__ __forceinline__ void write_row(const AttendArgs &a, int64_t row, int hd, float m, float l) {
   if (a.lse) a.lse[row] = l > 0.f || l != l ? (m + log2f(l)) * CUDART_LN2_F : -CUDART_INF_F;
 }

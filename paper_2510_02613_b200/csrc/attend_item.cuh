@@ -57,4 +57,12 @@ __device__ __forceinline__ float v_relative(uint32_t v, uint32_t largest) {
   return v == 255 ? CUDART_NAN_F : largest - v < 127 ? __uint_as_float((127 - (largest - v)) << 23) : 0.f;
 }
 
+// 16-byte piece c of row r of a tile with CH pieces a row: rotated so that eight rows' equal pieces
+// lie in different banks.
+template <int CH> __device__ __forceinline__ int swizzled(int r, int c) {
+  if constexpr (CH >= 8) return r * CH + (c ^ (r & 7));
+  else if constexpr (CH == 4) return r * CH + (c ^ ((r >> 1) & 3));
+  else return r * CH + (c ^ ((r >> 2) & 1));
+}
+
 }  // namespace emoe

@@ -1,0 +1,577 @@
+// attend_masked.cu - attention of packed query tokens over their own sequences' pages, each row with a mask: a window and
+// the first tokens, or a tree of drafted tokens.
+//
+// o = sum_j p_j v_j / sum_j p_j with p_j = 2^(s_j - m), s_j = scale * log2(e) * q.k_j over the tokens that the row
+// sees, m the largest s_j, in one pass: each part of the work keeps its own m, sum and unnormalised o in
+// 32 bits, and parts are joined by o = sum 2^(m_i - m) o_i.
+//
+// A tile of rows has a run of tokens: those that some row of it may see.  What a row sees of 32 of them is a word of bits,
+// made from two bounds or read from the tree's mask.  A step whose words are all ones - most of them: only the
+// ends of a window and the nodes of a tree have others - is computed without looking at them.
+#include <algorithm>
+
+#include "attend_item.cuh"
+#include "attend_masked.cuh"
+
+namespace emoe {
+namespace {
+
+constexpr int kRows = kMaskedRows, kWarps = 4, kStages = 2;
+// Tokens of one warp's step: the same bytes for both element sizes.
+template <bool FP8> constexpr int kGroupOf = FP8 ? 32 : 16;
+
+// Whether a word of two 16-bit elements, or of four e4m3 codes, has one that is infinite or not a number.
+template <typename T, bool FP8> __device__ __forceinline__ bool not_finite(uint32_t w) {
+  if constexpr (FP8) return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+  constexpr uint32_t kTop = __is_same(T, __half) ? 0x7c007c00u : 0x7f807f80u;
+  return __vcmpeq2(w & kTop, kTop) != 0;
+}
+
+// One warp's step covers 16 tokens (32 of an e4m3 cache): K and V rows come through a ring of its own in shared
+// memory, scores and products on the tensor cores with the 16 rows of the tile as the m side, running maximum
+// and sum in registers.  The four warps take every fourth group of tokens and are joined at the end.
+template <typename IO, int HD, bool FP8>
+__global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_kernel(const __grid_constant__ MaskedArgs a) {
+  using T = typename Operand<IO, FP8>::type;
+  constexpr int kGroup = kGroupOf<FP8>;
+  constexpr int ES = FP8 ? 1 : 2, CH = HD * ES / 16, kTile = kGroup * HD * ES, kStage = 2 * kTile;
+  constexpr uint32_t kAll = kGroup == 32 ? 0xffffffffu : (1u << (kGroup & 31)) - 1;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint16_t s_scale[kWarps][kStages][kGroup];
+  __shared__ uint32_t s_valid[kWarps][kStages];
+  __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % a.c.n_heads;
+  let_next_start();
+  const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
+  if (tile.rows == 0) return;
+  const Run run = run_of(a, tile);
+  const int64_t part = ((int64_t)unit * a.splits + split) * kRows;   // of the tile's first row
+  // tokens of this split: whole steps of the four warps
+  const int chunk = ((run.count + a.splits - 1) / a.splits + kWarps * kGroup - 1) / (kWarps * kGroup) * (kWarps * kGroup);
+  const int u0 = min(run.count, split * chunk), u1 = min(run.count, u0 + chunk);
+  if (u0 >= u1 && a.splits > 1) {   // nothing here: say so to the joining kernel
+    if (threadIdx.x < tile.rows) a.part_ml[part + threadIdx.x] = make_float2(-CUDART_INF_F, 0.f);
+    return;
+  }
+
+  const int groups = (u1 - u0 + kGroup - 1) / kGroup;
+  const int steps = groups > warp ? (groups - warp + kWarps - 1) / kWarps : 0;
+  const int32_t *const table = a.block_table + (int64_t)tile.seq * a.max_blocks;
+  uint8_t *const ring = smem + warp * (kStages * kStage);
+  const uint32_t ring_at = shared_address(ring);
+
+  // this lane's place in the run in step i (lanes beyond a group's tokens repeat them), -1 if there is none
+  auto place_of = [&](int i) {
+    const int u = u0 + (warp + kWarps * i) * kGroup + (lane & (kGroup - 1));
+    return i >= steps || u >= u1 ? -1 : u;
+  };
+  auto block_of = [&](int i) {
+    const int u = place_of(i);
+    return u < 0 ? 0 : table[(uint32_t)run.token(u) / (uint32_t)a.c.block_tokens];
+  };
+  auto vector_of = [&](int i, int block) {
+    const int u = place_of(i);
+    return u < 0 ? (int64_t)-1 : masked_vector(a, block, run.token(u), head);
+  };
+  uint32_t held_scale = 0, held_valid = 0;
+  auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
+    const uint32_t at = ring_at + (i % kStages) * kStage;
+    held_valid = __ballot_sync(0xffffffffu, vec >= 0);
+    if constexpr (FP8) held_scale = vec >= 0 ? a.c.k_scale[vec] | (uint32_t)a.c.v_scale[vec] << 8 : 0x007f;   // a token that is not there has no part in the largest scale of v
+#pragma unroll
+    for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
+      const int id = j * 32 + lane, row = id / CH, ch = id % CH;
+      const int64_t v = __shfl_sync(0xffffffffu, vec, row & (kGroup - 1));
+      if (kGroup * CH % 32 == 0 || id < kGroup * CH) {
+        const int64_t src = v < 0 ? 0 : v * (HD * ES) + ch * 16;
+        const uint32_t dst = at + swizzled<CH>(row, ch) * 16;
+        copy_async_16(dst, a.c.k + src, v < 0 ? 0 : 16);
+        copy_async_16(dst + kTile, a.c.v + src, v < 0 ? 0 : 16);
+      }
+    }
+  };
+  auto keep = [&](int i) {   // what the issue of step i found, for its use
+    if (FP8) s_scale[warp][i % kStages][lane] = (uint16_t)held_scale;
+    if (lane == 0) s_valid[warp][i % kStages] = held_valid;
+  };
+
+  // e4m3: the largest scale byte of v so far that a row (g, g + 8) sees, whose scale its o is relative to
+  uint32_t v_ref[2] = {0, 0};
+  constexpr int kTileGroup = FP8 ? 4 : 2;   // column tiles that are read together
+  float o[HD / 8 / kTileGroup][kTileGroup][4] = {}, m[2] = {-CUDART_INF_F, -CUDART_INF_F}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (i < steps) {
+      issue(i, vector_of(i, block_of(i)));
+      keep(i);
+    }
+    copy_async_commit();
+  }
+  int block = block_of(kStages - 1);   // the table is read a step ahead
+
+  // query rows g and g + 8 of the tile as matrix operands, from global memory; rows that do not exist are the last one again
+  uint32_t q[HD / 16][4];
+  float by_row[2];   // scores to log2 weights
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const IO *const src = (const IO *)a.q + row_at(a, tile, head, min(g + 8 * half, tile.rows - 1), a.q_stride);
+    by_row[half] = a.scale_log2;
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) {
+      if constexpr (!FP8) {
+        const uint32_t *p = (const uint32_t *)(src + ks * 16 + 2 * c);
+        q[ks][half] = p[0];
+        q[ks][2 + half] = p[4];
+      } else {   // four neighbouring elements, as the codes of a word come
+        const uint2 w = *(const uint2 *)(src + (ks >> 1) * 32 + c * 8 + (ks & 1) * 4);
+        q[ks][half] = w.x;
+        q[ks][2 + half] = w.y;
+      }
+    }
+    if constexpr (FP8) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks)
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const float2 f = Pair<IO>::unpack(q[ks][half + k]);
+          top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
+        }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float by = query_scale(top);
+      by_row[half] = a.scale_log2 / by;
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks)
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const float2 f = Pair<IO>::unpack(q[ks][half + k]);
+          q[ks][half + k] = Pair<T>::pack(f.x * by, f.y * by);
+        }
+    }
+  }
+  const Sight sight[2] = {Sight(a, tile, run, min(g, tile.rows - 1)), Sight(a, tile, run, min(g + 8, tile.rows - 1))};
+
+  for (int i = 0; i < steps; ++i) {
+    const int ahead = i + kStages - 1;
+    if (ahead < steps) issue(ahead, vector_of(ahead, block));
+    copy_async_commit();
+    block = block_of(ahead + 1);
+    const int base = u0 + (warp + kWarps * i) * kGroup;
+    uint32_t seen[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) seen[half] = sight[half].word(a, tile, run, base);
+    copy_async_wait<kStages - 1>();
+    __syncwarp();
+
+    const uint32_t k_at = ring_at + (i % kStages) * kStage, v_at = k_at + kTile;
+    const uint32_t valid = s_valid[warp][i % kStages] & kAll;
+    constexpr int kN = kGroup / 8, kP = kGroup / 16;   // column tiles of the scores, k steps of the second product
+    float s[kN][4] = {};
+    if constexpr (!FP8) {
+#pragma unroll
+      for (int ks = 0; ks < HD / 16; ++ks) {
+        uint32_t b[4];
+        ldmatrix_x4(b, k_at + swizzled<CH>((lane >> 4) * 8 + (lane & 7), ks * 2 + ((lane >> 3) & 1)) * 16);
+        mma_16816<T>(s[0], q[ks], b[0], b[1]);
+        mma_16816<T>(s[1], q[ks], b[2], b[3]);
+      }
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < HD / 32; ++kb)
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const uint2 w = *(const uint2 *)(ring + (i % kStages) * kStage + swizzled<CH>(j * 8 + g, kb * 2 + (c >> 1)) * 16 + (c & 1) * 8);
+          uint32_t b[4];
+          codes_to_half(b[0], b[1], w.x);
+          codes_to_half(b[2], b[3], w.y);
+          mma_16816<T>(s[j], q[2 * kb], b[0], b[1]);
+          mma_16816<T>(s[j], q[2 * kb + 1], b[2], b[3]);
+        }
+    }
+
+    seen[0] &= valid;
+    seen[1] &= valid;
+    const bool mixed = !__all_sync(0xffffffffu, (seen[0] & seen[1]) == kAll);
+    float k_by[kN][2], v_by[kN][2], v_raise[2] = {1.f, 1.f}, v_rest[2] = {1.f, 1.f};
+    if constexpr (FP8) {   // scales are powers of two; 255 is not a number and not counted in the largest of v so far
+      uint32_t largest[2];
+      uint32_t all_largest = 0;
+      if (!mixed) {
+        const uint32_t mine = s_scale[warp][i % kStages][lane] >> 8;
+        all_largest = largest[0] = largest[1] = __reduce_max_sync(0xffffffffu, mine == 255 ? 0 : mine);
+      } else {
+        largest[0] = largest[1] = 0;
+      }
+      uint32_t two[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        two[j] = *(const uint32_t *)&s_scale[warp][i % kStages][j * 8 + 2 * c];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) k_by[j][e] = scale_of(two[j] >> (16 * e) & 255);
+        if (mixed) {   // what a row does not see has no part in its largest scale
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t byte = two[j] >> (16 * e + 8) & 255;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+              if (byte != 255 && (seen[half] >> (j * 8 + 2 * c + e) & 1)) largest[half] = max(largest[half], byte);
+          }
+        }
+      }
+      if (mixed) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          largest[half] = max(largest[half], __shfl_xor_sync(0xffffffffu, largest[half], 1));
+          largest[half] = max(largest[half], __shfl_xor_sync(0xffffffffu, largest[half], 2));
+        }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t now = max(v_ref[half], largest[half]);
+        v_raise[half] = v_relative(v_ref[half], now);
+        v_ref[half] = now;
+        v_rest[half] = mixed ? 1.f : v_relative(all_largest, now);
+      }
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v_by[j][e] = mixed ? 1.f : v_relative(two[j] >> (16 * e + 8) & 255, all_largest);
+    }
+    float top[2] = {m[0], m[1]};
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int t = j * 8 + 2 * c + e;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float &x = s[j][2 * half + e];
+          x *= FP8 ? k_by[j][e] * by_row[half] : by_row[half];
+          if (mixed && !(seen[half] >> t & 1)) x = -CUDART_INF_F;
+          top[half] = fmaxf(top[half], x);
+        }
+      }
+    float alpha[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 1));
+      top[half] = fmaxf(top[half], __shfl_xor_sync(0xffffffffu, top[half], 2));
+      alpha[half] = exp2_fast(m[half] - (top[half] == -CUDART_INF_F ? 0.f : top[half]));
+      const float safe = top[half] == -CUDART_INF_F ? 0.f : top[half] - kWeightLift<T>;
+      m[half] = top[half];
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < kN; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float &x = s[j][2 * half + e];
+          x = exp2_fast(x - safe);
+          sum += x;
+          // (a NaN scale shows even where the weight has come to zero)
+          if constexpr (FP8) x *= v_by[j][e] * v_rest[half];
+        }
+      l[half] = l[half] * alpha[half] + sum;
+    }
+    uint32_t bad = 0;   // tokens of a mixed step with a value that is infinite or not a number
+    if (mixed) {
+      if constexpr (FP8) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+          const uint32_t two = *(const uint32_t *)&s_scale[warp][i % kStages][j * 8 + 2 * c];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+              if (seen[half] >> (j * 8 + 2 * c + e) & 1) s[j][2 * half + e] *= v_relative(two >> (16 * e + 8) & 255, v_ref[half]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < (kGroup * CH + 31) / 32; ++j) {
+        const int id = j * 32 + lane, row = id / CH;
+        if (kGroup * CH % 32 == 0 || id < kGroup * CH) {
+          const uint4 w = *(const uint4 *)(ring + (i % kStages) * kStage + kTile + swizzled<CH>(row, id % CH) * 16);
+          if (not_finite<T, FP8>(w.x) || not_finite<T, FP8>(w.y) || not_finite<T, FP8>(w.z) || not_finite<T, FP8>(w.w)) bad |= 1u << row;
+        }
+      }
+      bad = __reduce_or_sync(0xffffffffu, bad);
+    }
+    alpha[0] *= v_raise[0];
+    alpha[1] *= v_raise[1];
+    if (!__all_sync(0xffffffffu, alpha[0] == 1.f && alpha[1] == 1.f)) {
+#pragma unroll
+      for (int n = 0; n < HD / 8; ++n) {
+        float(&d)[4] = o[n / kTileGroup][n % kTileGroup];
+        d[0] *= alpha[0];
+        d[1] *= alpha[0];
+        d[2] *= alpha[1];
+        d[3] *= alpha[1];
+      }
+    }
+    // weights rounded to T, once, as the second product's operand: the result's own rounding is as large
+    uint32_t p[kP][4];
+#pragma unroll
+    for (int k = 0; k < kP; ++k) {
+      p[k][0] = Pair<T>::pack(s[2 * k][0], s[2 * k][1]);
+      p[k][1] = Pair<T>::pack(s[2 * k][2], s[2 * k][3]);
+      p[k][2] = Pair<T>::pack(s[2 * k + 1][0], s[2 * k + 1][1]);
+      p[k][3] = Pair<T>::pack(s[2 * k + 1][2], s[2 * k + 1][3]);
+    }
+    // A weight of zero does not silence such a value: its token goes, element by element, to the rows that see
+    // it, and is then cleared for the product.
+    while (__builtin_expect(bad != 0, 0)) {
+      const int t = __ffs(bad) - 1;
+      bad &= bad - 1;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int k = 0; k < kP; ++k)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (t >> 3 == 2 * k + e) word = p[k][2 * e + half];
+        const float2 two = Pair<T>::unpack(__shfl_sync(0xffffffffu, word, (lane & ~3) | (t >> 1 & 3)));
+        if (seen[half] >> t & 1) {
+          const float weight = t & 1 ? two.y : two.x;
+#pragma unroll
+          for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * e : n * 8 + 2 * c + e;
+              const uint8_t *const at = ring + (i % kStages) * kStage + kTile + swizzled<CH>(t, col * ES / 16) * 16 + col * ES % 16;
+              float v;
+              if constexpr (FP8) {
+                uint32_t lo, hi;
+                codes_to_half(lo, hi, *at);
+                v = Pair<__half>::unpack(lo).x;
+              } else {
+                v = Pair<T>::unpack(*(const uint16_t *)at).x;
+              }
+              o[n / kTileGroup][n % kTileGroup][2 * half + e] += weight * v;
+            }
+        }
+      }
+      __syncwarp();
+      for (int ch = lane; ch < CH; ch += 32)
+        *(uint4 *)(ring + (i % kStages) * kStage + kTile + swizzled<CH>(t, ch) * 16) = make_uint4(0, 0, 0, 0);
+      __syncwarp();
+    }
+    // Products with the n-th 16 (e4m3: 32) columns of v, pieces read with ldmatrix: two column tiles of an e4m3
+    // cache share 16-bit elements (two neighbouring columns) and are parted here.
+    constexpr int kReads = HD / 8 / kTileGroup;
+#pragma unroll
+    for (int n = 0; n < kReads; ++n) {
+      float(&d)[kTileGroup][4] = o[n];
+#pragma unroll
+      for (int k = 0; k < kP; ++k) {
+        uint32_t b[4];
+        ldmatrix_x4_trans(b, v_at + swizzled<CH>(16 * k + (lane & 15), 2 * n + (lane >> 4)) * 16);
+        if constexpr (FP8) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t x[4];   // column, column + 1 of tokens 2c, 2c + 1; of tokens 2c + 8, 2c + 9
+            codes_to_half(x[0], x[1], __byte_perm(b[2 * t], 0, 0x3120));
+            codes_to_half(x[2], x[3], __byte_perm(b[2 * t + 1], 0, 0x3120));
+            mma_16816<T>(d[2 * t], p[k], x[0], x[2]);
+            mma_16816<T>(d[2 * t + 1], p[k], x[1], x[3]);
+          }
+        } else {
+          mma_16816<T>(d[0], p[k], b[0], b[1]);
+          mma_16816<T>(d[1], p[k], b[2], b[3]);
+        }
+      }
+    }
+    if (ahead < steps) keep(ahead);
+    __syncwarp();
+  }
+  copy_async_wait<0>();
+
+  // the four warps' parts become one
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
+    l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+    if (c == 0) {
+      s_m[warp][g + 8 * half] = m[half] - kWeightLift<T>;
+      s_l[warp][g + 8 * half] = l[half];
+    }
+  }
+  __syncthreads();
+  constexpr int kPitch = HD + 4;
+  float *const joined = (float *)smem;
+#pragma unroll
+  for (int n = 0; n < HD / 8; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int col = FP8 ? (n >> 1) * 16 + 4 * c + (n & 1) + 2 * (e & 1) : n * 8 + 2 * c + (e & 1);
+      joined[(warp * kRows + g + 8 * (e >> 1)) * kPitch + col] = o[n / kTileGroup][n % kTileGroup][e] * (FP8 ? scale_of(v_ref[e >> 1]) : 1.f);
+    }
+  __syncthreads();
+  const int row = threadIdx.x >> 3;
+  if (row >= tile.rows) return;
+  float mm = -CUDART_INF_F, ll = 0.f, w[kWarps];
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, s_m[i][row]);
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    w[i] = mm == -CUDART_INF_F ? 0.f : exp2_fast(s_m[i][row] - mm);
+    ll += w[i] * s_l[i][row];
+    if (s_l[i][row] != s_l[i][row]) ll = w[i] = CUDART_NAN_F;   // a maximum does not carry a NaN: the sum does
+  }
+  const bool last = a.splits == 1;
+  const float by = last ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f;
+  IO *const out = (IO *)a.out + row_at(a, tile, head, row, a.out_stride);
+  for (int col = (threadIdx.x & 7) * 4; col < HD; col += 32) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const float4 y = *(const float4 *)&joined[(i * kRows + row) * kPitch + col];
+      x.x += w[i] * y.x;
+      x.y += w[i] * y.y;
+      x.z += w[i] * y.z;
+      x.w += w[i] * y.w;
+    }
+    if (last)
+      *(uint2 *)(out + col) = make_uint2(Pair<IO>::pack(x.x * by, x.y * by), Pair<IO>::pack(x.z * by, x.w * by));
+    else
+      *(float4 *)(a.part_o + (part + row) * HD + col) = x;
+  }
+  if ((threadIdx.x & 7) == 0) {
+    if (last) write_lse(a, tile, head, row, mm, ll);
+    else a.part_ml[part + row] = make_float2(mm, ll);
+  }
+}
+
+// Joins the splits of a tile's rows: a warp a row at a time, four splits read without waiting for one another.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kRows * 32) masked_join_kernel(const __grid_constant__ MaskedArgs a) {
+  constexpr int N = HD / 32;
+  const int row = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = blockIdx.x, head = unit % a.c.n_heads;
+  const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
+  if (row >= tile.rows) return;
+  const int64_t first = (int64_t)unit * a.splits * kRows + row;
+  wait_for_previous();
+  float m = -CUDART_INF_F;
+  for (int i = lane; i < a.splits; i += 32) m = fmaxf(m, a.part_ml[first + i * kRows].x);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  float l = 0.f, x[N] = {};
+  for (int i = 0; i < a.splits; i += 4) {
+    float w[4], y[4][N];
+    bool there[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t part = first + (int64_t)min(i + u, a.splits - 1) * kRows;
+      const float2 p = i + u < a.splits ? a.part_ml[part] : make_float2(-CUDART_INF_F, 0.f);
+      // an empty part (sum 0) does not count: nothing was written there
+      there[u] = p.y != 0.f;
+      w[u] = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+      l += there[u] ? w[u] * p.y : 0.f;
+      const float *const src = a.part_o + part * HD + lane * N;
+      if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
+      } else if constexpr (N == 2) {
+        *(float2 *)y[u] = *(const float2 *)src;
+      } else {
+        y[u][0] = src[0];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] += there[u] ? w[u] * y[u][j] : 0.f;
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  T *const out = (T *)a.out + row_at(a, tile, head, row, a.out_stride) + lane * N;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if constexpr (N >= 2) {
+      if (j % 2 == 0) *(uint32_t *)(out + j) = Pair<T>::pack(x[j] * by, x[j + (N > 1)] * by);
+    } else {
+      out[0] = (T)(x[0] * by);
+    }
+  }
+  if (lane == 0) write_lse(a, tile, head, row, m, l);
+}
+
+template <typename K>
+cudaError_t launch_after(K kernel, unsigned grid, int threads, size_t smem, cudaStream_t st, bool early, const MaskedArgs &a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename T, int HD, bool FP8>
+cudaError_t launch_rows(const MaskedArgs &a, cudaStream_t st) {
+  constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroupOf<FP8> * HD * (FP8 ? 1 : 2);
+  constexpr size_t join = (size_t)kWarps * kRows * (HD + 4) * 4;
+  constexpr size_t smem = ring > join ? ring : join;
+  cudaError_t e = allow_shared<masked_rows_kernel<T, HD, FP8>>();
+  if (e != cudaSuccess) return e;
+  const unsigned units = (unsigned)a.tiles * a.c.n_heads;
+  e = launch_after(masked_rows_kernel<T, HD, FP8>, units * a.splits, kWarps * 32, smem, st, false, a);
+  if (e != cudaSuccess || a.splits == 1) return e;
+  return launch_after(masked_join_kernel<T, HD>, units, kRows * 32, 0, st, true, a);
+}
+
+template <typename T, bool FP8>
+cudaError_t by_head_dim(const MaskedArgs &a, cudaStream_t st) {
+  switch (a.c.head_dim) {
+    case 32: return launch_rows<T, 32, FP8>(a, st);
+    case 64: return launch_rows<T, 64, FP8>(a, st);
+    case 128: return launch_rows<T, 128, FP8>(a, st);
+    case 256: return launch_rows<T, 256, FP8>(a, st);
+  }
+  return cudaErrorInvalidValue;
+}
+
+constexpr int kMostSplits = 64, kMostUnits = 8 * kSms;   // units beyond which the token axis is not split
+
+}  // namespace
+
+MaskedShape masked_shape(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens) {
+  MaskedShape s{};
+  const int64_t group = n_q_heads / n_heads;
+  // As many tiles for every sequence, or as the packed tokens make: what leaves fewer of them empty.
+  const int64_t each = (max_q * group + kMaskedRows - 1) / kMaskedRows, packed = n_tokens * group / kMaskedRows + n_seqs;
+  s.tiles_a_seq = each * n_seqs <= packed ? (int32_t)each : 0;
+  s.tiles = (int32_t)std::min(each * n_seqs, packed);
+  const int64_t unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>), units = (int64_t)s.tiles * n_heads;
+  // Splits: as many as make the sum of all the work over two blocks an SM, an item's start and end counting as
+  // 96 tokens, and of the last item least.
+  int64_t best = 1, cost = INT64_MAX;
+  for (int64_t n = 1; n <= kMostSplits && (n == 1 || ((n - 1) * unit < most_tokens && n * units <= kMostUnits)); ++n) {
+    const int64_t c = ((most_tokens + n - 1) / n + unit - 1) / unit * unit;
+    const int64_t t = units * n * (c + 96) / (2 * kSms) + c;
+    if (t < cost) cost = t, best = n;
+  }
+  s.splits = (int32_t)best;
+  s.parts = best > 1 ? units * best * kMaskedRows : 0;
+  return s;
+}
+
+int64_t masked_parts(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens) {
+  // Only calls whose units come to kMostUnits at most with their splits have any.
+  const int64_t group = n_q_heads / n_heads, unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>);
+  const int64_t each = (max_q * group + kMaskedRows - 1) / kMaskedRows, packed = n_tokens * group / kMaskedRows + n_seqs;
+  const int64_t splits = std::min<int64_t>(kMostSplits, (most_tokens + unit - 1) / unit);
+  return splits > 1 ? std::min<int64_t>(kMostUnits, std::min(each * n_seqs, packed) * n_heads * splits) * kMaskedRows : 0;
+}
+
+cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st) {
+  if (type == EMOE_TYPE_E4M3)
+    return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, st) : by_head_dim<__half, true>(a, st);
+  return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, st) : by_head_dim<__half, false>(a, st);
+}
+
+}  // namespace emoe

@@ -1,0 +1,120 @@
+// attend_masked.cuh - what the kernels of attention with masks share: tiles of rows, the tokens that they run
+// through, and which of these a row sees.
+#pragma once
+
+#include <math_constants.h>
+
+#include "convert.cuh"
+#include "serve.h"
+
+namespace emoe {
+
+// The n lowest bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1; }
+
+// Rows of a KV head in a sequence: its query tokens times the query heads of the KV head, a token's rows one
+// after the other.  A tile is up to R of them.
+struct RowTile {
+  int seq, row0, rows;   // rows 0: there is no such tile
+  int first, count;      // the sequence's query tokens: the first one, and how many are computed
+  int context;           // tokens before the query tokens (negative: more query tokens than tokens)
+  int length;            // tokens
+};
+
+// Packed: sequence s has the tiles from floor(q_start[s] * group / R) + s on, which leaves it enough of them and can
+// be said without a sum over the sequences before.  The whole warp looks for the sequence, 32 probes at a time.
+template <int R>
+__device__ __forceinline__ RowTile row_tile(const MaskedArgs &a, int tiles_a_seq, int tile) {
+  RowTile t;
+  int local;
+  const auto start_of = [&](int s) { return max(0, min(a.q_start[s], a.n_tokens)); };
+  if (tiles_a_seq) {
+    t.seq = tile / tiles_a_seq;
+    local = tile - t.seq * tiles_a_seq;
+  } else {
+    const auto tile_of = [&](int s) { return (int)((int64_t)start_of(s) * a.group / R) + s; };
+    int lo = 0, hi = a.n_seqs;   // the last sequence whose first tile is not behind this one
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, s = lo + (int)(threadIdx.x & 31) * step;
+      const int found = __popc(__ballot_sync(0xffffffffu, s < hi && tile_of(s) <= tile));
+      lo += max(0, found - 1) * step;
+      hi = min(hi, lo + step);
+    }
+    t.seq = lo;
+    local = tile - tile_of(lo);
+  }
+  t.first = start_of(t.seq);
+  const int all = max(0, start_of(t.seq + 1) - t.first);
+  t.count = min(all, a.max_q);
+  t.length = max(0, min(a.own_lens[t.seq], a.max_blocks * a.c.block_tokens));
+  t.context = t.length - all;
+  t.row0 = local * R;
+  t.rows = local < 0 ? 0 : max(0, min(R, t.count * a.group - t.row0));
+  if (all > a.max_q && local == 0 && a.c.status) *a.c.status = EMOE_ERR_TOO_LARGE;
+  return t;
+}
+
+// The tokens that some row of a tile may see, as one run: the first tokens, then those from `low` on.
+struct Run {
+  int count, sinks, low;
+  int seen;   // those before are seen by all rows that come after them (the first tokens and what joins on)
+  __device__ __forceinline__ int token(int u) const { return u < sinks ? u : u - sinks + low; }
+};
+__device__ __forceinline__ Run run_of(const MaskedArgs &a, const RowTile &t) {
+  Run r{t.length, 0, 0, 0};
+  if (a.mask) return r;
+  const int earliest = t.context + t.row0 / a.group, latest = t.context + (t.row0 + t.rows - 1) / a.group;
+  r.low = max(0, earliest - a.window + 1);
+  r.sinks = min(a.sinks, r.low);
+  r.seen = r.sinks + max(0, a.sinks - r.low);
+  r.count = r.sinks + max(0, latest + 1 - r.low);
+  return r;
+}
+
+// What one row of a tile sees of its run: a word of 32 tokens from u on.  (Tokens that the run does not have may be among them.)
+struct Sight {
+  int begin, end;        // window: the last tokens up to the row's own
+  int64_t mask;          // tree: word of the row's mask
+  __device__ __forceinline__ Sight(const MaskedArgs &a, const RowTile &t, const Run &r, int row) {
+    const int token = (t.row0 + row) / a.group, place = t.context + token;
+    begin = max(place - a.window + 1, r.low) - r.low + r.sinks;
+    end = place + 1 - r.low + r.sinks;
+    if (place < 0) end = 0;
+    mask = (int64_t)(t.first + token) * a.mask_words;
+  }
+  __device__ __forceinline__ uint32_t word(const MaskedArgs &a, const RowTile &t, const Run &r, int u) const {
+    if (!a.mask) return low_bits(end - u) & (low_bits(r.seen - u) | ~low_bits(begin - u));
+    const int node = u - t.context;
+    if (node <= -32) return 0xffffffffu;
+    const int i = max(node, 0) >> 5;
+    const uint32_t w0 = i < a.mask_words ? a.mask[mask + i] : 0;
+    if (node < 0) return w0 << -node | low_bits(-node);
+    const uint32_t w1 = i + 1 < a.mask_words ? a.mask[mask + i + 1] : 0;
+    return __funnelshift_r(w0, w1, node & 31);
+  }
+};
+
+// Vector index of token t, which lies on `block`; -1 (and the status word) if that is outside the pool.
+__device__ __forceinline__ int64_t masked_vector(const MaskedArgs &a, int block, int t, int head) {
+  const uint32_t off = (uint32_t)t % (uint32_t)a.c.block_tokens;
+  if (block < 0 || block >= a.num_blocks) {
+    if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
+    return -1;
+  }
+  return a.c.head_major ? ((int64_t)block * a.c.n_heads + head) * a.c.block_tokens + off
+                        : ((int64_t)block * a.c.block_tokens + off) * a.c.n_heads + head;
+}
+
+// Element offsets of a tile's row in q / out and in lse.
+__device__ __forceinline__ int64_t row_at(const MaskedArgs &a, const RowTile &t, int head, int row, int64_t stride) {
+  const int r = t.row0 + row, token = r / a.group;
+  return (int64_t)(t.first + token) * stride + (int64_t)(head * a.group + r - token * a.group) * a.c.head_dim;
+}
+__device__ __forceinline__ void write_lse(const MaskedArgs &a, const RowTile &t, int head, int row, float m, float l) {
+  const int r = t.row0 + row, token = r / a.group;
+  if (a.lse)
+    a.lse[(int64_t)(t.first + token) * a.n_q_heads + head * a.group + r - token * a.group] =
+        l > 0.f || l != l ? (m + log2f(l)) * CUDART_LN2_F : -CUDART_INF_F;
+}
+
+}  // namespace emoe

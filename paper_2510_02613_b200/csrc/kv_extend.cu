@@ -1,0 +1,287 @@
+// kv_extend.cu - blocks for the next tokens of a batch (tables, lengths, slots), and the move of an accepted path.
+#include <cooperative_groups.h>
+
+#include "serve.h"
+
+namespace emoe {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+
+struct Sums {
+  int64_t tokens;        // new ones
+  int32_t back, wanted;  // blocks
+};
+__device__ __forceinline__ Sums operator+(const Sums &a, const Sums &b) { return {a.tokens + b.tokens, a.back + b.back, a.wanted + b.wanted}; }
+__device__ __forceinline__ Sums shifted_up(const Sums &a, int d) {
+  return {__shfl_up_sync(0xffffffffu, a.tokens, d), __shfl_up_sync(0xffffffffu, a.back, d), __shfl_up_sync(0xffffffffu, a.wanted, d)};
+}
+__device__ __forceinline__ Sums running(Sums x, int lane) {   // sums of the lanes up to this one
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const Sums y = shifted_up(x, d);
+    if (lane >= d) x = x + y;
+  }
+  return x;
+}
+
+// One sequence's change.
+struct Change {
+  int64_t after;             // length
+  int32_t had, back, wanted; // blocks
+  int64_t tokens;
+  bool fits;                 // its row of the table
+};
+__device__ __forceinline__ Change change_of(const ExtendArgs &a, int32_t before, int32_t add) {
+  Change c;
+  c.after = max((int64_t)0, (int64_t)before + add);
+  c.tokens = max(0, add);
+  const int64_t bt = a.block_tokens, has = (c.after + bt - 1) / bt;
+  c.had = (int32_t)min((before + bt - 1) / bt, (int64_t)a.max_blocks);   // a length beyond the row has no more blocks than that
+  c.fits = add <= 0 || has <= a.max_blocks;
+  c.back = add < 0 ? max(0, c.had - (int32_t)min(has, (int64_t)a.max_blocks)) : 0;
+  c.wanted = add > 0 && c.fits ? max(0, (int32_t)has - c.had) : 0;
+  return c;
+}
+
+// Every block of the cluster sums up the whole batch for itself, from lengths that it keeps in shared memory: nothing
+// is handed from one to another, and with the one cluster barrier behind the loads the results may go over the
+// inputs.  (A second barrier only where blocks are given back, which may be taken again at once.)  What is written is then
+// shared out: new and returned blocks by groups of 32 sequences, flattened over a warp's lanes, slots by token, whose
+// sequence is found among the starts in shared memory.  A slot of a new token does not wait for the table: a
+// block that is not in it yet is read from the list.
+//
+// Bound by latency: loads, a scan, a barrier, loads that depend on it, stores; the slots' bytes at the most.
+__global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_constant__ ExtendArgs a) {
+  extern __shared__ int32_t s_seq[];   // [4][n_seqs]
+  __shared__ Sums s_warp[kWarps];
+  __shared__ int32_t s_taken;
+  int32_t *const s_before = s_seq, *const s_add = s_seq + a.n_seqs, *const s_first = s_seq + 2 * a.n_seqs, *const s_at = s_seq + 3 * a.n_seqs;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
+  const auto report = [&](int code) {
+    if (a.status) *a.status = code;
+  };
+
+  for (int i = threadIdx.x; i < a.n_seqs; i += kThreads) {
+    s_before[i] = max(0, a.lens[i]);
+    s_add[i] = a.add[i];
+  }
+  const int32_t n_free = max(0, min(*a.n_free, a.free_capacity));
+  if (threadIdx.x == 0) s_taken = 0;
+  __syncthreads();
+  // this thread's sequences, one after the other in the batch
+  const int per = (a.n_seqs + kThreads - 1) / kThreads, first = min(a.n_seqs, (int)threadIdx.x * per), last = min(a.n_seqs, first + per);
+  Sums mine{0, 0, 0};
+  for (int i = first; i < last; ++i) {
+    const Change c = change_of(a, s_before[i], s_add[i]);
+    mine = mine + Sums{c.tokens, c.back, c.wanted};
+  }
+  const Sums upto = running(mine, lane);
+  if (lane == 31) s_warp[warp] = upto;
+  __syncthreads();
+  if (warp == 0) s_warp[lane] = running(s_warp[lane], lane);
+  __syncthreads();
+  Sums before = upto;
+  before.tokens -= mine.tokens;
+  before.back -= mine.back;
+  before.wanted -= mine.wanted;
+  if (warp > 0) before = before + s_warp[warp - 1];
+  const Sums all = s_warp[kWarps - 1];
+  const int32_t room = a.free_capacity - n_free, back = min(all.back, room), top = n_free + back;
+
+  // what each sequence gets: its start, and where its blocks lie in the order of those given back or taken (-1: refused)
+  for (int i = first; i < last; ++i) {
+    const Change c = change_of(a, s_before[i], s_add[i]);
+    s_first[i] = (int32_t)min(before.tokens, (int64_t)a.n_slots);
+    const bool granted = c.fits && (c.tokens == 0 || before.tokens + c.tokens <= a.n_slots) && (c.wanted == 0 || before.wanted + c.wanted <= top);
+    if (!granted) report(EMOE_ERR_TOO_LARGE);
+    s_at[i] = !granted ? -1 : c.back ? before.back : before.wanted;
+    if (granted && c.wanted) atomicMax(&s_taken, before.wanted + c.wanted);
+    before = before + Sums{c.tokens, c.back, c.wanted};
+  }
+  if (all.back > room && threadIdx.x == 0) report(EMOE_ERR_TOO_LARGE);
+  const int32_t tokens = (int32_t)min(all.tokens, (int64_t)a.n_slots);
+  cluster.sync();   // all blocks have read what the results may go over
+
+  // Blocks of the 32 sequences of a group, one a lane at a time: body(sequence, its change, which of its blocks).
+  const auto for_blocks = [&](bool returned, auto body) {
+    for (int group = warp * blocks + rank; group * 32 < a.n_seqs; group += kWarps * blocks) {
+      const int i = group * 32 + lane;
+      Change c{};
+      int32_t n = 0;
+      if (i < a.n_seqs) {
+        c = change_of(a, s_before[i], s_add[i]);
+        n = s_at[i] < 0 ? 0 : returned ? c.back : c.wanted;
+      }
+      int32_t end = n;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int32_t y = __shfl_up_sync(0xffffffffu, end, d);
+        if (lane >= d) end += y;
+      }
+      const int32_t count = __shfl_sync(0xffffffffu, end, 31);
+      for (int32_t base = 0; base < count; base += 32) {
+        const int32_t j = base + lane;
+        int owner = 0;   // the first lane whose sum is above j
+#pragma unroll
+        for (int d = 16; d; d /= 2)
+          if (__shfl_sync(0xffffffffu, end, owner + d - 1) <= j) owner += d;
+        owner = min(owner, 31);
+        const int32_t start = __shfl_sync(0xffffffffu, end - n, owner);
+        if (j < count) body(group * 32 + owner, j - start);
+      }
+    }
+  };
+  if (all.back > 0) {
+    for_blocks(true, [&](int i, int32_t j) {
+      const Change c = change_of(a, s_before[i], s_add[i]);
+      const int32_t id = a.block_table[(int64_t)i * a.max_blocks + c.had - c.back + j], at = n_free + s_at[i] + j;
+      if (id < 0 || id >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
+      if (at < a.free_capacity) a.free_blocks[at] = id;
+    });
+    __threadfence();
+    cluster.sync();
+  }
+  const auto taken_block = [&](int i, int32_t j) { return a.free_blocks[top - 1 - (s_at[i] + j)]; };
+  for_blocks(false, [&](int i, int32_t j) {
+    const Change c = change_of(a, s_before[i], s_add[i]);
+    const int32_t id = taken_block(i, j);
+    if (id < 0 || id >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
+    a.block_table[(int64_t)i * a.max_blocks + c.had + j] = id;
+  });
+  if (rank == 0) {
+    for (int i = threadIdx.x; i < a.n_seqs; i += kThreads) {
+      const Change c = change_of(a, s_before[i], s_add[i]);
+      a.lens_out[i] = s_at[i] < 0 ? s_before[i] : (int32_t)c.after;
+      a.q_start[i] = s_first[i];
+    }
+    if (threadIdx.x == 0) {
+      a.q_start[a.n_seqs] = tokens;
+      *a.n_free_out = top - s_taken;
+    }
+  }
+  for (int i = rank * kThreads + threadIdx.x; i < a.n_slots; i += blocks * kThreads) {
+    int64_t slot = -1;
+    if (i < tokens) {
+      int lo = 0, hi = a.n_seqs;   // the last sequence that starts at or before i
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_first[mid] <= i) lo = mid;
+        else hi = mid;
+      }
+      if (s_at[lo] >= 0) {
+        const Change c = change_of(a, s_before[lo], s_add[lo]);
+        const uint32_t place = (uint32_t)(s_before[lo] + (i - s_first[lo])), column = place / (uint32_t)a.block_tokens;
+        const int32_t id = (int32_t)column < c.had ? a.block_table[(int64_t)lo * a.max_blocks + column] : taken_block(lo, (int32_t)column - c.had);
+        if (id >= 0 && id < a.num_blocks) slot = (int64_t)id * a.block_tokens + (place - column * (uint32_t)a.block_tokens);
+        else report(EMOE_ERR_BLOCK_TABLE);
+      }
+    }
+    a.slots[i] = slot;
+  }
+}
+
+// A thread takes one piece of the head vectors of a path, in one layer's keys or values, and moves it along
+// the whole path: sources are read in groups, in rising order, before they are written.  A place that is
+// written lies before all sources that are still to be read (the i-th node is at place i or behind it, and
+// nodes rise), so a path may overlap its own new places.
+// Bound by three loads one after the other (path, table, data), with many layers by the pieces' bytes.
+constexpr int kMoveThreads = 256, kAhead = 8;
+template <typename V>   // a piece: 8 or 16 bytes
+__global__ void __launch_bounds__(kMoveThreads) kv_keep_kernel(const __grid_constant__ KeepArgs a) {
+  extern __shared__ int2 s_move[];   // slots of a node and of its new place, -1 if there is no move
+  __shared__ int32_t s_end;
+  const int seq = blockIdx.y;
+  const int32_t q0 = a.q_start[seq], nodes = max(0, a.q_start[seq + 1] - q0), want = a.n_accepted[seq];
+  const int32_t most = max(0, min(want, a.max_accepted));
+  const int32_t *const path = a.accepted + (int64_t)seq * a.max_accepted;
+  const int64_t start = (int64_t)a.lens[seq] - nodes;
+  const auto report = [&]() {
+    if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
+  };
+  if (threadIdx.x == 0) s_end = most;
+  __syncthreads();
+  for (int i = threadIdx.x; i < most; i += kMoveThreads)
+    if (path[i] < 0 || path[i] >= nodes || (i > 0 && path[i] <= path[i - 1])) atomicMin(&s_end, i);
+  __syncthreads();
+  const int32_t count = s_end;
+  if (threadIdx.x == 0 && count < want) report();
+  const auto slot_of = [&](int64_t place) {
+    if (place < 0 || place >= (int64_t)a.max_blocks * a.c.block_tokens) return -1;
+    const int32_t column = (int32_t)(place / a.c.block_tokens), id = a.block_table[(int64_t)seq * a.max_blocks + column];
+    return id < 0 || id >= a.num_blocks ? -1 : (int32_t)(id * (int64_t)a.c.block_tokens + (place - (int64_t)column * a.c.block_tokens));
+  };
+  for (int i = threadIdx.x; i < count; i += kMoveThreads) {
+    int2 m = make_int2(-1, -1);
+    if (path[i] != i) {
+      m = make_int2(slot_of(start + path[i]), slot_of(start + i));
+      if (m.x < 0 || m.y < 0) {
+        m.x = -1;
+        report();
+      }
+    }
+    s_move[i] = m;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.change[seq] = count - nodes;
+  __syncthreads();
+
+  const uint32_t piece_of_head = a.pieces, of_pool = a.c.n_heads * piece_of_head;
+  const uint32_t item = blockIdx.x * kMoveThreads + threadIdx.x;
+  if (item < a.pools * of_pool) {
+    const uint32_t pool = item / of_pool, rest = item - pool * of_pool, head = rest / piece_of_head, piece = rest - head * piece_of_head;
+    V *const base = (V *)(a.c.k + pool * a.pool_bytes) + piece;
+    uint8_t *const scale = a.c.k_scale && piece == 0 ? a.c.k_scale + pool * a.pool_vectors : nullptr;
+    for (int i = 0; i < count; i += kAhead) {
+      V x[kAhead];
+      uint8_t y[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < count && s_move[i + j].x >= 0) {
+          const int64_t at = kv_vector(a.c, s_move[i + j].x, head);
+          x[j] = base[at * piece_of_head];
+          if (scale) y[j] = scale[at];
+        }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < count && s_move[i + j].x >= 0) {
+          const int64_t at = kv_vector(a.c, s_move[i + j].y, head);
+          base[at * piece_of_head] = x[j];
+          if (scale) scale[at] = y[j];
+        }
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_extend(const ExtendArgs &a, cudaStream_t st) {
+  const cudaError_t e = allow_shared<kv_extend_kernel>();
+  if (e != cudaSuccess) return e;
+  // A block writes a slot in 2 ns: more blocks, up to the 8 that a cluster always may have, for long slot maps.
+  int blocks = 1;
+  while (blocks < 8 && a.n_slots > 2048 * blocks) blocks *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = 16 * (size_t)a.n_seqs;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {(unsigned)blocks, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kv_extend_kernel, a);
+}
+
+cudaError_t launch_kv_keep(const KeepArgs &a, bool wide, cudaStream_t st) {
+  const dim3 grid((unsigned)(((uint64_t)a.pools * a.c.n_heads * a.pieces + kMoveThreads - 1) / kMoveThreads), a.n_seqs);
+  const size_t smem = sizeof(int2) * (size_t)a.max_accepted;
+  if (wide) kv_keep_kernel<uint4><<<grid, kMoveThreads, smem, st>>>(a);
+  else kv_keep_kernel<uint2><<<grid, kMoveThreads, smem, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace emoe

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "serve.h"
@@ -123,6 +124,27 @@ emoe_status_t check_attend_sizes(const emoe_kv_cache_t *c, int64_t n_seqs, int64
     return EMOE_ERR_TOO_LARGE;
   return EMOE_OK;
 }
+
+// Sizes of a call of emoe_kv_attend_tree or _window; window 0: a tree.
+emoe_status_t check_rows_sizes(const emoe_kv_cache_t *c, int64_t n_seqs, int64_t n_tokens, int64_t max_q, int64_t hq, int64_t max_blocks,
+                               bool tree, int64_t window, int64_t sinks) {
+  if (n_seqs < 0 || n_tokens < 0 || max_q <= 0 || hq <= 0 || max_blocks < 0 || hq % c->n_heads) return EMOE_ERR_SHAPE;
+  if (tree ? window != 0 || sinks != 0 : window <= 0 || sinks < 0) return EMOE_ERR_SHAPE;
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return EMOE_ERR_UNSUPPORTED;
+  // row and token numbers are kept in 32 bits
+  if (max_q > 1 << 24 || hq > 1 << 20 || n_seqs > 1 << 20 || n_tokens > 1 << 24 || n_tokens * hq >= 1 << 28 ||
+      max_blocks * c->block_tokens >= 1 << 30)
+    return EMOE_ERR_TOO_LARGE;
+  return EMOE_OK;
+}
+
+// Tokens that a tile of rows runs through at most.
+int64_t most_tokens(const emoe_kv_cache_t *c, int64_t max_blocks, bool tree, int64_t window, int64_t sinks) {
+  const int64_t all = max_blocks * c->block_tokens;
+  return tree ? all : std::min(all, sinks + window + kMaskedRows - 1);
+}
+
+constexpr int32_t kNoLimit = 1 << 30;   // of a window, or of the first tokens
 
 uint64_t up_256(uint64_t n) { return (n + 255) / 256 * 256; }
 
@@ -262,6 +284,181 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
   a.own_items = (uint32_t)s.own_items;
   a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;
   return cuda_status(launch_attend(a, c->type, p->io_type, (cudaStream_t)stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+emoe_status_t rows_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q, int32_t n_q_heads,
+                             int32_t max_blocks, bool tree, int32_t window, int32_t sinks, uint64_t *bytes) {
+  emoe_status_t st = check_cache(c);
+  if (st == EMOE_OK && !bytes) st = EMOE_ERR_INVALID_ARG;
+  if (st == EMOE_OK) st = check_rows_sizes(c, n_seqs, n_tokens, max_q, n_q_heads, max_blocks, tree, window, sinks);
+  if (st != EMOE_OK) return st;
+  *bytes = 0;
+  if (n_seqs == 0 || n_tokens == 0) return EMOE_OK;
+  const int64_t parts = masked_parts(c->n_heads, n_seqs, n_tokens, std::min(max_q, n_tokens), n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
+                                     most_tokens(c, max_blocks, tree, window, sinks));
+  *bytes = up_256(parts * sizeof(float2)) + up_256(parts * c->head_dim * sizeof(float));
+  return EMOE_OK;
+}
+
+emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_attend_rows_t *p, bool tree, void *stream) {
+  emoe_status_t st = check_cache_memory(c, layer);
+  if (st != EMOE_OK) return st;
+  if (!p || p->reserved || p->wait_limit_us < -1 || (!tree && (p->mask || p->mask_words))) return EMOE_ERR_INVALID_ARG;
+  if (p->io_type != EMOE_TYPE_BF16 && p->io_type != EMOE_TYPE_F16) return EMOE_ERR_INVALID_ARG;
+  const float scale_log2 = (float)(p->scale * kLog2e);
+  if (!std::isfinite(scale_log2)) return EMOE_ERR_INVALID_ARG;
+  if (c->type != EMOE_TYPE_E4M3 && c->type != p->io_type) return EMOE_ERR_UNSUPPORTED;
+  st = check_rows_sizes(c, p->n_seqs, p->n_tokens, p->max_q, p->n_q_heads, p->max_blocks, tree, p->window, p->sinks);
+  if (st != EMOE_OK) return st;
+  const int32_t max_q = std::min(p->max_q, p->n_tokens);
+  if (tree && (int64_t)p->mask_words * 32 < max_q) return EMOE_ERR_SHAPE;
+  if (p->n_seqs == 0 || p->n_tokens == 0) return EMOE_OK;
+  if (!p->q || !p->out || !p->own_lens || !p->q_start || (p->max_blocks && !p->block_table) || (tree && !p->mask)) return EMOE_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)p->n_q_heads * c->head_dim;
+  if (p->n_tokens > 1 && (p->q_stride < row || p->out_stride < row)) return EMOE_ERR_SHAPE;
+  if (!aligned(p->q, 16) || !aligned(p->out, 16) || !aligned(p->lse, 4) || !aligned(p->block_table, 4) || !aligned(p->own_lens, 4) ||
+      !aligned(p->q_start, 4) || !aligned(p->mask, 4) || !aligned(p->workspace, 256))
+    return EMOE_ERR_ALIGNMENT;
+  if (p->n_tokens > 1 && (p->q_stride % 8 || p->out_stride % 8)) return EMOE_ERR_ALIGNMENT;
+  const MaskedShape s = masked_shape(c->n_heads, p->n_seqs, p->n_tokens, max_q, p->n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
+                                     most_tokens(c, p->max_blocks, tree, p->window, p->sinks));
+  const uint64_t ml = up_256(s.parts * sizeof(float2)), need = ml + up_256(s.parts * c->head_dim * sizeof(float));
+  if (need && (!p->workspace || p->workspace_bytes < need)) return EMOE_ERR_INVALID_ARG;
+  if ((int64_t)s.tiles * c->n_heads * s.splits >= (int64_t)1 << 31) return EMOE_ERR_TOO_LARGE;
+  st = on_current_device(c->arena);
+  if (st != EMOE_OK) return st;
+  MaskedArgs a{};
+  a.c = layer_of(c, layer);
+  a.num_blocks = c->num_blocks;
+  a.q = p->q;
+  a.out = p->out;
+  a.lse = p->lse;
+  a.q_stride = p->n_tokens > 1 ? p->q_stride : row;
+  a.out_stride = p->n_tokens > 1 ? p->out_stride : row;
+  a.block_table = p->block_table;
+  a.own_lens = p->own_lens;
+  a.q_start = p->q_start;
+  a.mask = p->mask;
+  a.part_ml = (float2 *)p->workspace;
+  a.part_o = (float *)((uint8_t *)p->workspace + ml);
+  a.n_seqs = p->n_seqs;
+  a.n_tokens = p->n_tokens;
+  a.max_q = max_q;
+  a.n_q_heads = p->n_q_heads;
+  a.group = p->n_q_heads / c->n_heads;
+  a.max_blocks = p->max_blocks;
+  a.mask_words = p->mask_words;
+  a.window = std::min(p->window, kNoLimit);
+  a.sinks = std::min(p->sinks, kNoLimit);
+  a.scale_log2 = scale_log2;
+  a.tiles = s.tiles;
+  a.tiles_a_seq = s.tiles_a_seq;
+  a.splits = s.splits;
+  a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;
+  return cuda_status(launch_attend_masked(a, c->type, p->io_type, (cudaStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+emoe_status_t emoe_kv_attend_tree_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q,
+                                            int32_t n_q_heads, int32_t max_blocks, uint64_t *bytes) {
+  return rows_workspace(c, n_seqs, n_tokens, max_q, n_q_heads, max_blocks, true, 0, 0, bytes);
+}
+
+emoe_status_t emoe_kv_attend_window_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q,
+                                              int32_t n_q_heads, int32_t max_blocks, int32_t window, int32_t sinks, uint64_t *bytes) {
+  return rows_workspace(c, n_seqs, n_tokens, max_q, n_q_heads, max_blocks, false, window, sinks, bytes);
+}
+
+emoe_status_t emoe_kv_attend_tree(const emoe_kv_cache_t *c, int32_t layer, const emoe_attend_rows_t *p, void *stream) {
+  TraceRange trace("emoe_kv_attend_tree");
+  return attend_rows(c, layer, p, true, stream);
+}
+
+emoe_status_t emoe_kv_attend_window(const emoe_kv_cache_t *c, int32_t layer, const emoe_attend_rows_t *p, void *stream) {
+  TraceRange trace("emoe_kv_attend_window");
+  return attend_rows(c, layer, p, false, stream);
+}
+
+emoe_status_t emoe_kv_extend(const emoe_kv_cache_t *c, const emoe_extend_t *p, void *stream) {
+  TraceRange trace("emoe_kv_extend");
+  emoe_status_t st = check_cache(c);
+  if (st != EMOE_OK) return st;
+  if (!p || p->reserved || p->reserved2) return EMOE_ERR_INVALID_ARG;
+  if (p->n_seqs < 0 || p->max_blocks < 0 || p->free_capacity < 0 || p->n_slots < 0) return EMOE_ERR_SHAPE;
+  if (p->n_seqs > EMOE_KV_MAX_SEQS || (int64_t)p->n_seqs * p->max_blocks >= (int64_t)1 << 31 ||
+      (int64_t)p->max_blocks * c->block_tokens >= (int64_t)1 << 30 || p->n_slots > 1 << 30 || p->free_capacity > 1 << 30)
+    return EMOE_ERR_TOO_LARGE;
+  if (!p->n_free || !p->n_free_out || !p->q_start || (p->n_seqs && (!p->lens || !p->add || !p->lens_out)) ||
+      (p->n_seqs && p->max_blocks && !p->block_table) || (p->free_capacity && !p->free_blocks) || (p->n_slots && !p->slots))
+    return EMOE_ERR_INVALID_ARG;
+  if (!aligned(c->status, 4) || !aligned(p->lens, 4) || !aligned(p->add, 4) || !aligned(p->block_table, 4) || !aligned(p->free_blocks, 4) ||
+      !aligned(p->n_free, 4) || !aligned(p->q_start, 4) || !aligned(p->slots, 8) || !aligned(p->lens_out, 4) || !aligned(p->n_free_out, 4))
+    return EMOE_ERR_ALIGNMENT;
+  st = on_current_device(p->q_start);
+  if (st != EMOE_OK) return st;
+  ExtendArgs a{};
+  a.lens = p->lens;
+  a.add = p->add;
+  a.block_table = p->block_table;
+  a.free_blocks = p->free_blocks;
+  a.n_free = p->n_free;
+  a.q_start = p->q_start;
+  a.slots = p->slots;
+  a.lens_out = p->lens_out;
+  a.n_free_out = p->n_free_out;
+  a.status = c->status;
+  a.n_seqs = p->n_seqs;
+  a.max_blocks = p->max_blocks;
+  a.free_capacity = p->free_capacity;
+  a.n_slots = p->n_slots;
+  a.num_blocks = c->num_blocks;
+  a.block_tokens = c->block_tokens;
+  return cuda_status(launch_kv_extend(a, (cudaStream_t)stream));
+}
+
+emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *c, const emoe_keep_t *p, void *stream) {
+  TraceRange trace("emoe_kv_keep");
+  emoe_status_t st = check_cache_memory(c, 0);
+  if (st != EMOE_OK) return st;
+  if (!p || p->reserved) return EMOE_ERR_INVALID_ARG;
+  if (p->n_seqs < 0 || p->max_blocks < 0 || p->max_accepted < 0) return EMOE_ERR_SHAPE;
+  if (c->head_dim % 8) return EMOE_ERR_UNSUPPORTED;
+  const uint64_t vector = (uint64_t)c->head_dim * type_bytes(c->type), pieces = vector % 16 ? vector / 8 : vector / 16;
+  if (p->n_seqs > 65535 || p->max_accepted > EMOE_KV_MAX_ACCEPTED || (int64_t)p->max_blocks * c->block_tokens >= (int64_t)1 << 30 ||
+      (unsigned __int128)2 * c->n_layers * c->n_heads * pieces >= 1u << 31)
+    return EMOE_ERR_TOO_LARGE;
+  if (p->n_seqs == 0) return EMOE_OK;
+  if (!p->lens || !p->q_start || !p->n_accepted || !p->change || (p->max_accepted && !p->accepted) || (p->max_blocks && !p->block_table))
+    return EMOE_ERR_INVALID_ARG;
+  if (!aligned(p->block_table, 4) || !aligned(p->lens, 4) || !aligned(p->q_start, 4) || !aligned(p->accepted, 4) ||
+      !aligned(p->n_accepted, 4) || !aligned(p->change, 4))
+    return EMOE_ERR_ALIGNMENT;
+  st = on_current_device(c->arena);
+  if (st != EMOE_OK) return st;
+  KeepArgs a{};
+  a.c = layer_of(c, 0);
+  a.pool_vectors = pool_vectors(c);
+  a.pool_bytes = a.pool_vectors * vector;
+  a.block_table = p->block_table;
+  a.lens = p->lens;
+  a.q_start = p->q_start;
+  a.accepted = p->accepted;
+  a.n_accepted = p->n_accepted;
+  a.change = p->change;
+  a.pools = 2 * c->n_layers;
+  a.pieces = (uint32_t)pieces;
+  a.n_seqs = p->n_seqs;
+  a.max_blocks = p->max_blocks;
+  a.max_accepted = p->max_accepted;
+  a.num_blocks = c->num_blocks;
+  return cuda_status(launch_kv_keep(a, vector % 16 == 0, (cudaStream_t)stream));
 }
 
 emoe_status_t emoe_expert_arena_bytes(const emoe_expert_arena_t *e, uint64_t *bytes) {

@@ -38,6 +38,27 @@ cudaError_t launch_kv_append(const KvLayer &c, int type, const void *k, const vo
 cudaError_t launch_kv_gather(const KvLayer &c, int type, const int64_t *slots, int n, void *k, void *v,
                              int64_t ks, int64_t vs, int out_type, cudaStream_t st);
 
+struct ExtendArgs {
+  const int32_t *lens, *add;
+  int32_t *block_table, *free_blocks;
+  const int32_t *n_free;
+  int32_t *q_start;
+  int64_t *slots;
+  int32_t *lens_out, *n_free_out, *status;
+  int32_t n_seqs, max_blocks, free_capacity, n_slots, num_blocks, block_tokens;
+};
+cudaError_t launch_kv_extend(const ExtendArgs &a, cudaStream_t st);
+
+struct KeepArgs {
+  KvLayer c;                 // of layer 0: the others follow, K and V in turn
+  uint64_t pool_bytes, pool_vectors;
+  const int32_t *block_table, *lens, *q_start, *accepted, *n_accepted;
+  int32_t *change;
+  uint32_t pools, pieces;    // 2 * layers; pieces of a head vector
+  int32_t n_seqs, max_blocks, max_accepted, num_blocks;
+};
+cudaError_t launch_kv_keep(const KeepArgs &a, bool wide, cudaStream_t st);   // wide: pieces of 16 bytes, else of 8
+
 // How attention is cut: a function of what the caller knows on the host.
 struct AttendShape {
   int32_t seq_rows;                     // rows of one sequence and KV head: q_len * query heads per KV head
@@ -71,6 +92,35 @@ struct AttendArgs {
 };
 cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
+
+// Attention of packed query tokens over their own sequences, with masks: how it is cut.
+struct MaskedShape {
+  int32_t tiles, tiles_a_seq;      // row tiles of kMaskedRows rows; of each sequence, 0: as many as its tokens make
+  int32_t splits;                  // token ranges a tile
+  int64_t parts;                   // rows that go through the workspace
+};
+constexpr int kMaskedRows = 16;
+MaskedShape masked_shape(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens);
+// The most `parts` of a call of up to these sizes.
+int64_t masked_parts(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens);
+
+struct MaskedArgs {
+  KvLayer c;
+  int32_t num_blocks;
+  const void *q;
+  void *out;
+  float *lse;
+  int64_t q_stride, out_stride;         // elements from one query token to the next
+  const int32_t *block_table, *own_lens, *q_start;
+  const uint32_t *mask;                 // null: the window
+  float2 *part_ml;                      // [tile][head][split][row]: maximum (log2) and sum
+  float *part_o;                        // the same, [head_dim]
+  int32_t n_seqs, n_tokens, max_q, n_q_heads, group, max_blocks, mask_words, window, sinks;
+  float scale_log2;
+  int32_t tiles, tiles_a_seq, splits;
+  unsigned long long wait_ns;
+};
+cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st);
 
 // Calls of up to so many tokens keep what rounding takes from the hidden vectors.
 constexpr int kMoeWithRest = 8;

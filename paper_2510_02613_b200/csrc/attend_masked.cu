@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
   const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % a.c.n_heads;
   let_next_start();
   const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
-  if (tile.rows == 0) return;
+  if (tile.rows == 0 || (a.short_rows && tile.count * a.group > kRows)) return;
   const Run run = run_of(a, tile);
   const int64_t part = ((int64_t)unit * a.splits + split) * kRows;   // of the tile's first row
   // tokens of this split: whole steps of the four warps
@@ -444,31 +444,35 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
 }
 
 // Joins the splits of a tile's rows: a warp a row at a time, four splits read without waiting for one another.
-template <typename T, int HD>
+// TENSOR: parts of the tensor core kernel's tiles, 16 of their rows a block.
+template <typename T, int HD, bool TENSOR>
 __global__ void __launch_bounds__(kRows * 32) masked_join_kernel(const __grid_constant__ MaskedArgs a) {
-  constexpr int N = HD / 32;
-  const int row = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = blockIdx.x, head = unit % a.c.n_heads;
-  const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
-  if (row >= tile.rows) return;
-  const int64_t first = (int64_t)unit * a.splits * kRows + row;
+  constexpr int N = HD / 32, kOf = TENSOR ? kMaskedTensorRows : kRows, kBlocks = kOf / kRows;
+  const int unit = blockIdx.x / kBlocks, row = blockIdx.x % kBlocks * kRows + (threadIdx.x >> 5), lane = threadIdx.x & 31, head = unit % a.c.n_heads;
+  const int splits = TENSOR ? a.tensor_splits : a.splits;
+  const float2 *const ml = TENSOR ? a.tensor_ml : a.part_ml;
+  const float *const parts = TENSOR ? a.tensor_o : a.part_o;
+  const RowTile tile = row_tile<kOf>(a, TENSOR ? a.tensor_tiles_a_seq : a.tiles_a_seq, unit / a.c.n_heads);
   wait_for_previous();
+  if (row >= tile.rows || (a.short_rows && (tile.count * a.group > kRows) != TENSOR)) return;
+  const int64_t first = (int64_t)unit * splits * kOf + row;
   float m = -CUDART_INF_F;
-  for (int i = lane; i < a.splits; i += 32) m = fmaxf(m, a.part_ml[first + i * kRows].x);
+  for (int i = lane; i < splits; i += 32) m = fmaxf(m, ml[first + i * kOf].x);
 #pragma unroll
   for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   float l = 0.f, x[N] = {};
-  for (int i = 0; i < a.splits; i += 4) {
+  for (int i = 0; i < splits; i += 4) {
     float w[4], y[4][N];
     bool there[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int64_t part = first + (int64_t)min(i + u, a.splits - 1) * kRows;
-      const float2 p = i + u < a.splits ? a.part_ml[part] : make_float2(-CUDART_INF_F, 0.f);
+      const int64_t part = first + (int64_t)min(i + u, splits - 1) * kOf;
+      const float2 p = i + u < splits ? ml[part] : make_float2(-CUDART_INF_F, 0.f);
       // an empty part (sum 0) does not count: nothing was written there
       there[u] = p.y != 0.f;
       w[u] = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
       l += there[u] ? w[u] * p.y : 0.f;
-      const float *const src = a.part_o + part * HD + lane * N;
+      const float *const src = parts + part * HD + lane * N;
       if constexpr (N % 4 == 0) {
 #pragma unroll
         for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
@@ -519,59 +523,109 @@ cudaError_t launch_rows(const MaskedArgs &a, cudaStream_t st) {
   cudaError_t e = allow_shared<masked_rows_kernel<T, HD, FP8>>();
   if (e != cudaSuccess) return e;
   const unsigned units = (unsigned)a.tiles * a.c.n_heads;
-  e = launch_after(masked_rows_kernel<T, HD, FP8>, units * a.splits, kWarps * 32, smem, st, false, a);
-  if (e != cudaSuccess || a.splits == 1) return e;
-  return launch_after(masked_join_kernel<T, HD>, units, kRows * 32, 0, st, true, a);
+  return launch_after(masked_rows_kernel<T, HD, FP8>, units * a.splits, kWarps * 32, smem, st, false, a);
+}
+
+template <typename T, int HD>
+cudaError_t launch_joins(const MaskedArgs &a, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  if (a.tensor_tiles && a.tensor_splits > 1)
+    e = launch_after(masked_join_kernel<T, HD, true>, (unsigned)a.tensor_tiles * a.c.n_heads * (kMaskedTensorRows / kRows), kRows * 32, 0, st, true, a);
+  if (e == cudaSuccess && a.tiles && a.splits > 1)
+    e = launch_after(masked_join_kernel<T, HD, false>, (unsigned)a.tiles * a.c.n_heads, kRows * 32, 0, st, true, a);
+  return e;
+}
+
+// The row kernel, the tensor core kernel, the joins: each may start while the one before still runs and waits for it
+// before it ends, so that the last one ends last.
+template <typename T, int HD, bool FP8>
+cudaError_t launch_all(const MaskedArgs &a, int type, int io, cudaStream_t st) {
+  cudaError_t e = a.tiles ? launch_rows<T, HD, FP8>(a, st) : cudaSuccess;
+  if (e == cudaSuccess && a.tensor_tiles) e = launch_masked_tensor(a, type, io, a.tiles != 0, st);
+  return e == cudaSuccess ? launch_joins<T, HD>(a, st) : e;
 }
 
 template <typename T, bool FP8>
-cudaError_t by_head_dim(const MaskedArgs &a, cudaStream_t st) {
+cudaError_t by_head_dim(const MaskedArgs &a, int type, int io, cudaStream_t st) {
   switch (a.c.head_dim) {
-    case 32: return launch_rows<T, 32, FP8>(a, st);
-    case 64: return launch_rows<T, 64, FP8>(a, st);
-    case 128: return launch_rows<T, 128, FP8>(a, st);
-    case 256: return launch_rows<T, 256, FP8>(a, st);
+    case 32: return launch_all<T, 32, FP8>(a, type, io, st);
+    case 64: return launch_all<T, 64, FP8>(a, type, io, st);
+    case 128: return launch_all<T, 128, FP8>(a, type, io, st);
+    case 256: return launch_all<T, 256, FP8>(a, type, io, st);
   }
   return cudaErrorInvalidValue;
 }
 
-constexpr int kMostSplits = 64, kMostUnits = 8 * kSms;   // units beyond which the token axis is not split
+constexpr int kMostSplits = 64, kMostUnits = 8 * kSms, kMostTensorUnits = 2 * kSms;   // units beyond which the token axis is not split
+
+// Row tiles of R rows: as many for every sequence, or as the packed tokens make, what leaves fewer of them empty.
+void count_tiles(MaskedShape &s, const MaskedSizes &n, int64_t rows) {
+  const int64_t group = n.n_q_heads / n.n_heads, each = (n.max_q * group + rows - 1) / rows, packed = n.n_tokens * group / rows + n.n_seqs;
+  s.tiles_a_seq = each * n.n_seqs <= packed ? (int32_t)each : 0;
+  s.tiles = (int32_t)std::min(each * n.n_seqs, packed);
+}
+
+bool on_tensor(const MaskedSizes &n) {
+  MaskedShape s;
+  count_tiles(s, n, kMaskedRows);
+  return (n.head_dim == 64 || n.head_dim == 128) && (int64_t)n.max_q * (n.n_q_heads / n.n_heads) > kMaskedRows &&
+         (int64_t)s.tiles * n.n_heads * n.most_tokens >= 1 << 17;
+}
+
+int64_t row_unit(const MaskedSizes &n) { return kWarps * (n.e4m3 ? kGroupOf<true> : kGroupOf<false>); }
 
 }  // namespace
 
-MaskedShape masked_shape(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens) {
-  MaskedShape s{};
-  const int64_t group = n_q_heads / n_heads;
-  // As many tiles for every sequence, or as the packed tokens make: what leaves fewer of them empty.
-  const int64_t each = (max_q * group + kMaskedRows - 1) / kMaskedRows, packed = n_tokens * group / kMaskedRows + n_seqs;
-  s.tiles_a_seq = each * n_seqs <= packed ? (int32_t)each : 0;
-  s.tiles = (int32_t)std::min(each * n_seqs, packed);
-  const int64_t unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>), units = (int64_t)s.tiles * n_heads;
+MaskedShapes masked_shapes(const MaskedSizes &n) {
+  MaskedShapes s{};
+  const bool tensor = on_tensor(n);
+  if (tensor) {
+    // Blocks of up to 256 rows, one an SM: the number of splits with the fewest tiles one after the other, a block's
+    // start and end counting as three.
+    count_tiles(s.tensor, n, kMaskedTensorRows);
+    const int64_t units = (int64_t)s.tensor.tiles * n.n_heads, tiles = (n.most_tokens + 127) / 128;
+    int64_t best = 1, cost = INT64_MAX;
+    for (int64_t k = 1; k <= kMostSplits && k <= tiles && (k == 1 || k * units <= kMostTensorUnits); ++k) {
+      const int64_t c = ((units * k + kSms - 1) / kSms) * ((tiles + k - 1) / k + 3);
+      if (c < cost) cost = c, best = k;
+    }
+    s.tensor.splits = (int32_t)best;
+    s.tensor.parts = best > 1 ? units * best * kMaskedTensorRows : 0;
+  }
+  // Beside the tensor core kernel the row kernel takes sequences with few rows, unless there are so few that they do not matter there.
+  if (tensor && n.n_seqs * (int64_t)n.n_heads <= kSms / 2) return s;
+  count_tiles(s.rows, n, kMaskedRows);
+  if (tensor) s.rows.tiles = n.n_seqs, s.rows.tiles_a_seq = 1;
   // Splits: as many as make the sum of all the work over two blocks an SM, an item's start and end counting as
   // 96 tokens, and of the last item least.
+  const int64_t unit = row_unit(n), units = (int64_t)s.rows.tiles * n.n_heads;
   int64_t best = 1, cost = INT64_MAX;
-  for (int64_t n = 1; n <= kMostSplits && (n == 1 || ((n - 1) * unit < most_tokens && n * units <= kMostUnits)); ++n) {
-    const int64_t c = ((most_tokens + n - 1) / n + unit - 1) / unit * unit;
-    const int64_t t = units * n * (c + 96) / (2 * kSms) + c;
-    if (t < cost) cost = t, best = n;
+  for (int64_t k = 1; k <= kMostSplits && (k == 1 || ((k - 1) * unit < n.most_tokens && k * units <= kMostUnits)); ++k) {
+    const int64_t c = ((n.most_tokens + k - 1) / k + unit - 1) / unit * unit;
+    const int64_t t = units * k * (c + 96) / (2 * kSms) + c;
+    if (t < cost) cost = t, best = k;
   }
-  s.splits = (int32_t)best;
-  s.parts = best > 1 ? units * best * kMaskedRows : 0;
+  s.rows.splits = (int32_t)best;
+  s.rows.parts = best > 1 ? units * best * kMaskedRows : 0;
   return s;
 }
 
-int64_t masked_parts(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens) {
-  // Only calls whose units come to kMostUnits at most with their splits have any.
-  const int64_t group = n_q_heads / n_heads, unit = 4 * (e4m3 ? kGroupOf<true> : kGroupOf<false>);
-  const int64_t each = (max_q * group + kMaskedRows - 1) / kMaskedRows, packed = n_tokens * group / kMaskedRows + n_seqs;
-  const int64_t splits = std::min<int64_t>(kMostSplits, (most_tokens + unit - 1) / unit);
-  return splits > 1 ? std::min<int64_t>(kMostUnits, std::min(each * n_seqs, packed) * n_heads * splits) * kMaskedRows : 0;
+void masked_parts(const MaskedSizes &n, int64_t &rows, int64_t &tensor) {
+  // Only calls whose units come to kMostUnits (kMostTensorUnits) at most with their splits have any parts.
+  MaskedShape s;
+  const auto most = [&](int64_t tile_rows, int64_t unit, int64_t most_units) {
+    count_tiles(s, n, tile_rows);
+    const int64_t splits = std::min<int64_t>(kMostSplits, (n.most_tokens + unit - 1) / unit);
+    return splits > 1 ? std::min<int64_t>(most_units, (int64_t)s.tiles * n.n_heads * splits) * tile_rows : 0;
+  };
+  rows = most(kMaskedRows, row_unit(n), kMostUnits);
+  tensor = on_tensor(n) ? most(kMaskedTensorRows, 128, kMostTensorUnits) : 0;
 }
 
 cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st) {
   if (type == EMOE_TYPE_E4M3)
-    return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, st) : by_head_dim<__half, true>(a, st);
-  return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, st) : by_head_dim<__half, false>(a, st);
+    return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, true>(a, type, io, st) : by_head_dim<__half, true>(a, type, io, st);
+  return io == EMOE_TYPE_BF16 ? by_head_dim<__nv_bfloat16, false>(a, type, io, st) : by_head_dim<__half, false>(a, type, io, st);
 }
 
 }  // namespace emoe

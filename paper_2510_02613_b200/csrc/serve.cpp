@@ -290,6 +290,16 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *c, int32_t layer, const emoe
 
 namespace {
 
+MaskedSizes masked_sizes(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q, int32_t n_q_heads, int32_t max_blocks,
+                         bool tree, int32_t window, int32_t sinks) {
+  return {c->n_heads, n_seqs, n_tokens, std::min(max_q, n_tokens), n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
+          most_tokens(c, max_blocks, tree, window, sinks)};
+}
+
+uint64_t part_bytes(const emoe_kv_cache_t *c, int64_t parts) {   // maxima and sums, then outputs
+  return up_256(parts * sizeof(float2)) + up_256(parts * c->head_dim * sizeof(float));
+}
+
 emoe_status_t rows_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q, int32_t n_q_heads,
                              int32_t max_blocks, bool tree, int32_t window, int32_t sinks, uint64_t *bytes) {
   emoe_status_t st = check_cache(c);
@@ -298,9 +308,9 @@ emoe_status_t rows_workspace(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n
   if (st != EMOE_OK) return st;
   *bytes = 0;
   if (n_seqs == 0 || n_tokens == 0) return EMOE_OK;
-  const int64_t parts = masked_parts(c->n_heads, n_seqs, n_tokens, std::min(max_q, n_tokens), n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
-                                     most_tokens(c, max_blocks, tree, window, sinks));
-  *bytes = up_256(parts * sizeof(float2)) + up_256(parts * c->head_dim * sizeof(float));
+  int64_t rows, tensor;
+  masked_parts(masked_sizes(c, n_seqs, n_tokens, max_q, n_q_heads, max_blocks, tree, window, sinks), rows, tensor);
+  *bytes = part_bytes(c, rows) + part_bytes(c, tensor);
   return EMOE_OK;
 }
 
@@ -324,11 +334,10 @@ emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_at
       !aligned(p->q_start, 4) || !aligned(p->mask, 4) || !aligned(p->workspace, 256))
     return EMOE_ERR_ALIGNMENT;
   if (p->n_tokens > 1 && (p->q_stride % 8 || p->out_stride % 8)) return EMOE_ERR_ALIGNMENT;
-  const MaskedShape s = masked_shape(c->n_heads, p->n_seqs, p->n_tokens, max_q, p->n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
-                                     most_tokens(c, p->max_blocks, tree, p->window, p->sinks));
-  const uint64_t ml = up_256(s.parts * sizeof(float2)), need = ml + up_256(s.parts * c->head_dim * sizeof(float));
+  const MaskedShapes s = masked_shapes(masked_sizes(c, p->n_seqs, p->n_tokens, max_q, p->n_q_heads, p->max_blocks, tree, p->window, p->sinks));
+  const uint64_t of_rows = part_bytes(c, s.rows.parts), need = of_rows + part_bytes(c, s.tensor.parts);
   if (need && (!p->workspace || p->workspace_bytes < need)) return EMOE_ERR_INVALID_ARG;
-  if ((int64_t)s.tiles * c->n_heads * s.splits >= (int64_t)1 << 31) return EMOE_ERR_TOO_LARGE;
+  if ((int64_t)s.rows.tiles * c->n_heads * std::max(s.rows.splits, 1) >= (int64_t)1 << 31) return EMOE_ERR_TOO_LARGE;   // a grid's blocks
   st = on_current_device(c->arena);
   if (st != EMOE_OK) return st;
   MaskedArgs a{};
@@ -343,8 +352,11 @@ emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_at
   a.own_lens = p->own_lens;
   a.q_start = p->q_start;
   a.mask = p->mask;
-  a.part_ml = (float2 *)p->workspace;
-  a.part_o = (float *)((uint8_t *)p->workspace + ml);
+  uint8_t *const work = (uint8_t *)p->workspace;
+  a.part_ml = (float2 *)work;
+  a.part_o = (float *)(work + up_256(s.rows.parts * sizeof(float2)));
+  a.tensor_ml = (float2 *)(work + of_rows);
+  a.tensor_o = (float *)(work + of_rows + up_256(s.tensor.parts * sizeof(float2)));
   a.n_seqs = p->n_seqs;
   a.n_tokens = p->n_tokens;
   a.max_q = max_q;
@@ -355,9 +367,13 @@ emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_at
   a.window = std::min(p->window, kNoLimit);
   a.sinks = std::min(p->sinks, kNoLimit);
   a.scale_log2 = scale_log2;
-  a.tiles = s.tiles;
-  a.tiles_a_seq = s.tiles_a_seq;
-  a.splits = s.splits;
+  a.tiles = s.rows.tiles;
+  a.tiles_a_seq = s.rows.tiles_a_seq;
+  a.splits = s.rows.splits;
+  a.tensor_tiles = s.tensor.tiles;
+  a.tensor_tiles_a_seq = s.tensor.tiles_a_seq;
+  a.tensor_splits = s.tensor.splits;
+  a.short_rows = s.rows.tiles && s.tensor.tiles;
   a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;
   return cuda_status(launch_attend_masked(a, c->type, p->io_type, (cudaStream_t)stream));
 }

@@ -94,15 +94,23 @@ cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStre
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
 // Attention of packed query tokens over their own sequences, with masks: how it is cut.
+constexpr int kMaskedRows = 16, kMaskedTensorRows = 256;   // rows of a tile
 struct MaskedShape {
-  int32_t tiles, tiles_a_seq;      // row tiles of kMaskedRows rows; of each sequence, 0: as many as its tokens make
+  int32_t tiles, tiles_a_seq;      // row tiles: in all; of each sequence, 0: as many as its tokens make
   int32_t splits;                  // token ranges a tile
   int64_t parts;                   // rows that go through the workspace
 };
-constexpr int kMaskedRows = 16;
-MaskedShape masked_shape(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens);
-// The most `parts` of a call of up to these sizes.
-int64_t masked_parts(int n_heads, int n_seqs, int n_tokens, int max_q, int n_q_heads, int head_dim, bool e4m3, int64_t most_tokens);
+struct MaskedShapes {
+  MaskedShape rows, tensor;        // tiles 0: the kernel has nothing to do
+};
+struct MaskedSizes {
+  int32_t n_heads, n_seqs, n_tokens, max_q, n_q_heads, head_dim;
+  bool e4m3;
+  int64_t most_tokens;             // that a row sees
+};
+MaskedShapes masked_shapes(const MaskedSizes &n);
+// The most `parts` of a call of up to these sizes, of either kernel.
+void masked_parts(const MaskedSizes &n, int64_t &rows, int64_t &tensor);
 
 struct MaskedArgs {
   KvLayer c;
@@ -113,13 +121,16 @@ struct MaskedArgs {
   int64_t q_stride, out_stride;         // elements from one query token to the next
   const int32_t *block_table, *own_lens, *q_start;
   const uint32_t *mask;                 // null: the window
-  float2 *part_ml;                      // [tile][head][split][row]: maximum (log2) and sum
-  float *part_o;                        // the same, [head_dim]
+  float2 *part_ml, *tensor_ml;          // [tile][head][split][row]: maximum (log2) and sum
+  float *part_o, *tensor_o;             // the same, [head_dim]
   int32_t n_seqs, n_tokens, max_q, n_q_heads, group, max_blocks, mask_words, window, sinks;
   float scale_log2;
   int32_t tiles, tiles_a_seq, splits;
+  int32_t tensor_tiles, tensor_tiles_a_seq, tensor_splits;
+  int32_t short_rows;                   // both kernels run: sequences of up to kMaskedRows rows a head go to the row kernel
   unsigned long long wait_ns;
 };
+cudaError_t launch_masked_tensor(const MaskedArgs &a, int type, int io, bool early, cudaStream_t st);
 cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st);
 
 // Calls of up to so many tokens keep what rounding takes from the hidden vectors.

@@ -375,3 +375,60 @@ def test_offsets_beyond_32_bits():
     sees = [RR.window_sees(n, m, 150, 4) for n, m in zip(lens, counts)]
     out, lse = call(c, q, table, lens, starts, window=150, sinks=4, layer=0)
     compare(out, lse, RR.attend(ref, 0, q.double(), small, lens, starts, sees, hd ** -0.5), "bf16")
+
+
+MANY = [("bf16", "bf16", False, 16, 2, 8, 128), ("f16", "f16", True, 16, 4, 8, 64), ("e4m3", "bf16", False, 16, 2, 8, 128), ("e4m3", "f16", True, 8, 4, 8, 64),
+        ("bf16", "bf16", True, 24, 12, 1, 128), ("f16", "f16", False, 16, 5, 3, 128)]
+
+
+@pytest.mark.parametrize("kv,io,hm,block,hkv,group,hd", MANY)
+def test_what_many_rows_do_not_see_has_no_influence(kv, io, hm, block, hkv, group, hd):
+    """As above at sizes that go to the tensor core kernel: pieces of prompts, and trees, of many rows beside small ones."""
+    lens, counts = [1500, 900, 700, 130], [400, 129, 2, 130]
+    rng, ref, table, starts, q = setup(hd + group, kv, io, hm, block, hkv, group, hd, lens, counts)
+    poison(rng, ref, table, lens, counts, block, 30)
+    c, _, _ = device_cache(ref)
+    sees = [RR.window_sees(n, m, 450, 130) for n, m in zip(lens, counts)]
+    check(ref, c, q, table, lens, starts, sees, io, window=450, sinks=130)
+    bits = [tree_bits(rng, n, 0.5 if n == 129 else None) for n in counts]
+    sees = [RR.tree_sees(n, m, b) for n, m, b in zip(lens, counts, bits)]
+    check(ref, c, q, table, lens, starts, sees, io, bits=bits)
+
+
+MORE = [
+    # kv, io, hm, block, KV heads, group, hd, lengths, query tokens, window, sinks: many rows
+    ("bf16", "bf16", False, 16, 1, 1, 128, [2300], [2300], 600, 4),                          # a whole prompt, tiles of 256 tokens
+    ("bf16", "bf16", False, 16, 2, 2, 64, [3000, 2600], [1000, 900], 1 << 30, 0),             # causal
+    ("f16", "f16", True, 32, 2, 8, 128, [2500, 640, 1900], [17, 600, 1], 1000, 300),          # 136 rows, many, 8 of them
+    ("e4m3", "bf16", False, 16, 2, 4, 128, [2300, 700], [300, 700], 130, 4),                  # windows about as long as a tile
+    ("e4m3", "f16", True, 16, 2, 5, 64, [5000], [200], 2000, 1),
+    ("bf16", "bf16", False, 16, 8, 8, 128, [1100] * 20, [3] * 20, 900, 4),                    # 24 rows each
+    ("bf16", "bf16", False, 16, 4, 8, 128, [1300] + [700] * 40, [300] + [1] * 40, 500, 4),    # single tokens beside a piece
+    ("f16", "f16", False, 16, 1, 16, 128, [20000], [16], 1 << 30, 0),                         # split over the tokens
+    ("bf16", "bf16", False, 16, 1, 8, 128, [9000, 300], [16, 300], 8000, 77),
+]
+
+
+@pytest.mark.parametrize("kv,io,hm,block,hkv,group,hd,lens,counts,window,sinks", MORE)
+def test_window_with_many_rows(kv, io, hm, block, hkv, group, hd, lens, counts, window, sinks):
+    rng, ref, table, starts, q = setup(hd + len(lens) + window % 97, kv, io, hm, block, hkv, group, hd, lens, counts)
+    c, _, _ = device_cache(ref)
+    sees = [RR.window_sees(n, m, window, sinks) for n, m in zip(lens, counts)]
+    check(ref, c, q, table, lens, starts, sees, io, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("hd,kv", [(128, "bf16"), (64, "e4m3")])
+def test_waits_that_run_out_are_reported(hd, kv):
+    lens, counts = [3000], [200]
+    rng, ref, table, starts, q = setup(1, kv, "bf16", False, 16, 2, 8, hd, lens, counts)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    c, _, _ = device_cache(ref, status=status)
+    need = c.attend_window_workspace_bytes(1, 200, 200, 16, table.shape[1], 2000, 0)
+    args = (1, q, torch.empty_like(q), dev(table), dev(lens), dev(starts), 200, 2000)
+    work = torch.empty(max(1, need), dtype=torch.uint8, device="cuda")
+    c.attend_window(*args, workspace=work, wait_limit_us=-1)
+    torch.cuda.synchronize()
+    assert status.item() == 10 and torch.isnan(args[2]).any()
+    status.zero_()
+    check(ref, c, q, table, lens, starts, [RR.window_sees(3000, 200, 2000, 0)], "bf16", window=2000)
+    assert status.item() == 0

@@ -352,8 +352,12 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
-      // The next step's scores are on their way before this one's weights are waited for and announced.  (They
-      // were asked for a step ago; were they not done yet, their product does not need these weights.)
+      // The weights are announced before the next step's scores are waited for: those come behind the last step's product
+      // in the tensor cores' queue, and would hold up this one's.
+      if (busy) tmem_stored();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar.p_full(slot, half));   // one a warp: arrivals at one barrier go one by one
       if (i + 1 < n_steps) {
         ok = bar_wait_warp(bar.s_full(slot, half ^ 1), ((i + 1) >> 1) & 1, abort, a.wait_ns);
         if (!ok) break;
@@ -363,10 +367,6 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
           tmem_load(x[1], s_base + (half ^ 1) * kStep + 32);
         }
       }
-      if (busy) tmem_stored();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive(bar.p_full(slot, half));   // one a warp: arrivals at one barrier go one by one
     }
     if (!ok) tmem_stored();   // what was under way when a wait ran out
     // The last two products may be under way.  A parity tells one phase from the next only: each half has a

@@ -49,13 +49,14 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
     *abort = 1;
     return false;
   }
-  const unsigned long long t0 = now_ns();
+  unsigned long long t0 = 0;   // (the timer is read late: it takes long to answer)
   for (;;) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i) {
       if constexpr (PATIENT) __nanosleep(100);
       if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
     }
+    if (t0 == 0) t0 = now_ns();
     if (__any_sync(0xffffffffu, *abort != 0 || now_ns() - t0 > limit)) {
       *abort = 1;
       return false;

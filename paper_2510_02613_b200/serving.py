@@ -81,6 +81,15 @@ def _dense(t, what: str, inner: int):
     return t
 
 
+def _dense_pointer(t, what: str, shape, dtype: str, device):
+    """Address of a tensor of this shape (None: any size) and type, densely packed, beside the arena; ValueError otherwise.
+    (The first test is what a good call pays.)"""
+    if t is None or not (t.is_contiguous() and t.device == device and _names.get(t.dtype) == dtype and t.dim() == len(shape)
+                         and all([w is None or w == n for n, w in zip(t.shape, shape)])):
+        _dense(_shaped(t, what, shape, dtype, device), what, len(shape))
+    return t.data_ptr()
+
+
 def _workspace(t, device):
     """(address, bytes) of a workspace or None."""
     if t is None:
@@ -132,7 +141,7 @@ class KvCache:
         self._keep = (arena, scales, status)
         self._ref = ctypes.byref(self._c)
         self._row = n_heads * head_dim
-        L = _b.lib()
+        L = self._calls = _b.lib()
         self._append, self._gather, self._attend = L.emoe_kv_append, L.emoe_kv_gather, L.emoe_kv_attend
 
     @classmethod
@@ -229,30 +238,27 @@ class KvCache:
         its row of block_table (int32 [n, max_blocks]) or gives them back.  Receives q_start (int32 [n + 1]: where
         each sequence's new tokens begin among all), slots (int64, any size: a slot a new token, -1 behind the last), lens_out
         (may be lens) and n_free_out (may be n_free).  A sequence that there is no room for stays as it was, its slots -1."""
-        n = _shaped(lens, "lens", (None,), "int32", self.device).shape[0]
-        _shaped(block_table, "block_table", (n, None), "int32", self.device)
-        for t, what, shape, dtype in ((add, "add", (n,), "int32"), (free_blocks, "free_blocks", (None,), "int32"), (n_free, "n_free", (1,), "int32"),
-                                      (q_start, "q_start", (n + 1,), "int32"), (slots, "slots", (None,), "int64"),
-                                      (lens_out, "lens_out", (n,), "int32"), (n_free_out, "n_free_out", (1,), "int32")):
-            _dense(_shaped(t, what, shape, dtype, self.device), what, 1)
-        _dense(lens, "lens", 1)
-        _dense(block_table, "block_table", 2)
-        p = _b._Extend(*(t.data_ptr() for t in (lens, add, block_table, free_blocks, n_free, q_start, slots, lens_out, n_free_out)),
+        dev, at = self.device, _dense_pointer
+        p_lens = at(lens, "lens", (None,), "int32", dev)
+        n = lens.shape[0]
+        p = _b._Extend(p_lens, at(add, "add", (n,), "int32", dev), at(block_table, "block_table", (n, None), "int32", dev),
+                       at(free_blocks, "free_blocks", (None,), "int32", dev), at(n_free, "n_free", (1,), "int32", dev),
+                       at(q_start, "q_start", (n + 1,), "int32", dev), at(slots, "slots", (None,), "int64", dev),
+                       at(lens_out, "lens_out", (n,), "int32", dev), at(n_free_out, "n_free_out", (1,), "int32", dev),
                        n, block_table.shape[1], free_blocks.shape[0], slots.shape[0], 0, 0)
-        _check(_b.lib().emoe_kv_extend(self._ref, ctypes.byref(p), _stream_handle(stream)))
+        _check(self._calls.emoe_kv_extend(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
     def keep(self, block_table, lens, q_start, accepted, n_accepted, change, stream=None) -> None:
         """Moves the accepted nodes (int32 [n, most], rising node numbers, the first n_accepted [n] of each row) of the
         sequences' trees, their last q_start[s + 1] - q_start[s] tokens, to the front of these, in all layers.  change
         (int32 [n]) receives accepted less drafted tokens: the add of the next extend."""
-        n = _shaped(lens, "lens", (None,), "int32", self.device).shape[0]
-        for t, what, shape in ((block_table, "block_table", (n, None)), (accepted, "accepted", (n, None)), (q_start, "q_start", (n + 1,)),
-                               (n_accepted, "n_accepted", (n,)), (change, "change", (n,))):
-            _dense(_shaped(t, what, shape, "int32", self.device), what, len(shape))
-        _dense(lens, "lens", 1)
-        p = _b._Keep(*(t.data_ptr() for t in (block_table, lens, q_start, accepted, n_accepted, change)), n, block_table.shape[1],
-                     accepted.shape[1], 0)
-        _check(_b.lib().emoe_kv_keep(self._ref, ctypes.byref(p), _stream_handle(stream)))
+        dev, at = self.device, _dense_pointer
+        p_lens = at(lens, "lens", (None,), "int32", dev)
+        n = lens.shape[0]
+        p = _b._Keep(at(block_table, "block_table", (n, None), "int32", dev), p_lens, at(q_start, "q_start", (n + 1,), "int32", dev),
+                     at(accepted, "accepted", (n, None), "int32", dev), at(n_accepted, "n_accepted", (n,), "int32", dev),
+                     at(change, "change", (n,), "int32", dev), n, block_table.shape[1], accepted.shape[1], 0)
+        _check(self._calls.emoe_kv_keep(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
     def attend_tree_workspace_bytes(self, n_seqs: int, n_tokens: int, max_q: int, n_q_heads: int, max_blocks: int) -> int:
         """Enough for calls of up to these sizes on this cache."""
@@ -274,33 +280,38 @@ class KvCache:
         nodes of sequence s at q_start[s] (int32 [n_seqs + 1]), at most max_q of them: the last ones of its own_lens[s] tokens.
         A node sees all tokens before the nodes and those nodes whose bits its row of mask (int32 [n_tokens, words]) has.
         workspace, lse, wait_limit_us: as for attend."""
-        words = _dense(_shaped(mask, "mask", (q.shape[0], None), "int32", self.device), "mask", 2).shape[1]
-        self._attend_rows(_b.lib().emoe_kv_attend_tree, layer, q, out, block_table, own_lens, q_start, mask.data_ptr(), max_q, words, 0, 0,
+        bits = _dense_pointer(mask, "mask", (q.shape[0], None), "int32", self.device)
+        self._attend_rows(self._calls.emoe_kv_attend_tree, layer, q, out, block_table, own_lens, q_start, bits, max_q, mask.shape[1], 0, 0,
                           scale, lse, workspace, stream, wait_limit_us)
 
     def attend_window(self, layer: int, q, out, block_table, own_lens, q_start, max_q: int, window: int, sinks: int = 0,
                       scale: Optional[float] = None, lse=None, workspace=None, stream=None, wait_limit_us: int = 0) -> None:
         """Attention with a window: q, out and q_start as for attend_tree (single tokens and pieces of prompts, packed); a query
         token sees the last `window` tokens up to itself and the sequence's first `sinks` tokens."""
-        self._attend_rows(_b.lib().emoe_kv_attend_window, layer, q, out, block_table, own_lens, q_start, None, max_q, 0, min(window, 1 << 30),
+        self._attend_rows(self._calls.emoe_kv_attend_window, layer, q, out, block_table, own_lens, q_start, None, max_q, 0, min(window, 1 << 30),
                           min(sinks, 1 << 30), scale, lse, workspace, stream, wait_limit_us)
 
     def _attend_rows(self, call, layer, q, out, block_table, own_lens, q_start, mask, max_q, words, window, sinks, scale, lse, workspace, stream,
                      wait_limit_us):
-        t, hq, _ = q.shape
-        _shaped(q, "q", (t, hq, self.head_dim), None, self.device)
+        dev, at = self.device, _dense_pointer
+        t, hq, hd = q.shape
+        shape, row = (t, hq, self.head_dim), hq * self.head_dim
         if out.dtype != q.dtype:
             raise ValueError("out is %s, q %s" % (out.dtype, q.dtype))
-        _shaped(out, "out", (t, hq, self.head_dim), None, self.device)
-        strides = [_dense(x, what, 2).stride(0) if t > 1 else hq * self.head_dim for x, what in ((q, "q"), (out, "out"))]
-        n = _dense(_shaped(own_lens, "own_lens", (None,), "int32", self.device), "own_lens", 1).shape[0]
-        _dense(_shaped(q_start, "q_start", (n + 1,), "int32", self.device), "q_start", 1)
-        _dense(_shaped(block_table, "block_table", (n, None), "int32", self.device), "block_table", 2)
-        p = _b._AttendRows(q.data_ptr(), out.data_ptr(),
-                           None if lse is None else _dense(_shaped(lse, "lse", (t, hq), "float32", self.device), "lse", 2).data_ptr(),
-                           strides[0], strides[1], block_table.data_ptr(), own_lens.data_ptr(), q_start.data_ptr(), mask,
-                           *_workspace(workspace, self.device), n, t, max_q, hq, block_table.shape[1], words, window, sinks, _value_type(q, "q"),
-                           self.head_dim ** -0.5 if scale is None else scale, wait_limit_us, 0)
+        strides = [row, row]
+        for i, (x, what) in enumerate(((q, "q"), (out, "out"))):
+            if x.shape != shape or x.device != dev:
+                _shaped(x, what, shape, None, dev)
+            if not x.is_contiguous():
+                _dense(x, what, 2)
+                strides[i] = x.stride(0) if t > 1 else row
+        p_lens = at(own_lens, "own_lens", (None,), "int32", dev)
+        n = own_lens.shape[0]
+        work, size = _workspace(workspace, dev)
+        p = _b._AttendRows(q.data_ptr(), out.data_ptr(), None if lse is None else at(lse, "lse", (t, hq), "float32", dev), strides[0], strides[1],
+                           at(block_table, "block_table", (n, None), "int32", dev), p_lens, at(q_start, "q_start", (n + 1,), "int32", dev), mask,
+                           work, size, n, t, max_q, hq, block_table.shape[1], words, window, sinks, _value_type(q, "q"),
+                           hd ** -0.5 if scale is None else scale, wait_limit_us, 0)
         _check(call(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
 
 

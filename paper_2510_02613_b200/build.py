@@ -7,7 +7,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "serve.cpp", "kernels.cu", "kv_cache.cu", "kv_extend.cu", "attend.cu", "attend_prefix.cu", "attend_masked.cu", "attend_masked_tensor.cu", "moe.cu"]
+SOURCES = ["planner.cpp", "capi.cpp", "vmm.cpp", "placement.cpp", "cache.cpp", "validate.cpp", "serve.cpp", "kernels.cu", "kv_cache.cu", "kv_extend.cu", "attend.cu", "attend_prefix.cu", "attend_masked.cu", "attend_masked_few.cu", "attend_masked_tensor.cu", "moe.cu"]
 HEADERS = ["planner.h", "kernels.h", "internal.h", "serve.h", "convert.cuh", "attend_item.cuh", "attend_masked.cuh", "tensor.cuh", os.path.join("..", "..", "include", "emoe.h")]
 OUT = os.path.join(HERE, "libemoe.so")
 

@@ -20,13 +20,6 @@ constexpr int kRows = kMaskedRows, kWarps = 4, kStages = 2;
 // Tokens of one warp's step: the same bytes for both element sizes.
 template <bool FP8> constexpr int kGroupOf = FP8 ? 32 : 16;
 
-// Whether a word of two 16-bit elements, or of four e4m3 codes, has one that is infinite or not a number.
-template <typename T, bool FP8> __device__ __forceinline__ bool not_finite(uint32_t w) {
-  if constexpr (FP8) return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
-  constexpr uint32_t kTop = __is_same(T, __half) ? 0x7c007c00u : 0x7f807f80u;
-  return __vcmpeq2(w & kTop, kTop) != 0;
-}
-
 // One warp's step covers 16 tokens (32 of an e4m3 cache): K and V rows come through a ring of its own in shared
 // memory, scores and products on the tensor cores with the 16 rows of the tile as the m side, running maximum
 // and sum in registers.  The four warps take every fourth group of tokens and are joined at the end.
@@ -44,16 +37,11 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
   const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % a.c.n_heads;
   let_next_start();
   const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
-  if (tile.rows == 0 || (a.short_rows && tile.count * a.group > kRows)) return;
+  if (tile.rows == 0 || (a.short_rows && tile.count * a.group > a.short_rows)) return;
   const Run run = run_of(a, tile);
-  const int64_t part = ((int64_t)unit * a.splits + split) * kRows;   // of the tile's first row
-  // tokens of this split: whole steps of the four warps
-  const int chunk = ((run.count + a.splits - 1) / a.splits + kWarps * kGroup - 1) / (kWarps * kGroup) * (kWarps * kGroup);
+  // tokens of this split: whole steps of a warp
+  const int chunk = ((run.count + a.splits - 1) / a.splits + kGroup - 1) / kGroup * kGroup;
   const int u0 = min(run.count, split * chunk), u1 = min(run.count, u0 + chunk);
-  if (u0 >= u1 && a.splits > 1) {   // nothing here: say so to the joining kernel
-    if (threadIdx.x < tile.rows) a.part_ml[part + threadIdx.x] = make_float2(-CUDART_INF_F, 0.f);
-    return;
-  }
 
   const int groups = (u1 - u0 + kGroup - 1) / kGroup;
   const int steps = groups > warp ? (groups - warp + kWarps - 1) / kWarps : 0;
@@ -408,111 +396,86 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
       joined[(warp * kRows + g + 8 * (e >> 1)) * kPitch + col] = o[n / kTileGroup][n % kTileGroup][e] * (FP8 ? scale_of(v_ref[e >> 1]) : 1.f);
     }
   __syncthreads();
-  const int row = threadIdx.x >> 3;
-  if (row >= tile.rows) return;
-  float mm = -CUDART_INF_F, ll = 0.f, w[kWarps];
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, s_m[i][row]);
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    w[i] = mm == -CUDART_INF_F ? 0.f : exp2_fast(s_m[i][row] - mm);
-    ll += w[i] * s_l[i][row];
-    if (s_l[i][row] != s_l[i][row]) ll = w[i] = CUDART_NAN_F;   // a maximum does not carry a NaN: the sum does
-  }
-  const bool last = a.splits == 1;
-  const float by = last ? (ll > 0.f || ll != ll ? 1.f / ll : 0.f) : 1.f;
-  IO *const out = (IO *)a.out + row_at(a, tile, head, row, a.out_stride);
-  for (int col = (threadIdx.x & 7) * 4; col < HD; col += 32) {
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float4 y = *(const float4 *)&joined[(i * kRows + row) * kPitch + col];
-      x.x += w[i] * y.x;
-      x.y += w[i] * y.y;
-      x.z += w[i] * y.z;
-      x.w += w[i] * y.w;
-    }
-    if (last)
-      *(uint2 *)(out + col) = make_uint2(Pair<IO>::pack(x.x * by, x.y * by), Pair<IO>::pack(x.z * by, x.w * by));
-    else
-      *(float4 *)(a.part_o + (part + row) * HD + col) = x;
-  }
-  if ((threadIdx.x & 7) == 0) {
-    if (last) write_lse(a, tile, head, row, mm, ll);
-    else a.part_ml[part + row] = make_float2(mm, ll);
-  }
+  finish_rows<IO, HD, kRows, kWarps>(a, tile, head, unit, split, joined, s_m, s_l);
 }
 
-// Joins the splits of a tile's rows: a warp a row at a time, four splits read without waiting for one another.
-// TENSOR: parts of the tensor core kernel's tiles, 16 of their rows a block.
-template <typename T, int HD, bool TENSOR>
-__global__ void __launch_bounds__(kRows * 32) masked_join_kernel(const __grid_constant__ MaskedArgs a) {
-  constexpr int N = HD / 32, kOf = TENSOR ? kMaskedTensorRows : kRows, kBlocks = kOf / kRows;
-  const int unit = blockIdx.x / kBlocks, row = blockIdx.x % kBlocks * kRows + (threadIdx.x >> 5), lane = threadIdx.x & 31, head = unit % a.c.n_heads;
-  const int splits = TENSOR ? a.tensor_splits : a.splits;
-  const float2 *const ml = TENSOR ? a.tensor_ml : a.part_ml;
-  const float *const parts = TENSOR ? a.tensor_o : a.part_o;
-  const RowTile tile = row_tile<kOf>(a, TENSOR ? a.tensor_tiles_a_seq : a.tiles_a_seq, unit / a.c.n_heads);
+// Joins the parts of the rows of a tile of R: TEAM warps a row, four parts read without waiting for one another.
+constexpr int kJoinWarps = 16;
+struct JoinArgs {
+  MaskedArgs a;
+  const float2 *ml;          // [tile][head][part][row]
+  const float *o;
+  int32_t parts, tiles_a_seq;
+  int32_t least, most;       // rows of the sequences that count
+};
+template <typename T, int HD, int R, int TEAM>
+__global__ void __launch_bounds__(kJoinWarps * 32) masked_join_kernel(const __grid_constant__ JoinArgs j) {
+  constexpr int N = HD / 32, kMine = kJoinWarps / TEAM, kBlocks = (R + kMine - 1) / kMine;   // rows of a block, blocks of a tile
+  __shared__ float s_x[kJoinWarps][HD], s_l[kJoinWarps];
+  const MaskedArgs &a = j.a;
+  const int unit = blockIdx.x / kBlocks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, head = unit % a.c.n_heads, n = j.parts;
+  const int row = blockIdx.x % kBlocks * kMine + warp / TEAM;
+  const RowTile tile = row_tile<R>(a, j.tiles_a_seq, unit / a.c.n_heads);
   wait_for_previous();
-  if (row >= tile.rows || (a.short_rows && (tile.count * a.group > kRows) != TENSOR)) return;
-  const int64_t first = (int64_t)unit * splits * kOf + row;
-  float m = -CUDART_INF_F;
-  for (int i = lane; i < splits; i += 32) m = fmaxf(m, ml[first + i * kOf].x);
+  const int all = tile.count * a.group;
+  if (all < j.least || all > j.most) return;
+  const bool mine = row < tile.rows;
+  const int64_t first = (int64_t)unit * n * R + row;
+  float m = -CUDART_INF_F, l = 0.f, x[N] = {};
+  if (mine) {
+    for (int i = lane; i < n; i += 32) m = fmaxf(m, j.ml[first + (int64_t)i * R].x);
 #pragma unroll
-  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  float l = 0.f, x[N] = {};
-  for (int i = 0; i < splits; i += 4) {
-    float w[4], y[4][N];
-    bool there[4];
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int i = warp % TEAM * 4; i < n; i += TEAM * 4) {
+      float w[4], y[4][N];
+      bool there[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t part = first + (int64_t)min(i + u, splits - 1) * kOf;
-      const float2 p = i + u < splits ? ml[part] : make_float2(-CUDART_INF_F, 0.f);
-      // an empty part (sum 0) does not count: nothing was written there
-      there[u] = p.y != 0.f;
-      w[u] = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
-      l += there[u] ? w[u] * p.y : 0.f;
-      const float *const src = parts + part * HD + lane * N;
-      if constexpr (N % 4 == 0) {
+      for (int u = 0; u < 4; ++u) {
+        const int64_t at = first + (int64_t)min(i + u, n - 1) * R;
+        const float2 p = i + u < n ? j.ml[at] : make_float2(-CUDART_INF_F, 0.f);
+        // an empty part (sum 0) does not count
+        there[u] = p.y != 0.f;
+        w[u] = p.y != p.y ? CUDART_NAN_F : exp2_fast(p.x - m);
+        l += there[u] ? w[u] * p.y : 0.f;
+        const float *const src = j.o + at * HD + lane * N;
+        if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int j = 0; j < N; j += 4) *(float4 *)&y[u][j] = *(const float4 *)(src + j);
-      } else if constexpr (N == 2) {
-        *(float2 *)y[u] = *(const float2 *)src;
-      } else {
-        y[u][0] = src[0];
+          for (int k = 0; k < N; k += 4) *(float4 *)&y[u][k] = *(const float4 *)(src + k);
+        } else if constexpr (N == 2) {
+          *(float2 *)y[u] = *(const float2 *)src;
+        } else {
+          y[u][0] = src[0];
+        }
       }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] += there[u] ? w[u] * y[u][k] : 0.f;
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[j] += there[u] ? w[u] * y[u][j] : 0.f;
   }
+  if constexpr (TEAM > 1) {   // in the order of the warps
+#pragma unroll
+    for (int k = 0; k < N; ++k) s_x[warp][lane * N + k] = x[k];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    if (warp % TEAM == 0)
+#pragma unroll
+      for (int t = 1; t < TEAM; ++t) {
+        l += s_l[warp + t];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] += s_x[warp + t][lane * N + k];
+      }
+  }
+  if (!mine || warp % TEAM) return;
   const float by = l == 0.f ? 0.f : 1.f / l;
   T *const out = (T *)a.out + row_at(a, tile, head, row, a.out_stride) + lane * N;
+  if constexpr (N >= 2) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if constexpr (N >= 2) {
-      if (j % 2 == 0) *(uint32_t *)(out + j) = Pair<T>::pack(x[j] * by, x[j + (N > 1)] * by);
-    } else {
-      out[0] = (T)(x[0] * by);
-    }
+    for (int k = 0; k < N; k += 2) *(uint32_t *)(out + k) = Pair<T>::pack(x[k] * by, x[k + 1] * by);
+  } else {
+    out[0] = (T)(x[0] * by);
   }
   if (lane == 0) write_lse(a, tile, head, row, m, l);
-}
-
-template <typename K>
-cudaError_t launch_after(K kernel, unsigned grid, int threads, size_t smem, cudaStream_t st, bool early, const MaskedArgs &a) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = early ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename T, int HD, bool FP8>
@@ -520,29 +483,45 @@ cudaError_t launch_rows(const MaskedArgs &a, cudaStream_t st) {
   constexpr size_t ring = (size_t)kWarps * kStages * 2 * kGroupOf<FP8> * HD * (FP8 ? 1 : 2);
   constexpr size_t join = (size_t)kWarps * kRows * (HD + 4) * 4;
   constexpr size_t smem = ring > join ? ring : join;
-  cudaError_t e = allow_shared<masked_rows_kernel<T, HD, FP8>>();
+  const cudaError_t e = allow_shared<masked_rows_kernel<T, HD, FP8>>();
   if (e != cudaSuccess) return e;
-  const unsigned units = (unsigned)a.tiles * a.c.n_heads;
-  return launch_after(masked_rows_kernel<T, HD, FP8>, units * a.splits, kWarps * 32, smem, st, false, a);
+  masked_rows_kernel<T, HD, FP8><<<(unsigned)a.tiles * a.c.n_heads * a.splits, kWarps * 32, smem, st>>>(a);
+  return cudaGetLastError();
 }
 
-template <typename T, int HD>
-cudaError_t launch_joins(const MaskedArgs &a, cudaStream_t st) {
-  cudaError_t e = cudaSuccess;
-  if (a.tensor_tiles && a.tensor_splits > 1)
-    e = launch_after(masked_join_kernel<T, HD, true>, (unsigned)a.tensor_tiles * a.c.n_heads * (kMaskedTensorRows / kRows), kRows * 32, 0, st, true, a);
-  if (e == cudaSuccess && a.tiles && a.splits > 1)
-    e = launch_after(masked_join_kernel<T, HD, false>, (unsigned)a.tiles * a.c.n_heads, kRows * 32, 0, st, true, a);
-  return e;
+template <typename T, int HD, int R, int TEAM>
+cudaError_t launch_join_by(const JoinArgs &j, int tiles, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)tiles * j.a.c.n_heads * ((R * TEAM + kJoinWarps - 1) / kJoinWarps));
+  cfg.blockDim = dim3(kJoinWarps * 32);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, masked_join_kernel<T, HD, R, TEAM>, j);
+}
+template <typename T, int HD, int R>
+cudaError_t launch_join(const JoinArgs &j, int tiles, cudaStream_t st) {   // more than two groups of four parts go to four warps
+  return j.parts > 8 ? launch_join_by<T, HD, R, 4>(j, tiles, st) : launch_join_by<T, HD, R, 1>(j, tiles, st);
 }
 
 // The row kernel, the tensor core kernel, the joins: each may start while the one before still runs and waits for it
 // before it ends, so that the last one ends last.
 template <typename T, int HD, bool FP8>
 cudaError_t launch_all(const MaskedArgs &a, int type, int io, cudaStream_t st) {
-  cudaError_t e = a.tiles ? launch_rows<T, HD, FP8>(a, st) : cudaSuccess;
-  if (e == cudaSuccess && a.tensor_tiles) e = launch_masked_tensor(a, type, io, a.tiles != 0, st);
-  return e == cudaSuccess ? launch_joins<T, HD>(a, st) : e;
+  cudaError_t e = !a.tiles ? cudaSuccess : a.few ? launch_masked_few(a, type, io, st) : launch_rows<T, HD, FP8>(a, st);
+  if constexpr (HD == 64 || HD == 128) {
+    if (e == cudaSuccess && a.tensor_tiles) e = launch_masked_tensor(a, type, io, a.tiles != 0, st);
+    if (e == cudaSuccess && a.tensor_tiles && a.tensor_splits > 1)
+      e = launch_join<T, HD, kMaskedTensorRows>({a, a.tensor_ml, a.tensor_o, a.tensor_splits, a.tensor_tiles_a_seq, a.short_rows + 1, 1 << 30}, a.tensor_tiles, st);
+  }
+  if (e == cudaSuccess && a.tiles && a.splits > 1) {
+    const JoinArgs j{a, a.part_ml, a.part_o, a.splits, a.tiles_a_seq, 1, a.short_rows ? a.short_rows : 1 << 30};
+    e = a.few ? launch_join<T, HD, kMaskedFewRows>(j, a.tiles, st) : launch_join<T, HD, kRows>(j, a.tiles, st);
+  }
+  return e;
 }
 
 template <typename T, bool FP8>
@@ -556,7 +535,7 @@ cudaError_t by_head_dim(const MaskedArgs &a, int type, int io, cudaStream_t st) 
   return cudaErrorInvalidValue;
 }
 
-constexpr int kMostSplits = 64, kMostUnits = 8 * kSms, kMostTensorUnits = 2 * kSms;   // units beyond which the token axis is not split
+constexpr int64_t kMostSplits = 64, kMostUnits = 8 * kSms, kMostTensorSplits = 64, kMostTensorUnits = 2 * kSms;   // splits of a unit, units with their splits
 
 // Row tiles of R rows: as many for every sequence, or as the packed tokens make, what leaves fewer of them empty.
 void count_tiles(MaskedShape &s, const MaskedSizes &n, int64_t rows) {
@@ -567,59 +546,61 @@ void count_tiles(MaskedShape &s, const MaskedSizes &n, int64_t rows) {
 
 bool on_tensor(const MaskedSizes &n) {
   MaskedShape s;
-  count_tiles(s, n, kMaskedRows);
-  return (n.head_dim == 64 || n.head_dim == 128) && (int64_t)n.max_q * (n.n_q_heads / n.n_heads) > kMaskedRows &&
+  count_tiles(s, n, kRows);
+  return (n.head_dim == 64 || n.head_dim == 128) && (int64_t)n.max_q * (n.n_q_heads / n.n_heads) > kRows &&
          (int64_t)s.tiles * n.n_heads * n.most_tokens >= 1 << 17;
 }
-
-int64_t row_unit(const MaskedSizes &n) { return kWarps * (n.e4m3 ? kGroupOf<true> : kGroupOf<false>); }
 
 }  // namespace
 
 MaskedShapes masked_shapes(const MaskedSizes &n) {
   MaskedShapes s{};
   const bool tensor = on_tensor(n);
+  const int64_t group = n.n_q_heads / n.n_heads;
   if (tensor) {
     // Blocks of up to 256 rows, one an SM: the number of splits with the fewest tiles one after the other, a block's
     // start and end counting as three.
     count_tiles(s.tensor, n, kMaskedTensorRows);
     const int64_t units = (int64_t)s.tensor.tiles * n.n_heads, tiles = (n.most_tokens + 127) / 128;
     int64_t best = 1, cost = INT64_MAX;
-    for (int64_t k = 1; k <= kMostSplits && k <= tiles && (k == 1 || k * units <= kMostTensorUnits); ++k) {
+    for (int64_t k = 1; k <= kMostTensorSplits && k <= tiles && (k == 1 || k * units <= kMostTensorUnits); ++k) {
       const int64_t c = ((units * k + kSms - 1) / kSms) * ((tiles + k - 1) / k + 3);
       if (c < cost) cost = c, best = k;
     }
     s.tensor.splits = (int32_t)best;
     s.tensor.parts = best > 1 ? units * best * kMaskedTensorRows : 0;
   }
-  // Beside the tensor core kernel the row kernel takes sequences with few rows, unless there are so few that they do not matter there.
+  // Beside the tensor core kernel a row kernel takes sequences with few rows, unless there are so few that they do not matter there.
   if (tensor && n.n_seqs * (int64_t)n.n_heads <= kSms / 2) return s;
-  count_tiles(s.rows, n, kMaskedRows);
+  s.few = tensor ? group <= kMaskedFewRows : n.max_q * group <= kMaskedFewRows;
+  const int rows = s.few ? kMaskedFewRows : kRows;
+  count_tiles(s.rows, n, rows);
   if (tensor) s.rows.tiles = n.n_seqs, s.rows.tiles_a_seq = 1;
-  // Splits: as many as make the sum of all the work over two blocks an SM, an item's start and end counting as
-  // 96 tokens, and of the last item least.
-  const int64_t unit = row_unit(n), units = (int64_t)s.rows.tiles * n.n_heads;
-  int64_t best = 1, cost = INT64_MAX;
-  for (int64_t k = 1; k <= kMostSplits && (k == 1 || ((k - 1) * unit < n.most_tokens && k * units <= kMostUnits)); ++k) {
-    const int64_t c = ((n.most_tokens + k - 1) / k + unit - 1) / unit * unit;
-    const int64_t t = units * k * (c + 96) / (2 * kSms) + c;
-    if (t < cost) cost = t, best = k;
+  // Splits.  Three blocks an SM run at once; while they do 64 tokens of a block take 2.4 us, with fewer of them down to 1 us (what a
+  // step's chain waits for; e4m3 2.0 and 1.3); a block's start and end count as 64 tokens, the join, a launch, as
+  // 5 us and 1 us for 16 parts.  Times in tenths of a us and 64ths.  Measured, 64 sequences in a window of 1024, 4 heads: 1 split 28 us, 2 37,
+  // 3 33, 8 42; 128 in a window of 4095, 2 heads, e4m3: 92, 82, 80, 89; one sequence of 2375 tokens, 64 rows: 1 split 50 us, 4 21, 8 16, 16 14.
+  const int64_t units = (int64_t)s.rows.tiles * n.n_heads, full = n.e4m3 ? 20 : 24, least = n.e4m3 ? 13 : 10;
+  int64_t cost = INT64_MAX;
+  for (int64_t k = 1; k <= kMostSplits && (k == 1 || ((k - 1) * 16 < n.most_tokens && k * units <= kMostUnits)); ++k) {
+    const int64_t c = (n.most_tokens + k - 1) / k + 64, waves = units * k / (3 * kSms), rest = units * k % (3 * kSms);
+    const int64_t t = c * (full * waves + (rest ? std::max(least, full * rest / (3 * kSms)) : 0)) + (k > 1 ? 3200 + 40 * k : 0);
+    if (t < cost) cost = t, s.rows.splits = (int32_t)k;
   }
-  s.rows.splits = (int32_t)best;
-  s.rows.parts = best > 1 ? units * best * kMaskedRows : 0;
+  s.rows.parts = s.rows.splits > 1 ? units * s.rows.splits * rows : 0;
   return s;
 }
 
 void masked_parts(const MaskedSizes &n, int64_t &rows, int64_t &tensor) {
   // Only calls whose units come to kMostUnits (kMostTensorUnits) at most with their splits have any parts.
   MaskedShape s;
-  const auto most = [&](int64_t tile_rows, int64_t unit, int64_t most_units) {
+  const auto most = [&](int tile_rows, int64_t step, int64_t most_splits, int64_t most_units) {
     count_tiles(s, n, tile_rows);
-    const int64_t splits = std::min<int64_t>(kMostSplits, (n.most_tokens + unit - 1) / unit);
-    return splits > 1 ? std::min<int64_t>(most_units, (int64_t)s.tiles * n.n_heads * splits) * tile_rows : 0;
+    const int64_t splits = std::min(most_splits, (n.most_tokens + step - 1) / step);
+    return splits > 1 ? std::min(most_units, (int64_t)s.tiles * n.n_heads * splits) * tile_rows : 0;
   };
-  rows = most(kMaskedRows, row_unit(n), kMostUnits);
-  tensor = on_tensor(n) ? most(kMaskedTensorRows, 128, kMostTensorUnits) : 0;
+  rows = std::max(most(kMaskedFewRows, 16, kMostSplits, kMostUnits), most(kRows, 16, kMostSplits, kMostUnits));
+  tensor = on_tensor(n) ? most(kMaskedTensorRows, 128, kMostTensorSplits, kMostTensorUnits) : 0;
 }
 
 cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st) {

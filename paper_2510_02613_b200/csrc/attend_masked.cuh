@@ -117,4 +117,53 @@ __device__ __forceinline__ void write_lse(const MaskedArgs &a, const RowTile &t,
         l > 0.f || l != l ? (m + log2f(l)) * CUDART_LN2_F : -CUDART_INF_F;
 }
 
+// Whether a word of two 16-bit elements, or of four e4m3 codes, has one that is infinite or not a number.
+template <typename T, bool FP8> __device__ __forceinline__ bool not_finite(uint32_t w) {
+  if constexpr (FP8) return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+  constexpr uint32_t kTop = __is_same(T, __half) ? 0x7c007c00u : 0x7f807f80u;
+  return __vcmpeq2(w & kTop, kTop) != 0;
+}
+
+// The end of a block of a row kernel, all threads: the parts of its WARPS warps - s_m, s_l, and in `joined` [warp][row][HD + 4] -
+// become one, and the rows go out, or, where the tile's tokens are split, to the workspace for the join kernel.
+template <typename IO, int HD, int R, int WARPS>
+__device__ __forceinline__ void finish_rows(const MaskedArgs &a, const RowTile &tile, int head, int unit, int split, const float *joined,
+                                            const float (&s_m)[WARPS][R], const float (&s_l)[WARPS][R]) {
+  constexpr int kLanes = HD / 4 < 32 ? HD / 4 : 32;   // of a row, 4 columns each at a time
+  const bool last = a.splits == 1;
+  for (int row = threadIdx.x / kLanes; row < tile.rows; row += WARPS * 32 / kLanes) {
+    float m = -CUDART_INF_F, l = 0.f, w[WARPS];
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) m = fmaxf(m, s_m[i][row]);
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      w[i] = m == -CUDART_INF_F ? 0.f : exp2_fast(s_m[i][row] - m);
+      l += w[i] * s_l[i][row];
+      if (s_l[i][row] != s_l[i][row]) l = w[i] = CUDART_NAN_F;   // a maximum does not carry a NaN: the sum does
+    }
+    const int64_t part = ((int64_t)unit * a.splits + split) * R + row;
+    const float by = last ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
+    IO *const out = (IO *)a.out + row_at(a, tile, head, row, a.out_stride);
+    for (int col = threadIdx.x % kLanes * 4; col < HD; col += 128) {
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) {
+        const float4 y = *(const float4 *)&joined[(i * R + row) * (HD + 4) + col];
+        x.x += w[i] * y.x;
+        x.y += w[i] * y.y;
+        x.z += w[i] * y.z;
+        x.w += w[i] * y.w;
+      }
+      if (last)
+        *(uint2 *)(out + col) = make_uint2(Pair<IO>::pack(x.x * by, x.y * by), Pair<IO>::pack(x.z * by, x.w * by));
+      else
+        *(float4 *)(a.part_o + part * HD + col) = x;
+    }
+    if (threadIdx.x % kLanes == 0) {
+      if (last) write_lse(a, tile, head, row, m, l);
+      else a.part_ml[part] = make_float2(m, l);
+    }
+  }
+}
+
 }  // namespace emoe

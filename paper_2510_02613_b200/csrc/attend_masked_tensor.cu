@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
   let_next_start();
   const int unit = blockIdx.x / a.tensor_splits, split = blockIdx.x - unit * a.tensor_splits, head = unit % a.c.n_heads;
   const RowTile tile = row_tile<kRows>(a, a.tensor_tiles_a_seq, unit / a.c.n_heads);
-  if (tile.rows == 0 || (a.short_rows && tile.count * a.group <= kMaskedRows)) {   // (so few rows may be the other kernel's)
+  if (tile.rows == 0 || (a.short_rows && tile.count * a.group <= a.short_rows)) {   // (so few rows may be the other kernel's)
     wait_for_previous();
     return;
   }

@@ -94,7 +94,7 @@ cudaError_t launch_attend_prefix(const AttendArgs &a, int type, int io, cudaStre
 cudaError_t launch_attend(const AttendArgs &a, int type, int io, cudaStream_t st);
 
 // Attention of packed query tokens over their own sequences, with masks: how it is cut.
-constexpr int kMaskedRows = 16, kMaskedTensorRows = 256;   // rows of a tile
+constexpr int kMaskedFewRows = 8, kMaskedRows = 16, kMaskedTensorRows = 256;   // rows of a tile
 struct MaskedShape {
   int32_t tiles, tiles_a_seq;      // row tiles: in all; of each sequence, 0: as many as its tokens make
   int32_t splits;                  // token ranges a tile
@@ -102,11 +102,12 @@ struct MaskedShape {
 };
 struct MaskedShapes {
   MaskedShape rows, tensor;        // tiles 0: the kernel has nothing to do
+  int32_t few;                     // rows: tiles of kMaskedFewRows
 };
 struct MaskedSizes {
   int32_t n_heads, n_seqs, n_tokens, max_q, n_q_heads, head_dim;
   bool e4m3;
-  int64_t most_tokens;             // that a row sees
+  int64_t most_tokens;             // that a tile of rows runs through
 };
 MaskedShapes masked_shapes(const MaskedSizes &n);
 // The most `parts` of a call of up to these sizes, of either kernel.
@@ -121,15 +122,16 @@ struct MaskedArgs {
   int64_t q_stride, out_stride;         // elements from one query token to the next
   const int32_t *block_table, *own_lens, *q_start;
   const uint32_t *mask;                 // null: the window
-  float2 *part_ml, *tensor_ml;          // [tile][head][split][row]: maximum (log2) and sum
+  float2 *part_ml, *tensor_ml;          // [tile][head][part][row]: maximum (log2) and sum
   float *part_o, *tensor_o;             // the same, [head_dim]
   int32_t n_seqs, n_tokens, max_q, n_q_heads, group, max_blocks, mask_words, window, sinks;
   float scale_log2;
-  int32_t tiles, tiles_a_seq, splits;
+  int32_t tiles, tiles_a_seq, splits, few;
   int32_t tensor_tiles, tensor_tiles_a_seq, tensor_splits;
-  int32_t short_rows;                   // both kernels run: sequences of up to kMaskedRows rows a head go to the row kernel
+  int32_t short_rows;                   // both kernels run: sequences of up to so many rows a head go to the row kernel; 0: one runs
   unsigned long long wait_ns;
 };
+cudaError_t launch_masked_few(const MaskedArgs &a, int type, int io, cudaStream_t st);
 cudaError_t launch_masked_tensor(const MaskedArgs &a, int type, int io, bool early, cudaStream_t st);
 cudaError_t launch_attend_masked(const MaskedArgs &a, int type, int io, cudaStream_t st);
 

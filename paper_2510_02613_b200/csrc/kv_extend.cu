@@ -27,38 +27,54 @@ __device__ __forceinline__ Sums running(Sums x, int lane) {   // sums of the lan
   return x;
 }
 
-// One sequence's change.
+// n / block_tokens and what is left, n below 2^32: the quotient by the floor of (2^32 - 1) / block_tokens is one too small at most for n
+// below 2^31, two beyond.
+__device__ __forceinline__ uint32_t block_of(const ExtendArgs &a, uint32_t n, uint32_t &rest) {
+  uint32_t q = __umulhi(n, a.per_token);
+  rest = n - q * (uint32_t)a.block_tokens;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (rest >= (uint32_t)a.block_tokens) ++q, rest -= (uint32_t)a.block_tokens;
+  return q;
+}
+
+// One sequence's change.  (Lengths and block sizes are below 2^31, a length after below 2^32.)
 struct Change {
-  int64_t after;             // length
-  int32_t had, back, wanted; // blocks
-  int64_t tokens;
-  bool fits;                 // its row of the table
+  uint32_t after;              // length
+  int32_t had, back, wanted;   // blocks
+  int32_t tokens;
+  bool fits;                   // its row of the table
 };
 __device__ __forceinline__ Change change_of(const ExtendArgs &a, int32_t before, int32_t add) {
   Change c;
-  c.after = max((int64_t)0, (int64_t)before + add);
+  c.after = (uint32_t)max((int64_t)0, (int64_t)before + add);
   c.tokens = max(0, add);
-  const int64_t bt = a.block_tokens, has = (c.after + bt - 1) / bt;
-  c.had = (int32_t)min((before + bt - 1) / bt, (int64_t)a.max_blocks);   // a length beyond the row has no more blocks than that
-  c.fits = add <= 0 || has <= a.max_blocks;
-  c.back = add < 0 ? max(0, c.had - (int32_t)min(has, (int64_t)a.max_blocks)) : 0;
-  c.wanted = add > 0 && c.fits ? max(0, (int32_t)has - c.had) : 0;
+  const auto blocks_of = [&](uint32_t n) {
+    uint32_t rest;
+    const uint32_t q = block_of(a, n, rest);
+    return q + (rest != 0);
+  };
+  const uint32_t has = blocks_of(c.after), most = (uint32_t)a.max_blocks;
+  c.had = (int32_t)min(blocks_of((uint32_t)before), most);   // a length beyond the row has no more blocks than that
+  c.fits = add <= 0 || has <= most;
+  c.back = add < 0 ? max(0, c.had - (int32_t)min(has, most)) : 0;
+  c.wanted = add > 0 && c.fits ? (int32_t)has - c.had : 0;
   return c;
 }
 
 // Every block of the cluster sums up the whole batch for itself, from lengths that it keeps in shared memory: nothing
 // is handed from one to another, and with the one cluster barrier behind the loads the results may go over the
 // inputs.  (A second barrier only where blocks are given back, which may be taken again at once.)  What is written is then
-// shared out: new and returned blocks by groups of 32 sequences, flattened over a warp's lanes, slots by token, whose
-// sequence is found among the starts in shared memory.  A slot of a new token does not wait for the table: a
-// block that is not in it yet is read from the list.
+// shared out: new and returned blocks by groups of 32 sequences, flattened over a warp's lanes, slots by runs of 128
+// tokens a warp, whose sequences are found among the starts in shared memory: those of the run's ends by the warp, those between
+// by each lane.  A slot of a new token does not wait for the table: a block that is not in it yet is read from the list.
 //
-// Bound by latency: loads, a scan, a barrier, loads that depend on it, stores; the slots' bytes at the most.
+// Bound by latency: loads, a scan, a barrier, loads that depend on it, stores.
 __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_constant__ ExtendArgs a) {
-  extern __shared__ int32_t s_seq[];   // [4][n_seqs]
+  extern __shared__ int32_t s_seq[];   // [5][n_seqs]
   __shared__ Sums s_warp[kWarps];
   __shared__ int32_t s_taken;
-  int32_t *const s_before = s_seq, *const s_add = s_seq + a.n_seqs, *const s_first = s_seq + 2 * a.n_seqs, *const s_at = s_seq + 3 * a.n_seqs;
+  int32_t *const s_before = s_seq, *const s_add = s_seq + a.n_seqs, *const s_first = s_seq + 2 * a.n_seqs, *const s_at = s_seq + 3 * a.n_seqs, *const s_had = s_seq + 4 * a.n_seqs;
   cg::cluster_group cluster = cg::this_cluster();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
   const auto report = [&](int code) {
@@ -77,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
   Sums mine{0, 0, 0};
   for (int i = first; i < last; ++i) {
     const Change c = change_of(a, s_before[i], s_add[i]);
-    mine = mine + Sums{c.tokens, c.back, c.wanted};
+    mine = mine + Sums{(int64_t)c.tokens, c.back, c.wanted};
   }
   const Sums upto = running(mine, lane);
   if (lane == 31) s_warp[warp] = upto;
@@ -96,25 +112,26 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
   for (int i = first; i < last; ++i) {
     const Change c = change_of(a, s_before[i], s_add[i]);
     s_first[i] = (int32_t)min(before.tokens, (int64_t)a.n_slots);
+    s_had[i] = c.had;
     const bool granted = c.fits && (c.tokens == 0 || before.tokens + c.tokens <= a.n_slots) && (c.wanted == 0 || before.wanted + c.wanted <= top);
     if (!granted) report(EMOE_ERR_TOO_LARGE);
     s_at[i] = !granted ? -1 : c.back ? before.back : before.wanted;
     if (granted && c.wanted) atomicMax(&s_taken, before.wanted + c.wanted);
-    before = before + Sums{c.tokens, c.back, c.wanted};
+    before = before + Sums{(int64_t)c.tokens, c.back, c.wanted};
   }
   if (all.back > room && threadIdx.x == 0) report(EMOE_ERR_TOO_LARGE);
   const int32_t tokens = (int32_t)min(all.tokens, (int64_t)a.n_slots);
   cluster.sync();   // all blocks have read what the results may go over
 
-  // Blocks of the 32 sequences of a group, one a lane at a time: body(sequence, its change, which of its blocks).
-  const auto for_blocks = [&](bool returned, auto body) {
+  // Blocks of the 32 sequences of a group, four a lane at a time: read(sequence, which of its blocks) gives an id, and
+  // once four of them are under way write(sequence, which, id) takes them on.
+  const auto for_blocks = [&](bool returned, auto read, auto write) {
     for (int group = warp * blocks + rank; group * 32 < a.n_seqs; group += kWarps * blocks) {
       const int i = group * 32 + lane;
-      Change c{};
       int32_t n = 0;
-      if (i < a.n_seqs) {
-        c = change_of(a, s_before[i], s_add[i]);
-        n = s_at[i] < 0 ? 0 : returned ? c.back : c.wanted;
+      if (i < a.n_seqs && s_at[i] >= 0) {
+        const Change c = change_of(a, s_before[i], s_add[i]);
+        n = returned ? c.back : c.wanted;
       }
       int32_t end = n;
 #pragma unroll
@@ -123,35 +140,46 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
         if (lane >= d) end += y;
       }
       const int32_t count = __shfl_sync(0xffffffffu, end, 31);
-      for (int32_t base = 0; base < count; base += 32) {
-        const int32_t j = base + lane;
-        int owner = 0;   // the first lane whose sum is above j
+      for (int32_t base = 0; base < count; base += 4 * 32) {
+        int seq[4];
+        int32_t which[4], id[4];
 #pragma unroll
-        for (int d = 16; d; d /= 2)
-          if (__shfl_sync(0xffffffffu, end, owner + d - 1) <= j) owner += d;
-        owner = min(owner, 31);
-        const int32_t start = __shfl_sync(0xffffffffu, end - n, owner);
-        if (j < count) body(group * 32 + owner, j - start);
+        for (int k = 0; k < 4; ++k) {
+          const int32_t j = base + 32 * k + lane;
+          int owner = 0;   // the first lane whose sum is above j
+#pragma unroll
+          for (int d = 16; d; d /= 2)
+            if (__shfl_sync(0xffffffffu, end, owner + d - 1) <= j) owner += d;
+          owner = min(owner, 31);
+          seq[k] = group * 32 + owner;
+          const int32_t first = __shfl_sync(0xffffffffu, end - n, owner);
+          which[k] = j < count ? j - first : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) id[k] = which[k] < 0 ? 0 : read(seq[k], which[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (which[k] >= 0) {
+            if (id[k] < 0 || id[k] >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
+            write(seq[k], which[k], id[k]);
+          }
       }
     }
   };
+  const auto row_of = [&](int i) { return a.block_table + (int64_t)i * a.max_blocks + s_had[i]; };   // behind the blocks that the sequence had
   if (all.back > 0) {
-    for_blocks(true, [&](int i, int32_t j) {
-      const Change c = change_of(a, s_before[i], s_add[i]);
-      const int32_t id = a.block_table[(int64_t)i * a.max_blocks + c.had - c.back + j], at = n_free + s_at[i] + j;
-      if (id < 0 || id >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
-      if (at < a.free_capacity) a.free_blocks[at] = id;
-    });
+    for_blocks(
+        true,
+        [&](int i, int32_t j) { return row_of(i)[j - change_of(a, s_before[i], s_add[i]).back]; },
+        [&](int i, int32_t j, int32_t id) {
+          const int32_t at = n_free + s_at[i] + j;
+          if (at < a.free_capacity) a.free_blocks[at] = id;
+        });
     __threadfence();
     cluster.sync();
   }
   const auto taken_block = [&](int i, int32_t j) { return a.free_blocks[top - 1 - (s_at[i] + j)]; };
-  for_blocks(false, [&](int i, int32_t j) {
-    const Change c = change_of(a, s_before[i], s_add[i]);
-    const int32_t id = taken_block(i, j);
-    if (id < 0 || id >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
-    a.block_table[(int64_t)i * a.max_blocks + c.had + j] = id;
-  });
+  for_blocks(false, taken_block, [&](int i, int32_t j, int32_t id) { row_of(i)[j] = id; });
   if (rank == 0) {
     for (int i = threadIdx.x; i < a.n_seqs; i += kThreads) {
       const Change c = change_of(a, s_before[i], s_add[i]);
@@ -163,24 +191,51 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
       *a.n_free_out = top - s_taken;
     }
   }
-  for (int i = rank * kThreads + threadIdx.x; i < a.n_slots; i += blocks * kThreads) {
-    int64_t slot = -1;
-    if (i < tokens) {
-      int lo = 0, hi = a.n_seqs;   // the last sequence that starts at or before i
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_first[mid] <= i) lo = mid;
-        else hi = mid;
+  constexpr int kAtOnce = 4, kRun = 32 * kAtOnce;   // tokens of a thread whose table entries are read without waiting for one another
+  const auto sequence_of = [&](int i) {   // the last one that starts at token i or before: 32 probes at a time
+    int lo = 0;
+    for (int hi = a.n_seqs; hi - lo > 1;) {
+      const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const int found = __popc(__ballot_sync(0xffffffffu, at < hi && s_first[at] <= i));
+      lo += max(0, found - 1) * step;
+      hi = min(hi, lo + step);
+    }
+    return lo;
+  };
+  for (int run = rank + blocks * warp; run < (a.n_slots + kRun - 1) / kRun; run += blocks * kWarps) {
+    const int base = run * kRun + lane, first_seq = sequence_of(run * kRun), last_seq = sequence_of(run * kRun + kRun - 1);
+    int seq[kAtOnce], hi[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) seq[j] = first_seq, hi[j] = last_seq + 1;
+    for (int left = last_seq + 1 - first_seq; left > 1; left = (left + 1) >> 1)
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int mid = (seq[j] + hi[j]) >> 1;
+        if (hi[j] - seq[j] > 1) {
+          if (s_first[mid] <= base + j * 32) seq[j] = mid;
+          else hi[j] = mid;
+        }
       }
-      if (s_at[lo] >= 0) {
-        const Change c = change_of(a, s_before[lo], s_add[lo]);
-        const uint32_t place = (uint32_t)(s_before[lo] + (i - s_first[lo])), column = place / (uint32_t)a.block_tokens;
-        const int32_t id = (int32_t)column < c.had ? a.block_table[(int64_t)lo * a.max_blocks + column] : taken_block(lo, (int32_t)column - c.had);
-        if (id >= 0 && id < a.num_blocks) slot = (int64_t)id * a.block_tokens + (place - column * (uint32_t)a.block_tokens);
-        else report(EMOE_ERR_BLOCK_TABLE);
+    int32_t id[kAtOnce];
+    uint32_t off[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int i = base + j * 32, s = seq[j];
+      id[j] = -1;
+      off[j] = 0;
+      if (i < tokens && s_at[s] >= 0) {
+        const uint32_t column = block_of(a, (uint32_t)(s_before[s] + (i - s_first[s])), off[j]);
+        id[j] = (int32_t)column < s_had[s] ? a.block_table[(int64_t)s * a.max_blocks + column] : taken_block(s, (int32_t)column - s_had[s]);
+        if (id[j] < 0 || id[j] >= a.num_blocks) {
+          report(EMOE_ERR_BLOCK_TABLE);
+          id[j] = -1;
+        }
       }
     }
-    a.slots[i] = slot;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+      if (base + j * 32 < a.n_slots)
+        a.slots[base + j * 32] = id[j] < 0 ? -1 : (int64_t)id[j] * a.block_tokens + off[j];
   }
 }
 
@@ -266,7 +321,7 @@ cudaError_t launch_kv_extend(const ExtendArgs &a, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = 16 * (size_t)a.n_seqs;
+  cfg.dynamicSmemBytes = 20 * (size_t)a.n_seqs;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;

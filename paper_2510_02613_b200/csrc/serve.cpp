@@ -437,6 +437,7 @@ emoe_status_t emoe_kv_extend(const emoe_kv_cache_t *c, const emoe_extend_t *p, v
   a.n_slots = p->n_slots;
   a.num_blocks = c->num_blocks;
   a.block_tokens = c->block_tokens;
+  a.per_token = 0xffffffffu / (uint32_t)c->block_tokens;
   return cuda_status(launch_kv_extend(a, (cudaStream_t)stream));
 }
 

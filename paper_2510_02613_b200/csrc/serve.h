@@ -46,6 +46,7 @@ struct ExtendArgs {
   int64_t *slots;
   int32_t *lens_out, *n_free_out, *status;
   int32_t n_seqs, max_blocks, free_capacity, n_slots, num_blocks, block_tokens;
+  uint32_t per_token;                   // (2^32 - 1) / block_tokens
 };
 cudaError_t launch_kv_extend(const ExtendArgs &a, cudaStream_t st);
 

@@ -27,7 +27,7 @@ namespace {
 constexpr int kRows = 2 * kTile;
 constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
 // Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
-constexpr int kSoftmaxRegs = 160, kMmaRegs = 80, kCopyRegs = 112;
+constexpr int kSoftmaxRegs = 160, kMmaRegs = 64, kCopyRegs = 128;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
 constexpr int kKept = 4;                   // tiles whose marks and scales are kept
 constexpr unsigned long long kDrainNs = 1000000000ull;
@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_odd;
   __shared__ uint32_t s_there[kKept][4];   // tokens that are there: a word of 32 rows from each copying warp
+  __shared__ float s_query[FP8 ? kRows : 1];   // e4m3: the queries are this much smaller than those that are multiplied
   __shared__ float2 s_second[kTile];       // the second slot's maximum and sum, where the slots are joined
   __shared__ __align__(16) float s_scale[2][FP8 ? kKept : 1][FP8 ? kTile : 4];   // of K and V
   uint8_t *const smem = (uint8_t *)(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
@@ -181,38 +182,50 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
     const float c = fmaxf(fabsf(a.scale_log2), 0x1p-149f);
     float query_by = 1.f;   // e4m3: the row's query is this much smaller than the one that is multiplied
     {
-      // The row's query (stored by two threads, half each, where both slots have the same rows): rows that do
-      // not exist are zero, a negative scale turns the sign.
-      uint4 *const w = (uint4 *)x;
-      const uint4 *const src = (const uint4 *)((const IO *)a.q + row_at(a, tile, head, min(row, rows - 1), a.q_stride));
-      const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) w[i] = row < rows ? src[i] : make_uint4(0, 0, 0, 0);
-      if constexpr (FP8) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i)
+      // The queries, a row by neighbouring lanes: 32 rows a warp, 16 where the slots have the same ones.  Rows that do not exist are
+      // zero.  (Loops here and at the end are short on purpose: a block runs them once, from instructions that are not in its cache yet.)
+      constexpr int kRowsAtOnce = 32 / kPieces;
+      const bool negative = a.scale_log2 < 0.f;   // scores are multiplied by its magnitude: the queries take the sign
+      const int mine = alternate ? 16 : 32, base = warp * mine, piece = lane % kPieces;
+      const int64_t from = row_at(a, tile, head, min(base + lane, rows - 1), a.q_stride);
+#pragma unroll 2
+      for (int i = 0; i < mine; i += kRowsAtOnce) {
+        const int r = i + lane / kPieces, row = base + r;
+        const IO *const src = (const IO *)a.q + __shfl_sync(0xffffffffu, from, r) + piece * 8;
+        const uint32_t at = row / kTile * kTileBytes + piece_at(row % kTile, piece);
+        if (!FP8 && !negative) {
+          copy_async_16(q_at + at, src, row < rows ? 16 : 0);
+        } else if constexpr (!FP8) {
+          const uint4 v = row < rows ? *(const uint4 *)src : make_uint4(0, 0, 0, 0);
+          *(uint4 *)(smem + at) = make_uint4(v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u);
+        } else {
+          const uint4 v = row < rows ? *(const uint4 *)src : make_uint4(0, 0, 0, 0);
+          uint32_t top = 0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float2 f = Pair<IO>::unpack(word(w[i], k));
+            const float2 f = Pair<IO>::unpack(word(v, k));
             top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
           }
-        const float by = query_scale(top);
-        query_by = 1.f / by;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const float2 e0 = Pair<IO>::unpack(w[i].x), e1 = Pair<IO>::unpack(w[i].y), e2 = Pair<IO>::unpack(w[i].z), e3 = Pair<IO>::unpack(w[i].w);
-          w[i] = make_uint4(Pair<T>::pack(e0.x * by, e0.y * by), Pair<T>::pack(e1.x * by, e1.y * by), Pair<T>::pack(e2.x * by, e2.y * by),
-                            Pair<T>::pack(e3.x * by, e3.y * by));
+          for (int d = 1; d < kPieces; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+          float by = query_scale(top);
+          if (piece == 0) s_query[row] = 1.f / by;
+          by = negative ? -by : by;
+          const float2 e0 = Pair<IO>::unpack(v.x), e1 = Pair<IO>::unpack(v.y), e2 = Pair<IO>::unpack(v.z), e3 = Pair<IO>::unpack(v.w);
+          *(uint4 *)(smem + at) = make_uint4(Pair<T>::pack(e0.x * by, e0.y * by), Pair<T>::pack(e1.x * by, e1.y * by), Pair<T>::pack(e2.x * by, e2.y * by),
+                                             Pair<T>::pack(e3.x * by, e3.y * by));
         }
       }
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i)
-        if (!alternate || i / (kPieces / 2) == slot)
-          *(uint4 *)(smem + (alternate ? 0 : slot * kTileBytes) + piece_at(local, i)) =
-              make_uint4(w[i].x ^ sign, w[i].y ^ sign, w[i].z ^ sign, w[i].w ^ sign);
-      fence_async();
-      bar_arrive(bar.q_full());
+      if (!FP8 && !negative) {
+        copies_arrive(bar.q_full());
+      } else {
+        fence_async();
+        bar_arrive(bar.q_full());
+      }
+      if constexpr (FP8) {
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        query_by = s_query[row0 + local];
+      }
     }
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;   // lane 32 * (warp % 4) in the address's upper half
     const uint32_t s_base = tmem + lanes + kColS + slot * kTile, o_col = tmem + lanes + kColO + slot * HD;
@@ -466,7 +479,14 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
         if (last) write_lse(a, tile, head, row, m, l);
         else a.tensor_ml[part] = make_float2(m, l);
       }
-      IO *const out = (IO *)a.out + row_at(a, tile, head, min(row, rows - 1), a.out_stride);
+      // 32 columns at a time through shared memory (the queries' place), from a row a thread to 128 bytes of a row by 8 neighbouring lanes:
+      // a lane's rows are lane / 8 and every fourth one after it.
+      const int64_t mine = last ? row_at(a, tile, head, min(row, rows - 1), a.out_stride) : part * HD;
+      uint8_t *const stage = smem + (alternate ? 0 : slot * kTileBytes) + (warp & 3) * 4096;
+      const int lane_row = lane >> 3, piece = lane & 7, left = rows - row0 - (warp & 3) * 32 - lane_row;   // rows from the first one on
+      int64_t to[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(0xffffffffu, mine, 4 * i + lane_row) + piece * 4;
 #pragma unroll 1
       for (int j = 0; j < HD / 32; ++j) {
         float y[32];
@@ -481,18 +501,20 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
             y[e + 3] = y[e + 3] * to_first + z.w * to_second;
           }
         }
-        if (row < rows) {
-          if (last) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8)
-              *(uint4 *)(out + 32 * j + e) = make_uint4(Pair<IO>::pack(y[e] * by, y[e + 1] * by), Pair<IO>::pack(y[e + 2] * by, y[e + 3] * by),
-                                                        Pair<IO>::pack(y[e + 4] * by, y[e + 5] * by), Pair<IO>::pack(y[e + 6] * by, y[e + 7] * by));
-          } else {
+        for (int e = 0; e < 32; e += 4)
+          *(float4 *)(stage + lane * 128 + ((e / 4 ^ (lane & 7)) << 4)) = make_float4(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
+        __syncwarp();
+        float4 z[8];
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *(float4 *)(a.tensor_o + part * HD + 32 * j + e) = make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+        for (int i = 0; i < 8; ++i) z[i] = *(const float4 *)(stage + (4 * i + lane_row) * 128 + ((piece ^ (4 * i + lane_row & 7)) << 4));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (4 * i < left) {
+            if (last) *(uint2 *)((IO *)a.out + to[i] + 32 * j) = make_uint2(Pair<IO>::pack(z[i].x, z[i].y), Pair<IO>::pack(z[i].z, z[i].w));
+            else *(float4 *)(a.tensor_o + to[i] + 32 * j) = z[i];
           }
-        }
+        __syncwarp();
       }
     }
     fence_before();
@@ -527,6 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
         for (int i = 0; i < kStep / 16; ++i) mma_ts(o_at, s_at + half * kStep + i * 8, v + i * (2048 >> 4), kIdO, add || i > 0);
       };
       bool ok = bar_wait_warp(bar.q_full(), 0, abort, a.wait_ns);
+      if constexpr (!FP8) fence_async();   // (copied as ordinary writes)
       const auto tile_of = [&](int i) { return mine.step(i) >> 1; };
       const auto last_of_tile = [&](int i) { return i + 1 == mine.count || tile_of(i + 1) != tile_of(i); };
       // A slot that leaves out a tile of both still gives its buffers back, once they have been filled: the

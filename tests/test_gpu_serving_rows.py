@@ -432,3 +432,20 @@ def test_waits_that_run_out_are_reported(hd, kv):
     status.zero_()
     check(ref, c, q, table, lens, starts, [RR.window_sees(3000, 200, 2000, 0)], "bf16", window=2000)
     assert status.item() == 0
+
+
+@pytest.mark.parametrize("kv,io,hd", [("bf16", "bf16", 128), ("f16", "f16", 64), ("e4m3", "bf16", 128), ("e4m3", "f16", 64)])
+def test_scales_and_strides_with_many_rows(kv, io, hd):
+    """Any finite scale, rows of wider tensors, at sizes for the tensor core kernel: a whole tile of rows and half a one."""
+    lens, counts = [1900, 1400], [200, 9]
+    rng, ref, table, starts, q = setup(hd, kv, io, False, 16, 2, 8, hd, lens, counts)
+    c, _, _ = device_cache(ref)
+    wide = torch.full((209, 2, 16, hd), float("nan"), dtype=TORCH[io], device="cuda")
+    wide[:, 1] = q
+    outs = torch.full((209, 2, 16, hd), 7.0, dtype=TORCH[io], device="cuda")
+    sees = [RR.window_sees(n, m, 1000, 4) for n, m in zip(lens, counts)]
+    bits = [tree_bits(rng, n) for n in counts]
+    for scale in (0.05, -0.07, 0.0):
+        check(ref, c, wide[:, 1], table, lens, starts, sees, io, scale=scale, window=1000, sinks=4, out=outs[:, 0])
+        check(ref, c, wide[:, 1], table, lens, starts, [RR.tree_sees(*x) for x in zip(lens, counts, bits)], io, scale=scale, bits=bits, out=outs[:, 0])
+        assert (outs[:, 1] == 7).all()

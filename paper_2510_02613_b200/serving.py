@@ -84,10 +84,16 @@ def _dense(t, what: str, inner: int):
 def _dense_pointer(t, what: str, shape, dtype: str, device):
     """Address of a tensor of this shape (None: any size) and type, densely packed, beside the arena; ValueError otherwise.
     (The first test is what a good call pays.)"""
-    if t is None or not (t.is_contiguous() and t.device == device and _names.get(t.dtype) == dtype and t.dim() == len(shape)
-                         and all([w is None or w == n for n, w in zip(t.shape, shape)])):
+    if t is None or t.shape != shape or _names.get(t.dtype) != dtype or t.device != device or not t.is_contiguous():
         _dense(_shaped(t, what, shape, dtype, device), what, len(shape))
     return t.data_ptr()
+
+
+def _sizes(t, what: str, n: int):
+    """The n sizes of t; ValueError if it has not as many."""
+    if t is None or t.dim() != n:
+        raise ValueError("%s: %s, wanted a tensor of %d dimensions" % (what, "missing" if t is None else tuple(t.shape), n))
+    return t.shape
 
 
 def _workspace(t, device):
@@ -112,14 +118,16 @@ def _arena_pointer(arena, need: int, what: str):
 
 
 class KvCache:
-    """One rank's paged KV cache: emoe_kv_append, emoe_kv_gather, emoe_kv_attend.
+    """One rank's paged KV cache: emoe_kv_append, emoe_kv_gather, emoe_kv_attend, emoe_kv_extend, emoe_kv_attend_tree,
+    emoe_kv_attend_window, emoe_kv_keep.
 
     arena: tensor or device address, [n_layers][2][num_blocks][block_tokens][n_heads][head_dim] as
     emoe_reshard_kv lays it out (head_major: [n_heads][block_tokens] inside a block).  kv_type: "bf16",
     "f16" or "e4m3"; the last has scale bytes [n_layers][2][num_blocks][block_tokens][n_heads] in
     `scales`, a KV arena of head_dim 1 and elem_bytes 1.  status: optional int32 tensor of one element,
     set to 4 (EMOE_ERR_BLOCK_TABLE) by calls that meet an id outside the pool, to 10 (EMOE_ERR_DEVICE_TIMEOUT)
-    by an attend whose bounded waits run out."""
+    by an attend whose bounded waits run out, to 11 (EMOE_ERR_TOO_LARGE) by an extend that refuses a sequence and by an
+    attend_tree or attend_window that meets more than max_q query tokens."""
 
     def __init__(self, arena, *, n_layers: int, num_blocks: int, block_tokens: int, n_heads: int, head_dim: int,
                  kv_type: str = "bf16", scales=None, head_major: bool = False, status=None):
@@ -239,13 +247,13 @@ class KvCache:
         each sequence's new tokens begin among all), slots (int64, any size: a slot a new token, -1 behind the last), lens_out
         (may be lens) and n_free_out (may be n_free).  A sequence that there is no room for stays as it was, its slots -1."""
         dev, at = self.device, _dense_pointer
-        p_lens = at(lens, "lens", (None,), "int32", dev)
-        n = lens.shape[0]
-        p = _b._Extend(p_lens, at(add, "add", (n,), "int32", dev), at(block_table, "block_table", (n, None), "int32", dev),
-                       at(free_blocks, "free_blocks", (None,), "int32", dev), at(n_free, "n_free", (1,), "int32", dev),
-                       at(q_start, "q_start", (n + 1,), "int32", dev), at(slots, "slots", (None,), "int64", dev),
-                       at(lens_out, "lens_out", (n,), "int32", dev), at(n_free_out, "n_free_out", (1,), "int32", dev),
-                       n, block_table.shape[1], free_blocks.shape[0], slots.shape[0], 0, 0)
+        (n,), (_, width) = _sizes(lens, "lens", 1), _sizes(block_table, "block_table", 2)
+        (room,), (tokens,) = _sizes(free_blocks, "free_blocks", 1), _sizes(slots, "slots", 1)
+        one, seqs = (1,), (n,)
+        p = _b._Extend(at(lens, "lens", seqs, "int32", dev), at(add, "add", seqs, "int32", dev), at(block_table, "block_table", (n, width), "int32", dev),
+                       at(free_blocks, "free_blocks", (room,), "int32", dev), at(n_free, "n_free", one, "int32", dev),
+                       at(q_start, "q_start", (n + 1,), "int32", dev), at(slots, "slots", (tokens,), "int64", dev),
+                       at(lens_out, "lens_out", seqs, "int32", dev), at(n_free_out, "n_free_out", one, "int32", dev), n, width, room, tokens, 0, 0)
         _check(self._calls.emoe_kv_extend(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
     def keep(self, block_table, lens, q_start, accepted, n_accepted, change, stream=None) -> None:
@@ -253,11 +261,10 @@ class KvCache:
         sequences' trees, their last q_start[s + 1] - q_start[s] tokens, to the front of these, in all layers.  change
         (int32 [n]) receives accepted less drafted tokens: the add of the next extend."""
         dev, at = self.device, _dense_pointer
-        p_lens = at(lens, "lens", (None,), "int32", dev)
-        n = lens.shape[0]
-        p = _b._Keep(at(block_table, "block_table", (n, None), "int32", dev), p_lens, at(q_start, "q_start", (n + 1,), "int32", dev),
-                     at(accepted, "accepted", (n, None), "int32", dev), at(n_accepted, "n_accepted", (n,), "int32", dev),
-                     at(change, "change", (n,), "int32", dev), n, block_table.shape[1], accepted.shape[1], 0)
+        (n,), (_, width), (_, most) = _sizes(lens, "lens", 1), _sizes(block_table, "block_table", 2), _sizes(accepted, "accepted", 2)
+        p = _b._Keep(at(block_table, "block_table", (n, width), "int32", dev), at(lens, "lens", (n,), "int32", dev),
+                     at(q_start, "q_start", (n + 1,), "int32", dev), at(accepted, "accepted", (n, most), "int32", dev),
+                     at(n_accepted, "n_accepted", (n,), "int32", dev), at(change, "change", (n,), "int32", dev), n, width, most, 0)
         _check(self._calls.emoe_kv_keep(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
     def attend_tree_workspace_bytes(self, n_seqs: int, n_tokens: int, max_q: int, n_q_heads: int, max_blocks: int) -> int:
@@ -280,8 +287,9 @@ class KvCache:
         nodes of sequence s at q_start[s] (int32 [n_seqs + 1]), at most max_q of them: the last ones of its own_lens[s] tokens.
         A node sees all tokens before the nodes and those nodes whose bits its row of mask (int32 [n_tokens, words]) has.
         workspace, lse, wait_limit_us: as for attend."""
-        bits = _dense_pointer(mask, "mask", (q.shape[0], None), "int32", self.device)
-        self._attend_rows(self._calls.emoe_kv_attend_tree, layer, q, out, block_table, own_lens, q_start, bits, max_q, mask.shape[1], 0, 0,
+        words = _sizes(mask, "mask", 2)[1]
+        bits = _dense_pointer(mask, "mask", (q.shape[0], words), "int32", self.device)
+        self._attend_rows(self._calls.emoe_kv_attend_tree, layer, q, out, block_table, own_lens, q_start, bits, max_q, words, 0, 0,
                           scale, lse, workspace, stream, wait_limit_us)
 
     def attend_window(self, layer: int, q, out, block_table, own_lens, q_start, max_q: int, window: int, sinks: int = 0,
@@ -305,12 +313,11 @@ class KvCache:
             if not x.is_contiguous():
                 _dense(x, what, 2)
                 strides[i] = x.stride(0) if t > 1 else row
-        p_lens = at(own_lens, "own_lens", (None,), "int32", dev)
-        n = own_lens.shape[0]
+        (n,), (_, width) = _sizes(own_lens, "own_lens", 1), _sizes(block_table, "block_table", 2)
         work, size = _workspace(workspace, dev)
         p = _b._AttendRows(q.data_ptr(), out.data_ptr(), None if lse is None else at(lse, "lse", (t, hq), "float32", dev), strides[0], strides[1],
-                           at(block_table, "block_table", (n, None), "int32", dev), p_lens, at(q_start, "q_start", (n + 1,), "int32", dev), mask,
-                           work, size, n, t, max_q, hq, block_table.shape[1], words, window, sinks, _value_type(q, "q"),
+                           at(block_table, "block_table", (n, width), "int32", dev), at(own_lens, "own_lens", (n,), "int32", dev),
+                           at(q_start, "q_start", (n + 1,), "int32", dev), mask, work, size, n, t, max_q, hq, width, words, window, sinks, _value_type(q, "q"),
                            hd ** -0.5 if scale is None else scale, wait_limit_us, 0)
         _check(call(self._ref, layer, ctypes.byref(p), _stream_handle(stream)))
 

@@ -56,14 +56,16 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
     const int u = u0 + (warp + kWarps * i) * kGroup + (lane & (kGroup - 1));
     return i >= steps || u >= u1 ? -1 : u;
   };
-  auto block_of = [&](int i) {
+  // What the table says of it: the block, and the place there (beyond any block: there is no token).
+  constexpr uint32_t kNone = 0xffffffffu;
+  struct Found { int block; uint32_t off; };
+  auto find = [&](int i) {
     const int u = place_of(i);
-    return u < 0 ? 0 : table[(uint32_t)run.token(u) / (uint32_t)a.c.block_tokens];
+    if (u < 0) return Found{0, kNone};
+    const TokenPlace p = place_of_token(a, run.token(u));
+    return Found{table[p.column], p.off};
   };
-  auto vector_of = [&](int i, int block) {
-    const int u = place_of(i);
-    return u < 0 ? (int64_t)-1 : masked_vector(a, block, run.token(u), head);
-  };
+  auto vector_of = [&](const Found &f) { return f.off == kNone ? (int64_t)-1 : masked_vector(a, f.block, f.off, head); };
   uint32_t held_scale = 0, held_valid = 0;
   auto issue = [&](int i, int64_t vec) {   // starts the copies of step i
     const uint32_t at = ring_at + (i % kStages) * kStage;
@@ -93,12 +95,12 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) {
     if (i < steps) {
-      issue(i, vector_of(i, block_of(i)));
+      issue(i, vector_of(find(i)));
       keep(i);
     }
     copy_async_commit();
   }
-  int block = block_of(kStages - 1);   // the table is read a step ahead
+  Found next = find(kStages - 1);   // the table is read a step ahead
 
   // query rows g and g + 8 of the tile as matrix operands, from global memory; rows that do not exist are the last one again
   uint32_t q[HD / 16][4];
@@ -145,9 +147,9 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
 
   for (int i = 0; i < steps; ++i) {
     const int ahead = i + kStages - 1;
-    if (ahead < steps) issue(ahead, vector_of(ahead, block));
+    if (ahead < steps) issue(ahead, vector_of(next));
     copy_async_commit();
-    block = block_of(ahead + 1);
+    next = find(ahead + 1);
     const int base = u0 + (warp + kWarps * i) * kGroup;
     uint32_t seen[2];
 #pragma unroll

@@ -94,9 +94,18 @@ struct Sight {
   }
 };
 
-// Vector index of token t, which lies on `block`; -1 (and the status word) if that is outside the pool.
-__device__ __forceinline__ int64_t masked_vector(const MaskedArgs &a, int block, int t, int head) {
-  const uint32_t off = (uint32_t)t % (uint32_t)a.c.block_tokens;
+// A token's column of the table and its place in the block there.  (The quotient by the floor of (2^32 - 1) / block_tokens is one too small
+// at most: tokens are below 2^30.)
+struct TokenPlace { uint32_t column, off; };
+__device__ __forceinline__ TokenPlace place_of_token(const MaskedArgs &a, int token) {
+  const uint32_t bt = (uint32_t)a.c.block_tokens;
+  uint32_t q = __umulhi((uint32_t)token, a.per_token), off = (uint32_t)token - q * bt;
+  if (off >= bt) ++q, off -= bt;
+  return {q, off};
+}
+// Vector index of place `off` of `block`; -1 (and the status word) if that is outside the pool.
+// (The table is read apart from this and well before: a branch on what it says waits for it.)
+__device__ __forceinline__ int64_t masked_vector(const MaskedArgs &a, int block, uint32_t off, int head) {
   if (block < 0 || block >= a.num_blocks) {
     if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
     return -1;

@@ -419,8 +419,8 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
             for (; bits; bits &= bits - 1) {
               const int u = u0 + step * kStep + 32 * k + __ffs(bits) - 1;
               if (u >= u1) break;
-              const int token = run.token(u), block = a.block_table[(int64_t)tile.seq * a.max_blocks + token / a.c.block_tokens];
-              const int64_t vec = masked_vector(a, block, token, head);
+              const TokenPlace p = place_of_token(a, run.token(u));
+              const int64_t vec = masked_vector(a, a.block_table[(int64_t)tile.seq * a.max_blocks + p.column], p.off, head);
               if (vec < 0) continue;
 #pragma unroll
               for (int e = 0; e < 32; ++e) {
@@ -485,41 +485,48 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
         if (last) write_lse(a, tile, head, row, m, l);
         else a.tensor_ml[part] = make_float2(m, l);
       }
-      // 32 columns at a time through shared memory (the queries' place), from a row a thread to 128 bytes of a row by 8 neighbouring lanes:
-      // a lane's rows are lane / 8 and every fourth one after it.
+      // Columns go through shared memory (the queries' place), 128 bytes of a row at a time, from a row a thread to 8 neighbouring
+      // lanes a row: a lane's rows are lane / 8 and every fourth one after it.
+      constexpr int kBatch = HD / 64;   // 128-byte pieces of a row under way at once: what the place holds
       const int64_t mine = last ? row_at(a, tile, head, min(row, rows - 1), a.out_stride) : part * HD;
-      uint8_t *const stage = smem + (alternate ? 0 : slot * kTileBytes) + (warp & 3) * 4096;
+      uint8_t *const stage = smem + (alternate ? 0 : slot * kTileBytes) + (warp & 3) * (kBatch * 4096);
       const int lane_row = lane >> 3, piece = lane & 7, left = rows - row0 - (warp & 3) * 32 - lane_row;   // rows from the first one on
       int64_t to[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(0xffffffffu, mine, 4 * i + lane_row) + piece * 4;
 #pragma unroll 1
-      for (int j = 0; j < HD / 32; ++j) {
-        float y[32];
-        columns(y, j);
-        if (alternate) {
+      for (int j0 = 0; j0 < HD / 32; j0 += kBatch) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 z = joined ? *other_at(j, e) : make_float4(0.f, 0.f, 0.f, 0.f);
-            y[e] = y[e] * to_first + z.x * to_second;
-            y[e + 1] = y[e + 1] * to_first + z.y * to_second;
-            y[e + 2] = y[e + 2] * to_first + z.z * to_second;
-            y[e + 3] = y[e + 3] * to_first + z.w * to_second;
+        for (int b = 0; b < kBatch; ++b) {
+          float y[32];
+          columns(y, j0 + b);
+          if (alternate) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 z = joined ? *other_at(j0 + b, e) : make_float4(0.f, 0.f, 0.f, 0.f);
+              y[e] = y[e] * to_first + z.x * to_second;
+              y[e + 1] = y[e + 1] * to_first + z.y * to_second;
+              y[e + 2] = y[e + 2] * to_first + z.z * to_second;
+              y[e + 3] = y[e + 3] * to_first + z.w * to_second;
+            }
           }
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *(float4 *)(stage + b * 4096 + lane * 128 + ((e / 4 ^ (lane & 7)) << 4)) = make_float4(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
         }
-#pragma unroll
-        for (int e = 0; e < 32; e += 4)
-          *(float4 *)(stage + lane * 128 + ((e / 4 ^ (lane & 7)) << 4)) = make_float4(y[e] * by, y[e + 1] * by, y[e + 2] * by, y[e + 3] * by);
         __syncwarp();
-        float4 z[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = *(const float4 *)(stage + (4 * i + lane_row) * 128 + ((piece ^ (4 * i + lane_row & 7)) << 4));
+        for (int b = 0; b < kBatch; ++b) {
+          float4 z[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (4 * i < left) {
-            if (last) *(uint2 *)((IO *)a.out + to[i] + 32 * j) = make_uint2(Pair<IO>::pack(z[i].x, z[i].y), Pair<IO>::pack(z[i].z, z[i].w));
-            else *(float4 *)(a.tensor_o + to[i] + 32 * j) = z[i];
-          }
+          for (int i = 0; i < 8; ++i) z[i] = *(const float4 *)(stage + b * 4096 + (4 * i + lane_row) * 128 + ((piece ^ (4 * i + lane_row & 7)) << 4));
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (4 * i < left) {
+              if (last) *(uint2 *)((IO *)a.out + to[i] + 32 * (j0 + b)) = make_uint2(Pair<IO>::pack(z[i].x, z[i].y), Pair<IO>::pack(z[i].z, z[i].w));
+              else *(float4 *)(a.tensor_o + to[i] + 32 * (j0 + b)) = z[i];
+            }
+        }
         __syncwarp();
       }
     }
@@ -629,31 +636,30 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
       if (lane == 0) s_there[t % kKept][w] = word;
       __syncwarp();
     };
-    // this lane's token of a tile, -1 if there is none; its block; its vector index
-    const auto place_of = [&](int t) {
+    // What the table says of this lane's token of a tile: the block, and the place there (beyond any block: there is no token).
+    constexpr uint32_t kNone = 0xffffffffu;
+    struct Found { int block; uint32_t off; };
+    const auto find = [&](int t) {
       const int u = u0 + t * kTile + my_row;
-      return t < tiles && u < u1 ? u : -1;
+      if (t >= tiles || u >= u1) return Found{0, kNone};
+      const TokenPlace p = place_of_token(a, run.token(u));
+      return Found{table[p.column], p.off};
     };
-    const auto block_of = [&](int t) {
-      const int u = place_of(t);
-      return u < 0 ? 0 : table[(uint32_t)run.token(u) / (uint32_t)a.c.block_tokens];
-    };
-    const auto vector_of = [&](int t, int block) {
-      const int u = place_of(t);
-      return u < 0 ? (int64_t)-1 : masked_vector(a, block, run.token(u), head);
-    };
+    const auto vector_of = [&](const Found &f) { return f.off == kNone ? (int64_t)-1 : masked_vector(a, f.block, f.off, head); };
     // Order: K of an even tile, K of the next, V of both.  (With one row tile the scores run two tiles
     // ahead: a value buffer that waits for its products must not hold up the keys that those need.)
     bool ok = true;
     if constexpr (!FP8) {
-      int block[2] = {block_of(0), block_of(1)};   // the table is read a pair ahead
+      Found next[2] = {find(0), find(1)};   // the table is read a pair ahead
       for (int first = 0; first < tiles && ok; first += 2) {
-        const int64_t vec[2] = {vector_of(first, block[0]), vector_of(first + 1, block[1])};
-        block[0] = block_of(first + 2);
-        block[1] = block_of(first + 3);
+        int64_t vec[2];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int v = u >> 1, stage = u & 1, t = first + stage;
+          if (v == 0) {
+            vec[stage] = vector_of(next[stage]);
+            next[stage] = find(t + 2);
+          }
           if (t >= tiles || !ok) continue;
           if (t >= 2) ok = bar_wait_warp<true>(v ? bar.v_empty(stage) : bar.k_empty(stage), (t >> 1) + 1 & 1, abort, a.wait_ns);
           if (!ok) continue;
@@ -715,12 +721,12 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
           if (at >= 0) raw[parity][pass] = *(const uint4 *)(pool + at * HD + piece * 16);
         }
       };
-      int block[2] = {block_of(0), block_of(1)};   // the table is read a pair ahead
-      int64_t vec[2] = {vector_of(0, block[0]), vector_of(1, block[1])};
-      block[0] = block_of(2);
-      block[1] = block_of(3);
+      Found next[2] = {find(0), find(1)};   // the table is read a pair ahead
+      int64_t vec[2] = {vector_of(next[0]), vector_of(next[1])};
       load(0, 0, vec[0]);
       load(0, 1, vec[1]);
+      next[0] = find(2);
+      next[1] = find(3);
       for (int first = 0; first < tiles && ok; first += 2) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -756,8 +762,8 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
           if (v == 0) {
             load(1, stage, vec[stage]);
           } else {
-            vec[stage] = vector_of(t + 2, block[stage]);
-            block[stage] = block_of(t + 4);
+            vec[stage] = vector_of(next[stage]);
+            next[stage] = find(t + 4);
             load(0, stage, vec[stage]);
           }
         }

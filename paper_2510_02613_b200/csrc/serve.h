@@ -129,6 +129,7 @@ struct MaskedArgs {
   float scale_log2;
   int32_t tiles, tiles_a_seq, splits, few;
   int32_t tensor_tiles, tensor_tiles_a_seq, tensor_splits;
+  uint32_t per_token;                   // (2^32 - 1) / block_tokens
   int32_t short_rows;                   // both kernels run: sequences of up to so many rows a head go to the row kernel; 0: one runs
   unsigned long long wait_ns;
 };

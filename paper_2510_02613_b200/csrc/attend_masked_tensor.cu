@@ -440,6 +440,9 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
     if (n_steps == 0 || !ok) {
       m = -CUDART_INF_F;
       l = ok ? 0.f : CUDART_NAN_F;
+      // No score has waited for the queries, whose place the outputs go through: they are there soon, whoever has given up.
+      int late = 0;
+      bar_wait_warp(bar.q_full(), 0, &late, kDrainNs);
     } else {
       m -= kLift;
     }

@@ -449,3 +449,60 @@ def test_scales_and_strides_with_many_rows(kv, io, hd):
         check(ref, c, wide[:, 1], table, lens, starts, sees, io, scale=scale, window=1000, sinks=4, out=outs[:, 0])
         check(ref, c, wide[:, 1], table, lens, starts, [RR.tree_sees(*x) for x in zip(lens, counts, bits)], io, scale=scale, bits=bits, out=outs[:, 0])
         assert (outs[:, 1] == 7).all()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+def test_more_query_tokens_than_tokens_with_many_rows(kv):
+    lens, counts = [100, 1700, 3], [300, 260, 150]
+    rng, ref, table, starts, q = setup(13, kv, "bf16", False, 16, 4, 8, 128, lens, counts)
+    c, _, _ = device_cache(ref)
+    check(ref, c, q, table, lens, starts, [RR.window_sees(n, m, 1500, 4) for n, m in zip(lens, counts)], "bf16", window=1500, sinks=4)
+    bits = [tree_bits(rng, n, 0.4) for n in counts]
+    check(ref, c, q, table, lens, starts, [RR.tree_sees(n, m, b) for n, m, b in zip(lens, counts, bits)], "bf16", bits=bits)
+
+
+def test_on_three_streams_at_once():
+    """Calls of every kernel, each with a workspace of its own, give what they give alone."""
+    cases = []
+    for seed, (lens, counts) in enumerate((([3000, 2500], [200, 40]), ([1500] * 40, [1] * 40), ([2000, 900, 700], [2, 2, 1]))):
+        rng, ref, table, starts, q = setup(20 + seed, "bf16", "bf16", False, 16, 4, 8, 128, lens, counts)
+        c, _, _ = device_cache(ref)
+        want = call(c, q, table, lens, starts, window=1200, sinks=4)
+        need = c.attend_window_workspace_bytes(len(lens), q.shape[0], max(counts), 32, table.shape[1], 1200, 4)
+        cases.append((c, q, torch.empty_like(q), torch.empty(q.shape[:2], device="cuda"), dev(table), dev(lens), dev(starts), max(counts),
+                      torch.empty(max(1, need), dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), want))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, q, out, lse, table, lens, starts, max_q, work, st, _ in cases:
+            c.attend_window(1, q, out, table, lens, starts, max_q, 1200, 4, lse=lse, workspace=work, stream=st)
+    torch.cuda.synchronize()
+    for _, _, out, lse, _, _, _, _, _, _, want in cases:
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_prompts_in_pieces_then_single_tokens():
+    """Extend, append, attend_window step by step: pieces of prompts among sequences that decode, blocks behind the window given to nobody."""
+    rng = np.random.default_rng(14)
+    block, hkv, hd, pool, window, sinks = 8, 2, 128, 60, 50, 3
+    c, arena, _ = device_cache(filled(rng, (1, pool, block, hkv), hd, "bf16", False))
+    n, lens, q_start, n_free = 3, dev([0] * 3), dev([0] * 4), dev([pool])
+    table, free, slots = dev(np.full((n, 24), -1)), dev(rng.permutation(pool)), dev(np.zeros(128), np.int64)
+    kept = [[], [], []]
+    for add in ([40, 5, 33], [30, 1, 40], [1, 1, 40], [1, 1, 20], [1, 1, 1], [0, 1, 1]):
+        c.extend(lens, dev(add), table, free, n_free, q_start, slots, lens, n_free)
+        x = torch.from_numpy(rng.standard_normal((2, 128, hkv, hd))).to(torch.bfloat16).cuda()
+        c.append(0, x[0], x[1], slots)
+        q = torch.from_numpy(rng.standard_normal((128, 8, hd))).to(torch.bfloat16).cuda()
+        out = torch.empty_like(q)
+        work = torch.empty(max(1, c.attend_window_workspace_bytes(n, 128, 40, 8, 24, window, sinks)), dtype=torch.uint8, device="cuda")
+        c.attend_window(0, q, out, table, lens, q_start, 40, window, sinks, workspace=work)
+        at = q_start.tolist()
+        for s in range(n):
+            kept[s] += [x[:, i] for i in range(at[s], at[s + 1])]
+            seq = torch.stack(kept[s], 1).double()
+            see = torch.from_numpy(RR.window_sees(len(kept[s]), add[s], window, sinks)).cuda()
+            for h in range(8):
+                p = torch.softmax((q[at[s]:at[s + 1], h].double() @ seq[0, :, h // 4].T * hd ** -0.5).masked_fill(~see, float("-inf")), -1)
+                want, a = p @ seq[1, :, h // 4], p @ seq[1, :, h // 4].abs()
+                assert ((out[at[s]:at[s + 1], h].double() - want).abs() <= 2.2 * 2.0 ** -8 * a).all()
+    assert lens.tolist() == [len(k) for k in kept]

@@ -151,6 +151,23 @@ def test_workspaces_grow(kv, hd):
             assert need(*small) <= have and accepted(small, have), (big, small)
 
 
+def test_workspaces_of_trees_grow():
+    rng = np.random.default_rng(5)
+    c, n = _cache(num_blocks=100000, block_tokens=16, n_heads=4, head_dim=128), ctypes.c_uint64()
+
+    def need(*size):
+        assert B.lib().emoe_kv_attend_tree_workspace(ctypes.byref(c), *size, ctypes.byref(n)) == 0
+        return n.value
+    for _ in range(200):
+        big = [int(2 ** rng.uniform(0, 7)), int(2 ** rng.uniform(0, 11)), int(2 ** rng.uniform(0, 8)), 4 * int(rng.integers(1, 9)), int(2 ** rng.uniform(0, 12))]
+        have = need(*big)
+        for _ in range(10):
+            small = [int(rng.integers(1, x + 1)) for x in big]
+            small[3] = 4 * int(rng.integers(1, big[3] // 4 + 1))
+            p = B._AttendRows(1 << 20, 1 << 21, None, 1 << 20, 1 << 20, 1 << 22, 1 << 23, 1 << 25, 1 << 26, 1 << 28 if have else None, have, *small, 8, 0, 0, 0, 0.125, 0, 0)
+            assert need(*small) <= have and B.lib().emoe_kv_attend_tree(ctypes.byref(c), 0, ctypes.byref(p), None) != 1, (big, small)
+
+
 def test_python_checks():
     arena = torch.zeros(2 * 8 * 4 * 2 * 64 * 2, dtype=torch.uint8)
     c = E.KvCache(arena, n_layers=1, num_blocks=8, block_tokens=4, n_heads=2, head_dim=64)

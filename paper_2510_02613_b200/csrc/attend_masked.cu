@@ -23,7 +23,7 @@ template <bool FP8> constexpr int kGroupOf = FP8 ? 32 : 16;
 // One warp's step covers 16 tokens (32 of an e4m3 cache): K and V rows come through a ring of its own in shared
 // memory, scores and products on the tensor cores with the 16 rows of the tile as the m side, running maximum
 // and sum in registers.  The four warps take every fourth group of tokens and are joined at the end.  Three blocks an SM (registers, ring).
-// Measured, 48 trees of up to 13 nodes on up to 2750 tokens, 16 heads of their own, e4m3, head_dim 128: 125 us, 2.0 TB/s, DRAM at 32%, issue
+// Measured, 48 trees of up to 13 nodes on up to 2750 tokens, 16 heads of their own, e4m3, head_dim 128: 97 us, 2.6 TB/s; issue
 // slots 46%, integer pipe 37%: what bounds it is the chain of a step, with three warps a scheduler.
 template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_kernel(const __grid_constant__ MaskedArgs a) {
@@ -36,9 +36,10 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_ker
   __shared__ uint32_t s_valid[kWarps][kStages];
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits, head = unit % a.c.n_heads;
+  const int split = blockIdx.x % a.splits, unit_rank = blockIdx.x / a.splits, head = unit_rank % a.c.n_heads;
   let_next_start();
-  const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, unit / a.c.n_heads);
+  const int number = a.ranked ? ranked_tile(a, unit_rank / a.c.n_heads) : unit_rank / a.c.n_heads, unit = number * a.c.n_heads + head;
+  const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, number);
   if (tile.rows == 0 || (a.short_rows && tile.count * a.group > a.short_rows)) return;
   const Run run = run_of(a, tile);
   // tokens of this split: whole steps of a warp
@@ -599,6 +600,10 @@ MaskedShapes masked_shapes(const MaskedSizes &n) {
     if (t < cost) cost = t, s.rows.splits = (int32_t)k;
   }
   s.rows.parts = s.rows.splits > 1 ? units * s.rows.splits * rows : 0;
+  // Finding a rank costs a block about 1 us; it pays where blocks wait for others to end, if lengths differ.  Measured, 48 trees on 13 to
+  // 2750 tokens, 16 heads: e4m3 130 us as they come, 97 the longest first, bf16 106 and 88; 128 single tokens in a window of 512 that
+  // nearly all of them fill: 56 and 60.
+  s.ranked = n.by_length && s.rows.tiles_a_seq && n.n_seqs > 1 && n.n_seqs <= kMostRanked && units * s.rows.splits > 3 * kSms;
   return s;
 }
 

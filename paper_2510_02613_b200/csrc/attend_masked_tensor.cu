@@ -18,9 +18,9 @@
 // Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row), 8 and 9 issue the slots' products, 12-15 bring
 // K and V rows from their pages into the 128-byte-swizzled tiles that the products read (e4m3 codes widened on the way).
 //
-// Measured, bf16, head_dim 128: a tile of 128 tokens x 256 rows takes 2.15 us, a unit's start and end 4.9 us.  8192 tokens of a prompt
-// in a window of 4096, 32 on 4 heads: 628 us, 877 TFLOP/s, 52% of a library product's rate; 8 trees of 64 nodes on 16000 tokens: 181 us.  Three
-// chains take about as long as one another: without the softmax a tile would take 1.88 us, without the products 1.94, without
+// Measured, bf16, head_dim 128: a tile of 128 tokens x 256 rows takes 2.15 us, a unit's start and end about 7 us (queries and first tiles,
+// 192 KB a block, come for all blocks at once: 3 us; outputs 2.5 us).  8192 tokens of a prompt in a window of 4096, 32 on 4 heads: 635 us, 867
+// TFLOP/s, 51% of a library product's rate; 8 trees of 64 nodes on 16000 tokens: 181 us.  Three chains take about as long as one another: without the softmax a tile would take 1.88 us, without the products 1.94, without
 // exponentials as long as with them.  The products of S, 64 columns wide, are bound by shared memory (48 clocks for 16 of k, not 32); whole
 // tiles of 128 columns, which are not, leave no scores to work on while the next ones are made (2.86 us).
 #include "attend_item.cuh"
@@ -31,30 +31,9 @@ namespace emoe {
 namespace {
 
 constexpr int kRows = 2 * kTile;
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
 // Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
 constexpr int kSoftmaxRegs = 160, kMmaRegs = 64, kCopyRegs = 128;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
-constexpr int kKept = 4;                   // tiles whose marks and scales are kept
-constexpr unsigned long long kDrainNs = 1000000000ull;
-constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
-constexpr uint32_t kColS = 0, kColO = 256; // tensor memory columns: S (and P) of the slots, then O
-
-struct Bars {
-  uint32_t base;
-  __device__ __forceinline__ uint32_t k_full(int stage) const { return base + 8 * stage; }
-  __device__ __forceinline__ uint32_t k_empty(int stage) const { return base + 16 + 8 * stage; }
-  __device__ __forceinline__ uint32_t v_full(int stage) const { return base + 32 + 8 * stage; }
-  __device__ __forceinline__ uint32_t v_empty(int stage) const { return base + 48 + 8 * stage; }
-  __device__ __forceinline__ uint32_t s_full(int slot, int half) const { return base + 64 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t p_full(int slot, int half) const { return base + 96 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
-  __device__ __forceinline__ uint32_t drained(int slot) const { return base + 168 + 8 * slot; }
-  // a warp of a slot may make its exponentials: warps w of both slots share a quarter of the SM
-  __device__ __forceinline__ uint32_t turn(int slot, int w) const { return base + 184 + 32 * slot + 8 * w; }
-};
-constexpr int kBars = 31;
 
 // The steps of a slot: two runs of 64-token steps, or every second tile.
 struct Steps {

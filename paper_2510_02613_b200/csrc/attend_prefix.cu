@@ -29,34 +29,14 @@
 namespace emoe {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
 // Registers a thread of the four warpgroups, out of the 4 x 128 that the block is launched with.
 constexpr int kSoftmaxRegs = 152, kMmaRegs = 80, kCopyRegs = 128;
 static_assert(2 * kSoftmaxRegs + kMmaRegs + kCopyRegs <= 512, "the block has no more registers than it was launched with");
-constexpr int kKept = 4;                   // steps whose masks and scales are kept
-constexpr unsigned long long kDrainNs = 1000000000ull;
-constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
-constexpr uint32_t kColS = 0, kColO = 256; // tensor memory columns: S (and P) of the slots, then O
 
 // Which copying warp has a row of a tile, and which of its lanes finds it in the table.
 template <int ROWS> __device__ __forceinline__ constexpr int warp_of_row(int row) { return row / ROWS % kCopyWarps; }
 template <int ROWS> __device__ __forceinline__ constexpr int lane_of_row(int row) { return row / (ROWS * kCopyWarps) * ROWS + row % ROWS; }
 
-struct Bars {
-  uint32_t base;
-  __device__ __forceinline__ uint32_t k_full(int stage) const { return base + 8 * stage; }
-  __device__ __forceinline__ uint32_t k_empty(int stage) const { return base + 16 + 8 * stage; }
-  __device__ __forceinline__ uint32_t v_full(int stage) const { return base + 32 + 8 * stage; }
-  __device__ __forceinline__ uint32_t v_empty(int stage) const { return base + 48 + 8 * stage; }
-  __device__ __forceinline__ uint32_t s_full(int slot, int half) const { return base + 64 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t p_full(int slot, int half) const { return base + 96 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
-  __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
-  __device__ __forceinline__ uint32_t drained(int slot) const { return base + 168 + 8 * slot; }
-  // a warp of a slot may make its exponentials: warps w of both slots share a quarter of the SM
-  __device__ __forceinline__ uint32_t turn(int slot, int w) const { return base + 184 + 32 * slot + 8 * w; }
-};
-constexpr int kBars = 31;
 
 template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kThreads, 1) attend_prefix_kernel(const __grid_constant__ AttendArgs a) {

@@ -293,7 +293,7 @@ namespace {
 MaskedSizes masked_sizes(const emoe_kv_cache_t *c, int32_t n_seqs, int32_t n_tokens, int32_t max_q, int32_t n_q_heads, int32_t max_blocks,
                          bool tree, int32_t window, int32_t sinks) {
   return {c->n_heads, n_seqs, n_tokens, std::min(max_q, n_tokens), n_q_heads, c->head_dim, c->type == EMOE_TYPE_E4M3,
-          most_tokens(c, max_blocks, tree, window, sinks)};
+          most_tokens(c, max_blocks, tree, window, sinks), tree || sinks + (int64_t)window >= (int64_t)max_blocks * c->block_tokens};
 }
 
 uint64_t part_bytes(const emoe_kv_cache_t *c, int64_t parts) {   // maxima and sums, then outputs
@@ -374,6 +374,7 @@ emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_at
   a.tensor_tiles_a_seq = s.tensor.tiles_a_seq;
   a.tensor_splits = s.tensor.splits;
   a.few = s.few;
+  a.ranked = s.ranked;
   a.per_token = 0xffffffffu / (uint32_t)c->block_tokens;
   a.short_rows = !s.rows.tiles || !s.tensor.tiles ? 0 : s.few ? kMaskedFewRows : kMaskedRows;
   a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;

@@ -1,5 +1,5 @@
-// tensor.cuh - 5th-generation tensor cores as the attention kernels use them: barriers with bounded waits, operands in
-// 128-byte-swizzled shared memory, products, tensor memory, and pairs of 32-bit operations.
+// tensor.cuh - 5th-generation tensor cores as the attention kernels use them: the roles of a block's warps and their
+// barriers, bounded waits, operands in 128-byte-swizzled shared memory, products, tensor memory, and pairs of 32-bit operations.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -8,6 +8,28 @@
 namespace emoe {
 
 constexpr int kTile = 128, kStep = 64;     // rows of a slot and tokens that are brought in at once; tokens of a step
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp0 = 12, kCopyWarps = 4, kThreads = 512;
+constexpr int kKept = 4;                   // tiles whose marks and scales are kept
+constexpr unsigned long long kDrainNs = 1000000000ull;
+constexpr float kRaise = 8.f;              // log2 of how far the real maximum may pass the one in use
+constexpr uint32_t kColS = 0, kColO = 256; // tensor memory columns: S (and P) of the slots, then O
+
+// Barriers of a block: two stages of K and of V tiles, two slots with two buffers of scores each.
+struct Bars {
+  uint32_t base;
+  __device__ __forceinline__ uint32_t k_full(int stage) const { return base + 8 * stage; }
+  __device__ __forceinline__ uint32_t k_empty(int stage) const { return base + 16 + 8 * stage; }
+  __device__ __forceinline__ uint32_t v_full(int stage) const { return base + 32 + 8 * stage; }
+  __device__ __forceinline__ uint32_t v_empty(int stage) const { return base + 48 + 8 * stage; }
+  __device__ __forceinline__ uint32_t s_full(int slot, int half) const { return base + 64 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t p_full(int slot, int half) const { return base + 96 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t o_full(int slot, int half) const { return base + 128 + 16 * slot + 8 * half; }
+  __device__ __forceinline__ uint32_t q_full() const { return base + 160; }
+  __device__ __forceinline__ uint32_t drained(int slot) const { return base + 168 + 8 * slot; }
+  // a warp of a slot may make its exponentials: warps w of both slots share a quarter of the SM
+  __device__ __forceinline__ uint32_t turn(int slot, int w) const { return base + 184 + 32 * slot + 8 * w; }
+};
+constexpr int kBars = 31;
 
 __device__ __forceinline__ unsigned long long now_ns() {
   unsigned long long t;

@@ -506,3 +506,15 @@ def test_prompts_in_pieces_then_single_tokens():
                 want, a = p @ seq[1, :, h // 4], p @ seq[1, :, h // 4].abs()
                 assert ((out[at[s]:at[s + 1], h].double() - want).abs() <= 2.2 * 2.0 ** -8 * a).all()
     assert lens.tolist() == [len(k) for k in kept]
+
+
+@pytest.mark.parametrize("kv,io,group", [("e4m3", "bf16", 1), ("bf16", "bf16", 4), ("f16", "f16", 1)])
+def test_many_sequences_of_different_lengths(kv, io, group):
+    """More blocks than run at once: the longest sequences come first, equal ones and empty ones among them."""
+    lens = [int(x) for x in np.random.default_rng(1).integers(0, 300, 60)] + [300, 300, 0, 0, 17]
+    counts = [min(n, 1 + i % (13 if group == 1 else 3)) for i, n in enumerate(lens)]
+    rng, ref, table, starts, q = setup(15 + group, kv, io, group == 4, 16, 8, group, 64, lens, counts)
+    c, _, _ = device_cache(ref)
+    bits = [tree_bits(rng, n) for n in counts]
+    check(ref, c, q, table, lens, starts, [RR.tree_sees(n, m, b) for n, m, b in zip(lens, counts, bits)], io, bits=bits)
+    check(ref, c, q, table, lens, starts, [RR.window_sees(n, m, 1 << 30, 0) for n, m in zip(lens, counts)], io, window=1 << 30)

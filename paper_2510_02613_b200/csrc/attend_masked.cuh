@@ -57,9 +57,9 @@ __device__ __forceinline__ RowTile row_tile(const MaskedArgs &a, int tiles_a_seq
 // Blocks start in the order of their numbers: where not all of them run at once, sequences with many tokens come first, so that none
 // of those is left for the end.  The tile whose sequence has the rank that `tile` asks for; one thread a sequence, all of the block.
 constexpr int kMostRanked = 128;
-__device__ __forceinline__ int ranked_tile(const MaskedArgs &a, int tile) {
+__device__ __forceinline__ int ranked_tile(const MaskedArgs &a, int tiles_a_seq, int tile) {
   __shared__ int s_tokens[kMostRanked], s_seq;
-  const int t = threadIdx.x, wanted = tile / a.tiles_a_seq;
+  const int t = threadIdx.x, wanted = tile / tiles_a_seq;
   int mine = 0;
   if (t < a.n_seqs) {
     mine = max(0, min(a.own_lens[t], a.max_blocks * a.c.block_tokens));
@@ -71,7 +71,7 @@ __device__ __forceinline__ int ranked_tile(const MaskedArgs &a, int tile) {
   for (int i = 0; i < a.n_seqs; ++i) rank += s_tokens[i] > mine || (s_tokens[i] == mine && i < t);
   if (t < a.n_seqs && rank == wanted) s_seq = t;
   __syncthreads();
-  return s_seq * a.tiles_a_seq + tile - wanted * a.tiles_a_seq;
+  return s_seq * tiles_a_seq + tile - wanted * tiles_a_seq;
 }
 
 // The tokens that some row of a tile may see, as one run: the first tokens, then those from `low` on.

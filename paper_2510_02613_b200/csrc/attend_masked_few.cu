@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_few_kern
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const int split = blockIdx.x % a.splits, unit_rank = blockIdx.x / a.splits, head = unit_rank % a.c.n_heads;
   let_next_start();
-  const int number = a.ranked ? ranked_tile(a, unit_rank / a.c.n_heads) : unit_rank / a.c.n_heads, unit = number * a.c.n_heads + head;
+  const int number = a.ranked ? ranked_tile(a, a.tiles_a_seq, unit_rank / a.c.n_heads) : unit_rank / a.c.n_heads, unit = number * a.c.n_heads + head;
   const RowTile tile = row_tile<kRows>(a, a.tiles_a_seq, number);
   if (tile.rows == 0 || (a.short_rows && tile.count * a.group > a.short_rows)) return;
   const Run run = run_of(a, tile);

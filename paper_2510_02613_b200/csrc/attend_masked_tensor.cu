@@ -88,8 +88,10 @@ __global__ void __launch_bounds__(kThreads, 1) masked_tensor_kernel(const __grid
 
   // the item
   let_next_start();
-  const int unit = blockIdx.x / a.tensor_splits, split = blockIdx.x - unit * a.tensor_splits, head = unit % a.c.n_heads;
-  const RowTile tile = row_tile<kRows>(a, a.tensor_tiles_a_seq, unit / a.c.n_heads);
+  const int unit_rank = blockIdx.x / a.tensor_splits, split = blockIdx.x - unit_rank * a.tensor_splits, head = unit_rank % a.c.n_heads;
+  const int number = a.tensor_ranked ? ranked_tile(a, a.tensor_tiles_a_seq, unit_rank / a.c.n_heads) : unit_rank / a.c.n_heads;
+  const int unit = number * a.c.n_heads + head;
+  const RowTile tile = row_tile<kRows>(a, a.tensor_tiles_a_seq, number);
   if (tile.rows == 0 || (a.short_rows && tile.count * a.group <= a.short_rows)) {   // (so few rows may be the other kernel's)
     wait_for_previous();
     return;

@@ -375,6 +375,7 @@ emoe_status_t attend_rows(const emoe_kv_cache_t *c, int32_t layer, const emoe_at
   a.tensor_splits = s.tensor.splits;
   a.few = s.few;
   a.ranked = s.ranked;
+  a.tensor_ranked = s.tensor_ranked;
   a.per_token = 0xffffffffu / (uint32_t)c->block_tokens;
   a.short_rows = !s.rows.tiles || !s.tensor.tiles ? 0 : s.few ? kMaskedFewRows : kMaskedRows;
   a.wait_ns = p->wait_limit_us < 0 ? 0 : p->wait_limit_us ? p->wait_limit_us * 1000ull : kDefaultWaitNs;

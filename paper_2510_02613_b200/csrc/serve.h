@@ -104,7 +104,7 @@ struct MaskedShape {
 struct MaskedShapes {
   MaskedShape rows, tensor;        // tiles 0: the kernel has nothing to do
   int32_t few;                     // rows: tiles of kMaskedFewRows
-  int32_t ranked;                  // rows: sequences in the order of their lengths, the longest first
+  int32_t ranked, tensor_ranked;   // sequences in the order of their lengths, the longest first
 };
 struct MaskedSizes {
   int32_t n_heads, n_seqs, n_tokens, max_q, n_q_heads, head_dim;
@@ -129,7 +129,7 @@ struct MaskedArgs {
   float *part_o, *tensor_o;             // the same, [head_dim]
   int32_t n_seqs, n_tokens, max_q, n_q_heads, group, max_blocks, mask_words, window, sinks;
   float scale_log2;
-  int32_t tiles, tiles_a_seq, splits, few, ranked;
+  int32_t tiles, tiles_a_seq, splits, few, ranked, tensor_ranked;
   int32_t tensor_tiles, tensor_tiles_a_seq, tensor_splits;
   uint32_t per_token;                   // (2^32 - 1) / block_tokens
   int32_t short_rows;                   // both kernels run: sequences of up to so many rows a head go to the row kernel; 0: one runs

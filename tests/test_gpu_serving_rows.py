@@ -518,3 +518,15 @@ def test_many_sequences_of_different_lengths(kv, io, group):
     bits = [tree_bits(rng, n) for n in counts]
     check(ref, c, q, table, lens, starts, [RR.tree_sees(n, m, b) for n, m, b in zip(lens, counts, bits)], io, bits=bits)
     check(ref, c, q, table, lens, starts, [RR.window_sees(n, m, 1 << 30, 0) for n, m in zip(lens, counts)], io, window=1 << 30)
+
+
+@pytest.mark.parametrize("kv,io", [("bf16", "bf16"), ("e4m3", "f16")])
+def test_many_trees_of_different_lengths(kv, io):
+    """As above on the tensor core kernel: more blocks than SMs."""
+    lens = [int(x) for x in np.random.default_rng(2).integers(0, 700, 40)] + [700, 700, 0, 9]
+    counts = [min(n, 10 + i % 11) for i, n in enumerate(lens)]
+    rng, ref, table, starts, q = setup(17, kv, io, False, 16, 4, 8, 64, lens, counts)
+    c, _, _ = device_cache(ref)
+    bits = [tree_bits(rng, n) for n in counts]
+    check(ref, c, q, table, lens, starts, [RR.tree_sees(n, m, b) for n, m, b in zip(lens, counts, bits)], io, bits=bits)
+    check(ref, c, q, table, lens, starts, [RR.window_sees(n, m, 1 << 30, 0) for n, m in zip(lens, counts)], io, window=1 << 30)

@@ -920,7 +920,10 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const 
  * block_table and changes by add[s]:
  *   add > 0  it gets the blocks that lens[s] + add[s] tokens want more;
  *   add < 0  its last -add tokens are gone (at most all of them); the blocks that it has too many go
- *            back to the list (their entries in its row stay as they are, behind its length);
+ *            back to the list (their entries in its row stay as they are, behind its length).
+ *            Entries of -1 are no blocks and are passed over: whoever gives a block of a sequence
+ *            back by hand (one behind a window) sets its entry to -1, or it goes back twice.
+ *            Ids from num_blocks on are passed over too, and reported;
  * q_start[0 .. n_seqs]: the sum of max(add, 0) over the sequences before: the new tokens of all
  *   sequences are packed in this order (q, k, v, out of the step), at most n_slots.
  * slots[i], i < n_slots: slot of the i-th new token (block * block_tokens + offset), -1 behind the last:
@@ -936,7 +939,9 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const 
  * fit in n_slots, or if it wants blocks and the blocks wanted by the sequences up to it (those that
  * do not fit their rows apart) are more than there are.  status (as in emoe_kv_cache_t, optional) is set to
  * EMOE_ERR_TOO_LARGE then, and where a block that is given back finds no room in the list; to EMOE_ERR_BLOCK_TABLE
- * by an id outside the pool (its tokens get slot -1).  Negative lens count as 0, so does a negative *n_free.
+ * by an id outside the pool among the blocks of new tokens (the sequence grows all the same, these tokens get
+ * slot -1) or among those given back (-1 apart).  Ids below -1, which no call makes, go to the list and come from it
+ * as they are.  Negative lens count as 0, so does a negative *n_free.
  *
  * cache: only its block size, number of blocks and status are used.  n_seqs at most EMOE_KV_MAX_SEQS
  * (EMOE_ERR_TOO_LARGE), n_seqs * max_blocks below 2^31.  One launch.
@@ -972,7 +977,8 @@ emoe_status_t emoe_kv_extend(const emoe_kv_cache_t *cache, const emoe_extend_t *
  * _window: a query token at place p of its sequence sees the tokens j <= p with j > p - window or
  * j < sinks.  Single tokens of decoding sequences and pieces of prompts come in one call.  window at least 1
  * (2^30 and more: no limit), sinks at least 0.  Blocks without any token that a query token of the
- * sequence sees are not read, nor are their entries in the table: they may have been given back.
+ * sequence sees are not read, nor are their entries in the table: they may have been given back (and
+ * their entries set to -1, which emoe_kv_extend passes over when the sequence ends).
  *
  * A row that sees no token gives 0 and minus infinity.  What a row does not see - tokens that its mask leaves out,
  * what lies behind a sequence's length, in its last block, in the rest of the pool - has no influence on

@@ -9,6 +9,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int32_t kNoBlock = -1;   // an entry of the table whose block is not the sequence's any more
 
 struct Sums {
   int64_t tokens;        // new ones
@@ -70,7 +71,8 @@ __device__ __forceinline__ Change change_of(const ExtendArgs &a, int32_t before,
 // by each lane.  A slot of a new token does not wait for the table: a block that is not in it yet is read from the list.
 //
 // Bound by latency: loads, a scan, a barrier, loads that depend on it, stores.  Measured: 64 sequences with a new token each 9.8 us on the
-// stream (the call on the host; the kernel 7.5), 1021 with up to 127 and a slot map of 129672 16.5 us.
+// stream (the call on the host; the kernel 7.5), 1021 with up to 127 and a slot map of 129672 18.5 us (16.9 without the count of what does
+// not go back).
 __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_constant__ ExtendArgs a) {
   extern __shared__ int32_t s_seq[];   // [5][n_seqs]
   __shared__ Sums s_warp[kWarps];
@@ -82,19 +84,66 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
     if (a.status) *a.status = code;
   };
 
+  bool some_back = false;
   for (int i = threadIdx.x; i < a.n_seqs; i += kThreads) {
     s_before[i] = max(0, a.lens[i]);
     s_add[i] = a.add[i];
+    s_at[i] = 0;   // entries that do not go back
+    some_back |= s_add[i] < 0;
   }
   const int32_t n_free = max(0, min(*a.n_free, a.free_capacity));
   if (threadIdx.x == 0) s_taken = 0;
-  __syncthreads();
+  some_back = __syncthreads_or(some_back);
+
+  const auto check_id = [&](int32_t id) {
+    if (id < 0 || id >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
+  };
+  // Entries that do not go back - blocks that the sequence has given back before, ids beyond the pool - leave no hole in the list: each
+  // block of the cluster counts all of them, a lane the first entries of a sequence, the warp what is behind them.
+  const auto goes_back = [&](int32_t id) { return id != kNoBlock && id < a.num_blocks; };
+  const auto returned_row = [&](int i, const Change &c) { return a.block_table + (int64_t)i * a.max_blocks + (c.had - c.back); };
+  if (some_back) {
+    for (int i0 = warp * 32; i0 < a.n_seqs; i0 += kThreads) {
+      constexpr int kFirst = 8;
+      const int i = i0 + lane;
+      const int32_t *row = nullptr;
+      int32_t n = 0, none = 0, id[kFirst];
+      if (i < a.n_seqs) {
+        const Change c = change_of(a, s_before[i], s_add[i]);
+        n = c.back;
+        row = returned_row(i, c);
+      }
+#pragma unroll
+      for (int j = 0; j < kFirst; ++j) id[j] = j < n ? row[j] : 0;
+#pragma unroll
+      for (int j = 0; j < kFirst; ++j) {
+        if (id[j] != kNoBlock) check_id(id[j]);
+        none += !goes_back(id[j]);
+      }
+      for (uint32_t more = __ballot_sync(0xffffffffu, n > kFirst); more; more &= more - 1) {
+        const int owner = __ffs(more) - 1;
+        const int32_t end = __shfl_sync(0xffffffffu, n, owner);
+        const int32_t *const of = (const int32_t *)__shfl_sync(0xffffffffu, (unsigned long long)row, owner);
+        int32_t mine = 0;
+#pragma unroll 4
+        for (int32_t j = kFirst + lane; j < end; j += 32) {
+          const int32_t x = of[j];
+          if (x != kNoBlock) check_id(x);
+          mine += !goes_back(x);
+        }
+        mine = __reduce_add_sync(0xffffffffu, mine);
+        if (lane == owner) none += mine;
+      }
+      if (i < a.n_seqs) s_at[i] = none;
+    }
+    __syncthreads();
+  }
   // this thread's sequences, one after the other in the batch
   const int per = (a.n_seqs + kThreads - 1) / kThreads, first = min(a.n_seqs, (int)threadIdx.x * per), last = min(a.n_seqs, first + per);
   Sums mine{0, 0, 0};
   for (int i = first; i < last; ++i) {
     const Change c = change_of(a, s_before[i], s_add[i]);
-    mine = mine + Sums{(int64_t)c.tokens, c.back, c.wanted};
+    mine = mine + Sums{(int64_t)c.tokens, c.back - s_at[i], c.wanted};
   }
   const Sums upto = running(mine, lane);
   if (lane == 31) s_warp[warp] = upto;
@@ -112,21 +161,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
   // what each sequence gets: its start, and where its blocks lie in the order of those given back or taken (-1: refused)
   for (int i = first; i < last; ++i) {
     const Change c = change_of(a, s_before[i], s_add[i]);
+    const int32_t given = c.back - s_at[i];
     s_first[i] = (int32_t)min(before.tokens, (int64_t)a.n_slots);
     s_had[i] = c.had;
     const bool granted = c.fits && (c.tokens == 0 || before.tokens + c.tokens <= a.n_slots) && (c.wanted == 0 || before.wanted + c.wanted <= top);
     if (!granted) report(EMOE_ERR_TOO_LARGE);
     s_at[i] = !granted ? -1 : c.back ? before.back : before.wanted;
     if (granted && c.wanted) atomicMax(&s_taken, before.wanted + c.wanted);
-    before = before + Sums{(int64_t)c.tokens, c.back, c.wanted};
+    before = before + Sums{(int64_t)c.tokens, given, c.wanted};
   }
   if (all.back > room && threadIdx.x == 0) report(EMOE_ERR_TOO_LARGE);
   const int32_t tokens = (int32_t)min(all.tokens, (int64_t)a.n_slots);
   cluster.sync();   // all blocks have read what the results may go over
 
   // Blocks of the 32 sequences of a group, four a lane at a time: read(sequence, which of its blocks) gives an id, and
-  // once four of them are under way write(sequence, which, id) takes them on.
-  const auto for_blocks = [&](bool returned, auto read, auto write) {
+  // once four of them are under way use(sequence, which, id) takes them on, by all lanes of the warp in the blocks' order (which < 0: this
+  // lane has none).  start(sequence): the first one of a group that has any.
+  const auto for_blocks = [&](bool returned, auto start, auto read, auto use) {
     for (int group = warp * blocks + rank; group * 32 < a.n_seqs; group += kWarps * blocks) {
       const int i = group * 32 + lane;
       int32_t n = 0;
@@ -134,6 +185,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
         const Change c = change_of(a, s_before[i], s_add[i]);
         n = returned ? c.back : c.wanted;
       }
+      const uint32_t have = __ballot_sync(0xffffffffu, n > 0);
+      if (have == 0) continue;
+      start(group * 32 + __ffs(have) - 1);
       int32_t end = n;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
@@ -159,28 +213,36 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
 #pragma unroll
         for (int k = 0; k < 4; ++k) id[k] = which[k] < 0 ? 0 : read(seq[k], which[k]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (which[k] >= 0) {
-            if (id[k] < 0 || id[k] >= a.num_blocks) report(EMOE_ERR_BLOCK_TABLE);
-            write(seq[k], which[k], id[k]);
-          }
+        for (int k = 0; k < 4; ++k) use(seq[k], which[k], id[k]);
       }
     }
   };
   const auto row_of = [&](int i) { return a.block_table + (int64_t)i * a.max_blocks + s_had[i]; };   // behind the blocks that the sequence had
   if (all.back > 0) {
+    int32_t listed = 0;   // where the group's next id goes
     for_blocks(
-        true,
-        [&](int i, int32_t j) { return row_of(i)[j - change_of(a, s_before[i], s_add[i]).back]; },
-        [&](int i, int32_t j, int32_t id) {
-          const int32_t at = n_free + s_at[i] + j;
-          if (at < a.free_capacity) a.free_blocks[at] = id;
+        true, [&](int i) { listed = n_free + s_at[i]; },
+        [&](int i, int32_t j) { return returned_row(i, change_of(a, s_before[i], s_add[i]))[j]; },
+        [&](int, int32_t j, int32_t id) {
+          const bool goes = j >= 0 && goes_back(id);
+          const uint32_t those = __ballot_sync(0xffffffffu, goes);
+          if (goes) {
+            const int32_t at = listed + __popc(those & ((1u << lane) - 1));
+            if (at < a.free_capacity) a.free_blocks[at] = id;
+          }
+          listed += __popc(those);
         });
     __threadfence();
     cluster.sync();
   }
   const auto taken_block = [&](int i, int32_t j) { return a.free_blocks[top - 1 - (s_at[i] + j)]; };
-  for_blocks(false, taken_block, [&](int i, int32_t j, int32_t id) { row_of(i)[j] = id; });
+  for_blocks(
+      false, [](int) {}, taken_block,
+      [&](int i, int32_t j, int32_t id) {
+        if (j < 0) return;
+        check_id(id);
+        row_of(i)[j] = id;
+      });
   if (rank == 0) {
     for (int i = threadIdx.x; i < a.n_seqs; i += kThreads) {
       const Change c = change_of(a, s_before[i], s_add[i]);

@@ -243,7 +243,8 @@ class KvCache:
     def extend(self, lens, add, block_table, free_blocks, n_free, q_start, slots, lens_out, n_free_out, stream=None) -> None:
         """Blocks for a batch's next tokens, from lengths in device memory: sequence s of lens[s] tokens changes by
         add[s] (int32 [n] both), gets blocks from the end of free_blocks (int32; the first n_free [1] of it are free) into
-        its row of block_table (int32 [n, max_blocks]) or gives them back.  Receives q_start (int32 [n + 1]: where
+        its row of block_table (int32 [n, max_blocks]) or gives them back (entries of -1 apart: blocks that were given back by hand,
+        as those behind a window may be, have their entries set to that).  Receives q_start (int32 [n + 1]: where
         each sequence's new tokens begin among all), slots (int64, any size: a slot a new token, -1 behind the last), lens_out
         (may be lens) and n_free_out (may be n_free).  A sequence that there is no room for stays as it was, its slots -1."""
         dev, at = self.device, _dense_pointer

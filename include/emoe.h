@@ -935,7 +935,8 @@ emoe_status_t emoe_kv_attend(const emoe_kv_cache_t *cache, int32_t layer, const 
  * order; *n_free_out is what remains (may be n_free itself).  Entries that are taken stay in the array.
  *
  * A sequence is refused as a whole - lens_out = lens, its row as it was, slots -1 for its tokens, which
- * keep their places in the packed order - if it would not fit in max_blocks blocks, if its new tokens do not
+ * keep their places in the packed order (attention gives these no meaningful outputs, emoe_kv_keep has to be
+ * told by slots) - if it would not fit in max_blocks blocks, if its new tokens do not
  * fit in n_slots, or if it wants blocks and the blocks wanted by the sequences up to it (those that
  * do not fit their rows apart) are more than there are.  status (as in emoe_kv_cache_t, optional) is set to
  * EMOE_ERR_TOO_LARGE then, and where a block that is given back finds no room in the list; to EMOE_ERR_BLOCK_TABLE
@@ -1035,6 +1036,10 @@ emoe_status_t emoe_kv_attend_window(const emoe_kv_cache_t *cache, int32_t layer,
  * nodes: the add that takes the others from the sequence in the next emoe_kv_extend.
  * A path that does not rise, or leaves the nodes, ends there; that, and places outside the table or blocks outside the
  * pool (whose moves are left out), are reported in the status word (EMOE_ERR_BLOCK_TABLE).
+ * slots: those that the emoe_kv_extend made which took the nodes in.  A sequence that has none for any of
+ * its nodes was refused there - its last tokens are no nodes - and stays as it is: nothing moves, change[s] = 0.
+ * Without slots the caller sees to it that no sequence of the step was refused, or its own last tokens are
+ * overwritten and taken from it.
  * head_dim: a multiple of 8 (EMOE_ERR_UNSUPPORTED).  max_accepted at most EMOE_KV_MAX_ACCEPTED, n_seqs at most 2^16 - 1
  * (EMOE_ERR_TOO_LARGE).  Sequences hold blocks of their own.  One launch.
  */
@@ -1048,6 +1053,9 @@ typedef struct {
   int32_t *change;             /* [n_seqs]                                                     */
   int32_t n_seqs, max_blocks, max_accepted;
   uint32_t reserved;           /* zero                                                         */
+  const int64_t *slots;        /* optional [n_slots], at least q_start[n_seqs] of them           */
+  int32_t n_slots;             /* 0 without slots                                              */
+  uint32_t reserved2;          /* zero                                                         */
 } emoe_keep_t;
 emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *cache, const emoe_keep_t *args, void *cuda_stream);
 

@@ -104,7 +104,7 @@ class _AttendRows(ctypes.Structure):
 
 class _Keep(ctypes.Structure):
     _fields_ = [(n, _vp) for n in ("block_table", "lens", "q_start", "accepted", "n_accepted", "change")] + \
-               [(n, _i32) for n in ("n_seqs", "max_blocks", "max_accepted")] + [("reserved", _u32)]
+               [(n, _i32) for n in ("n_seqs", "max_blocks", "max_accepted")] + [("reserved", _u32), ("slots", _vp), ("n_slots", _i32), ("reserved2", _u32)]
 
 
 class _Moe(ctypes.Structure):

@@ -321,6 +321,14 @@ __global__ void __launch_bounds__(kMoveThreads) kv_keep_kernel(const __grid_cons
   const auto report = [&]() {
     if (a.c.status) *a.c.status = EMOE_ERR_BLOCK_TABLE;
   };
+  if (a.slots) {   // a sequence without a slot for any of its nodes has none of them: it was refused
+    bool some = nodes == 0;
+    for (int64_t i = (int64_t)q0 + threadIdx.x; i < (int64_t)q0 + nodes; i += kMoveThreads) some |= i >= 0 && i < a.n_slots && a.slots[i] >= 0;
+    if (!__syncthreads_or(some)) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) a.change[seq] = 0;
+      return;
+    }
+  }
   if (threadIdx.x == 0) s_end = most;
   __syncthreads();
   for (int i = threadIdx.x; i < most; i += kMoveThreads)

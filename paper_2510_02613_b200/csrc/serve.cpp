@@ -448,18 +448,19 @@ emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *c, const emoe_keep_t *p, void 
   TraceRange trace("emoe_kv_keep");
   emoe_status_t st = check_cache_memory(c, 0);
   if (st != EMOE_OK) return st;
-  if (!p || p->reserved) return EMOE_ERR_INVALID_ARG;
-  if (p->n_seqs < 0 || p->max_blocks < 0 || p->max_accepted < 0) return EMOE_ERR_SHAPE;
+  if (!p || p->reserved || p->reserved2) return EMOE_ERR_INVALID_ARG;
+  if (p->n_seqs < 0 || p->max_blocks < 0 || p->max_accepted < 0 || p->n_slots < 0) return EMOE_ERR_SHAPE;
   if (c->head_dim % 8) return EMOE_ERR_UNSUPPORTED;
   const uint64_t vector = (uint64_t)c->head_dim * type_bytes(c->type), pieces = vector % 16 ? vector / 8 : vector / 16;
   if (p->n_seqs > 65535 || p->max_accepted > EMOE_KV_MAX_ACCEPTED || (int64_t)p->max_blocks * c->block_tokens >= (int64_t)1 << 30 ||
       (unsigned __int128)2 * c->n_layers * c->n_heads * pieces >= 1u << 31)
     return EMOE_ERR_TOO_LARGE;
   if (p->n_seqs == 0) return EMOE_OK;
-  if (!p->lens || !p->q_start || !p->n_accepted || !p->change || (p->max_accepted && !p->accepted) || (p->max_blocks && !p->block_table))
+  if (!p->lens || !p->q_start || !p->n_accepted || !p->change || (p->max_accepted && !p->accepted) || (p->max_blocks && !p->block_table) ||
+      (p->n_slots && !p->slots))
     return EMOE_ERR_INVALID_ARG;
   if (!aligned(p->block_table, 4) || !aligned(p->lens, 4) || !aligned(p->q_start, 4) || !aligned(p->accepted, 4) ||
-      !aligned(p->n_accepted, 4) || !aligned(p->change, 4))
+      !aligned(p->n_accepted, 4) || !aligned(p->change, 4) || !aligned(p->slots, 8))
     return EMOE_ERR_ALIGNMENT;
   st = on_current_device(c->arena);
   if (st != EMOE_OK) return st;
@@ -472,6 +473,7 @@ emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *c, const emoe_keep_t *p, void 
   a.q_start = p->q_start;
   a.accepted = p->accepted;
   a.n_accepted = p->n_accepted;
+  a.slots = p->slots;
   a.change = p->change;
   a.pools = 2 * c->n_layers;
   a.pieces = (uint32_t)pieces;
@@ -479,6 +481,7 @@ emoe_status_t emoe_kv_keep(const emoe_kv_cache_t *c, const emoe_keep_t *p, void 
   a.max_blocks = p->max_blocks;
   a.max_accepted = p->max_accepted;
   a.num_blocks = c->num_blocks;
+  a.n_slots = p->n_slots;
   return cuda_status(launch_kv_keep(a, vector % 16 == 0, (cudaStream_t)stream));
 }
 

@@ -54,9 +54,10 @@ struct KeepArgs {
   KvLayer c;                 // of layer 0: the others follow, K and V in turn
   uint64_t pool_bytes, pool_vectors;
   const int32_t *block_table, *lens, *q_start, *accepted, *n_accepted;
+  const int64_t *slots;      // null: every sequence has its nodes
   int32_t *change;
   uint32_t pools, pieces;    // 2 * layers; pieces of a head vector
-  int32_t n_seqs, max_blocks, max_accepted, num_blocks;
+  int32_t n_seqs, max_blocks, max_accepted, num_blocks, n_slots;
 };
 cudaError_t launch_kv_keep(const KeepArgs &a, bool wide, cudaStream_t st);   // wide: pieces of 16 bytes, else of 8
 

@@ -257,15 +257,18 @@ class KvCache:
                        at(lens_out, "lens_out", seqs, "int32", dev), at(n_free_out, "n_free_out", one, "int32", dev), n, width, room, tokens, 0, 0)
         _check(self._calls.emoe_kv_extend(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
-    def keep(self, block_table, lens, q_start, accepted, n_accepted, change, stream=None) -> None:
+    def keep(self, block_table, lens, q_start, accepted, n_accepted, change, stream=None, slots=None) -> None:
         """Moves the accepted nodes (int32 [n, most], rising node numbers, the first n_accepted [n] of each row) of the
         sequences' trees, their last q_start[s + 1] - q_start[s] tokens, to the front of these, in all layers.  change
-        (int32 [n]) receives accepted less drafted tokens: the add of the next extend."""
+        (int32 [n]) receives accepted less drafted tokens: the add of the next extend.  slots: those of the extend that took the
+        nodes in; a sequence that was refused there, which has no nodes, stays as it is then (change 0)."""
         dev, at = self.device, _dense_pointer
         (n,), (_, width), (_, most) = _sizes(lens, "lens", 1), _sizes(block_table, "block_table", 2), _sizes(accepted, "accepted", 2)
+        places = None if slots is None else at(slots, "slots", (_sizes(slots, "slots", 1)[0],), "int64", dev) or 8   # (an empty one has no address, and is not read)
         p = _b._Keep(at(block_table, "block_table", (n, width), "int32", dev), at(lens, "lens", (n,), "int32", dev),
                      at(q_start, "q_start", (n + 1,), "int32", dev), at(accepted, "accepted", (n, most), "int32", dev),
-                     at(n_accepted, "n_accepted", (n,), "int32", dev), at(change, "change", (n,), "int32", dev), n, width, most, 0)
+                     at(n_accepted, "n_accepted", (n,), "int32", dev), at(change, "change", (n,), "int32", dev), n, width, most, 0,
+                     places, 0 if slots is None else slots.shape[0], 0)
         _check(self._calls.emoe_kv_keep(self._ref, ctypes.byref(p), _stream_handle(stream)))
 
     def attend_tree_workspace_bytes(self, n_seqs: int, n_tokens: int, max_q: int, n_q_heads: int, max_blocks: int) -> int:

@@ -63,7 +63,7 @@ __device__ __forceinline__ int ranked_tile(const MaskedArgs &a, int tiles_a_seq,
   int mine = 0;
   if (t < a.n_seqs) {
     mine = max(0, min(a.own_lens[t], a.max_blocks * a.c.block_tokens));
-    if (!a.mask) mine = min(mine, a.window + a.sinks);
+    if (!a.mask) mine = (int)min((uint32_t)mine, (uint32_t)a.window + (uint32_t)a.sinks);   // (the two come to 2^31 where neither has a limit)
     s_tokens[t] = mine;
   }
   __syncthreads();

@@ -901,7 +901,8 @@ typedef struct {
   uint32_t reserved;           /* zero                                                         */
   int32_t wait_limit_us;       /* bound of the waits inside the kernels in microseconds; 0: the  */
                                /* default, 4 s; -1: a wait that is not over when it is first   */
-                               /* polled runs out at once (to exercise that path)              */
+                               /* polled runs out at once (to exercise that path).  Waits are   */
+                               /* polled every few us: a limit may be passed by about 10        */
   uint32_t reserved2;          /* zero                                                         */
 } emoe_attend_t;
 emoe_status_t emoe_kv_attend_workspace(const emoe_kv_cache_t *cache, int32_t n_seqs, int32_t q_len,

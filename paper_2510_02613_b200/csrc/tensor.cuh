@@ -62,7 +62,8 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {   // w
 }
 // For whole warps: false, in every lane, if the phase does not complete within `limit` nanoseconds (0: is not
 // over already) or another role has given up.  The lanes agree on each try, so that a wait that is over already
-// costs one try and no divergence.
+// costs one try and no divergence.  A try waits by itself, 4 us where nothing comes: the timer, which takes long to answer, is read
+// from the first one on that failed, and a wait runs out up to two tries after its limit.
 // PATIENT: who has time sleeps between tries and leaves the issue slots to the others.
 template <bool PATIENT = false>
 __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort, unsigned long long limit) {
@@ -71,15 +72,13 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
     *abort = 1;
     return false;
   }
-  unsigned long long t0 = 0;   // (the timer is read late: it takes long to answer)
+  unsigned long long t0 = 0;
   for (;;) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i) {
-      if constexpr (PATIENT) __nanosleep(100);
-      if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-    }
-    if (t0 == 0) t0 = now_ns();
-    if (__any_sync(0xffffffffu, *abort != 0 || now_ns() - t0 > limit)) {
+    if constexpr (PATIENT) __nanosleep(100);
+    if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+    const unsigned long long now = now_ns();
+    if (t0 == 0) t0 = now;
+    if (__any_sync(0xffffffffu, *abort != 0 || now - t0 > limit)) {
       *abort = 1;
       return false;
     }

@@ -990,7 +990,9 @@ emoe_status_t emoe_kv_extend(const emoe_kv_cache_t *cache, const emoe_extend_t *
  * first max_q are computed, each at the place that it has.  Tokens on a block id outside the pool are left out and
  * reported (EMOE_ERR_BLOCK_TABLE).  own_lens beyond max_blocks * block_tokens count as that, negative ones as 0; query tokens
  * whose places would be negative see nothing (but _tree nodes that there are, by their bits).
- * Precision, types, head_dim, bounded waits, lse and workspaces are as for emoe_kv_attend; a call over a
+ * Precision is as for emoe_kv_attend: scores, maxima, sums and outputs are kept in 32 bits; each weight is rounded once to
+ * the 16-bit type (f16 on an e4m3 cache) before it meets v, the outputs once at the end.  Types, head_dim,
+ * bounded waits, lse and workspaces are as there too; a call over a
  * shared prefix is joined with one of these by lse.  n_tokens, max_q, max_blocks are host values: a captured call
  * follows q_start, own_lens, tables and masks from replay to replay.
  * Sizes beyond 2^24 query tokens, 2^28 rows or 2^30 tokens a sequence: EMOE_ERR_TOO_LARGE.

@@ -24,7 +24,8 @@ template <bool FP8> constexpr int kGroupOf = FP8 ? 32 : 16;
 // memory, scores and products on the tensor cores with the 16 rows of the tile as the m side, running maximum
 // and sum in registers.  The four warps take every fourth group of tokens and are joined at the end.  Three blocks an SM (registers, ring).
 // Measured, 48 trees of up to 13 nodes on up to 2750 tokens, 16 heads of their own, e4m3, head_dim 128: 97 us, 2.6 TB/s; issue
-// slots 46%, integer pipe 37%: what bounds it is the chain of a step, with three warps a scheduler.
+// slots 46%, integer pipe 37%: what bounds it is the chain of a step, with three warps a scheduler.  (168 registers hold it but for 8 to 28 bytes
+// that go to memory with e4m3 at 64 and 128; at 256 it has 255 registers, one block an SM, and 28 to 124 bytes go.)
 template <typename IO, int HD, bool FP8>
 __global__ void __launch_bounds__(kWarps * 32, HD < 256 ? 3 : 1) masked_rows_kernel(const __grid_constant__ MaskedArgs a) {
   using T = typename Operand<IO, FP8>::type;
@@ -550,7 +551,8 @@ void count_tiles(MaskedShape &s, const MaskedSizes &n, int64_t rows) {
   s.tiles = (int32_t)std::min(each * n.n_seqs, packed);
 }
 
-// Whether sequences with more than 16 rows a head go to the tensor core kernel.  It takes 128 rows at least at once, so that it
+// Whether sequences with more than 16 rows a head go to the tensor core kernel, which has head_dim 64 and 128 only (at 256, O of two slots alone
+// would fill tensor memory).  It takes 128 rows at least at once, so that it
 // pays from about 2^17 row tiles (of 16 rows) x heads x tokens on, with few rows later.  Measured, 4 heads, us of the row kernel and of
 // the other one, bf16 and e4m3:
 //   64 and more rows: 1 x 128 rows x 2000 tokens (2^16) 18.9, 20.2 and 20.9, 20.9;  4 x 128 x 1000 (2^17) 22.3, 18.0 and 27.0, 21.0;

@@ -55,7 +55,9 @@ __device__ __forceinline__ RowTile row_tile(const MaskedArgs &a, int tiles_a_seq
 }
 
 // Blocks start in the order of their numbers: where not all of them run at once, sequences with many tokens come first, so that none
-// of those is left for the end.  The tile whose sequence has the rank that `tile` asks for; one thread a sequence, all of the block.
+// of those is left for the end.  The tile whose sequence has the rank that `tile` asks for; one thread a sequence, all of the block: more
+// sequences than a row kernel's block has threads stay as they come.  That costs the less the more there are: of trees of 5 to 13 nodes on 13 to
+// 2750 tokens, 16 heads, e4m3, 129 took 267 us as they came and 239 the longest first, 256 490 and 460, 512 941 and 930.
 constexpr int kMostRanked = 128;
 __device__ __forceinline__ int ranked_tile(const MaskedArgs &a, int tiles_a_seq, int tile) {
   __shared__ int s_tokens[kMostRanked], s_seq;

@@ -18,11 +18,15 @@
 // Warps: 0-3 and 4-7 the softmax of the two slots (a thread a row), 8 and 9 issue the slots' products, 12-15 bring
 // K and V rows from their pages into the 128-byte-swizzled tiles that the products read (e4m3 codes widened on the way).
 //
-// Measured, bf16, head_dim 128: a tile of 128 tokens x 256 rows takes 2.15 us, a unit's start and end about 7 us (queries and first tiles,
-// 192 KB a block, come for all blocks at once: 3 us; outputs 2.5 us).  8192 tokens of a prompt in a window of 4096, 32 on 4 heads: 635 us, 867
-// TFLOP/s, 51% of a library product's rate; 8 trees of 64 nodes on 16000 tokens: 181 us.  Three chains take about as long as one another: without the softmax a tile would take 1.88 us, without the products 1.94, without
-// exponentials as long as with them.  The products of S, 64 columns wide, are bound by shared memory (48 clocks for 16 of k, not 32); whole
-// tiles of 128 columns, which are not, leave no scores to work on while the next ones are made (2.86 us).
+// Measured, bf16, head_dim 128, at 1965 MHz: a tile of 128 tokens x 256 rows takes 2.2 us, a unit's start and end 8 us (queries and first
+// tiles, 192 KB a block, come for all blocks at once: 3 us; outputs 2.5 us).  8192 tokens of a prompt in a window of 4096, 32 on 4 heads, are
+// 1024 units of 33 tiles, 7 rounds on 148 SMs: 572 us by that.  Called for a second the power limit brings the clock down: 637 us at 1762 MHz, 597 at
+// 1822, 855 to 920 TFLOP/s, 51 to 55% of a library product's rate.  8 trees of 64 nodes on 16000 tokens: 167 us at 1965 MHz, 182 at 1777.  The same
+// prompt on an e4m3 cache: 1060 us at 1965 MHz (codes are widened on their way into shared memory, and each score takes two scales; which of
+// the two bounds it was not measured).  Three chains take about as long as one another: of 2.15 us a tile, when it was looked at, 1.88 were
+// left without the softmax, 1.94 without the products, 2.15 without the exponentials.  The products of S, 64 columns wide, are bound by
+// shared memory (48 clocks for 16 of k, not 32); whole tiles of 128 columns, which are not, leave no scores to work on while the next ones are
+// made (2.86 us).
 #include "attend_item.cuh"
 #include "attend_masked.cuh"
 #include "tensor.cuh"

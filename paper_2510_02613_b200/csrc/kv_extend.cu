@@ -71,7 +71,7 @@ __device__ __forceinline__ Change change_of(const ExtendArgs &a, int32_t before,
 // by each lane.  A slot of a new token does not wait for the table: a block that is not in it yet is read from the list.
 //
 // Bound by latency: loads, a scan, a barrier, loads that depend on it, stores.  Measured: 64 sequences with a new token each 9.8 us on the
-// stream (the call on the host; the kernel 7.5), 1021 with up to 127 and a slot map of 129672 18.5 us (16.9 without the count of what does
+// stream (the call on the host; the kernel 8.3), 1021 with up to 127 and a slot map of 129672 18.5 us (16.9 without the count of what does
 // not go back).
 __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_constant__ ExtendArgs a) {
   extern __shared__ int32_t s_seq[];   // [5][n_seqs]
@@ -306,8 +306,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_extend_kernel(const __grid_con
 // the whole path: sources are read in groups, in rising order, before they are written.  A place that is
 // written lies before all sources that are still to be read (the i-th node is at place i or behind it, and
 // nodes rise), so a path may overlap its own new places.
-// Bound by three loads one after the other (path, table, data).  Measured: 16 paths in 4 layers 8.7 us on the stream (the call on
-// the host; the kernel 6), 128 in 24 layers, 22 MB read and written, 10.6 us.
+// Bound by three loads one after the other (path, table, data).  Measured: 16 paths in 4 layers 8.8 us on the stream (the call on
+// the host; the kernel 6), 128 in 24 layers, 22 MB read and written, 10.5 to 12 us.
 constexpr int kMoveThreads = 256, kAhead = 8;
 template <typename V>   // a piece: 8 or 16 bytes
 __global__ void __launch_bounds__(kMoveThreads) kv_keep_kernel(const __grid_constant__ KeepArgs a) {
